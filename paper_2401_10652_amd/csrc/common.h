@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "../../include/autochunk_decode.h"
 #include "../../include/autochunk_rt.h"
 
 namespace ac {
@@ -157,6 +158,16 @@ __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
   return v;
+}
+// An fp32 number as three bf16 ones that sum to it exactly: each is cut off (not rounded, so none overflows) to the 8 bits that it holds of
+// what is left.  An infinity or NaN is its own first term.
+struct Bf16Terms { bf16_t hi, mid, lo; };
+__device__ __forceinline__ Bf16Terms split_bf16(float v) {
+  const bool finite = fabsf(v) < INFINITY;
+  const float hi = finite ? __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v) & 0xffff0000u) : v;
+  const float rest = finite ? v - hi : 0.f;
+  const float mid = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, rest) & 0xffff0000u);
+  return Bf16Terms{f2bf(hi), f2bf(mid), f2bf(rest - mid)};
 }
 // Sum over groups of G consecutive lanes (G a power of two <= 64).  Within sixteen lanes by rotations of the row: once lanes 8 apart hold the same sum
 // a rotation by 4 is an exchange of lanes 4 apart, and so on, the sums (and bits) of the exchanges at no trip through LDS.
@@ -337,6 +348,27 @@ hipError_t launch_gather_columns(const void* src, void* dst, int64_t n, int64_t 
 hipError_t launch_layernorm_channel_major(const void* src, int64_t stride_c, const void* gain,
                                           const void* shift, void* dst, int64_t ldd, int64_t positions,
                                           int64_t channels, float eps, int dtype, hipStream_t s);
+
+// A linear layer with 4-bit weights, the append to an 8-bit cache and the attention over it: see autochunk_decode.h.
+struct LinearW4Args {
+  const void* x; int64_t ldx;
+  const void* w; int64_t ldw;           // bytes
+  const void* scale; int64_t lds;
+  const void* zero; int64_t ldz;        // null: 8 everywhere
+  int64_t group;
+  const void* bias;
+  const void* resid; int64_t ldr;
+  void* out; int64_t ldo;
+  int64_t m, n, k;
+  int act, dtype;
+};
+hipError_t launch_linear_w4(const LinearW4Args& g, hipStream_t s);
+hipError_t launch_cache_append(const void* q, int64_t ldq, void* q_out, int64_t ldqo, int heads, const void* k, int64_t ldk, const void* v,
+                               int64_t ldv, const ac_kv_cache& cache, const ac_cache_rows& rows, const ac_rotary* rotary, int dtype,
+                               hipStream_t s);
+hipError_t launch_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int heads, const ac_kv_cache& cache,
+                                  const ac_cache_rows& rows, int causal, float scale, void* workspace, int dtype, hipStream_t s);
+uint64_t cache_attention_workspace_bytes(int heads, const ac_kv_cache& cache, const ac_cache_rows& rows, int causal, int dtype);
 
 // hipErrorInvalidValue-style refusal with a message for ac_last_error().
 void set_error(const char* fmt, ...);

@@ -19,8 +19,8 @@ struct Sequence { int64_t begin, rows, length; };   // its first row, its rows, 
 
 __device__ __forceinline__ Sequence sequence(const ac_cache_rows& r, int64_t b) {
   const int64_t lo = r.row_begin[b], hi = r.row_begin[b + 1];
-  const int64_t from = lo < 0 ? 0 : lo, to = hi < r.rows ? hi : r.rows;
-  return Sequence{from, to > from ? to - from : 0, r.length[b]};
+  const int64_t from = lo < 0 ? 0 : lo, to = hi < r.rows ? hi : r.rows, n = r.length[b];
+  return Sequence{from, to > from ? to - from : 0, n > 0 ? n : 0};
 }
 
 // ---- append ----------------------------------------------------------------------------------------------------------
@@ -287,137 +287,189 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
   return (m >> 7 & 0x01010101u) * 0xffu;
 }
 
+// n / d for n < 2^31 by one multiplication and one addition: with l = ceil(log2 d), the quotient is (hi32(n * mul) + n) >> l for
+// mul = floor(2^32 (2^l - d) / d) + 1 (Granlund and Montgomery, "Division by invariant integers using multiplication", 1994).
+struct Divisor { uint32_t d, mul, shift; };
+Divisor divisor(uint32_t d) {
+  uint32_t l = 0;
+  while ((1ull << l) < d) ++l;
+  return Divisor{d, (uint32_t)((((1ull << l) - d) << 32) / d + 1), l};
+}
+__device__ __forceinline__ int quotient(int n, const Divisor& v) { return (int)((__umulhi((uint32_t)n, v.mul) + (uint32_t)n) >> v.shift); }
+
 struct CacheAttnArgs {
   const void* q; void* out;
   int64_t ldq, ldo;
-  int heads, group;                 // query heads, of a key head
+  int heads;
   ac_kv_cache cache;
   ac_cache_rows rows;
   int causal;
   float scale;                      // times log2 e
-  int splits; int64_t least;        // runs of keys, and the fewest keys of one (a multiple of 64)
+  Divisor group, blocks;            // query heads of a key head, blocks of a page
+  int splits, least;                // runs of keys, and the fewest keys of one (a multiple of 256)
   float* part_o; float* part_ml;    // [splits][rows][heads][head_dim], [splits][rows][heads][2]
+  int teams;                        // that share the parts of one row and head
 };
 
-// The keys that one of `splits` blocks takes of `seen` keys: runs of the same length, whole steps of 64.
-__device__ __forceinline__ int64_t run_length(int64_t seen, int splits, int64_t least) {
-  const int64_t even = (seen + splits - 1) / splits, n = (even + 63) / 64 * 64;
+// The keys of one of `splits` runs over `seen` keys: runs of the same length, whole steps of a block's four waves.
+__device__ __forceinline__ int run_length(int seen, int splits, int least) {
+  const int even = (seen + splits - 1) / splits, n = (even + 255) / 256 * 256;
   return n > least ? n : least;
 }
 
-// One block: 16 query rows (the rows of a sequence with the query heads of one key head, head fastest) over one run of keys, in
-// steps of 64 that its four waves take in turn.  S^T = K Q^T and O^T = V^T P^T, both by v_mfma_f32_16x16x32_bf16 with a query row
-// to a column, so a lane holds probabilities of one row and the running maximum and sum are per-lane scalars.  Row a of key tile j is token
-// 16 (a / 4) + 4 j + a mod 4 of the step: quarter g of the wave then holds the scores of block g, with that block's two scales in one
-// register each, and the probabilities of its 16 tokens in the order in which the cache holds their values.  No code passes through LDS.
-template <typename T, int HD>
+// What a sequence's rows see: the rows of a tile are (row of the sequence, query head of the key head), head fastest.
+struct Sight {
+  int begin, rows, first, held, all;     // first row, rows, token of row 0, tokens that have a place, rows times heads
+  __device__ Sight(const CacheAttnArgs& g, int b) {
+    const Sequence s = sequence(g.rows, b);
+    const int64_t most = g.rows.ld_page_table * g.cache.page;
+    begin = (int)s.begin;
+    rows = (int)s.rows;
+    first = (int)(s.length - s.rows);
+    held = (int)(s.length < most ? s.length : most);
+    all = rows * (int)g.group.d;
+  }
+};
+
+// One block: 16 RT query rows over one run of keys, in steps of 64 that its four waves take in turn.  S^T = K Q^T and O^T = V^T P^T, both by
+// v_mfma_f32_16x16x32_bf16 with a query row to a column, so a lane holds probabilities of one row and the running maximum and sum are
+// per-lane scalars.  Row a of key tile j is token 16 (a / 4) + 4 j + a mod 4 of the step: quarter g of the wave then holds the scores of
+// block g, with that block's two scales in one register each, and the probabilities of its 16 tokens in the order in which the cache
+// holds their values.  No code passes through LDS.  What bounds it is HBM: a step's values are on their way while its scores are computed, the next step's
+// keys while its values are multiplied, and page numbers are read two steps ahead.
+template <typename T, int HD, int RT>
 __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
   constexpr int NT = Terms<T>::kN, W16 = HD / 64, REST = HD % 64 / 32, DT = HD / 16;
   constexpr int FR = HD / 32;                          // fragments of 32 of a row
+  constexpr int ROWS = 16 * RT;
   extern __shared__ float joined[];                    // [4][16][HD] and [4][16][2]
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c16 = lane % 16, quarter = lane / 16;
-  const int64_t page = g.cache.page, blocks = page / kBlock, b = blockIdx.z;
-  const int kvh = blockIdx.y % g.cache.heads;
-  const Sequence sq = sequence(g.rows, b);
-  const int64_t all = sq.rows * g.group, first = sq.length - sq.rows;
-  const int64_t held = sq.length < g.rows.ld_page_table * page ? sq.length : g.rows.ld_page_table * page;
-  const int32_t* table = g.rows.page_table + b * g.rows.ld_page_table;
-  const uint8_t* kbase = (const uint8_t*)g.cache.k + (int64_t)kvh * page * HD;
-  const uint8_t* vbase = (const uint8_t*)g.cache.v + (int64_t)kvh * page * HD;
+  const int kv = g.cache.heads, kvh = blockIdx.y % kv, tiles = gridDim.y / kv, group = g.group.d, blocks = g.blocks.d;
+  const Sight sq(g, blockIdx.z);
+  const int32_t* table = g.rows.page_table + blockIdx.z * g.rows.ld_page_table;
+  const uint8_t* kbase = (const uint8_t*)g.cache.k + (int64_t)kvh * g.cache.page * HD + (c16 % 4) * HD + quarter * 16;
+  const uint8_t* vbase = (const uint8_t*)g.cache.v + (int64_t)kvh * g.cache.page * HD + c16 * kBlock;
 
-  for (int64_t tile = blockIdx.y / g.cache.heads; tile * 16 < all; tile += gridDim.y / g.cache.heads) {
-    const int64_t r = tile * 16 + c16, rr = r < all ? r : all - 1;
-    const int64_t row = sq.begin + rr / g.group;
-    const int head = kvh * g.group + (int)(rr % g.group);
-    const int64_t sees = r >= all ? 0 : g.causal ? first + rr / g.group + 1 : held;           // keys before this one
-    int64_t seen = held, fewest = held;                                                        // the most and the fewest of the tile's rows
+  for (int tile = blockIdx.y / kv; tile * ROWS < sq.all; tile += tiles) {
+    int sees[RT];                                       // a row sees the keys before this one
+    int seen = sq.held, fewest = sq.held;               // the most and the fewest of the tile's rows
     if (g.causal) {
-      const int64_t last = tile * 16 + 15 < all ? tile * 16 + 15 : all - 1;
-      if (first + last / g.group + 1 < held) seen = first + last / g.group + 1;
-      fewest = first + tile * 16 / g.group + 1;
+      const int last = sq.first + quotient(tile * ROWS + ROWS - 1 < sq.all ? tile * ROWS + ROWS - 1 : sq.all - 1, g.group) + 1;
+      if (last < sq.held) seen = last;
+      fewest = sq.first + quotient(tile * ROWS, g.group) + 1;
     }
     if (seen < 0) seen = 0;
-    const int64_t len = run_length(seen, g.splits, g.least), k_lo = blockIdx.x * len, k_hi = k_lo + len < seen ? k_lo + len : seen;
+    const int len = run_length(seen, g.splits, g.least), k_lo = (int)blockIdx.x * len < seen ? blockIdx.x * len : seen;
+    const int k_hi = seen - k_lo < len ? seen : k_lo + len;
 
-    bf16x8 qf[FR][NT];
-#pragma unroll
-    for (int f = 0; f < FR; ++f) {
-      const int d = f < 2 * W16 ? f / 2 * 64 + quarter * 16 + f % 2 * 8 : W16 * 64 + quarter * 8;
-      float v[8];
-      load8((const T*)g.q + row * g.ldq + (int64_t)head * HD + d, v);
-      to_terms(v, qf[f]);
-    }
-    f32x4 o[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
-
-    for (int64_t k0 = k_lo + wave * 64; k0 < k_hi; k0 += 256) {
-      // a lane reads keys of block c16 / 4 of the step and the values of block `quarter`
-      const int64_t kb = k0 / kBlock + c16 / 4, vb = k0 / kBlock + quarter;
-      int64_t kp = -1, vp = -1;
-      if (kb * kBlock < k_hi) kp = table[kb / blocks];
-      if (vb * kBlock < k_hi) vp = table[vb / blocks];
-      const bool have_k = kp >= 0 && kp < g.cache.pages, have_v = vp >= 0 && vp < g.cache.pages;
-      const uint8_t* kc = kbase + kp * g.cache.stride_page + (kb % blocks * kBlock + c16 % 4) * HD;
-      const uint8_t* vc = vbase + vp * g.cache.stride_page + (vb % blocks * HD + c16) * kBlock;
-      float ks = 0.f, vs = 0.f;
-      if (have_v) {
-        const int64_t at = vp * g.cache.stride_scale + kvh * blocks + vb % blocks;
-        ks = g.cache.k_scale[at] * g.scale;
-        vs = g.cache.v_scale[at];
-      }
-      f32x4 s[4];
+    // page numbers of the step at key k0 (-1 behind the run's end), and where its codes lie
+    auto number = [&](int k0, int block) {
+      const int b = k0 / kBlock + block;
+      return b * kBlock < k_hi ? table[quotient(b, g.blocks)] : -1;
+    };
+    auto offset = [&](int k0, int block, int page, int64_t stride, int in_block) {
+      const int b = k0 / kBlock + block, in_page = b - quotient(b, g.blocks) * blocks;
+      return page >= 0 && page < g.cache.pages ? page * stride + in_page * in_block : (int64_t)-1;
+    };
+    u32x4 kw[4][W16 + 1];
+    u32x2 kr[4];
+    auto load_keys = [&](int64_t at) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        u32x4 kw[W16 + 1];
+        const uint8_t* kc = kbase + at + j * 4 * HD;
 #pragma unroll
-        for (int i = 0; i < W16; ++i) kw[i] = have_k ? *reinterpret_cast<const u32x4*>(kc + j * 4 * HD + i * 64 + quarter * 16) : u32x4{0, 0, 0, 0};
-        u32x2 kr = {0, 0};
-        if (REST && have_k) kr = *reinterpret_cast<const u32x2*>(kc + j * 4 * HD + W16 * 64 + quarter * 8);
-#pragma unroll
-        for (int f = 0; f < FR; ++f) {
-          const bf16x8 kf = f < 2 * W16 ? codes_bf16(kw[f / 2][f % 2 * 2], kw[f / 2][f % 2 * 2 + 1]) : codes_bf16(kr[0], kr[1]);
-#pragma unroll
-          for (int u = NT - 1; u >= 0; --u) s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[f][u], s[j], 0, 0, 0);
-        }
+        for (int i = 0; i < W16; ++i) kw[j][i] = at >= 0 ? *reinterpret_cast<const u32x4*>(kc + i * 64) : u32x4{0, 0, 0, 0};
+        kr[j] = REST && at >= 0 ? *reinterpret_cast<const u32x2*>(kc + W16 * 64 - quarter * 8) : u32x2{0, 0};
       }
+    };
+
+    int k0 = k_lo + wave * 64;
+    int kp = number(k0, c16 / 4), vp = number(k0, quarter), kp2 = number(k0 + 256, c16 / 4), vp2 = number(k0 + 256, quarter);
+    bf16x8 qf[RT][FR][NT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const int r = tile * ROWS + t * 16 + c16, rr = r < sq.all ? r : sq.all - 1, rq = quotient(rr, g.group);
+      sees[t] = r >= sq.all ? 0 : g.causal ? sq.first + rq + 1 : sq.held;
+#pragma unroll
+      for (int f = 0; f < FR; ++f) {
+        const int d = f < 2 * W16 ? f / 2 * 64 + quarter * 16 + f % 2 * 8 : W16 * 64 + quarter * 8;
+        float v[8];
+        load8((const T*)g.q + (sq.begin + rq) * g.ldq + (int64_t)(kvh * group + rr - rq * group) * HD + d, v);
+        to_terms(v, qf[t][f]);
+      }
+    }
+    load_keys(offset(k0, c16 / 4, kp, g.cache.stride_page, kBlock * HD));
+    f32x4 o[RT][DT];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      m[t] = -INFINITY;
+      l[t] = 0.f;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    for (; k0 < k_hi; k0 += 256) {
+      const int64_t va = offset(k0, quarter, vp, g.cache.stride_page, kBlock * HD);
+      const int64_t sa = offset(k0, quarter, vp, g.cache.stride_scale, 1);
       u32x4 vw[DT];
 #pragma unroll
-      for (int d = 0; d < DT; ++d) vw[d] = have_v ? *reinterpret_cast<const u32x4*>(vc + d * 16 * kBlock) : u32x4{0, 0, 0, 0};
+      for (int d = 0; d < DT; ++d) vw[d] = va >= 0 ? *reinterpret_cast<const u32x4*>(vbase + va + d * 16 * kBlock) : u32x4{0, 0, 0, 0};
+      const float ks = sa >= 0 ? g.cache.k_scale[sa + kvh * blocks] * g.scale : 0.f, vs = sa >= 0 ? g.cache.v_scale[sa + kvh * blocks] : 0.f;
+      const int kp3 = number(k0 + 512, c16 / 4), vp3 = number(k0 + 512, quarter);
 
-      const int64_t left = (have_v ? sees : 0) - vb * kBlock;      // of this lane's block, the tokens its row sees
-      float big = -INFINITY;
+      f32x4 s[RT][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 4; ++j) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[j][i] = 4 * j + i < left ? s[j][i] * ks : -INFINITY;
-          big = fmaxf(big, s[j][i]);
+        for (int t = 0; t < RT; ++t) s[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int f = 0; f < FR; ++f) {
+          const bf16x8 kf = f < 2 * W16 ? codes_bf16(kw[j][f / 2][f % 2 * 2], kw[j][f / 2][f % 2 * 2 + 1]) : codes_bf16(kr[j][0], kr[j][1]);
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int u = NT - 1; u >= 0; --u) s[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][f][u], s[t][j], 0, 0, 0);
         }
-      big = fmaxf(big, __shfl_xor(big, 16, 64));
-      big = fmaxf(big, __shfl_xor(big, 32, 64));
-      const float m_new = fmaxf(m, big), ref = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(m - ref);
-      m = m_new;
-      float p[16], sum = 0.f;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(s[e / 4][e % 4] - ref);
-        sum += p[e];
       }
-      l = fmaf(l, alpha, sum);
-      bf16x8 pf[2][NT];
+      load_keys(offset(k0 + 256, c16 / 4, kp2, g.cache.stride_page, kBlock * HD));
+      kp = kp2; vp = vp2; kp2 = kp3; vp2 = vp3;
+
+      const int vb = (k0 / kBlock + quarter) * kBlock;
+      bf16x8 pf[RT][2][NT];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float pv[8];
+      for (int t = 0; t < RT; ++t) {
+        const int left = (va >= 0 ? sees[t] : 0) - vb;        // of this lane's block, the tokens its row sees
+        float big = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) pv[e] = p[8 * u + e] * vs;
-        to_terms(pv, pf[u]);
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            s[t][j][i] = 4 * j + i < left ? s[t][j][i] * ks : -INFINITY;
+            big = fmaxf(big, s[t][j][i]);
+          }
+        big = fmaxf(big, __shfl_xor(big, 16, 64));
+        big = fmaxf(big, __shfl_xor(big, 32, 64));
+        const float m_new = fmaxf(m[t], big), ref = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f(m[t] - ref);
+        m[t] = m_new;
+        float p[16], sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(s[t][e / 4][e % 4] - ref);
+          sum += p[e];
+        }
+        l[t] = fmaf(l[t], alpha, sum);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          float pv[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) pv[e] = p[8 * u + e] * vs;
+          to_terms(pv, pf[t][u]);
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
       }
-#pragma unroll
-      for (int d = 0; d < DT; ++d) o[d] *= alpha;
       bool poisoned = false;                                         // whether a code that not every row sees is NaN
       if (k0 + 64 > fewest) {
         uint32_t any = 0;
@@ -426,8 +478,8 @@ __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
           // tokens past the last that the tile's rows see may hold anything
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int64_t n = seen - vb * kBlock - 4 * i;
-            vw[d][i] = n >= 4 ? vw[d][i] : n <= 0 ? 0u : vw[d][i] & (0xffffffffu >> (8 * (4 - (int)n)));
+            const int n = seen - vb - 4 * i;
+            vw[d][i] = n >= 4 ? vw[d][i] : n <= 0 ? 0u : vw[d][i] & (0xffffffffu >> (8 * (4 - n)));
             any |= nan_bytes(vw[d][i]);
           }
         }
@@ -440,86 +492,168 @@ __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
           for (int u = 0; u < 2; ++u) {
             const bf16x8 vf = codes_bf16(vw[d][2 * u], vw[d][2 * u + 1]);
 #pragma unroll
-            for (int t = NT - 1; t >= 0; --t) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[u][t], o[d], 0, 0, 0);
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+              for (int x = NT - 1; x >= 0; --x) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t][u][x], o[t][d], 0, 0, 0);
           }
       } else {
         // A NaN times a probability of 0 is NaN, so NaN values are counted apart, among the tokens that a row sees.
-        bf16x8 seen_f[2];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) seen_f[e / 8][e % 8] = e < left ? (bf16_t)1.0f : (bf16_t)0.0f;
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          f32x4 count = {0.f, 0.f, 0.f, 0.f};
+          for (int t = 0; t < RT; ++t) {
+            f32x4 count = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const uint32_t n0 = nan_bytes(vw[d][2 * u]), n1 = nan_bytes(vw[d][2 * u + 1]);
-            const bf16x8 vf = codes_bf16(vw[d][2 * u] & ~n0, vw[d][2 * u + 1] & ~n1);
-            const bf16x8 nf = codes_bf16(n0 & 0x38383838u, n1 & 0x38383838u);      // 0x38 is 1
+            for (int u = 0; u < 2; ++u) {
+              const uint32_t n0 = nan_bytes(vw[d][2 * u]), n1 = nan_bytes(vw[d][2 * u + 1]);
+              const bf16x8 vf = codes_bf16(vw[d][2 * u] & ~n0, vw[d][2 * u + 1] & ~n1);
+              const bf16x8 nf = codes_bf16(n0 & 0x38383838u, n1 & 0x38383838u);      // 0x38 is 1
+              bf16x8 seen_f;
 #pragma unroll
-            for (int t = NT - 1; t >= 0; --t) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[u][t], o[d], 0, 0, 0);
-            count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf, seen_f[u], count, 0, 0, 0);
+              for (int e = 0; e < 8; ++e) seen_f[e] = 8 * u + e < sees[t] - vb ? (bf16_t)1.0f : (bf16_t)0.0f;
+#pragma unroll
+              for (int x = NT - 1; x >= 0; --x) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t][u][x], o[t][d], 0, 0, 0);
+              count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf, seen_f, count, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (count[i] > 0.f) o[t][d][i] = __builtin_nanf("");
           }
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (count[i] > 0.f) o[d][i] = __builtin_nanf("");
-        }
       }
     }
 
-    // join the four waves
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
+    // join the four waves, 16 rows at a time
     float* ml = joined + 4 * 16 * HD;
 #pragma unroll
-    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(&joined[(wave * 16 + c16) * HD + d * 16 + quarter * 4]) = o[d];
-    if (quarter == 0) { ml[(wave * 16 + c16) * 2] = m; ml[(wave * 16 + c16) * 2 + 1] = l; }
-    __syncthreads();
-    for (int e = threadIdx.x; e < 16 * HD; e += 256) {
-      const int rt = e / HD, d = e % HD;
-      const int64_t rq = tile * 16 + rt;
-      if (rq >= all) continue;
-      float top = ml[rt * 2];
+    for (int t = 0; t < RT; ++t) {
+      l[t] += __shfl_xor(l[t], 16, 64);
+      l[t] += __shfl_xor(l[t], 32, 64);
 #pragma unroll
-      for (int u = 1; u < 4; ++u) top = fmaxf(top, ml[(u * 16 + rt) * 2]);
-      const float ref = top == -INFINITY ? 0.f : top;
-      float total = 0.f, v = 0.f;
+      for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(&joined[(wave * 16 + c16) * HD + d * 16 + quarter * 4]) = o[t][d];
+      if (quarter == 0) { ml[(wave * 16 + c16) * 2] = m[t]; ml[(wave * 16 + c16) * 2 + 1] = l[t]; }
+      __syncthreads();
+      for (int e = threadIdx.x; e < 16 * HD; e += 256) {
+        const int rt = e / HD, d = e % HD, ro = tile * ROWS + t * 16 + rt;
+        if (ro >= sq.all) continue;
+        float top = ml[rt * 2];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float f = __builtin_amdgcn_exp2f(ml[(u * 16 + rt) * 2] - ref);
-        total = fmaf(f, ml[(u * 16 + rt) * 2 + 1], total);
-        v = fmaf(f, joined[(u * 16 + rt) * HD + d], v);
+        for (int u = 1; u < 4; ++u) top = fmaxf(top, ml[(u * 16 + rt) * 2]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        float total = 0.f, v = 0.f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float f = __builtin_amdgcn_exp2f(ml[(u * 16 + rt) * 2] - ref);
+          total = fmaf(f, ml[(u * 16 + rt) * 2 + 1], total);
+          v = fmaf(f, joined[(u * 16 + rt) * HD + d], v);
+        }
+        const int oq = quotient(ro, g.group), ohead = kvh * group + ro - oq * group;
+        if (g.splits == 1) {
+          Elem<T>::st((T*)g.out + (sq.begin + oq) * g.ldo + (int64_t)ohead * HD + d, total == 0.f ? 0.f : v / total);
+        } else {
+          const int64_t at = (blockIdx.x * g.rows.rows + sq.begin + oq) * g.heads + ohead;
+          g.part_o[at * HD + d] = v;
+          if (d == 0) { g.part_ml[at * 2] = top; g.part_ml[at * 2 + 1] = total; }
+        }
       }
-      const int64_t orow = sq.begin + rq / g.group;
-      const int ohead = kvh * g.group + (int)(rq % g.group);
-      if (g.splits == 1) {
-        Elem<T>::st((T*)g.out + orow * g.ldo + (int64_t)ohead * HD + d, total == 0.f ? 0.f : v / total);
-      } else {
-        const int64_t at = (blockIdx.x * g.rows.rows + orow) * g.heads + ohead;
-        g.part_o[at * HD + d] = v;
-        if (d == 0) { g.part_ml[at * 2] = top; g.part_ml[at * 2 + 1] = total; }
-      }
+      __syncthreads();
     }
-    __syncthreads();
   }
 }
 
-int64_t row_tiles(const ac_cache_rows& r, int group) {
-  int64_t n = r.max_rows < r.rows ? r.max_rows : r.rows;
-  if (n < 1) n = 1;
-  return (n * group + 15) / 16;
+// Joins the runs' parts.  A team of HD / 4 lanes takes every g.teams-th part of one (row, head), each lane four elements; the teams of an item, side
+// by side in a block, then add theirs up in LDS.  Rows that belong to no sequence have no parts and are left alone.
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) cache_attention_join(CacheAttnArgs g) {
+  constexpr int LANES = HD / 4, TEAMS = 256 / LANES;
+  __shared__ float sums[TEAMS][HD + 2];
+  const int team = threadIdx.x / LANES, lane = threadIdx.x % LANES, each = TEAMS / g.teams, mine = team / g.teams, nth = team % g.teams;
+  const int64_t items = g.rows.rows * g.heads, item = (int64_t)blockIdx.x * each + mine, row = item / g.heads;
+  const bool live = mine < each && item < items && row >= g.rows.row_begin[0] && row < g.rows.row_begin[g.rows.batch];
+  float top = -INFINITY, total = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (live) {
+#pragma unroll 4
+    for (int i = nth; i < g.splits; i += g.teams) {
+      const int64_t at = i * items + item;
+      const float mi = g.part_ml[at * 2], li = g.part_ml[at * 2 + 1];
+      const f32x4 o = *reinterpret_cast<const f32x4*>(g.part_o + at * HD + lane * 4);
+      const float next = fmaxf(top, mi), ref = next == -INFINITY ? 0.f : next;
+      const float a = __builtin_amdgcn_exp2f(top - ref), f = __builtin_amdgcn_exp2f(mi - ref);
+      top = next;
+      total = fmaf(total, a, f * li);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(v[e], a, f * o[e]);
+    }
+    float* to = sums[team];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) to[lane * 4 + e] = v[e];
+    if (lane == 0) { to[HD] = top; to[HD + 1] = total; }
+  }
+  __syncthreads();
+  if (!live || nth != 0) return;
+  float ref = top;
+  for (int i = 1; i < g.teams; ++i) ref = fmaxf(ref, sums[team + i][HD]);
+  if (ref == -INFINITY) ref = 0.f;
+  float sum = 0.f, w[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < g.teams; ++i) {
+    const float f = __builtin_amdgcn_exp2f(sums[team + i][HD] - ref);
+    sum = fmaf(f, sums[team + i][HD + 1], sum);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = fmaf(f, sums[team + i][lane * 4 + e], w[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = sum == 0.f ? 0.f : w[e] / sum;
+  store4((T*)g.out + row * g.ldo + (item - row * g.heads) * HD + lane * 4, w);
 }
 
-template <typename T, int HD>
-hipError_t attention_launch(const CacheAttnArgs& a, hipStream_t s) {
-  int64_t tiles = row_tiles(a.rows, a.group);
-  const int64_t most = 65535 / a.cache.heads;
+// Two row tiles a block (where the registers allow) read the keys once for both.
+int tile_rows(const ac_cache_rows& r, const ac_kv_cache& c, int group) {
+  const int64_t n = (r.max_rows < r.rows ? r.max_rows : r.rows) * group;
+  return n > 16 && c.head_dim <= 128 ? 32 : 16;
+}
+int row_tiles(const ac_cache_rows& r, const ac_kv_cache& c, int group) {
+  const int64_t n = (r.max_rows < r.rows ? r.max_rows : r.rows) * group, rows = tile_rows(r, c, group);
+  return n < 1 ? 1 : (int)((n + rows - 1) / rows);
+}
+
+// Runs of keys: as many as fill the chip, and no longer than kLongRun, so that sequences of all lengths, of which the host knows only the longest,
+// keep it filled to the end.
+constexpr int kMostSplits = 128, kLeastRun = 256, kLongRun = 2048, kPlaces = 1024;
+int key_splits(int heads, const ac_kv_cache& c, const ac_cache_rows& r) {
+  const int64_t blocks = (int64_t)row_tiles(r, c, heads / c.heads) * c.heads * r.batch;
+  int64_t n = blocks > 0 ? kPlaces / blocks : 1;
+  if (r.batch > 1 && n < r.max_length / kLongRun) n = r.max_length / kLongRun;
+  const int64_t most = (r.max_length + kLeastRun - 1) / kLeastRun;
+  if (n > most) n = most;
+  if (n > kMostSplits) n = kMostSplits;
+  return n < 1 ? 1 : (int)n;
+}
+
+template <typename T, int HD, int RT>
+hipError_t attention_rows_launch(const CacheAttnArgs& a, hipStream_t s) {
+  int tiles = row_tiles(a.rows, a.cache, a.group.d);
+  const int most = 65535 / a.cache.heads;
   if (tiles > most) tiles = most;
   const dim3 grid((unsigned)a.splits, (unsigned)(tiles * a.cache.heads), (unsigned)a.rows.batch);
   constexpr size_t lds = (size_t)(4 * 16 * HD + 4 * 16 * 2) * sizeof(float);
-  static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(cache_attention<T, HD>),
+  static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(cache_attention<T, HD, RT>),
                                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (attr_status != hipSuccess) return attr_status;
-  hipLaunchKernelGGL((cache_attention<T, HD>), grid, dim3(256), lds, s, a);
+  hipLaunchKernelGGL((cache_attention<T, HD, RT>), grid, dim3(256), lds, s, a);
+  return hipGetLastError();
+}
+
+template <typename T, int HD>
+hipError_t attention_launch(CacheAttnArgs a, hipStream_t s) {
+  hipError_t e;
+  if (HD <= 128 && tile_rows(a.rows, a.cache, a.group.d) == 32)
+    e = attention_rows_launch<T, HD, HD <= 128 ? 2 : 1>(a, s);
+  else
+    e = attention_rows_launch<T, HD, 1>(a, s);
+  if (e != hipSuccess || a.splits == 1) return e;
+  constexpr int TEAMS = 256 / (HD / 4);
+  a.teams = a.splits / 4 < 1 ? 1 : a.splits / 4 > TEAMS ? TEAMS : a.splits / 4;
+  const int64_t items = a.rows.rows * a.heads, each = TEAMS / a.teams;
+  hipLaunchKernelGGL((cache_attention_join<T, HD>), dim3((unsigned)((items + each - 1) / each)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -570,12 +704,18 @@ hipError_t launch_cache_append(const void* q, int64_t ldq, void* q_out, int64_t 
   return dtype == AC_BF16 ? append_width<bf16_t>(a, s) : append_width<float>(a, s);
 }
 
-uint64_t cache_attention_workspace_bytes(int heads, const ac_kv_cache& cache, const ac_cache_rows& rows, int causal, int dtype) { return 0; }
+uint64_t cache_attention_workspace_bytes(int heads, const ac_kv_cache& cache, const ac_cache_rows& rows, int causal, int dtype) {
+  const int n = key_splits(heads, cache, rows);
+  return n == 1 ? 0 : (uint64_t)n * rows.rows * heads * (cache.head_dim + 2) * sizeof(float);
+}
 
 hipError_t launch_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int heads, const ac_kv_cache& cache,
                                   const ac_cache_rows& rows, int causal, float scale, void* workspace, int dtype, hipStream_t s) {
   if (rows.batch <= 0 || rows.rows <= 0) return hipSuccess;
-  CacheAttnArgs a{q, out, ldq, ldo, heads, heads / cache.heads, cache, rows, causal, scale * kLog2e, 1, 64, nullptr, nullptr};
+  const int n = key_splits(heads, cache, rows);
+  float* parts = (float*)workspace;
+  CacheAttnArgs a{q, out, ldq, ldo, heads, cache, rows, causal, scale * kLog2e, divisor(heads / cache.heads), divisor(cache.page / kBlock),
+                  n, kLeastRun, parts, n > 1 ? parts + (uint64_t)n * rows.rows * heads * cache.head_dim : nullptr, 1};
   return dtype == AC_BF16 ? attention_width<bf16_t>(a, s) : attention_width<float>(a, s);
 }
 

@@ -2192,8 +2192,8 @@ static int cache_ok(const char* what, const ac_kv_cache* c, const ac_cache_rows*
       c->heads > 4096 || c->head_dim < 1 || !r->row_begin || !r->length || !r->page_table || r->ld_page_table < 0 || r->batch < 0 || r->rows < 0 ||
       r->max_rows < 0 || r->max_length < 0)
     return fail(AC_ERR_ARG, "%s: bad cache or rows", what);
-  if (r->batch > 65535 || r->rows > 0x7fffffffll || r->max_length > 0x7fffffffll)
-    return fail(AC_ERR_UNSUPPORTED, "%s: at most 65535 sequences, 2^31 - 1 rows and tokens", what);
+  if (r->batch > 65535 || r->rows > 1 << 30 || r->max_length > 1 << 30 || r->ld_page_table > (1 << 30) / c->page)
+    return fail(AC_ERR_UNSUPPORTED, "%s: at most 65535 sequences, 2^30 rows and places of a sequence", what);
   const int d = c->head_dim;
   if (d != 32 && d != 64 && d != 96 && d != 128 && d != 192 && d != 256)
     return fail(AC_ERR_UNSUPPORTED, "%s: heads of 32, 64, 96, 128, 192 or 256", what);
@@ -2254,6 +2254,7 @@ int ac_op_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, in
   if (!q || !out || heads < 1 || heads > 65536 || heads % cache->heads != 0 || ldq < (int64_t)heads * cache->head_dim ||
       ldo < (int64_t)heads * cache->head_dim || !(scale > 0.f) || !(scale < INFINITY) || !dtype_ok(dtype))
     return fail(AC_ERR_ARG, "%s: bad argument", what);
+  if (rows->rows * heads > 1 << 30) return fail(AC_ERR_UNSUPPORTED, "%s: at most 2^30 rows times heads", what);
   if (!rows_on(q, ldq, 16, dtype) || !rows_on(out, ldo, 16, dtype))
     return fail(AC_ERR_ALIGN, "%s: rows start at multiples of 16 bytes", what);
   const uint64_t need = cache_attention_workspace_bytes(heads, *cache, *rows, causal != 0, dtype);

@@ -73,7 +73,7 @@ for what in (attention, append):
     for r in (dict(row_begin=None), dict(length=None), dict(page_table=None), dict(ld_page_table=-1), dict(batch=-1), dict(rows=-1), dict(max_rows=-1),
               dict(max_length=-1)):
         refused(B.AC_ERR_ARG, what=what, r=rows(**r))
-    for r in (dict(batch=65536), dict(rows=1 << 31), dict(max_length=1 << 31)):
+    for r in (dict(batch=65536), dict(rows=(1 << 30) + 1), dict(max_length=(1 << 30) + 1), dict(ld_page_table=(1 << 25) + 1)):
         refused(B.AC_ERR_UNSUPPORTED, what=what, r=rows(**r))
     refused(B.AC_ERR_UNSUPPORTED, what=what, c=cache(head_dim=80, stride_page=1 << 20))
     for c in (dict(k=(1 << 40) + 8), dict(v=(1 << 40) + 8), dict(stride_page=2 * 32 * 64 + 8)):

@@ -10,13 +10,13 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_NAME = "libautochunk_rt.so"
 LIB_PATH = os.path.join(HERE, LIB_NAME)
 
-SOURCES = ["rowwise.hip", "linear.hip", "pair.hip", "layer_f32.hip", "attention.hip", "linear_w4.hip", "cache.hip", "runtime.hip", "search.hip"]
+SOURCES = ["rowwise.hip", "linear.hip", "pair.hip", "layer_f32.hip", "attention.hip", "linear_w4.hip", "cache.hip", "cache_prefill.hip", "runtime.hip", "search.hip"]
 
-# Per-file extras.  attention.hip, cache.hip: keep MFMA results in VGPRs; the softmax reads every score
+# Per-file extras.  attention.hip, cache*.hip: keep MFMA results in VGPRs; the softmax reads every score
 # right after the matrix op, and accumulator-register copies would double its VALU work.
 # search.hip (host only): its cost function is compared bit for bit, so no fused multiply-adds.
-EXTRA_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "cache.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-               "search.hip": ["-ffp-contract=off"]}
+VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+EXTRA_FLAGS = {"attention.hip": VGPR_FORM, "cache.hip": VGPR_FORM, "cache_prefill.hip": VGPR_FORM, "search.hip": ["-ffp-contract=off"]}
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",

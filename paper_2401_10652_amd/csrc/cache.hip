@@ -4,24 +4,11 @@
 // Why a power of two: a block fills token by token, and where a later token asks for a larger scale the older codes move by whole
 // exponents, exactly but for subnormal ones; with any other scale each move would round once more.  Why 16 tokens: the quarters of a
 // wave then hold one block each, see the attention.
-#include "common.h"
+#include "cache.h"
 
 namespace ac {
 
 namespace {
-
-constexpr int kBlock = 16;
-constexpr float kLog2e = 1.4426950408889634f;
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-struct Sequence { int64_t begin, rows, length; };   // its first row, its rows, its tokens with them
-
-__device__ __forceinline__ Sequence sequence(const ac_cache_rows& r, int64_t b) {
-  const int64_t lo = r.row_begin[b], hi = r.row_begin[b + 1];
-  const int64_t from = lo < 0 ? 0 : lo, to = hi < r.rows ? hi : r.rows, n = r.length[b];
-  return Sequence{from, to > from ? to - from : 0, n > 0 ? n : 0};
-}
 
 // ---- append ----------------------------------------------------------------------------------------------------------
 
@@ -274,62 +261,6 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
 }
-
-// Eight e4m3 codes as bf16, which holds each exactly.
-__device__ __forceinline__ bf16x8 codes_bf16(uint32_t lo, uint32_t hi) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
-  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-// The bytes of a word that are NaN, as 0xff each.
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
-  const uint32_t m = (w & 0x7f7f7f7fu) + 0x01010101u;      // bit 7 of a byte: its low seven bits were all ones
-  return (m >> 7 & 0x01010101u) * 0xffu;
-}
-
-// n / d for n < 2^31 by one multiplication and one addition: with l = ceil(log2 d), the quotient is (hi32(n * mul) + n) >> l for
-// mul = floor(2^32 (2^l - d) / d) + 1 (Granlund and Montgomery, "Division by invariant integers using multiplication", 1994).
-struct Divisor { uint32_t d, mul, shift; };
-Divisor divisor(uint32_t d) {
-  uint32_t l = 0;
-  while ((1ull << l) < d) ++l;
-  return Divisor{d, (uint32_t)((((1ull << l) - d) << 32) / d + 1), l};
-}
-__device__ __forceinline__ int quotient(int n, const Divisor& v) { return (int)((__umulhi((uint32_t)n, v.mul) + (uint32_t)n) >> v.shift); }
-
-struct CacheAttnArgs {
-  const void* q; void* out;
-  int64_t ldq, ldo;
-  int heads;
-  ac_kv_cache cache;
-  ac_cache_rows rows;
-  int causal;
-  float scale;                      // times log2 e
-  Divisor group, blocks;            // query heads of a key head, blocks of a page
-  int splits, least;                // runs of keys, and the fewest keys of one (a multiple of 256)
-  float* part_o; float* part_ml;    // [splits][rows][heads][head_dim], [splits][rows][heads][2]
-  int teams;                        // that share the parts of one row and head
-};
-
-// The keys of one of `splits` runs over `seen` keys: runs of the same length, whole steps of a block's four waves.
-__device__ __forceinline__ int run_length(int seen, int splits, int least) {
-  const int even = (seen + splits - 1) / splits, n = (even + 255) / 256 * 256;
-  return n > least ? n : least;
-}
-
-// What a sequence's rows see: the rows of a tile are (row of the sequence, query head of the key head), head fastest.
-struct Sight {
-  int begin, rows, first, held, all;     // first row, rows, token of row 0, tokens that have a place, rows times heads
-  __device__ Sight(const CacheAttnArgs& g, int b) {
-    const Sequence s = sequence(g.rows, b);
-    const int64_t most = g.rows.ld_page_table * g.cache.page;
-    begin = (int)s.begin;
-    rows = (int)s.rows;
-    first = (int)(s.length - s.rows);
-    held = (int)(s.length < most ? s.length : most);
-    all = rows * (int)g.group.d;
-  }
-};
 
 // One block: 16 RT query rows over one run of keys, in steps of 64 that its four waves take in turn.  S^T = K Q^T and O^T = V^T P^T, both by
 // v_mfma_f32_16x16x32_bf16 with a query row to a column, so a lane holds probabilities of one row and the running maximum and sum are
@@ -605,32 +536,30 @@ __global__ void __launch_bounds__(256) cache_attention_join(CacheAttnArgs g) {
   store4((T*)g.out + row * g.ldo + (item - row * g.heads) * HD + lane * 4, w);
 }
 
-// Two row tiles a block (where the registers allow) read the keys once for both.
-int tile_rows(const ac_cache_rows& r, const ac_kv_cache& c, int group) {
-  const int64_t n = (r.max_rows < r.rows ? r.max_rows : r.rows) * group;
-  return n > 16 && c.head_dim <= 128 ? 32 : 16;
-}
-int row_tiles(const ac_cache_rows& r, const ac_kv_cache& c, int group) {
-  const int64_t n = (r.max_rows < r.rows ? r.max_rows : r.rows) * group, rows = tile_rows(r, c, group);
-  return n < 1 ? 1 : (int)((n + rows - 1) / rows);
-}
+// How a call is computed: rows in tiles of 16 or 32, or of 128 by the kernel for prompts; and runs of keys.
+struct Shape { int rows, tiles, splits; };
 
 // Runs of keys: as many as fill the chip, and no longer than kLongRun, so that sequences of all lengths, of which the host knows only the longest,
 // keep it filled to the end.
-constexpr int kMostSplits = 128, kLeastRun = 256, kLongRun = 2048, kPlaces = 1024;
-int key_splits(int heads, const ac_kv_cache& c, const ac_cache_rows& r) {
-  const int64_t blocks = (int64_t)row_tiles(r, c, heads / c.heads) * c.heads * r.batch;
-  int64_t n = blocks > 0 ? kPlaces / blocks : 1;
-  if (r.batch > 1 && n < r.max_length / kLongRun) n = r.max_length / kLongRun;
+constexpr int kMostSplits = 128, kLeastRun = 256, kLongRun = 2048, kPlaces = 1024, kPromptPlaces = 256, kPromptRows = 64;
+Shape shape(int heads, const ac_kv_cache& c, const ac_cache_rows& r, int dtype) {
+  const int64_t rows = (r.max_rows < r.rows ? r.max_rows : r.rows) * (heads / c.heads);
+  const bool prompt = dtype == AC_BF16 && c.pages > 0 && rows > kPromptRows;
+  Shape s;
+  s.rows = prompt ? 128 : rows > 16 && c.head_dim <= 128 ? 32 : 16;      // (two tiles of 16, where the registers allow, read the keys once for both)
+  s.tiles = rows < 1 ? 1 : (int)((rows + s.rows - 1) / s.rows);
+  const int64_t blocks = (int64_t)s.tiles * c.heads * r.batch;
+  int64_t n = blocks > 0 ? (prompt ? kPromptPlaces : kPlaces) / blocks : 1;
+  if (!prompt && r.batch > 1 && n < r.max_length / kLongRun) n = r.max_length / kLongRun;
   const int64_t most = (r.max_length + kLeastRun - 1) / kLeastRun;
   if (n > most) n = most;
   if (n > kMostSplits) n = kMostSplits;
-  return n < 1 ? 1 : (int)n;
+  s.splits = n < 1 ? 1 : (int)n;
+  return s;
 }
 
 template <typename T, int HD, int RT>
-hipError_t attention_rows_launch(const CacheAttnArgs& a, hipStream_t s) {
-  int tiles = row_tiles(a.rows, a.cache, a.group.d);
+hipError_t attention_rows_launch(const CacheAttnArgs& a, int tiles, hipStream_t s) {
   const int most = 65535 / a.cache.heads;
   if (tiles > most) tiles = most;
   const dim3 grid((unsigned)a.splits, (unsigned)(tiles * a.cache.heads), (unsigned)a.rows.batch);
@@ -643,12 +572,11 @@ hipError_t attention_rows_launch(const CacheAttnArgs& a, hipStream_t s) {
 }
 
 template <typename T, int HD>
-hipError_t attention_launch(CacheAttnArgs a, hipStream_t s) {
+hipError_t attention_launch(CacheAttnArgs a, const Shape& shape, hipStream_t s) {
   hipError_t e;
-  if (HD <= 128 && tile_rows(a.rows, a.cache, a.group.d) == 32)
-    e = attention_rows_launch<T, HD, HD <= 128 ? 2 : 1>(a, s);
-  else
-    e = attention_rows_launch<T, HD, 1>(a, s);
+  if (shape.rows == 128) e = launch_cache_prefill(a, shape.tiles, s);
+  else if (shape.rows == 32) e = attention_rows_launch<T, HD, HD <= 128 ? 2 : 1>(a, shape.tiles, s);
+  else e = attention_rows_launch<T, HD, 1>(a, shape.tiles, s);
   if (e != hipSuccess || a.splits == 1) return e;
   constexpr int TEAMS = 256 / (HD / 4);
   a.teams = a.splits / 4 < 1 ? 1 : a.splits / 4 > TEAMS ? TEAMS : a.splits / 4;
@@ -658,14 +586,14 @@ hipError_t attention_launch(CacheAttnArgs a, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t attention_width(const CacheAttnArgs& a, hipStream_t s) {
+hipError_t attention_width(const CacheAttnArgs& a, const Shape& shape, hipStream_t s) {
   switch (a.cache.head_dim) {
-    case 32: return attention_launch<T, 32>(a, s);
-    case 64: return attention_launch<T, 64>(a, s);
-    case 96: return attention_launch<T, 96>(a, s);
-    case 128: return attention_launch<T, 128>(a, s);
-    case 192: return attention_launch<T, 192>(a, s);
-    case 256: return attention_launch<T, 256>(a, s);
+    case 32: return attention_launch<T, 32>(a, shape, s);
+    case 64: return attention_launch<T, 64>(a, shape, s);
+    case 96: return attention_launch<T, 96>(a, shape, s);
+    case 128: return attention_launch<T, 128>(a, shape, s);
+    case 192: return attention_launch<T, 192>(a, shape, s);
+    case 256: return attention_launch<T, 256>(a, shape, s);
     default: return hipErrorNotSupported;
   }
 }
@@ -705,18 +633,19 @@ hipError_t launch_cache_append(const void* q, int64_t ldq, void* q_out, int64_t 
 }
 
 uint64_t cache_attention_workspace_bytes(int heads, const ac_kv_cache& cache, const ac_cache_rows& rows, int causal, int dtype) {
-  const int n = key_splits(heads, cache, rows);
+  const int n = shape(heads, cache, rows, dtype).splits;
   return n == 1 ? 0 : (uint64_t)n * rows.rows * heads * (cache.head_dim + 2) * sizeof(float);
 }
 
 hipError_t launch_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int heads, const ac_kv_cache& cache,
                                   const ac_cache_rows& rows, int causal, float scale, void* workspace, int dtype, hipStream_t s) {
   if (rows.batch <= 0 || rows.rows <= 0) return hipSuccess;
-  const int n = key_splits(heads, cache, rows);
+  const Shape sh = shape(heads, cache, rows, dtype);
+  const int n = sh.splits;
   float* parts = (float*)workspace;
   CacheAttnArgs a{q, out, ldq, ldo, heads, cache, rows, causal, scale * kLog2e, divisor(heads / cache.heads), divisor(cache.page / kBlock),
                   n, kLeastRun, parts, n > 1 ? parts + (uint64_t)n * rows.rows * heads * cache.head_dim : nullptr, 1};
-  return dtype == AC_BF16 ? attention_width<bf16_t>(a, s) : attention_width<float>(a, s);
+  return dtype == AC_BF16 ? attention_width<bf16_t>(a, sh, s) : attention_width<float>(a, sh, s);
 }
 
 }  // namespace ac

@@ -321,6 +321,14 @@ def test_attention_over_many_tokens(B, dtype, counts, lengths):
     attention_case(B, dtype, counts, lengths, 4, 2, 64, 32, seed=31)
 
 
+@pytest.mark.parametrize("d", [32, 64, 96, 128, 192, 256])
+@pytest.mark.parametrize("counts,lengths,heads,heads_kv,page,causal", [
+    ([65], [65], 1, 1, 16, True), ([150], [700], 2, 1, 48, True), ([128], [333], 1, 1, 32, False), ([257, 3, 0, 90], [257, 1400, 0, 95], 2, 2, 64, True),
+    ([31], [1029], 9, 3, 16, True)])
+def test_attention_prompts(B, d, counts, lengths, heads, heads_kv, page, causal):
+    attention_case(B, "bf16", counts, lengths, heads, heads_kv, d, page, causal, seed=d)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_attention_forms(B, dtype):
     attention_case(B, dtype, [3, 20], [90, 50], 4, 2, 64, 32, seed=1, gap=48)                           # pages apart

@@ -34,7 +34,7 @@ __device__ __forceinline__ bf16x8 scaled_bf16(uint32_t lo, uint32_t hi, float s)
 // Two waves of 256 registers share a SIMD where that is enough for the sums of a row, else one has it alone.
 template <int HD> constexpr int sides() { return HD <= 128 ? 2 : 1; }
 template <int HD> constexpr size_t lds_bytes() {
-  constexpr size_t ring = (size_t)sides<HD>() * 4 * kTile * HD, join = sides<HD>() == 2 ? (size_t)kRowsOfBlock * (HD + 2) * sizeof(float) : 0;
+  constexpr size_t ring = (size_t)sides<HD>() * (4 * kTile * HD + 64) + (HD + 1) * sizeof(int), join = sides<HD>() == 2 ? (size_t)kRowsOfBlock * (HD + 2) * sizeof(float) : 0;
   return ring > join ? ring : join;
 }
 
@@ -49,14 +49,13 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
   const Sight sq(g, blockIdx.z);
   // most keys first
   const int tiles = (sq.all + kRowsOfBlock - 1) / kRowsOfBlock;
-  // (read through the scalar cache: this kernel writes none of them)
-  const auto* table = (const __attribute__((address_space(4))) int32_t*)g.rows.page_table + blockIdx.z * g.rows.ld_page_table;
-  const auto* k_scale = (const __attribute__((address_space(4))) float*)g.cache.k_scale;
-  const auto* v_scale = (const __attribute__((address_space(4))) float*)g.cache.v_scale;
+  const int32_t* table = g.rows.page_table + blockIdx.z * g.rows.ld_page_table;
   const uint32_t n_pages = (uint32_t)min(g.cache.pages, (int64_t)0x7fffffff);
   const uint8_t* kbase = (const uint8_t*)g.cache.k + (int64_t)kvh * g.cache.page * HD;
   const uint8_t* vbase = (const uint8_t*)g.cache.v + (int64_t)kvh * g.cache.page * HD;
   uint8_t* const ring = smem + side * 4 * TILE;        // two tiles of keys, two of values
+  float* const scales = reinterpret_cast<float*>(smem + SIDES * 4 * TILE) + side * 16;
+  int* const nan_at = reinterpret_cast<int*>(smem + SIDES * (4 * TILE + 64));    // of each element the first token with a NaN value; [HD]: of all
   const int k_block = lane >> 2 & 1, k_token = 4 * (l32 >> 3) + (lane & 3);      // what row l32 of a tile of 32 keys is
 
   for (int nth = blockIdx.y; nth < tiles; nth += gridDim.y) {
@@ -74,72 +73,86 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
     const int limit = min(wave_seen, k_hi);
     const int mine = limit > key_of(0) ? ((limit - k_lo + kTile - 1) / kTile - side + SIDES - 1) / SIDES : 0;    // steps with keys that this wave's rows see
 
-    // The four blocks of a tile: their pages' numbers (-1 behind the run's end), and from these their scales and where their codes lie, all in scalar
-    // registers.  A block that is not there is read from the first page, and its scores are masked.
-    struct Pages { int n[4]; };
-    struct Scales { float k[4], v[4]; int there; };    // there: bit b, block b
-    auto pages_of = [&](int step) __attribute__((always_inline)) {
-      Pages p;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int b = key_of(step) / kBlock + i;
-        p.n[i] = b * kBlock < k_hi ? table[quotient(b, g.blocks)] : -1;
-      }
-      return p;
+    // Lane x keeps the books of block x mod 4 of a tile: its page's number (-1 behind the run's end), and from it where its codes and scales lie.  A
+    // block that is not there is read from the first page, and its scores are masked.
+    auto number = [&](int step) __attribute__((always_inline)) {
+      const int b = key_of(step) / kBlock + (lane & 3);
+      return b * kBlock < k_hi ? table[quotient(b, g.blocks)] : -1;
     };
-    auto place_of = [&](int step, int i, int page, int64_t stride, int each) {
-      const int b = key_of(step) / kBlock + i;
-      return (uint32_t)page < n_pages ? page * stride + (b - quotient(b, g.blocks) * blocks) * each : (int64_t)0;
-    };
-    auto scales_of = [&](int step, const Pages& p) __attribute__((always_inline)) {
-      Scales s;
-      s.there = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t at = place_of(step, i, p.n[i], g.cache.stride_scale, 1) + kvh * blocks;
-        const bool there = (uint32_t)p.n[i] < n_pages;
-        s.k[i] = there ? k_scale[at] : 1.f;
-        s.v[i] = there ? v_scale[at] : 1.f;
-        s.there |= there ? 1 << i : 0;
-      }
-      return s;
+    struct Place { int64_t codes, scale; int there; };     // bytes and floats from the key head's first; there: bit i, block i (the same for all lanes)
+    auto place_of = [&](int step, int page) __attribute__((always_inline)) {
+      const int b = key_of(step) / kBlock + (lane & 3), in_page = b - quotient(b, g.blocks) * blocks;
+      const bool have = (uint32_t)page < n_pages;
+      const int64_t p = have ? page : 0, i = have ? in_page : 0;
+      return Place{p * g.cache.stride_page + i * BLOCK, p * g.cache.stride_scale + i, (int)(__ballot(have) & 15)};
     };
     // 1 KB a load, the four waves of a side in turn
-    auto load = [&](const uint8_t* from, bool values, uint8_t* to, int step, const Pages& p) __attribute__((always_inline)) {
+    auto load = [&](const uint8_t* from, bool values, uint8_t* to, const Place& p) __attribute__((always_inline)) {
+      const int lo = (int)(uint32_t)p.codes, hi = (int)(p.codes >> 32);
 #pragma unroll
       for (int n = 0; n < (CHUNKS + 3) / 4; ++n) {
-        const int chunk = n * 4 + rowset;
+        const int chunk = n * 4 + rowset, at = chunk * 1024 + lane * 16;
         if (CHUNKS % 4 != 0 && chunk >= CHUNKS) break;
-        int64_t off;
-        if (HD >= 64) {
-          const int i = chunk * 1024 / BLOCK;
-          off = place_of(step, i, i == 0 ? p.n[0] : i == 1 ? p.n[1] : i == 2 ? p.n[2] : p.n[3], g.cache.stride_page, BLOCK);
-          if (1024 % BLOCK != 0 && BLOCK % 1024 != 0) {       // (a KB of two blocks, with heads of 96)
-            const int j = min(i + 1, 3), edge = (i + 1) * BLOCK - chunk * 1024;
-            const int64_t other = place_of(step, j, j == 1 ? p.n[1] : j == 2 ? p.n[2] : p.n[3], g.cache.stride_page, BLOCK);
-            if (lane * 16 >= edge) off = other;
-          }
-        } else {
-          const int64_t even = place_of(step, 2 * chunk, chunk == 0 ? p.n[0] : p.n[2], g.cache.stride_page, BLOCK);
-          const int64_t odd = place_of(step, 2 * chunk + 1, chunk == 0 ? p.n[1] : p.n[3], g.cache.stride_page, BLOCK);
-          off = half ? odd : even;
-        }
-        const int at = chunk * 1024 + lane * 16, in = at % BLOCK, token = in / HD, piece = in % HD / 16;
+        const int in = at % BLOCK, token = in / HD, piece = in % HD / 16;
         const uint32_t place = values ? in : token * HD + (piece ^ swizzle<HD>(token, at / BLOCK)) * 16;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + off + place),
+        uint32_t olo, ohi;
+        if (BLOCK % 1024 == 0) {
+          olo = __builtin_amdgcn_readlane(lo, chunk * 1024 / BLOCK);
+          ohi = __builtin_amdgcn_readlane(hi, chunk * 1024 / BLOCK);
+        } else {               // (a KB of two blocks, with heads of 32 and 96)
+          olo = __shfl(lo, at / BLOCK, 64);
+          ohi = __shfl(hi, at / BLOCK, 64);
+        }
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + (int64_t)((uint64_t)ohi << 32 | olo) + place),
                                          (__attribute__((address_space(3))) void*)(to + chunk * 1024), 16, 0, 0);
       }
     };
-    auto load_keys = [&](int step, const Pages& p) __attribute__((always_inline)) { load(kbase, false, ring + step % 2 * TILE, step, p); };
-    auto load_values = [&](int step, const Pages& p) __attribute__((always_inline)) { load(vbase, true, ring + (2 + step % 2) * TILE, step, p); };
-    // this wave's loads have landed and its LDS reads are done, then every wave's
-    auto arrived = [&]() {
+    // The keys of tile step + 2 with their scales, the values of tile step + 1 with theirs: the scales, eight floats, to the place that this
+    // step's parity names (lanes 0 to 3 the keys', 4 to 7 the values').
+    auto load_tiles = [&](int step, const Place& keys, const Place& values) __attribute__((always_inline)) {
+      load(kbase, false, ring + (step & 1) * TILE, keys);
+      load(vbase, true, ring + (2 + (step + 1 & 1)) * TILE, values);
+      if (rowset == 0 && lane < 8) {
+        const float* from = lane < 4 ? g.cache.k_scale + keys.scale : g.cache.v_scale + values.scale;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + kvh * blocks),
+                                         (__attribute__((address_space(3))) void*)(scales + (step & 1) * 8), 4, 0, 0);
+      }
+    };
+    // This wave's loads have landed and its LDS reads are done, then every wave's.  In between, of the values of tile `step` if not every row of
+    // the block sees all its keys: a NaN value times a probability of 0 is NaN, so each wave takes NaN values among those that it loaded as zeros and notes
+    // the first token of each element that has one, for the end.
+    const int first_seen = sees_of(tile * kRowsOfBlock);
+    auto landed = [&]() __attribute__((always_inline)) {
       asm volatile("" ::: "memory");
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_waitcnt(7 << 4);
+    };
+    auto all_waves = [&]() __attribute__((always_inline)) {
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
       __builtin_amdgcn_sched_barrier(0);
+    };
+    auto arrived = [&](int step, int there) __attribute__((always_inline)) {
+      landed();
+      if (key_of(step) < k_hi && (key_of(step) + kTile > first_seen || there != 15)) {
+        for (int n = 0; n < (CHUNKS + 3) / 4; ++n) {
+          const int at = (n * 4 + rowset) * 1024 + lane * 16;
+          if (CHUNKS % 4 != 0 && at >= TILE) break;
+          u32x4* const mine = reinterpret_cast<u32x4*>(ring + (2 + (step & 1)) * TILE + at);
+          const u32x4 w = *mine, x = {nan_bytes(w[0]), nan_bytes(w[1]), nan_bytes(w[2]), nan_bytes(w[3])};
+          if ((x[0] | x[1] | x[2] | x[3]) != 0) {
+            *mine = w & ~x;
+            const int word = x[0] ? 0 : x[1] ? 1 : x[2] ? 2 : 3;
+            const int token = key_of(step) + at / BLOCK * kBlock + 4 * word + __builtin_ctz(x[0] ? x[0] : x[1] ? x[1] : x[2] ? x[2] : x[3]) / 8;
+            if (there >> (at / BLOCK) & 1) {
+              atomicMin(&nan_at[at % BLOCK / kBlock], token);
+              atomicMin(&nan_at[HD], token);
+            }
+          }
+        }
+        landed();
+      }
+      all_waves();
     };
 
     bf16x8 qf[2 * C];
@@ -152,10 +165,8 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-    float m = -INFINITY, m_exp = 0.f, l = 0.f;
-    int nan_at[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d) nan_at[d] = 0x7fffffff;
+    float m = -INFINITY, l = 0.f;
+    for (int e = threadIdx.x; e <= HD; e += blockDim.x) nan_at[e] = 0x7fffffff;
 
     auto key_frag = [&](int step, int t, int c) __attribute__((always_inline)) {
       const uint8_t* at = ring + step % 2 * TILE + (2 * t + k_block) * BLOCK + k_token * HD;
@@ -168,15 +179,17 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] = 0.f;
     };
-    // the scales of this lane's blocks, of tile t of 32 keys
-    auto key_scale = [&](const Scales& s, int t) { return k_block ? s.k[2 * t + 1] : s.k[2 * t]; };
-    auto value_scale = [&](const Scales& s, int t) { return half ? s.v[2 * t + 1] : s.v[2 * t]; };
-    auto bounded = [&](int step, const Scales& s) { return key_of(step) + kTile > fewest || s.there != 15; };   // not every row sees every key
-    auto mask = [&](f32x16 (&s)[2], int step, const Scales& sc) __attribute__((always_inline)) {
+    // of tile t of 32 keys, the scales of this lane's blocks: of the tile whose keys (values) came with step `step`
+    auto key_scale = [&](int step, int t) { return scales[(step & 1) * 8 + 2 * t + k_block]; };
+    auto value_scale = [&](int step, int t, int there) {
+      const float s = scales[(step & 1) * 8 + 4 + 2 * t + half];
+      return there >> (2 * t + half) & 1 ? s : 1.f;
+    };
+    auto bounded = [&](int step, int there) { return key_of(step) + kTile > fewest || there != 15; };   // not every row sees every key
+    auto mask = [&](f32x16 (&s)[2], int step, int there) __attribute__((always_inline)) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const bool there = sc.there >> (2 * t + half) & 1;
-        const int n = (there ? sees : 0) - key_of(step) - (2 * t + half) * kBlock;
+        const int n = (there >> (2 * t + half) & 1 ? sees : 0) - key_of(step) - (2 * t + half) * kBlock;
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (i >= n) s[t][i] = -INFINITY;
@@ -190,18 +203,17 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
         const float next = fmaxf(m, mx), ref = next == -INFINITY ? 0.f : next;
         const float a = __builtin_amdgcn_exp2f(m - ref);
         m = next;
-        m_exp = ref;
         l *= a;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d] *= a;
       }
     };
-    auto scores = [&](f32x16 (&s)[2], int step, const Scales& sc) __attribute__((always_inline)) {
+    auto scores = [&](f32x16 (&s)[2], int step) __attribute__((always_inline)) {
       zero(s[0]);
       zero(s[1]);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const float ks = key_scale(sc, t);
+        const float ks = key_scale(step, t);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
           const u32x4 w = key_frag(step, t, c);
@@ -219,13 +231,12 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
       new_max(mx);
     };
 
-    // Probabilities of `cur` (tile `step`, whose maximum m_exp holds), their products with the tile's values, and meanwhile the scores of the tile
+    // Probabilities of `cur` (tile `step`, whose maximum m holds), their products with the tile's values, and meanwhile the scores of the tile
     // after it into `next` (of what LDS holds, behind the last tile): 16-byte fragments in turn, two matrix instructions each and each with its share
-    // of the exponentials.  A NaN value times a probability of 0 is NaN: of a tile of which not every row sees every key (`part`), NaN values
-    // are taken as zeros and the first token that has one is noted in nan_at, for the end.
-    auto work = [&](f32x16 (&cur)[2], f32x16 (&next)[2], int step, const Scales& sc, const Scales& sn, bool part) __attribute__((always_inline)) {
-      constexpr int NQK = 2 * C, N = NQK + 2 * DT, PD = 3, LAST = NQK + DT;   // LAST: fragments before the second half's products
-      const float vs[2] = {value_scale(sc, 0), value_scale(sc, 1)}, ks[2] = {key_scale(sn, 0), key_scale(sn, 1)};
+    // of the exponentials.
+    auto work = [&](f32x16 (&cur)[2], f32x16 (&next)[2], int step, int there) __attribute__((always_inline)) {
+      constexpr int NQK = 2 * C, N = NQK + 2 * DT, PD = 2, LAST = NQK + DT;   // LAST: fragments before the second half's products
+      const float vs[2] = {value_scale(step - 1, 0, there), value_scale(step - 1, 1, there)}, ks[2] = {key_scale(step - 1, 0), key_scale(step - 1, 1)};
       zero(next[0]);
       zero(next[1]);
       auto frag = [&](int j) __attribute__((always_inline)) {
@@ -238,6 +249,7 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
       bf16x8 pf[2][2];
       float sum = 0.f;
       int done = 0;
+      const float m_exp = m == -INFINITY ? 0.f : m;
       auto exponential = [&](int e) __attribute__((always_inline)) {
         const float p = __builtin_amdgcn_exp2f(fmaf(cur[e / 16][e % 16], g.scale, -m_exp));
         sum += p;
@@ -245,70 +257,57 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
       };
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        u32x4 w = fr[j % PD];
+        const u32x4 w = fr[j % PD];
         const int t = j < NQK ? j / C : (j - NQK) / DT, c = j < NQK ? j % C : (j - NQK) % DT;
         if (j < NQK) {
           next[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(scaled_bf16(w[0], w[1], ks[t]), qf[2 * c], next[t], 0, 0, 0);
           next[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(scaled_bf16(w[2], w[3], ks[t]), qf[2 * c + 1], next[t], 0, 0, 0);
         } else {
-          if (part) {
-            const u32x4 n = {nan_bytes(w[0]), nan_bytes(w[1]), nan_bytes(w[2]), nan_bytes(w[3])};
-            if (__any((n[0] | n[1] | n[2] | n[3]) != 0)) {
-              const int at = key_of(step) + (2 * t + half) * kBlock;
-              for (int i = 0; i < 4; ++i) {
-                const uint32_t x = i == 0 ? n[0] : i == 1 ? n[1] : i == 2 ? n[2] : n[3];
-                if (x != 0) nan_at[c] = min(nan_at[c], at + 4 * i + __builtin_ctz(x) / 8);
-              }
-              w &= ~n;
-            }
-          }
           o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(scaled_bf16(w[0], w[1], vs[t]), pf[t][0], o[c], 0, 0, 0);
           o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(scaled_bf16(w[2], w[3], vs[t]), pf[t][1], o[c], 0, 0, 0);
         }
         if (j + PD < N) fr[j % PD] = frag(j + PD);
-        // the first half's exponentials are done before its products begin, the second's before those
+        // the first half's exponentials are done before the next tile's second half needs registers, the second's before its products
+        const int due = j < C ? (j + 1) * 16 / C : j < LAST ? 16 + (j + 1 - C) * 16 / (LAST - C) : 32;
 #pragma unroll
-        for (int x = 0; x < 31 / LAST + 2; ++x)
-          if (done < 32 && done < (j + 1) * 32 / LAST) exponential(done++);
+        for (int x = 0; x < 16; ++x)
+          if (done < due) exponential(done++);
         __builtin_amdgcn_sched_barrier(0);
       }
       l += sum;
     };
 
     f32x16 s_a[2], s_b[2];
-    const Pages p0 = pages_of(0);
-    Pages p1 = pages_of(1), p2 = pages_of(2);
-    Scales sc = scales_of(0, p0), sn = scales_of(1, p1);
-    load_keys(0, p0);
-    load_values(0, p0);
-    load_keys(1, p1);
-    arrived();
+    // (the places of the first two tiles: as if the steps -2 and -1 had brought in the keys of tiles 0 and 1 and the values of tile 0)
+    Place now = place_of(0, number(0)), next = place_of(1, number(1));
+    int coming = number(2);
+    load_tiles(-2, now, now);
+    landed();
+    all_waves();
     if (mine > 0) {
-      scores(s_a, 0, sc);
-      if (bounded(0, sc)) mask(s_a, 0, sc);
+      scores(s_a, 0);
+      if (bounded(0, now.there)) mask(s_a, 0, now.there);
       take_max(s_a);
     }
-    __syncthreads();     // the first tile's keys are overwritten from the first step on
+    load_tiles(-1, next, now);
+    arrived(0, now.there);
     // Values of tile `step` and keys of step + 1 are in LDS, their other places free.
-    auto iteration = [&](f32x16 (&cur)[2], f32x16 (&next)[2], int step) __attribute__((always_inline)) {
-      const Pages p3 = pages_of(step + 3);
-      const Scales s2 = scales_of(step + 2, p2);
+    auto iteration = [&](f32x16 (&cur)[2], f32x16 (&nxt)[2], int step) __attribute__((always_inline)) {
+      const Place after = place_of(step + 2, coming);
+      coming = number(step + 3);
       asm volatile("" ::: "memory");
       __builtin_amdgcn_sched_barrier(0);
-      load_keys(step + 2, p2);
-      load_values(step + 1, p1);
+      load_tiles(step, after, next);
       if (step < mine) {
-        work(cur, next, step, sc, sn, bounded(step, sc));
+        work(cur, nxt, step, now.there);
         if (step + 1 < mine) {
-          if (bounded(step + 1, sn)) mask(next, step + 1, sn);
-          take_max(next);
+          if (bounded(step + 1, next.there)) mask(nxt, step + 1, next.there);
+          take_max(nxt);
         }
       }
-      arrived();
-      sc = sn;
-      sn = s2;
-      p1 = p2;
-      p2 = p3;
+      arrived(step + 1, next.there);
+      now.there = next.there;
+      next = after;
     };
     for (int step = 0; step < steps; step += 2) {
       iteration(s_a, s_b, step);
@@ -316,13 +315,12 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
     }
 
     // elements whose row sees a NaN value that was taken as zero
+    if (nan_at[HD] != 0x7fffffff) {
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-      if (!__any(nan_at[d] != 0x7fffffff)) continue;
-      const int first = min(nan_at[d], __shfl_xor(nan_at[d], 32, 64));
+      for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (__shfl(first, 8 * (i / 4) + 4 * half + i % 4, 64) < sees) o[d][i] = __builtin_nanf("");
+        for (int i = 0; i < 16; ++i)
+          if (nan_at[d * 32 + 8 * (i / 4) + 4 * half + i % 4] < sees) o[d][i] = __builtin_nanf("");
     }
 
     // the second half of the keys to LDS (pieces of four elements turned by the row, against bank conflicts), the first joins

@@ -255,22 +255,23 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
         sum += p;
         pf[e / 16][e % 16 / 8][e % 8] = f2bf(p);
       };
+      auto converted = [&](int h) __attribute__((always_inline)) {      // instruction h's codes, of fragment h / 2
+        const int j = h / 2;
+        const u32x4& w = fr[j % PD];
+        return scaled_bf16(w[h % 2 * 2], w[h % 2 * 2 + 1], j < NQK ? ks[j / C] : vs[(j - NQK) / DT]);
+      };
+      bf16x8 a = converted(0);
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const u32x4 w = fr[j % PD];
-        const int t = j < NQK ? j / C : (j - NQK) / DT, c = j < NQK ? j % C : (j - NQK) % DT;
-        if (j < NQK) {
-          next[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(scaled_bf16(w[0], w[1], ks[t]), qf[2 * c], next[t], 0, 0, 0);
-          next[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(scaled_bf16(w[2], w[3], ks[t]), qf[2 * c + 1], next[t], 0, 0, 0);
-        } else {
-          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(scaled_bf16(w[0], w[1], vs[t]), pf[t][0], o[c], 0, 0, 0);
-          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(scaled_bf16(w[2], w[3], vs[t]), pf[t][1], o[c], 0, 0, 0);
-        }
-        if (j + PD < N) fr[j % PD] = frag(j + PD);
+      for (int h = 0; h < 2 * N; ++h) {
+        const int j = h / 2, t = j < NQK ? j / C : (j - NQK) / DT, c = j < NQK ? j % C : (j - NQK) % DT;
+        if (j < NQK) next[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[2 * c + h % 2], next[t], 0, 0, 0);
+        else o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[t][h % 2], o[c], 0, 0, 0);
+        if (h + 1 < 2 * N) a = converted(h + 1);
+        if (h % 2 == 0 && j + PD < N) fr[j % PD] = frag(j + PD);
         // the first half's exponentials are done before the next tile's second half needs registers, the second's before its products
-        const int due = j < C ? (j + 1) * 16 / C : j < LAST ? 16 + (j + 1 - C) * 16 / (LAST - C) : 32;
+        const int due = h < 2 * C ? (h + 1) * 16 / (2 * C) : h < 2 * LAST ? 16 + (h + 1 - 2 * C) * 16 / (2 * (LAST - C)) : 32;
 #pragma unroll
-        for (int x = 0; x < 16; ++x)
+        for (int x = 0; x < (7 + C) / C; ++x)
           if (done < due) exponential(done++);
         __builtin_amdgcn_sched_barrier(0);
       }

@@ -30,16 +30,6 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
   return (m >> 7 & 0x01010101u) * 0xffu;
 }
 
-// n / d for n < 2^31 by one multiplication and one addition: with l = ceil(log2 d), the quotient is (hi32(n * mul) + n) >> l for
-// mul = floor(2^32 (2^l - d) / d) + 1 (Granlund and Montgomery, "Division by invariant integers using multiplication", 1994).
-struct Divisor { uint32_t d, mul, shift; };
-inline Divisor divisor(uint32_t d) {
-  uint32_t l = 0;
-  while ((1ull << l) < d) ++l;
-  return Divisor{d, (uint32_t)((((1ull << l) - d) << 32) / d + 1), l};
-}
-__device__ __forceinline__ int quotient(int n, const Divisor& v) { return (int)((__umulhi((uint32_t)n, v.mul) + (uint32_t)n) >> v.shift); }
-
 struct CacheAttnArgs {
   const void* q; void* out;
   int64_t ldq, ldo;

@@ -149,6 +149,16 @@ __device__ __forceinline__ void split_row(int64_t m, int64_t period, int64_t& q,
   r = (int64_t)((uint32_t)m - qq * (uint32_t)period);
 }
 
+// n / d for n < 2^31 by one multiplication and one addition: with l = ceil(log2 d), the quotient is (hi32(n * mul) + n) >> l for
+// mul = floor(2^32 (2^l - d) / d) + 1 (Granlund and Montgomery, "Division by invariant integers using multiplication", 1994).
+struct Divisor { uint32_t d, mul, shift; };
+inline Divisor divisor(uint32_t d) {
+  uint32_t l = 0;
+  while ((1ull << l) < d) ++l;
+  return Divisor{d, (uint32_t)((((1ull << l) - d) << 32) / d + 1), l};
+}
+__device__ __forceinline__ int quotient(int n, const Divisor& v) { return (int)((__umulhi((uint32_t)n, v.mul) + (uint32_t)n) >> v.shift); }
+
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -355,7 +365,7 @@ struct LinearW4Args {
   const void* w; int64_t ldw;           // bytes
   const void* scale; int64_t lds;
   const void* zero; int64_t ldz;        // null: 8 everywhere
-  int64_t group;
+  Divisor group;
   const void* bias;
   const void* resid; int64_t ldr;
   void* out; int64_t ldo;

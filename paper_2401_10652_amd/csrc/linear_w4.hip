@@ -14,6 +14,7 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+constexpr int kTileRows = 96;  // rows from which the tiles of 128 x 128 take the product
 constexpr int kStep = 128;   // columns a wave takes at a time: 16 bytes of codes a lane
 
 // Slots 0..7 of a fragment hold columns 0 4 1 5 2 6 3 7, the order in which a word of eight codes comes apart.
@@ -100,7 +101,7 @@ __global__ void __launch_bounds__(512) linear_w4(LinearW4Args g) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) ones[i] = (bf16_t)1.0f;
 
-  const int64_t groups = (g.k + g.group - 1) / g.group;
+  const int groups = quotient((int)g.k - 1, g.group) + 1;
   for (int64_t k0 = (int64_t)wave * kStep; k0 < g.k; k0 += (int64_t)waves * kStep) {
     u32x4 codes[CT];
     const int64_t at = k0 / 2 + quarter * 16;
@@ -122,7 +123,7 @@ __global__ void __launch_bounds__(512) linear_w4(LinearW4Args g) {
     for (int c = 0; c < CT; ++c) transpose_quarters(codes[c]);
 #pragma unroll
     for (int j0 = 0; j0 < 4; j0 += SUBS) {
-      const int64_t gi = (k0 + j0 * 32) / g.group < groups ? (k0 + j0 * 32) / g.group : groups - 1;
+      const int gi = min(quotient((int)k0 + j0 * 32, g.group), groups - 1);
       f32x4 sum[MB], part[MB][CT];
 #pragma unroll
       for (int r = 0; r < MB; ++r) {
@@ -178,26 +179,231 @@ hipError_t launch_subs(const LinearW4Args& g, hipStream_t s) {
   const int waves = 4;
   const dim3 grid((unsigned)((g.n + 16 * CT - 1) / (16 * CT)), (unsigned)((g.m + 16 * MB - 1) / (16 * MB)));
   const size_t lds = (size_t)waves * 16 * MB * 16 * CT * sizeof(float);
-  if (g.group == 32)
+  if (g.group.d == 32)
     hipLaunchKernelGGL((linear_w4<T, NT, MB, CT, 1, VEC>), grid, dim3(waves * kWave), lds, s, g);
-  else if (g.group == 64)
+  else if (g.group.d == 64)
     hipLaunchKernelGGL((linear_w4<T, NT, MB, CT, 2, VEC>), grid, dim3(waves * kWave), lds, s, g);
   else
     hipLaunchKernelGGL((linear_w4<T, NT, MB, CT, 4, VEC>), grid, dim3(waves * kWave), lds, s, g);
   return hipGetLastError();
 }
 
-template <typename T, int NT>
-hipError_t launch_rows(const LinearW4Args& g, hipStream_t s) {
+template <typename T, int NT, int MB, int CT>
+hipError_t launch_vec(const LinearW4Args& g, hipStream_t s) {
   constexpr int64_t V = Elem<T>::kVec;
   const bool vec = (uintptr_t)g.x % 16 == 0 && (g.m == 1 || g.ldx % V == 0);
-  return vec ? launch_subs<T, NT, 1, 1, true>(g, s) : launch_subs<T, NT, 1, 1, false>(g, s);
+  return vec ? launch_subs<T, NT, MB, CT, true>(g, s) : launch_subs<T, NT, MB, CT, false>(g, s);
+}
+
+template <typename T, int NT>
+hipError_t launch_rows(const LinearW4Args& g, hipStream_t s) {
+  if (g.m <= 16) return launch_vec<T, NT, 1, 1>(g, s);
+  if (g.m <= 32 || NT == 3) return launch_vec<T, NT, 2, 1>(g, s);
+  return launch_vec<T, NT, NT == 3 ? 2 : 4, 1>(g, s);
+}
+
+// ---- many rows ---------------------------------------------------------------------------------------------------------
+//
+// From kTileRows rows on the matrix cores bound the product.  A block owns 128 rows and 128 columns; of its eight waves four own 64 x 64 each, and
+// its two sets of four take a half of k each, so that two waves share a SIMD also where there are few blocks, and add up in LDS.  x and the codes
+// come to LDS by direct loads, two steps of 64 columns of k ahead; codes become whole numbers code - zero in bf16 (exact where the zero is a whole number), and
+// a group's sum is scaled in fp32.  Scales and zeros of eight groups at a time lie in LDS.
+constexpr int kTileM = 128, kTileN = 128, kTileK = 64, kStages = 3;
+constexpr int kXBytes = kTileM * kTileK * 2, kWBytes = kTileN * kTileK / 2, kStageBytes = kXBytes + kWBytes;
+constexpr int kScaleBytes = 2 * 8 * kTileN * 2;                     // scales and zeros of eight groups
+constexpr int kSetBytes = kStages * kStageBytes + 2 * kScaleBytes;   // of a set of four waves
+__device__ const uint32_t kZeros[4] = {0, 0, 0, 0};
+
+// Codes 0 .. 7 of a word, less `zero`, as bf16 in their own order.
+__device__ __forceinline__ bf16x8 codes_less(uint32_t w, float zero) {
+  const uint32_t even = w & 0x0f0f0f0fu, odd = w >> 4 & 0x0f0f0f0fu;
+  bf16x8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[2 * i] = f2bf((float)(even >> (8 * i) & 0xffu) - zero);
+    r[2 * i + 1] = f2bf((float)(odd >> (8 * i) & 0xffu) - zero);
+  }
+  return r;
+}
+
+// G32: groups of 32, two to a step.
+template <bool G32>
+__global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), l32 = lane % 32, half = lane / 32;
+  const int set = wave / 4, w4 = wave % 4, wm = w4 / 2, wn = w4 % 2, tid = threadIdx.x % 256;
+  const int64_t m0 = (int64_t)blockIdx.y * kTileM, n0 = (int64_t)blockIdx.x * kTileN;
+  uint8_t* const ring = smem + set * kSetBytes;
+  bf16_t* const scales = reinterpret_cast<bf16_t*>(ring + kStages * kStageBytes);     // [2][scale, zero][8][128]
+  const int all = (int)((g.k + kTileK - 1) / kTileK), steps = (all + 1) / 2, first = set * steps;    // (the second set's last step may lie past k: zeros)
+  const int groups = quotient((int)g.k - 1, g.group) + 1, chunk0 = quotient(first * kTileK, g.group) / 8;
+
+  const uint8_t* const wrow = (const uint8_t*)g.w + min(n0 + tid / 2, g.n - 1) * g.ldw + tid % 2 * 16;
+  // 1 KB a load: of x eight rows, the pieces of a row turned by the row; of the codes 32 rows
+  auto load = [&](int i) __attribute__((always_inline)) {
+    const int64_t k0 = (int64_t)(first + i) * kTileK;
+    uint8_t* const to = ring + i % kStages * kStageBytes;
+#pragma unroll
+    for (int n = 0; n < kXBytes / 4096; ++n) {
+      const int row = (n * 4 + w4) * 8 + lane / 8;
+      const int64_t m = min(m0 + row, g.m - 1), k = k0 + (lane % 8 ^ (row & 7)) * 8;
+      const void* src = k < g.k ? (const void*)((const bf16_t*)g.x + m * g.ldx + k) : (const void*)kZeros;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                       (__attribute__((address_space(3))) void*)(to + (n * 4 + w4) * 1024), 16, 0, 0);
+    }
+    const void* src = k0 + tid % 2 * 32 < g.k ? (const void*)(wrow + k0 / 2) : (const void*)kZeros;
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                     (__attribute__((address_space(3))) void*)(to + kXBytes + w4 * 1024), 16, 0, 0);
+  };
+  constexpr int kLoads = kXBytes / 4096 + 1;      // of a wave for a step
+  // all loads but those of the youngest step have landed and LDS is read, in this wave and then in every
+  auto arrived = [&]() __attribute__((always_inline)) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(kLoads | 7 << 4);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // thread tid: the scales (tid < 128) or zeros of column tid mod 128, groups 8 c .. 8 c + 7
+  const int64_t sn = min(n0 + tid % 128, g.n - 1);
+  const bf16_t* const srow = tid < 128 ? (const bf16_t*)g.scale + sn * g.lds : g.zero ? (const bf16_t*)g.zero + sn * g.ldz : nullptr;
+  bf16_t eight[8];
+  auto fetch = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) eight[e] = srow ? srow[min(8 * c + e, groups - 1)] : (bf16_t)8.0f;
+  };
+  auto keep = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) scales[(c & 1) * (2 * 8 * kTileN) + tid / 128 * (8 * kTileN) + e * kTileN + tid % 128] = eight[e];
+  };
+
+  f32x16 total[2][2];
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) total[r][c][e] = 0.f;
+
+  load(0);
+  fetch(chunk0);
+  keep(chunk0);
+  load(1);
+  arrived();
+  int kept = chunk0;
+  for (int i = 0; i < steps; ++i) {
+    const int g0 = quotient((first + i) * kTileK, g.group);
+    const bool fresh = g0 / 8 == kept;             // the first step of eight groups: the next eight take the place of those before, which are not read any more
+    if (fresh) fetch(kept + 1);
+    load(i + 2);
+    const uint8_t* const tile = ring + i % kStages * kStageBytes;
+    const uint8_t* const xt = tile + (wm * 64 + l32) * (kTileK * 2);
+    u32x4 cw[2];
+    float s[2][2], z[2][2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int col = wn * 64 + c * 32 + l32;
+      cw[c] = *reinterpret_cast<const u32x4*>(tile + kXBytes + col * 32 + half * 16);
+#pragma unroll
+      for (int e = 0; e < (G32 ? 2 : 1); ++e) {
+        const bf16_t* at = scales + ((g0 + e) / 8 & 1) * (2 * 8 * kTileN) + (g0 + e) % 8 * kTileN + col;
+        s[c][e] = bf2f(at[0]);
+        z[c][e] = bf2f(at[8 * kTileN]);
+      }
+      if (G32) {      // words 0, 1: columns 0 .. 31 of k, in both halves of the wave; 2, 3: the other 32
+        auto a = __builtin_amdgcn_permlane32_swap(cw[c][0], cw[c][1], false, false);
+        auto b = __builtin_amdgcn_permlane32_swap(cw[c][2], cw[c][3], false, false);
+        cw[c] = u32x4{(uint32_t)a[0], (uint32_t)b[0], (uint32_t)a[1], (uint32_t)b[1]};
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < (G32 ? 2 : 1); ++e) {
+      f32x16 part[2][2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) part[r][c][x] = 0.f;
+#pragma unroll
+      for (int q = e * 2; q < (G32 ? e * 2 + 2 : 4); ++q) {
+        const int piece = G32 ? 2 * q + half : half * 4 + q;
+        bf16x8 a[2], b[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) a[r] = *reinterpret_cast<const bf16x8*>(xt + r * 32 * (kTileK * 2) + (piece ^ (l32 & 7)) * 16);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) b[c] = codes_less(cw[c][q], z[c][e]);
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) part[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[r], b[c], part[r][c], 0, 0, 0);
+      }
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) total[r][c][x] = fmaf(s[c][e], part[r][c][x], total[r][c][x]);
+    }
+    if (fresh) keep(++kept);
+    arrived();
+  }
+
+  // the second set's sums through LDS (no load is on its way to it any more)
+  __builtin_amdgcn_s_waitcnt(7 << 4);
+  __syncthreads();
+  float* const joined = reinterpret_cast<float*>(smem) + w4 * 64 * 64;
+  if (set == 1) {
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) joined[(r * 32 + 8 * (x / 4) + 4 * half + x % 4) * 64 + c * 32 + l32] = total[r][c][x];
+  }
+  __syncthreads();
+  if (set == 1) return;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int64_t n = n0 + wn * 64 + c * 32 + l32;
+    const float bias = g.bias && n < g.n ? bf2f(((const bf16_t*)g.bias)[n]) : 0.f;
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const int in = r * 32 + 8 * (x / 4) + 4 * half + x % 4;
+        const int64_t m = m0 + wm * 64 + in;
+        if (m >= g.m || n >= g.n) continue;
+        float v = apply_act_rt(total[r][c][x] + joined[in * 64 + c * 32 + l32] + bias, g.act);
+        if (g.resid) v += bf2f(((const bf16_t*)g.resid)[m * g.ldr + n]);
+        ((bf16_t*)g.out)[m * g.ldo + n] = f2bf(v);
+      }
+  }
+}
+
+// Rows of x that direct loads can take: 16-byte pieces that hold columns of k alone.
+bool tiles_take(const LinearW4Args& g) {
+  return g.dtype == AC_BF16 && g.m >= kTileRows && (uintptr_t)g.x % 16 == 0 && g.ldx % 8 == 0 && g.k % 8 == 0;
+}
+
+template <bool G32>
+hipError_t launch_tiles(const LinearW4Args& g, hipStream_t s) {
+  constexpr size_t lds = 2 * kSetBytes;
+  static_assert(lds >= 4 * 64 * 64 * sizeof(float) && lds <= 160 * 1024, "one block a CU");
+  static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(linear_w4_tiles<G32>),
+                                                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (attr_status != hipSuccess) return attr_status;
+  const dim3 grid((unsigned)((g.n + kTileN - 1) / kTileN), (unsigned)((g.m + kTileM - 1) / kTileM));
+  hipLaunchKernelGGL((linear_w4_tiles<G32>), grid, dim3(512), lds, s, g);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_linear_w4(const LinearW4Args& g, hipStream_t s) {
   if (g.m <= 0 || g.n <= 0) return hipSuccess;
+  if (tiles_take(g)) return g.group.d == 32 ? launch_tiles<true>(g, s) : launch_tiles<false>(g, s);
   return g.dtype == AC_BF16 ? launch_rows<bf16_t, 1>(g, s) : launch_rows<float, 3>(g, s);
 }
 

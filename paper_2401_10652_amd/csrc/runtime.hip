@@ -2173,7 +2173,7 @@ int ac_op_linear_w4(const void* x, int64_t ldx, const void* w, int64_t ldw, cons
                     int64_t ldz, int64_t group, const void* bias, const void* residual, int64_t ldr, void* out, int64_t ldo, int64_t m,
                     int64_t n, int64_t k, int activation, int dtype, void* stream) {
   if (m == 0 || n == 0) return AC_OK;
-  if (!x || !w || !scale || !out || m < 0 || n < 0 || k < 1 || k > (1ll << 31) || n > (1ll << 31) || ldx < k || ldo < n ||
+  if (!x || !w || !scale || !out || m < 0 || n < 0 || k < 1 || k > 1 << 30 || n > 1 << 30 || group > 1 << 30 || ldx < k || ldo < n ||
       (residual && ldr < n) || group < 1 || lds < ceil_div(k, group) || (zero && ldz < ceil_div(k, group)) || !dtype_ok(dtype) ||
       activation < 0 || activation > AC_ACT_SILU)
     return fail(AC_ERR_ARG, "ac_op_linear_w4: bad argument");
@@ -2182,7 +2182,7 @@ int ac_op_linear_w4(const void* x, int64_t ldx, const void* w, int64_t ldw, cons
   if (m > 16 * 65535ll) return fail(AC_ERR_UNSUPPORTED, "ac_op_linear_w4: at most %lld rows", 16 * 65535ll);
   if (ldw < ceil_div(k, 2)) return fail(AC_ERR_ARG, "ac_op_linear_w4: rows of codes overlap");
   if (ldw % 16 != 0 || (uintptr_t)w % 16 != 0) return fail(AC_ERR_ALIGN, "ac_op_linear_w4: rows of codes start at multiples of 16 bytes");
-  return hip_status(launch_linear_w4(LinearW4Args{x, ldx, w, ldw, scale, lds, zero, ldz, group, bias, residual, ldr, out, ldo, m, n, k,
+  return hip_status(launch_linear_w4(LinearW4Args{x, ldx, w, ldw, scale, lds, zero, ldz, divisor((uint32_t)group), bias, residual, ldr, out, ldo, m, n, k,
                                                   activation, dtype}, (hipStream_t)stream), "linear_w4");
 }
 

@@ -66,11 +66,19 @@ def test_linear_w4(B, dtype, m, n, k, group):
     assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)
 
 
+@pytest.mark.parametrize("m,n,k,group", [(96, 128, 64, 32), (128, 1, 8, 64), (129, 300, 200, 128), (200, 70, 520, 64), (257, 129, 1000, 32), (300, 384, 1024, 256),
+                                          (150, 40, 100, 32), (128, 200, 333, 64)])
+def test_linear_w4_of_many_rows(B, m, n, k, group):
+    for zero in (False, True):
+        got, ref, bound = linear_case(B, "bf16", m, n, k, group, zero, seed=m + n)
+        assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("zero", [False, True])
 @pytest.mark.parametrize("act,bias,residual", [("none", False, False), ("gelu_erf", True, False), ("gelu_tanh", False, True), ("relu", True, True)])
 def test_linear_w4_epilogues(B, dtype, zero, act, bias, residual):
-    for m in (1, 20, 100):
+    for m in (1, 20, 100, 140):
         got, ref, bound = linear_case(B, dtype, m, 72, 320, 64, zero, bias, residual, act, seed=m)
         assert (np.abs(got - ref) <= bound).all(), (m, np.max(np.abs(got - ref) / bound))
 
@@ -86,14 +94,15 @@ def test_linear_w4_strides(B, dtype, pad, wide):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_linear_w4_rows_keep_to_themselves(B, dtype):
     """NaN and infinities of one row reach no other; large and tiny rows keep their precision."""
-    m, k = 20, 160
-    x = D.normal((m, k), 3)
-    x[3, 7], x[17, 159], x[5] = np.nan, np.inf, x[5] * 1e30
-    x[6] *= 1e-30
-    got, ref, bound = linear_case(B, dtype, m, 40, k, 32, bias=False, residual=False, x=x)
-    assert np.isnan(got[[3, 17]]).all()
-    rest = [i for i in range(m) if i not in (3, 17)]
-    assert (np.abs(got - ref)[rest] <= bound[rest]).all()
+    for m in (20, 130):
+        k = 160
+        x = D.normal((m, k), 3)
+        x[3, 7], x[17, 159], x[5] = np.nan, np.inf, x[5] * 1e30
+        x[6] *= 1e-30
+        got, ref, bound = linear_case(B, dtype, m, 40, k, 32, bias=False, residual=False, x=x)
+        assert not np.isfinite(got[[3, 17]]).any()
+        rest = [i for i in range(m) if i not in (3, 17)]
+        assert (np.abs(got - ref)[rest] <= bound[rest]).all()
 
 
 def test_linear_w4_in_place_residual_and_no_rows(B):

@@ -226,6 +226,21 @@ __device__ __forceinline__ bf16x8 codes_less(uint32_t w, float zero) {
   return r;
 }
 
+template <int ACT> __device__ __forceinline__ void activate8(float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = apply_act_bf16<ACT>(v[e]);
+}
+__device__ __forceinline__ void activate(float (&v)[8], int act) {
+  switch (act) {
+    case AC_ACT_GELU_ERF: return activate8<AC_ACT_GELU_ERF>(v);
+    case AC_ACT_GELU_TANH: return activate8<AC_ACT_GELU_TANH>(v);
+    case AC_ACT_RELU: return activate8<AC_ACT_RELU>(v);
+    case AC_ACT_SIGMOID: return activate8<AC_ACT_SIGMOID>(v);
+    case AC_ACT_SILU: return activate8<AC_ACT_SILU>(v);
+    default: return;
+  }
+}
+
 // G32: groups of 32, two to a step.
 template <bool G32>
 __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
@@ -350,35 +365,54 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
     arrived();
   }
 
-  // the second set's sums through LDS (no load is on its way to it any more)
+  // the sums meet in LDS (no load is on its way to it any more), and leave it row by row
   __builtin_amdgcn_s_waitcnt(7 << 4);
   __syncthreads();
-  float* const joined = reinterpret_cast<float*>(smem) + w4 * 64 * 64;
-  if (set == 1) {
+  float* const joined = reinterpret_cast<float*>(smem);            // [128][128]
 #pragma unroll
-    for (int r = 0; r < 2; ++r)
+  for (int pass = 1; pass >= 0; --pass) {
+    if (set == pass) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+      for (int r = 0; r < 2; ++r)
 #pragma unroll
-        for (int x = 0; x < 16; ++x) joined[(r * 32 + 8 * (x / 4) + 4 * half + x % 4) * 64 + c * 32 + l32] = total[r][c][x];
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            float* const at = joined + (wm * 64 + r * 32 + 8 * (x / 4) + 4 * half + x % 4) * kTileN + wn * 64 + c * 32 + l32;
+            *at = pass == 1 ? total[r][c][x] : total[r][c][x] + *at;
+          }
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  if (set == 1) return;
+  const bool wide = g.ldo % 8 == 0 && (uintptr_t)g.out % 16 == 0 && (!g.resid || (g.ldr % 8 == 0 && (uintptr_t)g.resid % 16 == 0));
+  const int c8 = threadIdx.x % 16 * 8;
+  const int64_t n = n0 + c8;
+  if (n >= g.n) return;
+  const int cols = (int)min(g.n - n, (int64_t)8);
+  float bias[8];
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const int64_t n = n0 + wn * 64 + c * 32 + l32;
-    const float bias = g.bias && n < g.n ? bf2f(((const bf16_t*)g.bias)[n]) : 0.f;
+  for (int e = 0; e < 8; ++e) bias[e] = g.bias && e < cols ? bf2f(((const bf16_t*)g.bias)[n + e]) : 0.f;
+  for (int row = threadIdx.x / 16; row < kTileM && m0 + row < g.m; row += 32) {
+    const f32x4 lo = *reinterpret_cast<const f32x4*>(joined + row * kTileN + c8), hi = *reinterpret_cast<const f32x4*>(joined + row * kTileN + c8 + 4);
+    float v[8];
 #pragma unroll
-    for (int r = 0; r < 2; ++r)
+    for (int e = 0; e < 4; ++e) { v[e] = lo[e] + bias[e]; v[4 + e] = hi[e] + bias[4 + e]; }
+    activate(v, g.act);
+    bf16_t* const out = (bf16_t*)g.out + (m0 + row) * g.ldo + n;
+    const bf16_t* const resid = (const bf16_t*)g.resid + (m0 + row) * g.ldr + n;
+    if (wide && cols == 8) {
+      if (g.resid) {
+        float r[8];
+        load_vec(resid, r);
 #pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        const int in = r * 32 + 8 * (x / 4) + 4 * half + x % 4;
-        const int64_t m = m0 + wm * 64 + in;
-        if (m >= g.m || n >= g.n) continue;
-        float v = apply_act_rt(total[r][c][x] + joined[in * 64 + c * 32 + l32] + bias, g.act);
-        if (g.resid) v += bf2f(((const bf16_t*)g.resid)[m * g.ldr + n]);
-        ((bf16_t*)g.out)[m * g.ldo + n] = f2bf(v);
+        for (int e = 0; e < 8; ++e) v[e] += r[e];
       }
+      store_vec(out, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < cols) out[e] = f2bf(g.resid ? v[e] + bf2f(resid[e]) : v[e]);
+    }
   }
 }
 

@@ -8,6 +8,8 @@
 // scale multiplies a group's sum once, in fp32: no weight is ever rounded.  fp32 rows are three bf16 terms that sum to them exactly.
 #include "common.h"
 
+#include <type_traits>
+
 namespace ac {
 
 namespace {
@@ -204,19 +206,21 @@ hipError_t launch_rows(const LinearW4Args& g, hipStream_t s) {
 
 // ---- many rows ---------------------------------------------------------------------------------------------------------
 //
-// From kTileRows rows on the matrix cores bound the product.  A block owns 128 rows and 128 columns; of its eight waves four own 64 x 64 each, and
-// its two sets of four take a half of k each, so that two waves share a SIMD also where there are few blocks, and add up in LDS.  x and the codes
-// come to LDS by direct loads, two steps of 64 columns of k ahead; codes become whole numbers code - zero in bf16 (exact where the zero is a whole number), and
-// a group's sum is scaled in fp32.  Scales and zeros of eight groups at a time lie in LDS.
-constexpr int kTileM = 128, kTileN = 128, kTileK = 64, kStages = 3;
-constexpr int kXBytes = kTileM * kTileK * 2, kWBytes = kTileN * kTileK / 2, kStageBytes = kXBytes + kWBytes;
-constexpr int kScaleBytes = 2 * 8 * kTileN * 2;                     // scales and zeros of eight groups
-constexpr int kSetBytes = kStages * kStageBytes + 2 * kScaleBytes;   // of a set of four waves
-__device__ const uint32_t kZeros[4] = {0, 0, 0, 0};
+// From kTileRows rows on the matrix cores bound the product, if loads are far enough ahead: a step of 64 columns of k is half a microsecond, and what no
+// block has read yet takes two and more to come.  A block owns 128 rows and 128 columns; of its eight waves four own 32 columns each (whose codes are
+// then converted once for all rows), and its two sets of four take a half of k each, so that two waves share a SIMD also where there are few
+// blocks, and add up in LDS.  x comes to LDS by direct loads three steps ahead, the codes to the registers of the wave that multiplies with them
+// four steps ahead, and blocks that read the same rows of x at a time begin at different steps, so that one has them brought to the cache for the
+// others.  Codes become whole numbers code - zero in bf16 (exact where the zero is a whole number), and a group's sum is scaled in fp32.
+// Scales and zeros of eight groups at a time lie in LDS, each wave's its own.
+constexpr int kTileM = 128, kTileN = 128, kTileK = 64, kStages = 4;
+constexpr int kXBytes = kTileM * kTileK * 2;
+constexpr int kSetBytes = kStages * kXBytes + 4 * 2 * 1024;          // of a set of four waves: x, and two times eight groups' scales and zeros of each wave
 
 // Codes 0 .. 7 of a word, less `zero`, as bf16 in their own order.
 __device__ __forceinline__ bf16x8 codes_less(uint32_t w, float zero) {
-  const uint32_t even = w & 0x0f0f0f0fu, odd = w >> 4 & 0x0f0f0f0fu;
+  uint32_t even = w & 0x0f0f0f0fu, odd = w >> 4 & 0x0f0f0f0fu;
+  asm("" : "+v"(even), "+v"(odd));       // (bytes from here on, which convert without another mask)
   bf16x8 r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -241,128 +245,159 @@ __device__ __forceinline__ void activate(float (&v)[8], int act) {
   }
 }
 
-// G32: groups of 32, two to a step.
-template <bool G32>
+// GS: groups of a step.
+template <int GS>
 __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), l32 = lane % 32, half = lane / 32;
-  const int set = wave / 4, w4 = wave % 4, wm = w4 / 2, wn = w4 % 2, tid = threadIdx.x % 256;
+  const int set = wave / 4, w4 = wave % 4;
   const int64_t m0 = (int64_t)blockIdx.y * kTileM, n0 = (int64_t)blockIdx.x * kTileN;
   uint8_t* const ring = smem + set * kSetBytes;
-  bf16_t* const scales = reinterpret_cast<bf16_t*>(ring + kStages * kStageBytes);     // [2][scale, zero][8][128]
-  const int all = (int)((g.k + kTileK - 1) / kTileK), steps = (all + 1) / 2, first = set * steps;    // (the second set's last step may lie past k: zeros)
-  const int groups = quotient((int)g.k - 1, g.group) + 1, chunk0 = quotient(first * kTileK, g.group) / 8;
+  uint8_t* const scales = ring + kStages * kXBytes + w4 * 2048;          // [2][scale, zero][32][8]
+  const int all = ((int)g.k + kTileK - 1) / kTileK, steps = (all + 1) / 2, first = set * steps;    // (the second set's last step may lie past k: zeros)
+  const int groups = quotient((int)g.k - 1, g.group) + 1, col = w4 * 32 + l32;
+  // consecutive blocks are on different XCDs; those of one that share rows of x begin at different steps
+  const int turn = (blockIdx.x / 8 * 3) % steps;
+  auto step_of = [&](int t) { return first + (t + turn >= steps ? t + turn - steps : t + turn); };
 
-  const uint8_t* const wrow = (const uint8_t*)g.w + min(n0 + tid / 2, g.n - 1) * g.ldw + tid % 2 * 16;
-  // 1 KB a load: of x eight rows, the pieces of a row turned by the row; of the codes 32 rows
-  auto load = [&](int i) __attribute__((always_inline)) {
-    const int64_t k0 = (int64_t)(first + i) * kTileK;
-    uint8_t* const to = ring + i % kStages * kStageBytes;
-#pragma unroll
-    for (int n = 0; n < kXBytes / 4096; ++n) {
-      const int row = (n * 4 + w4) * 8 + lane / 8;
-      const int64_t m = min(m0 + row, g.m - 1), k = k0 + (lane % 8 ^ (row & 7)) * 8;
-      const void* src = k < g.k ? (const void*)((const bf16_t*)g.x + m * g.ldx + k) : (const void*)kZeros;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                       (__attribute__((address_space(3))) void*)(to + (n * 4 + w4) * 1024), 16, 0, 0);
-    }
-    const void* src = k0 + tid % 2 * 32 < g.k ? (const void*)(wrow + k0 / 2) : (const void*)kZeros;
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                     (__attribute__((address_space(3))) void*)(to + kXBytes + w4 * 1024), 16, 0, 0);
+  // Direct loads by buffer addresses: base and step in scalar registers, 32 bits a lane; an offset past the buffer's range brings zeros.  (The compiler
+  // waits for all loads in flight before it uses the result of any while a direct load of the other kind is among them.)
+  constexpr uint32_t kPastRange = 0x80000000u;
+  auto to_lds = [](const void* base, uint32_t lane_off, uint32_t off, uint8_t* to) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, 0x7fffffff, 0x00027000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)to, 16, lane_off, off, 0, 0);
   };
-  constexpr int kLoads = kXBytes / 4096 + 1;      // of a wave for a step
-  // all loads but those of the youngest step have landed and LDS is read, in this wave and then in every
-  auto arrived = [&]() __attribute__((always_inline)) {
+  // 1 KB a load: eight rows of x, the eight pieces of a row turned by the row.  Rows past the last are the last again.
+  const int xpiece = (lane % 8 ^ lane / 8) * 8;
+  const bf16_t* const x0 = (const bf16_t*)g.x + m0 * g.ldx;
+  uint32_t xoff[kXBytes / 4096];
+#pragma unroll
+  for (int n = 0; n < kXBytes / 4096; ++n) xoff[n] = (uint32_t)(min((int64_t)(n * 32 + w4 * 8 + lane / 8), g.m - 1 - m0) * g.ldx + xpiece) * 2;
+  auto load_x = [&](int t, int stage) __attribute__((always_inline)) {
+    const int k0 = t < steps ? step_of(t) * kTileK : (int)g.k;
+    const bool in = k0 + xpiece < (int)g.k;
+#pragma unroll
+    for (int n = 0; n < kXBytes / 4096; ++n) to_lds(x0, in ? xoff[n] : kPastRange, (uint32_t)k0 * 2, ring + stage * kXBytes + w4 * 1024 + n * 4096);
+  };
+  // a lane's codes of a step: of its column, columns 32 half .. 32 half + 31 of k (past the last, where x is zero, some that are there)
+  const uint8_t* const w0 = (const uint8_t*)g.w + n0 * g.ldw;
+  const uint32_t woff = (uint32_t)(min((int64_t)col, g.n - 1 - n0) * g.ldw), wlast = ((int)g.k - 1) / 2 & ~15;
+  auto load_w = [&](int t) __attribute__((always_inline)) {
+    return *reinterpret_cast<const u32x4*>(w0 + woff + min((uint32_t)step_of(t) * (kTileK / 2) + half * 16, wlast));
+  };
+  // Groups 8 c .. 8 c + 7 of the lane's column, the scales in the lower half of the wave and the zeros in the upper, to their place.
+  const int sn = (int)min((int64_t)col, g.n - 1 - n0);
+  const bf16_t *const s0 = (const bf16_t*)g.scale + n0 * g.lds, *const z0 = g.zero ? (const bf16_t*)g.zero + n0 * g.ldz : s0;
+  const uint32_t soff = (uint32_t)(sn * (half && g.zero ? g.ldz : g.lds)) * 2;
+  const bool wide = g.lds % 8 == 0 && (uintptr_t)g.scale % 16 == 0 && (!g.zero || (g.ldz % 8 == 0 && (uintptr_t)g.zero % 16 == 0));
+  auto load_scales = [&](int c, int place) __attribute__((always_inline)) {
+    if (wide && 8 * c + 8 <= groups) {
+      if (half == 0) to_lds(s0, soff, 16 * c, scales + place * 1024);
+      else to_lds(z0, soff, 16 * c, scales + place * 1024);
+    } else {
+      const bf16_t* const from = (half ? z0 : s0) + soff / 2;
+      uint16_t v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = __builtin_bit_cast(uint16_t, from[min(8 * c + e, groups - 1)]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) reinterpret_cast<uint16_t*>(scales + place * 1024 + lane * 16)[e] = v[e];
+    }
+  };
+  auto chunk_of = [&](int step) { return min(quotient(step * kTileK, g.group), groups - 1) / 8; };
+  const int chunk_first = chunk_of(first), chunk_last = chunk_of(first + steps - 1);
+  auto chunk_after = [&](int c) { return c == chunk_last ? chunk_first : c + 1; };
+
+  // all loads but the youngest N have landed and LDS is read, in this wave and then in every
+  auto arrived = [&](auto n) __attribute__((always_inline)) {
+    constexpr int N = decltype(n)::value;
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(kLoads | 7 << 4);
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 7 << 4);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
-  // thread tid: the scales (tid < 128) or zeros of column tid mod 128, groups 8 c .. 8 c + 7
-  const int64_t sn = min(n0 + tid % 128, g.n - 1);
-  const bf16_t* const srow = tid < 128 ? (const bf16_t*)g.scale + sn * g.lds : g.zero ? (const bf16_t*)g.zero + sn * g.ldz : nullptr;
-  bf16_t eight[8];
-  auto fetch = [&](int c) __attribute__((always_inline)) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) eight[e] = srow ? srow[min(8 * c + e, groups - 1)] : (bf16_t)8.0f;
-  };
-  auto keep = [&](int c) __attribute__((always_inline)) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) scales[(c & 1) * (2 * 8 * kTileN) + tid / 128 * (8 * kTileN) + e * kTileN + tid % 128] = eight[e];
-  };
+  using all_landed = std::integral_constant<int, 0>;
+  using two_steps = std::integral_constant<int, 2 * (kXBytes / 4096 + 1)>;      // the loads of a step: of x, and of codes
 
-  f32x16 total[2][2];
+  f32x16 total[4], zero16;
 #pragma unroll
-  for (int r = 0; r < 2; ++r)
+  for (int x = 0; x < 16; ++x) zero16[x] = 0.f;
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) total[r][c][e] = 0.f;
+  for (int r = 0; r < 4; ++r) total[r] = zero16;
 
-  load(0);
-  fetch(chunk0);
-  keep(chunk0);
-  load(1);
-  arrived();
-  int kept = chunk0;
-  for (int i = 0; i < steps; ++i) {
-    const int g0 = quotient((first + i) * kTileK, g.group);
-    const bool fresh = g0 / 8 == kept;             // the first step of eight groups: the next eight take the place of those before, which are not read any more
-    if (fresh) fetch(kept + 1);
-    load(i + 2);
-    const uint8_t* const tile = ring + i % kStages * kStageBytes;
-    const uint8_t* const xt = tile + (wm * 64 + l32) * (kTileK * 2);
-    u32x4 cw[2];
-    float s[2][2], z[2][2];
+  u32x4 codes[kStages];
+  int chunk = chunk_of(step_of(0)), place = 0;
+  load_scales(chunk, 0);
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const int col = wn * 64 + c * 32 + l32;
-      cw[c] = *reinterpret_cast<const u32x4*>(tile + kXBytes + col * 32 + half * 16);
+  for (int t = 0; t < kStages - 1; ++t) {
+    codes[t] = load_w(t);
+    load_x(t, t);
+  }
+  load_scales(chunk_after(chunk), 1);
+  arrived(all_landed{});
+  for (int t0 = 0; t0 < steps; t0 += kStages) {
 #pragma unroll
-      for (int e = 0; e < (G32 ? 2 : 1); ++e) {
-        const bf16_t* at = scales + ((g0 + e) / 8 & 1) * (2 * 8 * kTileN) + (g0 + e) % 8 * kTileN + col;
-        s[c][e] = bf2f(at[0]);
-        z[c][e] = bf2f(at[8 * kTileN]);
+    for (int u = 0; u < kStages; ++u) {
+      const int t = t0 + u;
+      if (t >= steps) break;
+      const int step = step_of(t), g0 = quotient(step * kTileK, g.group), c = min(g0, groups - 1) / 8;
+      if (c != chunk) {          // (its scales landed steps ago; those before them are not read any more)
+        chunk = c;
+        place ^= 1;
+        load_scales(chunk_after(chunk), place ^ 1);
       }
-      if (G32) {      // words 0, 1: columns 0 .. 31 of k, in both halves of the wave; 2, 3: the other 32
-        auto a = __builtin_amdgcn_permlane32_swap(cw[c][0], cw[c][1], false, false);
-        auto b = __builtin_amdgcn_permlane32_swap(cw[c][2], cw[c][3], false, false);
-        cw[c] = u32x4{(uint32_t)a[0], (uint32_t)b[0], (uint32_t)a[1], (uint32_t)b[1]};
+      codes[(u + kStages - 1) % kStages] = load_w(t + kStages - 1);
+      load_x(t + kStages - 1, (u + kStages - 1) % kStages);
+      const uint8_t* const xt = ring + u * kXBytes + l32 * (kTileK * 2);
+      u32x4 cw = codes[u];
+      // product q takes 16 columns of k: word q of the lane's codes, columns 32 half + 8 q; with groups of 32 words change halves first, so that both
+      // halves of the wave are in one group
+      if (GS == 2) {
+        auto a = __builtin_amdgcn_permlane32_swap(cw[0], cw[1], false, false);
+        auto b = __builtin_amdgcn_permlane32_swap(cw[2], cw[3], false, false);
+        cw = u32x4{(uint32_t)a[0], (uint32_t)b[0], (uint32_t)a[1], (uint32_t)b[1]};
       }
+      auto x_frag = [&](int q, int r) __attribute__((always_inline)) {
+        const int piece = GS == 2 ? 2 * q + half : half * 4 + q;
+        return *reinterpret_cast<const bf16x8*>(xt + r * 32 * (kTileK * 2) + (piece ^ (l32 & 7)) * 16);
+      };
+      float s[GS], z[GS];
+#pragma unroll
+      for (int e = 0; e < GS; ++e) {
+        const uint8_t* const at = scales + place * 1024 + l32 * 16 + min(g0 + e, groups - 1) % 8 * 2;
+        s[e] = bf2f(*reinterpret_cast<const bf16_t*>(at));
+        z[e] = g.zero ? bf2f(*reinterpret_cast<const bf16_t*>(at + 512)) : 8.f;
+      }
+      // a product's fragments are read and its codes converted under the one before
+      bf16x8 a[4], b[2];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) a[r] = x_frag(0, r);
+      b[0] = codes_less(cw[0], z[0]);
+      constexpr int EACH = 4 / GS;
+#pragma unroll
+      for (int e = 0; e < GS; ++e) {
+        f32x16 part[4];
+#pragma unroll
+        for (int p = 0; p < EACH; ++p) {
+          const int q = e * EACH + p;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            part[r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[r], b[q & 1], p == 0 ? zero16 : part[r], 0, 0, 0);
+            if (q < 3) a[r] = x_frag(q + 1, r);
+          }
+          if (q < 3) b[(q + 1) & 1] = codes_less(cw[q + 1], z[(q + 1) / EACH]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) total[r][x] = fmaf(s[e], part[r][x], total[r][x]);
+        asm volatile("" : "+v"(total[0]), "+v"(total[1]), "+v"(total[2]), "+v"(total[3]));    // (here and not later, or the groups' sums live side by side)
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      arrived(two_steps{});
     }
-#pragma unroll
-    for (int e = 0; e < (G32 ? 2 : 1); ++e) {
-      f32x16 part[2][2];
-#pragma unroll
-      for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-          for (int x = 0; x < 16; ++x) part[r][c][x] = 0.f;
-#pragma unroll
-      for (int q = e * 2; q < (G32 ? e * 2 + 2 : 4); ++q) {
-        const int piece = G32 ? 2 * q + half : half * 4 + q;
-        bf16x8 a[2], b[2];
-#pragma unroll
-        for (int r = 0; r < 2; ++r) a[r] = *reinterpret_cast<const bf16x8*>(xt + r * 32 * (kTileK * 2) + (piece ^ (l32 & 7)) * 16);
-#pragma unroll
-        for (int c = 0; c < 2; ++c) b[c] = codes_less(cw[c][q], z[c][e]);
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) part[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[r], b[c], part[r][c], 0, 0, 0);
-      }
-#pragma unroll
-      for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-          for (int x = 0; x < 16; ++x) total[r][c][x] = fmaf(s[c][e], part[r][c][x], total[r][c][x]);
-    }
-    if (fresh) keep(++kept);
-    arrived();
   }
 
   // the sums meet in LDS (no load is on its way to it any more), and leave it row by row
@@ -373,18 +408,16 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
   for (int pass = 1; pass >= 0; --pass) {
     if (set == pass) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r)
+      for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-          for (int x = 0; x < 16; ++x) {
-            float* const at = joined + (wm * 64 + r * 32 + 8 * (x / 4) + 4 * half + x % 4) * kTileN + wn * 64 + c * 32 + l32;
-            *at = pass == 1 ? total[r][c][x] : total[r][c][x] + *at;
-          }
+        for (int x = 0; x < 16; ++x) {
+          float* const at = joined + (r * 32 + 8 * (x / 4) + 4 * half + x % 4) * kTileN + col;
+          *at = pass == 1 ? total[r][x] : total[r][x] + *at;
+        }
     }
     __syncthreads();
   }
-  const bool wide = g.ldo % 8 == 0 && (uintptr_t)g.out % 16 == 0 && (!g.resid || (g.ldr % 8 == 0 && (uintptr_t)g.resid % 16 == 0));
+  const bool wide_out = g.ldo % 8 == 0 && (uintptr_t)g.out % 16 == 0 && (!g.resid || (g.ldr % 8 == 0 && (uintptr_t)g.resid % 16 == 0));
   const int c8 = threadIdx.x % 16 * 8;
   const int64_t n = n0 + c8;
   if (n >= g.n) return;
@@ -400,7 +433,7 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
     activate(v, g.act);
     bf16_t* const out = (bf16_t*)g.out + (m0 + row) * g.ldo + n;
     const bf16_t* const resid = (const bf16_t*)g.resid + (m0 + row) * g.ldr + n;
-    if (wide && cols == 8) {
+    if (wide_out && cols == 8) {
       if (g.resid) {
         float r[8];
         load_vec(resid, r);
@@ -416,20 +449,21 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
   }
 }
 
-// Rows of x that direct loads can take: 16-byte pieces that hold columns of k alone.
+// Rows of x that direct loads can take: 16-byte pieces that hold columns of k alone; and offsets within a tile of 32 bits.
 bool tiles_take(const LinearW4Args& g) {
-  return g.dtype == AC_BF16 && g.m >= kTileRows && (uintptr_t)g.x % 16 == 0 && g.ldx % 8 == 0 && g.k % 8 == 0;
+  return g.dtype == AC_BF16 && g.m >= kTileRows && (uintptr_t)g.x % 16 == 0 && g.ldx % 8 == 0 && g.k % 8 == 0 && g.k < 1 << 22 && g.ldx < 1 << 22 && g.ldw < 1 << 24 &&
+         g.lds < 1 << 22 && g.ldz < 1 << 22;
 }
 
-template <bool G32>
+template <int GS>
 hipError_t launch_tiles(const LinearW4Args& g, hipStream_t s) {
   constexpr size_t lds = 2 * kSetBytes;
   static_assert(lds >= 4 * 64 * 64 * sizeof(float) && lds <= 160 * 1024, "one block a CU");
-  static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(linear_w4_tiles<G32>),
+  static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(linear_w4_tiles<GS>),
                                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (attr_status != hipSuccess) return attr_status;
   const dim3 grid((unsigned)((g.n + kTileN - 1) / kTileN), (unsigned)((g.m + kTileM - 1) / kTileM));
-  hipLaunchKernelGGL((linear_w4_tiles<G32>), grid, dim3(512), lds, s, g);
+  hipLaunchKernelGGL((linear_w4_tiles<GS>), grid, dim3(512), lds, s, g);
   return hipGetLastError();
 }
 
@@ -437,7 +471,7 @@ hipError_t launch_tiles(const LinearW4Args& g, hipStream_t s) {
 
 hipError_t launch_linear_w4(const LinearW4Args& g, hipStream_t s) {
   if (g.m <= 0 || g.n <= 0) return hipSuccess;
-  if (tiles_take(g)) return g.group.d == 32 ? launch_tiles<true>(g, s) : launch_tiles<false>(g, s);
+  if (tiles_take(g)) return g.group.d == 32 ? launch_tiles<2>(g, s) : launch_tiles<1>(g, s);
   return g.dtype == AC_BF16 ? launch_rows<bf16_t, 1>(g, s) : launch_rows<float, 3>(g, s);
 }
 

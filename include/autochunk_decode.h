@@ -47,7 +47,7 @@ typedef struct ac_kv_cache {
 
 /*
  * The rows of one call and where their sequences' tokens lie.  Sequence b has the rows row_begin[b] .. row_begin[b + 1] - 1 of
- * the call's matrices (possibly none), which are the last of its length[b] tokens; token t lies in page
+ * the call's matrices (possibly none; rows past the matrices' n_rows do not exist), which are the last of its length[b] tokens; token t lies in page
  * page_table[b * ld_page_table + t / page], at place t mod page.  Places past ld_page_table pages do not exist; a page number outside
  * [0, pages) names no memory: what would be stored there is dropped, what would be read there counts as masked.  So do rows that a length
  * shorter than the sequence's rows would put in front of token 0.  max_rows and max_length: the most rows and tokens of one
@@ -57,7 +57,7 @@ typedef struct ac_cache_rows {
   const int32_t* row_begin;         /* dev, [batch + 1] */
   const int32_t* length;            /* dev, [batch] */
   const int32_t* page_table;        /* dev, [batch][ld_page_table] */
-  int64_t ld_page_table, batch, rows, max_rows, max_length;
+  int64_t ld_page_table, batch, max_rows, max_length;
 } ac_cache_rows;
 
 /*
@@ -77,8 +77,8 @@ typedef struct ac_rotary {
 } ac_rotary;
 
 /*
- * Rotates the rows' keys (and queries) and stores keys and values in the cache.  k, v: [rows][cache->heads * head_dim], rows ldk, ldv apart;
- * q (may be NULL): [rows][heads * head_dim], its rotated rows go to q_out, which may be q.  rotary may be NULL (positions are in the rows already).
+ * Rotates the rows' keys (and queries) and stores keys and values in the cache.  k, v: [n_rows][cache->heads * head_dim], rows ldk, ldv apart;
+ * q (may be NULL): [n_rows][heads * head_dim], its rotated rows go to q_out, which may be q.  rotary may be NULL (positions are in the rows already).
  * A block that gets rows takes as its scale the least power of two s >= 2^-100 with |x| <= 448 s for all its finite new elements, or the scale that it has if it holds older
  * tokens and that one is larger; elements are stored as the nearest e4m3 number (ties to even) of x / s, infinities and NaN as NaN.  Where older tokens' scale
  * grows, their codes are rewritten as the nearest of code * (old scale / s), which is exact for all but the smallest numbers.  Tokens of a block
@@ -86,21 +86,22 @@ typedef struct ac_rotary {
  * All rows and q_out's on 8-byte (bf16) / 16-byte (fp32) boundaries, tables on 16-byte ones, ld_table a multiple of 4, else AC_ERR_ALIGN.
  */
 int ac_op_cache_append(const void* q, int64_t ldq, void* q_out, int64_t ldqo, int heads, const void* k, int64_t ldk, const void* v,
-                       int64_t ldv, const ac_kv_cache* cache, const ac_cache_rows* rows, const ac_rotary* rotary, int dtype,
-                       void* stream);
+                       int64_t ldv, int64_t n_rows, const ac_kv_cache* cache, const ac_cache_rows* rows, const ac_rotary* rotary,
+                       int dtype, void* stream);
 
 /*
  * out[r, h] = softmax(scale * q[r, h] . k) v over the tokens that row r sees: all of its sequence's, or with causal != 0 those up to its own place.
  * Query head h reads head h / (heads / cache->heads) of the cache (heads a multiple of cache->heads).  A row that sees nothing (length 0)
- * comes out as zeros; tokens that a row does not see do not reach it, whatever their codes.  q, out: [rows][heads * head_dim], rows on
+ * comes out as zeros; tokens that a row does not see do not reach it, whatever their codes.  q, out: [n_rows][heads * head_dim], rows on
  * 16-byte boundaries, else AC_ERR_ALIGN.  Few rows over many tokens are split over the tokens, and the parts joined by a second kernel:
  * workspace (dev, 16-byte aligned) holds them, ac_cache_attention_workspace_bytes() large (0: none needed), else AC_ERR_WORKSPACE.
- * Results do not depend on what else runs, but on the split: on max_rows, max_length, batch and rows.
+ * Results do not depend on what else runs, but on the split: on max_rows, max_length, batch and n_rows.
  */
-int ac_op_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int heads, const ac_kv_cache* cache,
+int ac_op_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int64_t n_rows, int heads, const ac_kv_cache* cache,
                           const ac_cache_rows* rows, int causal, float scale, void* workspace, uint64_t workspace_bytes, int dtype,
                           void* stream);
-uint64_t ac_cache_attention_workspace_bytes(int heads, const ac_kv_cache* cache, const ac_cache_rows* rows, int causal, int dtype);
+uint64_t ac_cache_attention_workspace_bytes(int64_t n_rows, int heads, const ac_kv_cache* cache, const ac_cache_rows* rows, int causal,
+                                            int dtype);
 
 #ifdef __cplusplus
 }

@@ -89,7 +89,7 @@ class ac_kv_cache(C.Structure):
 
 class ac_cache_rows(C.Structure):
     _fields_ = [("row_begin", C.c_void_p), ("length", C.c_void_p), ("page_table", C.c_void_p), ("ld_page_table", C.c_int64),
-                ("batch", C.c_int64), ("rows", C.c_int64), ("max_rows", C.c_int64), ("max_length", C.c_int64)]
+                ("batch", C.c_int64), ("max_rows", C.c_int64), ("max_length", C.c_int64)]
 
 
 class ac_rotary(C.Structure):
@@ -161,11 +161,11 @@ SIGNATURES = {
     "ac_op_group_norm": (INT, [VP, VP, VP, VP, VP, U64, I64, I64, INT, INT, C.c_float, INT, INT, VP]),
     "ac_op_conv3x3": (INT, [VP, VP, VP, INT, VP, VP, I64, INT, INT, INT, INT, INT, VP]),
     "ac_op_linear_w4": (INT, [VP, I64, VP, I64, VP, I64, VP, I64, I64, VP, VP, I64, VP, I64, I64, I64, I64, INT, INT, VP]),
-    "ac_op_cache_append": (INT, [VP, I64, VP, I64, INT, VP, I64, VP, I64, C.POINTER(ac_kv_cache), C.POINTER(ac_cache_rows),
+    "ac_op_cache_append": (INT, [VP, I64, VP, I64, INT, VP, I64, VP, I64, I64, C.POINTER(ac_kv_cache), C.POINTER(ac_cache_rows),
                                  C.POINTER(ac_rotary), INT, VP]),
-    "ac_op_cache_attention": (INT, [VP, I64, VP, I64, INT, C.POINTER(ac_kv_cache), C.POINTER(ac_cache_rows), INT, F32, VP, U64,
+    "ac_op_cache_attention": (INT, [VP, I64, VP, I64, I64, INT, C.POINTER(ac_kv_cache), C.POINTER(ac_cache_rows), INT, F32, VP, U64,
                                     INT, VP]),
-    "ac_cache_attention_workspace_bytes": (U64, [INT, C.POINTER(ac_kv_cache), C.POINTER(ac_cache_rows), INT, INT]),
+    "ac_cache_attention_workspace_bytes": (U64, [I64, INT, C.POINTER(ac_kv_cache), C.POINTER(ac_cache_rows), INT, INT]),
     "ac_chunk_trace": (INT, [C.POINTER(ac_graph_node), INT, INT, INT, INT, INT, I32P, U8P, INTP]),
     "ac_chunk_search": (INT, [C.POINTER(ac_graph_node), INT, INT, INT, INT, C.POINTER(ac_chunk_candidate), I32P, U8P,
                               INT, INTP, INTP, INTP]),
@@ -211,8 +211,10 @@ def _check(status, where):
 
 
 def _stream():
+    """The address of torch's current stream; without the stream object, whose making takes longer than a launch."""
     import torch
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(torch.cuda.current_device()) if raw is not None else torch.cuda.current_stream().cuda_stream
 
 
 def _ptr(t):
@@ -492,40 +494,44 @@ def ac_op_conv3x3(x, weight, out, bias=None, bias_per_image=False, residual=None
 
 
 # ---- decoding ---------------------------------------------------------------------------------
+# (A step of a few microseconds waits for these functions: checks are plain comparisons, addresses go to the library as numbers.)
 
-def _require(tensor, dtype, what):
-    if tensor is not None and tensor.dtype != dtype:
-        raise TypeError(f"{what} is {tensor.dtype}, not {dtype}")
-
-
-def _inner(t, what):
-    """Tensors whose rows the library steps through: elements of a row side by side."""
-    if t is not None and t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{what}: the last dimension is not contiguous")
-    return t
+def _bad(what, t, want):
+    raise ValueError(f"{what} is {tuple(t.shape)} with strides {t.stride()}: {want}")
 
 
-def _ld(t):
-    """Elements between a matrix's rows; of a single row, whatever it is wide."""
-    return 0 if t is None else t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+def _matrix(t, what, dtype, rows, cols):
+    """(address, elements between rows) of a [rows, cols] tensor with elements of a row side by side; (None, 0) of None."""
+    if t is None:
+        return None, 0
+    if t.dtype is not dtype:
+        raise TypeError(f"{what} is {t.dtype}, not {dtype}")
+    if t.shape != (rows, cols):
+        _bad(what, t, f"({rows}, {cols}) is wanted")
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
+        _bad(what, t, "elements of a row side by side are wanted")
+    return t.data_ptr(), ld if rows > 1 else max(ld, cols)
 
 
 def ac_op_linear_w4(x, w, scale, out, group, zero=None, bias=None, residual=None, activation=AC_ACT_NONE):
     """x [m, k], w uint8 [n, bytes of a row] (two codes a byte, the even column's in the low bits), scale and zero
     [n, ceil(k / group)] -> out [m, n]."""
     import torch
-    (m, k), n = x.shape, w.shape[0]
-    _require(w, torch.uint8, "w")
-    for t, what, shape in ((scale, "scale", (n, -(-k // group))), (zero, "zero", (n, -(-k // group))), (bias, "bias", (n,)),
-                           (residual, "residual", (m, n)), (out, "out", (m, n))):
-        if t is not None and tuple(t.shape) != shape:
-            raise ValueError(f"{what} is {tuple(t.shape)}, not {shape}")
-        _require(_inner(t, what), x.dtype, what)
-    if w.shape[1] < (k + 1) // 2:
-        raise ValueError(f"w holds {2 * w.shape[1]} columns, not {k}")
-    _check(lib().ac_op_linear_w4(_ptr(_inner(x, "x")), _ld(x), _ptr(_inner(w, "w")), _ld(w), _ptr(scale), _ld(scale), _ptr(zero), _ld(zero),
-                                 group, _ptr(bias), _ptr(residual), _ld(residual), _ptr(out), _ld(out), m, n, k, activation, _dt(x),
-                                 _stream()), "ac_op_linear_w4")
+    (m, k), (n, row), dt = x.shape, w.shape, x.dtype
+    groups = -(-k // group)
+    xp, ldx = _matrix(x, "x", dt, m, k)
+    wp, ldw = _matrix(w, "w", torch.uint8, n, row)
+    sp, lds = _matrix(scale, "scale", dt, n, groups)
+    zp, ldz = _matrix(zero, "zero", dt, n, groups)
+    rp, ldr = _matrix(residual, "residual", dt, m, n)
+    op, ldo = _matrix(out, "out", dt, m, n)
+    if bias is not None and (bias.dtype is not dt or bias.shape != (n,) or (n > 1 and bias.stride(0) != 1)):
+        _bad("bias", bias, f"({n},) of {dt}, contiguous, is wanted")
+    if 2 * row < k:
+        _bad("w", w, f"{k} columns are wanted")
+    _check(lib().ac_op_linear_w4(xp, ldx, wp, ldw, sp, lds, zp, ldz, group, None if bias is None else bias.data_ptr(), rp, ldr, op, ldo, m, n, k,
+                                 activation, _dt(x), _stream()), "ac_op_linear_w4")
 
 
 def kv_cache(k, v, k_scale, v_scale) -> ac_kv_cache:
@@ -533,15 +539,15 @@ def kv_cache(k, v, k_scale, v_scale) -> ac_kv_cache:
     fp32 [pages, heads, page / 16]; pages may lie further apart than they are long.  Keeps the tensors alive."""
     import torch
     pages, heads, page, d = k.shape
-    if tuple(v.shape) != (pages, heads, page // 16, d, 16) or any(tuple(s.shape) != (pages, heads, page // 16) for s in (k_scale, v_scale)):
+    if v.shape != (pages, heads, page // 16, d, 16) or any(s.shape != (pages, heads, page // 16) for s in (k_scale, v_scale)):
         raise ValueError(f"k {tuple(k.shape)}, v {tuple(v.shape)}, scales {tuple(k_scale.shape)}, {tuple(v_scale.shape)} are no cache")
     for t, what in ((k, "k"), (v, "v"), (k_scale, "k_scale"), (v_scale, "v_scale")):
         if pages and not t[0].is_contiguous():
-            raise ValueError(f"{what}: a page is not contiguous")
+            _bad(what, t, "contiguous pages are wanted")
     if k.element_size() != 1 or v.element_size() != 1:
         raise TypeError(f"codes are {k.dtype}, {v.dtype}: one byte each is wanted")
-    _require(k_scale, torch.float32, "k_scale")
-    _require(v_scale, torch.float32, "v_scale")
+    if k_scale.dtype is not torch.float32 or v_scale.dtype is not torch.float32:
+        raise TypeError(f"scales are {k_scale.dtype}, {v_scale.dtype}: float32 is wanted")
     apart = lambda t: t.stride(0) if pages > 1 else t.numel()  # noqa: E731
     if apart(k) != apart(v) or apart(k_scale) != apart(v_scale):
         raise ValueError("pages of keys and of values lie differently far apart")
@@ -550,20 +556,18 @@ def kv_cache(k, v, k_scale, v_scale) -> ac_kv_cache:
     return c
 
 
-def cache_rows(row_begin, length, page_table, max_rows, max_length, rows=None) -> ac_cache_rows:
-    """A call's rows: row_begin int32 [batch + 1], length int32 [batch], page_table int32 [batch, pages of a sequence], on the device.  rows:
-    those of the call's matrices (by default as many as the call's k or q has).  Keeps the tensors alive."""
+def cache_rows(row_begin, length, page_table, max_rows, max_length) -> ac_cache_rows:
+    """A call's rows: row_begin int32 [batch + 1], length int32 [batch], page_table int32 [batch, pages of a sequence], on the device.  Keeps the
+    tensors alive."""
     import torch
-    batch = length.shape[0]
-    if row_begin.shape[0] != batch + 1 or page_table.shape[0] != batch:
-        raise ValueError(f"{batch} lengths, {row_begin.shape[0]} row bounds, {page_table.shape[0]} rows of pages")
-    for t, what in ((row_begin, "row_begin"), (length, "length"), (page_table, "page_table")):
-        _require(_inner(t, what), torch.int32, what)
-    ld = page_table.stride(0) if batch > 1 else page_table.shape[1]
-    if batch > 1 and ld < page_table.shape[1]:
-        raise ValueError("page_table: rows overlap")
-    r = ac_cache_rows(row_begin.data_ptr(), length.data_ptr(), page_table.data_ptr(), ld, batch, -1 if rows is None else rows,
-                      max_rows, max_length)
+    batch, pages = page_table.shape
+    if length.shape != (batch,) or row_begin.shape != (batch + 1,):
+        raise ValueError(f"{tuple(length.shape)} lengths, {tuple(row_begin.shape)} row bounds, {batch} rows of pages")
+    for t, what in ((row_begin, "row_begin"), (length, "length")):
+        if t.dtype is not torch.int32 or not t.is_contiguous():
+            raise TypeError(f"{what} is {t.dtype} with strides {t.stride()}: contiguous int32 is wanted")
+    table, ld = _matrix(page_table, "page_table", torch.int32, batch, pages)
+    r = ac_cache_rows(row_begin.data_ptr(), length.data_ptr(), table, ld, batch, max_rows, max_length)
     r.keep = (row_begin, length, page_table)
     return r
 
@@ -571,61 +575,56 @@ def cache_rows(row_begin, length, page_table, max_rows, max_length, rows=None) -
 def rotary(cos, sin, positions=None, sections=None, interleaved=False) -> ac_rotary:
     """cos, sin fp32 [positions, pairs]; positions int32 [axes, rows] or None; sections: pairs of each axis.  Keeps the tensors alive."""
     import torch
-    pairs = cos.shape[1]
-    if sin.shape != cos.shape or _ld(sin) != _ld(cos):
-        raise ValueError("cos and sin differ in shape or stride")
-    for t, what in ((cos, "cos"), (sin, "sin")):
-        _require(_inner(t, what), torch.float32, what)
-    _require(_inner(positions, "positions"), torch.int32, "positions")
+    rows, pairs = cos.shape
+    cp, ld = _matrix(cos, "cos", torch.float32, rows, pairs)
+    sp, lds = _matrix(sin, "sin", torch.float32, rows, pairs)
+    if ld != lds:
+        raise ValueError(f"rows of cos are {ld} apart, of sin {lds}")
     sections = (pairs,) if sections is None else tuple(sections)
-    if len(sections) > 4 or (positions is not None and positions.shape[0] != len(sections)):
+    if len(sections) > 4 or (positions is not None and (positions.dim() != 2 or positions.shape[0] != len(sections))):
         raise ValueError(f"{len(sections)} sections, positions {None if positions is None else tuple(positions.shape)}")
-    r = ac_rotary(cos.data_ptr(), sin.data_ptr(), cos.shape[0], _ld(cos), None if positions is None else positions.data_ptr(), _ld(positions),
-                  pairs, int(interleaved), len(sections), (C.c_int32 * 4)(*sections))
+    pp, ldp = (None, 0) if positions is None else _matrix(positions, "positions", torch.int32, *positions.shape)
+    r = ac_rotary(cp, sp, rows, ld, pp, ldp, pairs, int(interleaved), len(sections), (C.c_int32 * 4)(*sections))
     r.keep = (cos, sin, positions)
     r.n_positions = None if positions is None else positions.shape[1]
     return r
 
 
-def _of_rows(rows, n):
-    """`rows` for matrices of n rows."""
-    if rows.rows == n:
-        return rows
-    if rows.rows >= 0:
-        raise ValueError(f"{n} rows, and {rows.rows} described")
-    r = ac_cache_rows.from_buffer_copy(rows)
-    r.rows = n
-    return r
-
-
 def ac_op_cache_append(k, v, cache, rows, q=None, q_out=None, rotary=None):
     """k, v [rows, heads of the cache * head_dim], q and q_out [rows, heads * head_dim] (views of one projection's rows are fine)."""
-    n, kv = k.shape[0], cache.heads * cache.head_dim
-    for t, what, width in ((k, "k", kv), (v, "v", kv), (q, "q", None), (q_out, "q_out", None if q is None else q.shape[1])):
-        if t is not None and (t.shape[0] != n or (width is not None and t.shape[1] != width) or t.shape[1] % cache.head_dim):
-            raise ValueError(f"{what} is {tuple(t.shape)}: {n} rows of {width or 'heads of'} {cache.head_dim} are wanted")
-        _require(_inner(t, what), k.dtype, what)
+    n, d, dt = k.shape[0], cache.head_dim, k.dtype
+    kv = cache.heads * d
+    kp, ldk = _matrix(k, "k", dt, n, kv)
+    vp, ldv = _matrix(v, "v", dt, n, kv)
+    qp, ldq, op, ldo, heads = None, 0, None, 0, 0
+    if q is not None:
+        width = q.shape[1]
+        heads = width // d
+        if width % d or q_out is None:
+            _bad("q", q, f"heads of {d}, and a place for the rotated ones, are wanted")
+        qp, ldq = _matrix(q, "q", dt, n, width)
+        op, ldo = _matrix(q_out, "q_out", dt, n, width)
     if rotary is not None and rotary.n_positions is not None and rotary.n_positions < n:
         raise ValueError(f"{rotary.n_positions} positions for {n} rows")
-    _check(lib().ac_op_cache_append(_ptr(q), _ld(q), _ptr(q_out), _ld(q_out), 0 if q is None else q.shape[1] // cache.head_dim, _ptr(k), _ld(k),
-                                    _ptr(v), _ld(v), C.byref(cache), C.byref(_of_rows(rows, n)), None if rotary is None else C.byref(rotary),
-                                    _dt(k), _stream()), "ac_op_cache_append")
+    _check(lib().ac_op_cache_append(qp, ldq, op, ldo, heads, kp, ldk, vp, ldv, n, C.byref(cache), C.byref(rows),
+                                    None if rotary is None else C.byref(rotary), _dt(k), _stream()), "ac_op_cache_append")
 
 
 def ac_cache_attention_workspace_bytes(q, cache, rows, causal=True):
-    return int(lib().ac_cache_attention_workspace_bytes(q.shape[1] // cache.head_dim, C.byref(cache), C.byref(_of_rows(rows, q.shape[0])),
-                                                        int(causal), _dt(q)))
+    n, width = q.shape
+    return int(lib().ac_cache_attention_workspace_bytes(n, width // cache.head_dim, C.byref(cache), C.byref(rows), int(causal), _dt(q)))
 
 
 def ac_op_cache_attention(q, out, cache, rows, causal=True, scale=None, workspace=None):
     """q, out [rows, heads * head_dim]; scale: 1 / sqrt(head_dim) by default."""
-    if q.shape != out.shape or q.shape[1] % cache.head_dim:
-        raise ValueError(f"q {tuple(q.shape)}, out {tuple(out.shape)}, heads of {cache.head_dim}")
-    _require(_inner(out, "out"), q.dtype, "out")
-    _check(lib().ac_op_cache_attention(_ptr(_inner(q, "q")), _ld(q), _ptr(out), _ld(out), q.shape[1] // cache.head_dim, C.byref(cache),
-                                       C.byref(_of_rows(rows, q.shape[0])), int(causal), cache.head_dim ** -0.5 if scale is None else scale,
-                                       _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _dt(q),
-                                       _stream()), "ac_op_cache_attention")
+    (n, width), d = q.shape, cache.head_dim
+    if width % d:
+        _bad("q", q, f"heads of {d} are wanted")
+    qp, ldq = _matrix(q, "q", q.dtype, n, width)
+    op, ldo = _matrix(out, "out", q.dtype, n, width)
+    ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _check(lib().ac_op_cache_attention(qp, ldq, op, ldo, n, width // d, C.byref(cache), C.byref(rows), int(causal),
+                                       d ** -0.5 if scale is None else scale, ws, size, _dt(q), _stream()), "ac_op_cache_attention")
 
 
 # ---- helpers for callers (buffers only) ------------------------------------------------------

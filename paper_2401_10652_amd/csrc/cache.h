@@ -12,7 +12,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 struct Sequence { int64_t begin, rows, length; };   // its first row, its rows, its tokens with them
 
-__device__ __forceinline__ Sequence sequence(const ac_cache_rows& r, int64_t b) {
+__device__ __forceinline__ Sequence sequence(const CacheRows& r, int64_t b) {
   const int64_t lo = r.row_begin[b], hi = r.row_begin[b + 1];
   const int64_t from = lo < 0 ? 0 : lo, to = hi < r.rows ? hi : r.rows, n = r.length[b];
   return Sequence{from, to > from ? to - from : 0, n > 0 ? n : 0};
@@ -35,7 +35,7 @@ struct CacheAttnArgs {
   int64_t ldq, ldo;
   int heads;
   ac_kv_cache cache;
-  ac_cache_rows rows;
+  CacheRows rows;
   int causal;
   float scale;                      // times log2 e
   Divisor group, blocks;            // query heads of a key head, blocks of a page

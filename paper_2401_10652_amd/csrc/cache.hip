@@ -70,7 +70,7 @@ struct AppendArgs {
   int64_t ldq, ldqo, ldk, ldv;
   int heads;
   ac_kv_cache cache;
-  ac_cache_rows rows;
+  CacheRows rows;
   ac_rotary rot;
 };
 
@@ -542,7 +542,7 @@ struct Shape { int rows, tiles, splits; };
 // Runs of keys: as many as fill the chip, and no longer than kLongRun, so that sequences of all lengths, of which the host knows only the longest,
 // keep it filled to the end.
 constexpr int kMostSplits = 128, kLeastRun = 256, kLongRun = 2048, kPlaces = 1024, kPromptPlaces = 256, kPromptRows = 64;
-Shape shape(int heads, const ac_kv_cache& c, const ac_cache_rows& r, int dtype) {
+Shape shape(int heads, const ac_kv_cache& c, const CacheRows& r, int dtype) {
   const int64_t rows = (r.max_rows < r.rows ? r.max_rows : r.rows) * (heads / c.heads);
   const bool prompt = dtype == AC_BF16 && c.pages > 0 && rows > kPromptRows;
   Shape s;
@@ -625,20 +625,20 @@ hipError_t append_width(const AppendArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_cache_append(const void* q, int64_t ldq, void* q_out, int64_t ldqo, int heads, const void* k, int64_t ldk, const void* v,
-                               int64_t ldv, const ac_kv_cache& cache, const ac_cache_rows& rows, const ac_rotary* rotary, int dtype,
+                               int64_t ldv, const ac_kv_cache& cache, const CacheRows& rows, const ac_rotary* rotary, int dtype,
                                hipStream_t s) {
   if (rows.batch <= 0 || rows.rows <= 0) return hipSuccess;
   AppendArgs a{q, k, v, q_out, ldq, ldqo, ldk, ldv, q ? heads : 0, cache, rows, rotary ? *rotary : ac_rotary{}};
   return dtype == AC_BF16 ? append_width<bf16_t>(a, s) : append_width<float>(a, s);
 }
 
-uint64_t cache_attention_workspace_bytes(int heads, const ac_kv_cache& cache, const ac_cache_rows& rows, int causal, int dtype) {
+uint64_t cache_attention_workspace_bytes(int heads, const ac_kv_cache& cache, const CacheRows& rows, int causal, int dtype) {
   const int n = shape(heads, cache, rows, dtype).splits;
   return n == 1 ? 0 : (uint64_t)n * rows.rows * heads * (cache.head_dim + 2) * sizeof(float);
 }
 
 hipError_t launch_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int heads, const ac_kv_cache& cache,
-                                  const ac_cache_rows& rows, int causal, float scale, void* workspace, int dtype, hipStream_t s) {
+                                  const CacheRows& rows, int causal, float scale, void* workspace, int dtype, hipStream_t s) {
   if (rows.batch <= 0 || rows.rows <= 0) return hipSuccess;
   const Shape sh = shape(heads, cache, rows, dtype);
   const int n = sh.splits;

@@ -373,12 +373,13 @@ struct LinearW4Args {
   int act, dtype;
 };
 hipError_t launch_linear_w4(const LinearW4Args& g, hipStream_t s);
+struct CacheRows : ac_cache_rows { int64_t rows; };   // with the rows of the call's matrices
 hipError_t launch_cache_append(const void* q, int64_t ldq, void* q_out, int64_t ldqo, int heads, const void* k, int64_t ldk, const void* v,
-                               int64_t ldv, const ac_kv_cache& cache, const ac_cache_rows& rows, const ac_rotary* rotary, int dtype,
+                               int64_t ldv, const ac_kv_cache& cache, const CacheRows& rows, const ac_rotary* rotary, int dtype,
                                hipStream_t s);
 hipError_t launch_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int heads, const ac_kv_cache& cache,
-                                  const ac_cache_rows& rows, int causal, float scale, void* workspace, int dtype, hipStream_t s);
-uint64_t cache_attention_workspace_bytes(int heads, const ac_kv_cache& cache, const ac_cache_rows& rows, int causal, int dtype);
+                                  const CacheRows& rows, int causal, float scale, void* workspace, int dtype, hipStream_t s);
+uint64_t cache_attention_workspace_bytes(int heads, const ac_kv_cache& cache, const CacheRows& rows, int causal, int dtype);
 
 // hipErrorInvalidValue-style refusal with a message for ac_last_error().
 void set_error(const char* fmt, ...);

@@ -2187,12 +2187,12 @@ int ac_op_linear_w4(const void* x, int64_t ldx, const void* w, int64_t ldw, cons
 }
 
 // What append and attention ask of a cache and of the rows' descriptions; AC_OK, or the refusal.
-static int cache_ok(const char* what, const ac_kv_cache* c, const ac_cache_rows* r) {
+static int cache_ok(const char* what, const ac_kv_cache* c, const ac_cache_rows* r, int64_t n_rows) {
   if (!c || !r || !c->k || !c->v || !c->k_scale || !c->v_scale || c->pages < 0 || c->page < 16 || c->page % 16 != 0 || c->heads < 1 ||
-      c->heads > 4096 || c->head_dim < 1 || !r->row_begin || !r->length || !r->page_table || r->ld_page_table < 0 || r->batch < 0 || r->rows < 0 ||
+      c->heads > 4096 || c->head_dim < 1 || !r->row_begin || !r->length || !r->page_table || r->ld_page_table < 0 || r->batch < 0 || n_rows < 0 ||
       r->max_rows < 0 || r->max_length < 0)
     return fail(AC_ERR_ARG, "%s: bad cache or rows", what);
-  if (r->batch > 65535 || r->rows > 1 << 30 || r->max_length > 1 << 30 || r->ld_page_table > (1 << 30) / c->page)
+  if (r->batch > 65535 || n_rows > 1 << 30 || r->max_length > 1 << 30 || r->ld_page_table > (1 << 30) / c->page)
     return fail(AC_ERR_UNSUPPORTED, "%s: at most 65535 sequences, 2^30 rows and places of a sequence", what);
   const int d = c->head_dim;
   if (d != 32 && d != 64 && d != 96 && d != 128 && d != 192 && d != 256)
@@ -2210,12 +2210,12 @@ static bool rows_on(const void* p, int64_t ld, int64_t bytes, int dtype) {
 }
 
 int ac_op_cache_append(const void* q, int64_t ldq, void* q_out, int64_t ldqo, int heads, const void* k, int64_t ldk, const void* v,
-                       int64_t ldv, const ac_kv_cache* cache, const ac_cache_rows* rows, const ac_rotary* rotary, int dtype,
-                       void* stream) {
+                       int64_t ldv, int64_t n_rows, const ac_kv_cache* cache, const ac_cache_rows* rows, const ac_rotary* rotary,
+                       int dtype, void* stream) {
   const char* const what = "ac_op_cache_append";
-  if (const int st = cache_ok(what, cache, rows)) return st;
+  if (const int st = cache_ok(what, cache, rows, n_rows)) return st;
   const int64_t d = cache->head_dim, kv = cache->heads * d;
-  if (rows->rows == 0 || rows->batch == 0) return AC_OK;
+  if (n_rows == 0 || rows->batch == 0) return AC_OK;
   if (!k || !v || ldk < kv || ldv < kv || !dtype_ok(dtype) || (q && (!q_out || heads < 1 || heads > 4096 || ldq < heads * d || ldqo < heads * d)))
     return fail(AC_ERR_ARG, "%s: bad argument", what);
   if (rotary) {
@@ -2227,7 +2227,7 @@ int ac_op_cache_append(const void* q, int64_t ldq, void* q_out, int64_t ldqo, in
       sum += rotary->section[i];
     }
     if ((rotary->pairs > 0 && (!rotary->cos || !rotary->sin)) || rotary->pairs < 0 || !sections || 2 * (int64_t)rotary->pairs > d || sum != rotary->pairs || rotary->table_rows < 1 ||
-        rotary->ld_table < rotary->pairs || (rotary->positions && rotary->axes > 1 && rotary->ld_positions < rows->rows))
+        rotary->ld_table < rotary->pairs || (rotary->positions && rotary->axes > 1 && rotary->ld_positions < n_rows))
       return fail(AC_ERR_ARG, "%s: bad rotation", what);
     if (rotary->pairs % 4 != 0) return fail(AC_ERR_UNSUPPORTED, "%s: pairs in multiples of 4", what);
     if ((uintptr_t)rotary->cos % 16 != 0 || (uintptr_t)rotary->sin % 16 != 0 || rotary->ld_table % 4 != 0)
@@ -2236,31 +2236,33 @@ int ac_op_cache_append(const void* q, int64_t ldq, void* q_out, int64_t ldqo, in
   const int64_t on = dtype == AC_BF16 ? 8 : 16;
   if (!rows_on(k, ldk, on, dtype) || !rows_on(v, ldv, on, dtype) || (q && (!rows_on(q, ldq, on, dtype) || !rows_on(q_out, ldqo, on, dtype))))
     return fail(AC_ERR_ALIGN, "%s: rows start at multiples of %lld bytes", what, (long long)on);
-  return hip_status(launch_cache_append(q, ldq, q_out, ldqo, heads, k, ldk, v, ldv, *cache, *rows, rotary, dtype, (hipStream_t)stream),
+  return hip_status(launch_cache_append(q, ldq, q_out, ldqo, heads, k, ldk, v, ldv, *cache, CacheRows{*rows, n_rows}, rotary, dtype, (hipStream_t)stream),
                     "cache_append");
 }
 
-uint64_t ac_cache_attention_workspace_bytes(int heads, const ac_kv_cache* cache, const ac_cache_rows* rows, int causal, int dtype) {
-  if (cache_ok("ac_cache_attention_workspace_bytes", cache, rows) || heads < 1 || heads % cache->heads != 0 || !dtype_ok(dtype)) return 0;
-  return cache_attention_workspace_bytes(heads, *cache, *rows, causal != 0, dtype);
+uint64_t ac_cache_attention_workspace_bytes(int64_t n_rows, int heads, const ac_kv_cache* cache, const ac_cache_rows* rows, int causal,
+                                            int dtype) {
+  if (cache_ok("ac_cache_attention_workspace_bytes", cache, rows, n_rows) || heads < 1 || heads % cache->heads != 0 || !dtype_ok(dtype)) return 0;
+  return cache_attention_workspace_bytes(heads, *cache, CacheRows{*rows, n_rows}, causal != 0, dtype);
 }
 
-int ac_op_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int heads, const ac_kv_cache* cache,
+int ac_op_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int64_t n_rows, int heads, const ac_kv_cache* cache,
                           const ac_cache_rows* rows, int causal, float scale, void* workspace, uint64_t workspace_bytes, int dtype,
                           void* stream) {
   const char* const what = "ac_op_cache_attention";
-  if (const int st = cache_ok(what, cache, rows)) return st;
-  if (rows->rows == 0 || rows->batch == 0) return AC_OK;
+  if (const int st = cache_ok(what, cache, rows, n_rows)) return st;
+  if (n_rows == 0 || rows->batch == 0) return AC_OK;
   if (!q || !out || heads < 1 || heads > 65536 || heads % cache->heads != 0 || ldq < (int64_t)heads * cache->head_dim ||
       ldo < (int64_t)heads * cache->head_dim || !(scale > 0.f) || !(scale < INFINITY) || !dtype_ok(dtype))
     return fail(AC_ERR_ARG, "%s: bad argument", what);
-  if (rows->rows * heads > 1 << 30) return fail(AC_ERR_UNSUPPORTED, "%s: at most 2^30 rows times heads", what);
+  if (n_rows * heads > 1 << 30) return fail(AC_ERR_UNSUPPORTED, "%s: at most 2^30 rows times heads", what);
   if (!rows_on(q, ldq, 16, dtype) || !rows_on(out, ldo, 16, dtype))
     return fail(AC_ERR_ALIGN, "%s: rows start at multiples of 16 bytes", what);
-  const uint64_t need = cache_attention_workspace_bytes(heads, *cache, *rows, causal != 0, dtype);
+  const CacheRows all{*rows, n_rows};
+  const uint64_t need = cache_attention_workspace_bytes(heads, *cache, all, causal != 0, dtype);
   if (need > 0 && (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0))
     return fail(AC_ERR_WORKSPACE, "%s: workspace of %llu bytes, %llu needed", what, (unsigned long long)workspace_bytes, (unsigned long long)need);
-  return hip_status(launch_cache_attention(q, ldq, out, ldo, heads, *cache, *rows, causal != 0, scale, workspace, dtype, (hipStream_t)stream),
+  return hip_status(launch_cache_attention(q, ldq, out, ldo, heads, *cache, all, causal != 0, scale, workspace, dtype, (hipStream_t)stream),
                     "cache_attention");
 }
 

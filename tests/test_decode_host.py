@@ -9,7 +9,7 @@ def cache(**kw):
     return B.ac_kv_cache(**{**d, **kw})
 
 def rows(**kw):
-    d = dict(row_begin=1 << 44, length=1 << 45, page_table=1 << 46, ld_page_table=4, batch=3, rows=3, max_rows=1, max_length=100)
+    d = dict(row_begin=1 << 44, length=1 << 45, page_table=1 << 46, ld_page_table=4, batch=3, max_rows=1, max_length=100)
     return B.ac_cache_rows(**{**d, **kw})
 
 def rot(sections=(32,), **kw):
@@ -23,12 +23,12 @@ def byref(x):
     import ctypes
     return None if x is None else ctypes.byref(x)
 
-def attention(c=None, r=None, q=X, ldq=256, out=Y, ldo=256, heads=4, causal=1, scale=0.1, ws=W, ws_bytes=1 << 40, dtype=B.AC_BF16, no=()):
-    return L.ac_op_cache_attention(q, ldq, out, ldo, heads, None if "cache" in no else byref(c or cache()), None if "rows" in no else byref(r or rows()),
+def attention(c=None, r=None, q=X, ldq=256, out=Y, ldo=256, n=3, heads=4, causal=1, scale=0.1, ws=W, ws_bytes=1 << 40, dtype=B.AC_BF16, no=()):
+    return L.ac_op_cache_attention(q, ldq, out, ldo, n, heads, None if "cache" in no else byref(c or cache()), None if "rows" in no else byref(r or rows()),
                                    causal, scale, ws, ws_bytes, dtype, None)
 
-def append(c=None, r=None, ro=None, q=X, ldq=512, q_out=Y, ldqo=256, heads=4, k=W, ldk=512, v=W + 4096, ldv=512, dtype=B.AC_BF16):
-    return L.ac_op_cache_append(q, ldq, q_out, ldqo, heads, k, ldk, v, ldv, byref(c or cache()), byref(r or rows()), byref(ro), dtype, None)
+def append(c=None, r=None, ro=None, n=3, q=X, ldq=512, q_out=Y, ldqo=256, heads=4, k=W, ldk=512, v=W + 4096, ldv=512, dtype=B.AC_BF16):
+    return L.ac_op_cache_append(q, ldq, q_out, ldqo, heads, k, ldk, v, ldv, n, byref(c or cache()), byref(r or rows()), byref(ro), dtype, None)
 
 def linear(x=X, ldx=256, w=Y, ldw=128, scale=W, lds=2, zero=None, ldz=0, group=128, bias=None, residual=None, ldr=0, out=W + 4096, ldo=64, m=4, n=64,
            k=256, act=0, dtype=B.AC_BF16):
@@ -66,15 +66,17 @@ def test_cache_refusals(lib):
 for what in (attention, append):
     assert what() == 0, L.ac_last_error()
     assert kernels()
-    assert what(r=rows(batch=0)) == 0 and what(r=rows(rows=0)) == 0 and kernels() == []
+    assert what(r=rows(batch=0)) == 0 and what(n=0) == 0 and kernels() == []
     for c in (dict(k=None), dict(v=None), dict(k_scale=None), dict(v_scale=None), dict(pages=-1), dict(page=0), dict(page=24), dict(heads=0), dict(head_dim=0),
               dict(stride_page=2 * 32 * 64 - 16), dict(stride_scale=3)):
         refused(B.AC_ERR_ARG, what=what, c=cache(**c))
-    for r in (dict(row_begin=None), dict(length=None), dict(page_table=None), dict(ld_page_table=-1), dict(batch=-1), dict(rows=-1), dict(max_rows=-1),
+    for r in (dict(row_begin=None), dict(length=None), dict(page_table=None), dict(ld_page_table=-1), dict(batch=-1), dict(max_rows=-1),
               dict(max_length=-1)):
         refused(B.AC_ERR_ARG, what=what, r=rows(**r))
-    for r in (dict(batch=65536), dict(rows=(1 << 30) + 1), dict(max_length=(1 << 30) + 1), dict(ld_page_table=(1 << 25) + 1)):
+    for r in (dict(batch=65536), dict(max_length=(1 << 30) + 1), dict(ld_page_table=(1 << 25) + 1)):
         refused(B.AC_ERR_UNSUPPORTED, what=what, r=rows(**r))
+    refused(B.AC_ERR_ARG, what=what, n=-1)
+    refused(B.AC_ERR_UNSUPPORTED, what=what, n=(1 << 30) + 1)
     refused(B.AC_ERR_UNSUPPORTED, what=what, c=cache(head_dim=80, stride_page=1 << 20))
     for c in (dict(k=(1 << 40) + 8), dict(v=(1 << 40) + 8), dict(stride_page=2 * 32 * 64 + 8)):
         refused(B.AC_ERR_ALIGN, what=what, c=cache(**c))
@@ -108,14 +110,14 @@ for kw in (dict(q=None), dict(out=None), dict(heads=0), dict(heads=3), dict(ldq=
     refused(B.AC_ERR_ARG, what=attention, **kw)
 for kw in (dict(q=X + 8), dict(out=Y + 8), dict(ldq=260), dict(ldo=260)):
     refused(B.AC_ERR_ALIGN, what=attention, **kw)
-r = rows(batch=1, rows=1, max_length=65536, ld_page_table=2048)
-need = L.ac_cache_attention_workspace_bytes(4, byref(cache()), byref(r), 1, B.AC_BF16)
+r = rows(batch=1, max_length=65536, ld_page_table=2048)
+need = L.ac_cache_attention_workspace_bytes(3, 4, byref(cache()), byref(r), 1, B.AC_BF16)
 if need:
     for kw in (dict(ws=None), dict(ws_bytes=need - 1), dict(ws=W + 8)):
         refused(B.AC_ERR_WORKSPACE, what=attention, r=r, **kw)
     assert attention(r=r, ws_bytes=need) == 0
-assert L.ac_cache_attention_workspace_bytes(3, byref(cache()), byref(r), 1, B.AC_BF16) == 0
-assert L.ac_cache_attention_workspace_bytes(4, None, byref(r), 1, B.AC_BF16) == 0
+assert L.ac_cache_attention_workspace_bytes(3, 3, byref(cache()), byref(r), 1, B.AC_BF16) == 0
+assert L.ac_cache_attention_workspace_bytes(3, 4, None, byref(r), 1, B.AC_BF16) == 0
 """)
 
 
@@ -152,6 +154,8 @@ def test_binding_refuses_tensors_that_do_not_fit():
         B.rotary(torch.zeros(4, 8), torch.zeros(4, 4))
     with pytest.raises(ValueError):
         B.rotary(torch.zeros(4, 8), torch.zeros(4, 8), torch.zeros((2, 5), dtype=torch.int32))
+    with pytest.raises(ValueError):
+        B.ac_op_cache_attention(x[:, ::2], x[:, ::2], B.kv_cache(u8(3, 2, 32, 32), u8(3, 2, 2, 32, 16), s, s), rows)
     w, sc, y = u8(8, 16), torch.ones(8, 1), torch.zeros(2, 8)
     for kw in (dict(scale=sc[:4]), dict(out=y[:, :4]), dict(zero=sc[:4]), dict(bias=torch.zeros(3)), dict(w=u8(8, 8))):
         a = {**dict(x=torch.zeros(2, 32), w=w, scale=sc, out=y, group=32), **kw}

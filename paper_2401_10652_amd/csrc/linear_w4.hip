@@ -16,41 +16,44 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kTileRows = 96;  // rows from which the tiles of 128 x 128 take the product
 constexpr int kStep = 128;   // columns a wave takes at a time: 16 bytes of codes a lane
 
 // Slots 0..7 of a fragment hold columns 0 4 1 5 2 6 3 7, the order in which a word of eight codes comes apart.
 constexpr int kSlot[8] = {0, 4, 1, 5, 2, 6, 3, 7};
 
-// x[row][k .. k + 8) as NT bf16 terms, zeros past the row's end.
-template <bool VEC>
-__device__ __forceinline__ void load_x(const bf16_t* row, int64_t k, int64_t cols, bf16x8 (&f)[1]) {
-  bf16x8 v;
-  if (VEC && k + 8 <= cols) {
-    v = *reinterpret_cast<const bf16x8*>(row + k);
-  } else {
+// Eight numbers of a row of x as NT bf16 terms in the order of the slots.  An fp32 number is three terms that sum to it.
+template <typename T> struct Eight { T v[8]; };
+__device__ __forceinline__ void to_terms(const Eight<bf16_t>& x, bf16x8 (&f)[1]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = k + i < cols ? row[k + i] : (bf16_t)0.0f;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) f[0][i] = v[kSlot[i]];
+  for (int i = 0; i < 8; ++i) f[0][i] = x.v[kSlot[i]];
 }
-template <bool VEC>
-__device__ __forceinline__ void load_x(const float* row, int64_t k, int64_t cols, bf16x8 (&f)[3]) {
-  float v[8];
-  if (VEC && k + 8 <= cols) {
-    const f32x4 a = *reinterpret_cast<const f32x4*>(row + k), b = *reinterpret_cast<const f32x4*>(row + k + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = k + i < cols ? row[k + i] : 0.0f;
-  }
+__device__ __forceinline__ void to_terms(const Eight<float>& x, bf16x8 (&f)[3]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const Bf16Terms b = split_bf16(v[kSlot[i]]);
+    const Bf16Terms b = split_bf16(x.v[kSlot[i]]);
     f[0][i] = b.hi; f[1][i] = b.mid; f[2][i] = b.lo;
   }
+}
+// row[k .. k + 8): whole, or (MASKED) zeros from `cols` on.
+template <bool MASKED, typename T>
+__device__ __forceinline__ Eight<T> load_eight(const T* row, int k, int cols) {
+  constexpr int V = Elem<T>::kVec;
+  typedef T vec __attribute__((ext_vector_type(V)));
+  Eight<T> r;
+  if (MASKED) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.v[i] = row[min(k + i, cols - 1)];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.v[i] = k + i < cols ? r.v[i] : (T)0.0f;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8 / V; ++j) {
+      const vec t = *reinterpret_cast<const vec*>(row + k + j * V);
+#pragma unroll
+      for (int i = 0; i < V; ++i) r.v[j * V + i] = t[i];
+    }
+  }
+  return r;
 }
 
 // Word i of the lanes of quarter q of a wave becomes word q of quarter i.
@@ -71,14 +74,17 @@ __device__ __forceinline__ bf16x8 codes_plus_16(uint32_t w) {
   return __builtin_bit_cast(bf16x8, r);
 }
 
-// A block owns 16 * MB rows and 16 * CT columns; its waves take steps of 128 columns of k in turn and add their sums in LDS, in the
-// order of the waves.  SUBS: runs of 32 columns that share a scale within a step (1, 2 or 4).
+// A block owns 16 * MB rows and 16 * CT columns; its waves take steps of 128 columns of k in turn, the next ones' codes and scales on their way while one
+// is multiplied, and add their sums in LDS, in the order of the waves.  SUBS: runs of 32 columns that share a scale within a step (1, 2 or 4).
+constexpr int kMostWaves = 8;
+
 template <typename T, int NT, int MB, int CT, int SUBS, bool VEC>
-__global__ void __launch_bounds__(512) linear_w4(LinearW4Args g) {
+__global__ void __launch_bounds__(kMostWaves * 64) linear_w4(LinearW4Args g) {
   extern __shared__ float joined[];   // [waves][16 MB][16 CT]
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+  constexpr int ROWS = 16 * MB, COLS = 16 * CT, GS = 4 / SUBS, AHEAD = 2;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
   const int c16 = lane % 16, quarter = lane / 16;
-  const int64_t n0 = (int64_t)blockIdx.x * (16 * CT), m0 = (int64_t)blockIdx.y * (16 * MB);
+  const int64_t n0 = (int64_t)blockIdx.x * COLS, m0 = (int64_t)blockIdx.y * ROWS;
   const uint8_t* w[CT];
   const T *scale[CT], *zero[CT];
 #pragma unroll
@@ -86,13 +92,13 @@ __global__ void __launch_bounds__(512) linear_w4(LinearW4Args g) {
     const int64_t n = n0 + 16 * c + c16 < g.n ? n0 + 16 * c + c16 : g.n - 1;
     w[c] = (const uint8_t*)g.w + n * g.ldw;
     scale[c] = (const T*)g.scale + n * g.lds;
-    zero[c] = g.zero ? (const T*)g.zero + n * g.ldz : nullptr;
+    zero[c] = (const T*)g.zero + n * g.ldz;
   }
   const T* x[MB];
 #pragma unroll
   for (int r = 0; r < MB; ++r) {
-    const int64_t m = m0 + 16 * r + c16;
-    x[r] = m < g.m ? (const T*)g.x + m * g.ldx : nullptr;
+    const int64_t m = m0 + 16 * r + c16 < g.m ? m0 + 16 * r + c16 : g.m - 1;     // (rows past the last are the last again, and are not stored)
+    x[r] = (const T*)g.x + m * g.ldx + quarter * 8;
   }
   f32x4 total[MB][CT];
 #pragma unroll
@@ -104,59 +110,93 @@ __global__ void __launch_bounds__(512) linear_w4(LinearW4Args g) {
   for (int i = 0; i < 8; ++i) ones[i] = (bf16_t)1.0f;
 
   const int groups = quotient((int)g.k - 1, g.group) + 1;
-  for (int64_t k0 = (int64_t)wave * kStep; k0 < g.k; k0 += (int64_t)waves * kStep) {
-    u32x4 codes[CT];
-    const int64_t at = k0 / 2 + quarter * 16;
+  const uint32_t last_piece = ((int)g.k - 1) / 2 & ~15;
+  struct Step { u32x4 codes[CT]; T scale[CT][GS], zero[CT][GS]; };
+  auto load_x = [&](int r, int k0, Eight<T> (&to)[4]) __attribute__((always_inline)) {
+    if (VEC && k0 + kStep <= (int)g.k) {
 #pragma unroll
-    for (int c = 0; c < CT; ++c) codes[c] = 2 * at < g.k ? *reinterpret_cast<const u32x4*>(w[c] + at) : u32x4{0, 0, 0, 0};
-    bf16x8 xf[MB][4][NT];
+      for (int j = 0; j < 4; ++j) to[j] = load_eight<false>(x[r], k0 + j * 32, 0);
+    } else {
 #pragma unroll
-    for (int r = 0; r < MB; ++r)
+      for (int j = 0; j < 4; ++j) to[j] = load_eight<true>(x[r], k0 + j * 32, (int)g.k - quarter * 8);
+    }
+  };
+  // (past the end of k, where x is zero, codes and scales that are there)
+  auto fetch = [&](int k0) __attribute__((always_inline)) {
+    Step s;
+    const uint32_t at = min((uint32_t)k0 / 2 + quarter * 16, last_piece);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (x[r]) {
-          load_x<VEC>(x[r], k0 + j * 32 + quarter * 8, g.k, xf[r][j]);
-        } else {
+    for (int c = 0; c < CT; ++c) {
+      s.codes[c] = *reinterpret_cast<const u32x4*>(w[c] + at);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) xf[r][j][t] = bf16x8{};
-        }
+      for (int e = 0; e < GS; ++e) {
+        const int gi = min(quotient(k0 + e * SUBS * 32, g.group), groups - 1);
+        s.scale[c][e] = scale[c][gi];
+        s.zero[c][e] = g.zero ? zero[c][gi] : (T)8.0f;
       }
+    }
+    return s;
+  };
+  const int steps = ((int)g.k + kStep - 1) / kStep;
+  Step ring[AHEAD];
 #pragma unroll
-    for (int c = 0; c < CT; ++c) transpose_quarters(codes[c]);
+  for (int d = 0; d < AHEAD; ++d)
+    if (wave + d * waves < steps) ring[d] = fetch((wave + d * waves) * kStep);
+  for (int i0 = wave; i0 < steps; i0 += waves * AHEAD) {
 #pragma unroll
-    for (int j0 = 0; j0 < 4; j0 += SUBS) {
-      const int gi = min(quotient((int)k0 + j0 * 32, g.group), groups - 1);
-      f32x4 sum[MB], part[MB][CT];
+    for (int d = 0; d < AHEAD; ++d) {
+      const int i = i0 + d * waves, k0 = i * kStep;
+      if (i >= steps) break;
+      Step& now = ring[d];
+      bf16x8 xf[MB][4][NT];
 #pragma unroll
       for (int r = 0; r < MB; ++r) {
-        sum[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+        Eight<T> raw[4];
+        load_x(r, k0, raw);
 #pragma unroll
-        for (int j = j0; j < j0 + SUBS; ++j)
-#pragma unroll
-          for (int t = NT - 1; t >= 0; --t) sum[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[r][j][t], ones, sum[r], 0, 0, 0);
+        for (int j = 0; j < 4; ++j) to_terms(raw[j], xf[r][j]);
       }
 #pragma unroll
-      for (int c = 0; c < CT; ++c) {
+      for (int c = 0; c < CT; ++c) transpose_quarters(now.codes[c]);
 #pragma unroll
-        for (int r = 0; r < MB; ++r) part[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int e = 0; e < GS; ++e) {
+        f32x4 sum[MB], part[MB][CT];
 #pragma unroll
-        for (int j = j0; j < j0 + SUBS; ++j) {
-          const bf16x8 wf = codes_plus_16(codes[c][j]);
+        for (int r = 0; r < MB; ++r) {
+          sum[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int j = e * SUBS; j < (e + 1) * SUBS; ++j)
+#pragma unroll
+            for (int t = NT - 1; t >= 0; --t) sum[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[r][j][t], ones, sum[r], 0, 0, 0);
+        }
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+#pragma unroll
+          for (int r = 0; r < MB; ++r) part[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int j = e * SUBS; j < (e + 1) * SUBS; ++j) {
+            const bf16x8 wf = codes_plus_16(now.codes[c][j]);
+#pragma unroll
+            for (int r = 0; r < MB; ++r)
+#pragma unroll
+              for (int t = NT - 1; t >= 0; --t) part[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[r][j][t], wf, part[r][c], 0, 0, 0);
+          }
+          const float s = Elem<T>::ld(&now.scale[c][e]), off = -16.0f - Elem<T>::ld(&now.zero[c][e]);
 #pragma unroll
           for (int r = 0; r < MB; ++r)
 #pragma unroll
-            for (int t = NT - 1; t >= 0; --t) part[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[r][j][t], wf, part[r][c], 0, 0, 0);
+            for (int i = 0; i < 4; ++i) total[r][c][i] = fmaf(s, fmaf(off, sum[r][i], part[r][c][i]), total[r][c][i]);
         }
-        const float s = Elem<T>::ld(scale[c] + gi), off = -16.0f - (zero[c] ? Elem<T>::ld(zero[c] + gi) : 8.0f);
-#pragma unroll
-        for (int r = 0; r < MB; ++r)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) total[r][c][i] = fmaf(s, fmaf(off, sum[r][i], part[r][c][i]), total[r][c][i]);
       }
+      if (i + AHEAD * waves < steps) now = fetch((i + AHEAD * waves) * kStep);
     }
   }
 
-  constexpr int ROWS = 16 * MB, COLS = 16 * CT;
+  // what the first element that this thread finishes is joined with, on its way before the waves meet
+  const int e0 = threadIdx.x;
+  const bool mine = e0 < ROWS * COLS && m0 + e0 / COLS < g.m && n0 + e0 % COLS < g.n;
+  const float bias0 = mine && g.bias ? Elem<T>::ld((const T*)g.bias + n0 + e0 % COLS) : 0.f;
+  const float resid0 = mine && g.resid ? Elem<T>::ld((const T*)g.resid + (m0 + e0 / COLS) * g.ldr + n0 + e0 % COLS) : 0.f;
 #pragma unroll
   for (int r = 0; r < MB; ++r)
 #pragma unroll
@@ -164,30 +204,37 @@ __global__ void __launch_bounds__(512) linear_w4(LinearW4Args g) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) joined[(wave * ROWS + 16 * r + 4 * quarter + i) * COLS + 16 * c + c16] = total[r][c][i];
   __syncthreads();
-  for (int e = threadIdx.x; e < ROWS * COLS; e += blockDim.x) {
+  for (int e = e0; e < ROWS * COLS; e += blockDim.x) {
     const int64_t m = m0 + e / COLS, n = n0 + e % COLS;
     if (m >= g.m || n >= g.n) continue;
     float v = 0.f;
     for (int u = 0; u < waves; ++u) v += joined[u * ROWS * COLS + e];
-    if (g.bias) v += Elem<T>::ld((const T*)g.bias + n);
+    v += e == e0 ? bias0 : g.bias ? Elem<T>::ld((const T*)g.bias + n) : 0.f;
     v = apply_act_rt(v, g.act);
-    if (g.resid) v += Elem<T>::ld((const T*)g.resid + m * g.ldr + n);
+    v += e == e0 ? resid0 : g.resid ? Elem<T>::ld((const T*)g.resid + m * g.ldr + n) : 0.f;
     Elem<T>::st((T*)g.out + m * g.ldo + n, v);
   }
 }
 
 template <typename T, int NT, int MB, int CT, bool VEC>
 hipError_t launch_subs(const LinearW4Args& g, hipStream_t s) {
-  const int waves = 4;
+  const int64_t steps = (g.k + kStep - 1) / kStep;
+  int waves = 4;
+  while (waves < kMostWaves && waves < steps) waves *= 2;
   const dim3 grid((unsigned)((g.n + 16 * CT - 1) / (16 * CT)), (unsigned)((g.m + 16 * MB - 1) / (16 * MB)));
+  static_assert((size_t)kMostWaves * 16 * MB * 16 * CT * sizeof(float) <= 64 * 1024, "the waves' sums fit what a kernel has unasked");
   const size_t lds = (size_t)waves * 16 * MB * 16 * CT * sizeof(float);
-  if (g.group.d == 32)
-    hipLaunchKernelGGL((linear_w4<T, NT, MB, CT, 1, VEC>), grid, dim3(waves * kWave), lds, s, g);
-  else if (g.group.d == 64)
-    hipLaunchKernelGGL((linear_w4<T, NT, MB, CT, 2, VEC>), grid, dim3(waves * kWave), lds, s, g);
-  else
-    hipLaunchKernelGGL((linear_w4<T, NT, MB, CT, 4, VEC>), grid, dim3(waves * kWave), lds, s, g);
-  return hipGetLastError();
+  auto run = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(waves * kWave), lds, s, g);
+    return hipGetLastError();
+  };
+  if constexpr (CT * NT < 12) {
+    if (g.group.d == 64) return run(linear_w4<T, NT, MB, CT, 2, VEC>);
+    if constexpr (CT < 4) {
+      if (g.group.d == 32) return run(linear_w4<T, NT, MB, CT, 1, VEC>);
+    }
+  }
+  return run(linear_w4<T, NT, MB, CT, 4, VEC>);
 }
 
 template <typename T, int NT, int MB, int CT>
@@ -197,16 +244,23 @@ hipError_t launch_vec(const LinearW4Args& g, hipStream_t s) {
   return vec ? launch_subs<T, NT, MB, CT, true>(g, s) : launch_subs<T, NT, MB, CT, false>(g, s);
 }
 
+// Column tiles of a wave share what it does for x: as many as leave a block for each of the 256 CUs (small groups at most two, for registers).  us, one, two
+// and four tiles: 64 rows 2048 x 2048 8.0, 9.9, 14.1 (256, 128, 64 blocks); 64 rows 8192 x 2048 19.4, 19.4, 15.2; 256 rows 2048 x 2048 27.5, 19.0, 15.4.
+template <typename T, int NT, int MB>
+hipError_t launch_columns(const LinearW4Args& g, hipStream_t s) {
+  const int64_t rows = (g.m + 16 * MB - 1) / (16 * MB), columns = (g.n + 15) / 16;
+  if (rows * ((columns + 3) / 4) >= 256 && g.group.d >= (NT == 3 ? 128 : 64)) return launch_vec<T, NT, MB, 4>(g, s);
+  return rows * ((columns + 1) / 2) >= 256 ? launch_vec<T, NT, MB, 2>(g, s) : launch_vec<T, NT, MB, 1>(g, s);
+}
+
 template <typename T, int NT>
 hipError_t launch_rows(const LinearW4Args& g, hipStream_t s) {
-  if (g.m <= 16) return launch_vec<T, NT, 1, 1>(g, s);
-  if (g.m <= 32 || NT == 3) return launch_vec<T, NT, 2, 1>(g, s);
-  return launch_vec<T, NT, NT == 3 ? 2 : 4, 1>(g, s);
+  return g.m <= 16 ? launch_columns<T, NT, 1>(g, s) : launch_columns<T, NT, 2>(g, s);
 }
 
 // ---- many rows ---------------------------------------------------------------------------------------------------------
 //
-// From kTileRows rows on the matrix cores bound the product, if loads are far enough ahead: a step of 64 columns of k is half a microsecond, and what no
+// Of many rows the matrix cores bound the product, if loads are far enough ahead: a step of 64 columns of k is half a microsecond, and what no
 // block has read yet takes two and more to come.  A block owns 128 rows and 128 columns; of its eight waves four own 32 columns each (whose codes are
 // then converted once for all rows), and its two sets of four take a half of k each, so that two waves share a SIMD also where there are few
 // blocks, and add up in LDS.  x comes to LDS by direct loads three steps ahead, the codes to the registers of the wave that multiplies with them
@@ -450,8 +504,10 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
 }
 
 // Rows of x that direct loads can take: 16-byte pieces that hold columns of k alone; and offsets within a tile of 32 bits.
+// Products of less than 48 tiles are left to the kernel above, which has blocks for the whole chip then (us, tiles and rows: 256 rows 2048 x 2048, 32 tiles, 26
+// and 15; 512 rows 2048 x 2048, 64 tiles, 27 and 28; 128 rows 8192 x 2048 27 and 36; 512 rows 6144 x 2048 30 and 105).
 bool tiles_take(const LinearW4Args& g) {
-  return g.dtype == AC_BF16 && g.m >= kTileRows && (uintptr_t)g.x % 16 == 0 && g.ldx % 8 == 0 && g.k % 8 == 0 && g.k < 1 << 22 && g.ldx < 1 << 22 && g.ldw < 1 << 24 &&
+  return g.dtype == AC_BF16 && g.m >= 96 && g.m * g.n >= 48 * kTileM * kTileN && (uintptr_t)g.x % 16 == 0 && g.ldx % 8 == 0 && g.k % 8 == 0 && g.k < 1 << 22 && g.ldx < 1 << 22 && g.ldw < 1 << 24 &&
          g.lds < 1 << 22 && g.ldz < 1 << 22;
 }
 

@@ -66,8 +66,8 @@ def test_linear_w4(B, dtype, m, n, k, group):
     assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)
 
 
-@pytest.mark.parametrize("m,n,k,group", [(96, 128, 64, 32), (128, 1, 8, 64), (129, 300, 200, 128), (200, 70, 520, 64), (257, 129, 1000, 32), (300, 384, 1024, 256),
-                                          (150, 40, 100, 32), (128, 200, 333, 64)])
+@pytest.mark.parametrize("m,n,k,group", [(96, 8192, 64, 32), (6200, 129, 8, 64), (1029, 800, 200, 128), (2600, 310, 520, 64), (257, 3100, 1000, 32), (512, 1600, 1032, 256),
+                                          (1500, 600, 100, 32), (128, 6500, 333, 64), (300, 384, 1024, 256), (40, 2050, 96, 32), (70, 8200, 200, 64), (130, 5000, 160, 128)])
 def test_linear_w4_of_many_rows(B, m, n, k, group):
     for zero in (False, True):
         got, ref, bound = linear_case(B, "bf16", m, n, k, group, zero, seed=m + n)
@@ -78,28 +78,28 @@ def test_linear_w4_of_many_rows(B, m, n, k, group):
 @pytest.mark.parametrize("zero", [False, True])
 @pytest.mark.parametrize("act,bias,residual", [("none", False, False), ("gelu_erf", True, False), ("gelu_tanh", False, True), ("relu", True, True)])
 def test_linear_w4_epilogues(B, dtype, zero, act, bias, residual):
-    for m in (1, 20, 100, 140):
-        got, ref, bound = linear_case(B, dtype, m, 72, 320, 64, zero, bias, residual, act, seed=m)
+    for m, n in ((1, 72), (20, 72), (130, 6148)):
+        got, ref, bound = linear_case(B, dtype, m, n, 320, 64, zero, bias, residual, act, seed=m)
         assert (np.abs(got - ref) <= bound).all(), (m, np.max(np.abs(got - ref) / bound))
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("pad,wide", [(1, 0), (8, 16), (5, 48)])
 def test_linear_w4_strides(B, dtype, pad, wide):
-    for m in (1, 7, 40):
-        got, ref, bound = linear_case(B, dtype, m, 50, 200, 32, seed=m, pad=pad, wide=wide)
+    for m, n in ((1, 50), (7, 50), (40, 50), (200, 4001)):
+        got, ref, bound = linear_case(B, dtype, m, n, 200, 32, seed=m, pad=pad, wide=wide)
         assert (np.abs(got - ref) <= bound).all(), (m, np.max(np.abs(got - ref) / bound))
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_linear_w4_rows_keep_to_themselves(B, dtype):
     """NaN and infinities of one row reach no other; large and tiny rows keep their precision."""
-    for m in (20, 130):
+    for m, n in ((20, 40), (130, 6500)):
         k = 160
         x = D.normal((m, k), 3)
         x[3, 7], x[17, 159], x[5] = np.nan, np.inf, x[5] * 1e30
         x[6] *= 1e-30
-        got, ref, bound = linear_case(B, dtype, m, 40, k, 32, bias=False, residual=False, x=x)
+        got, ref, bound = linear_case(B, dtype, m, n, k, 32, bias=False, residual=False, x=x)
         assert not np.isfinite(got[[3, 17]]).any()
         rest = [i for i in range(m) if i not in (3, 17)]
         assert (np.abs(got - ref)[rest] <= bound[rest]).all()

@@ -262,18 +262,18 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
   for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
 }
 
-// One block: 16 RT query rows over one run of keys, in steps of 64 that its four waves take in turn.  S^T = K Q^T and O^T = V^T P^T, both by
+// One block: 16 query rows over one run of keys, in steps of 64 that its four waves take in turn.  S^T = K Q^T and O^T = V^T P^T, both by
 // v_mfma_f32_16x16x32_bf16 with a query row to a column, so a lane holds probabilities of one row and the running maximum and sum are
 // per-lane scalars.  Row a of key tile j is token 16 (a / 4) + 4 j + a mod 4 of the step: quarter g of the wave then holds the scores of
 // block g, with that block's two scales in one register each, and the probabilities of its 16 tokens in the order in which the cache
 // holds their values.  No code passes through LDS.  What bounds it is HBM: a step's values are on their way while its scores are computed, the next step's
 // keys while its values are multiplied, and page numbers are read two steps ahead.
-template <typename T, int HD, int RT>
+template <typename T, int HD>
 __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
   constexpr int NT = Terms<T>::kN, W16 = HD / 64, REST = HD % 64 / 32, DT = HD / 16;
   constexpr int FR = HD / 32;                          // fragments of 32 of a row
-  constexpr int ROWS = 16 * RT;
-  extern __shared__ float joined[];                    // [4][16][HD] and [4][16][2]
+  constexpr int LD = HD + 4;                           // floats a row of sums in LDS: rows begin four banks apart
+  extern __shared__ float joined[];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c16 = lane % 16, quarter = lane / 16;
   const int kv = g.cache.heads, kvh = blockIdx.y % kv, tiles = gridDim.y / kv, group = g.group.d, blocks = g.blocks.d;
   const Sight sq(g, blockIdx.z);
@@ -281,13 +281,12 @@ __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
   const uint8_t* kbase = (const uint8_t*)g.cache.k + (int64_t)kvh * g.cache.page * HD + (c16 % 4) * HD + quarter * 16;
   const uint8_t* vbase = (const uint8_t*)g.cache.v + (int64_t)kvh * g.cache.page * HD + c16 * kBlock;
 
-  for (int tile = blockIdx.y / kv; tile * ROWS < sq.all; tile += tiles) {
-    int sees[RT];                                       // a row sees the keys before this one
+  for (int tile = blockIdx.y / kv; tile * 16 < sq.all; tile += tiles) {
     int seen = sq.held, fewest = sq.held;               // the most and the fewest of the tile's rows
     if (g.causal) {
-      const int last = sq.first + quotient(tile * ROWS + ROWS - 1 < sq.all ? tile * ROWS + ROWS - 1 : sq.all - 1, g.group) + 1;
+      const int last = sq.first + quotient(tile * 16 + 15 < sq.all ? tile * 16 + 15 : sq.all - 1, g.group) + 1;
       if (last < sq.held) seen = last;
-      fewest = sq.first + quotient(tile * ROWS, g.group) + 1;
+      fewest = sq.first + quotient(tile * 16, g.group) + 1;
     }
     if (seen < 0) seen = 0;
     const int len = run_length(seen, g.splits, g.least), k_lo = (int)blockIdx.x * len < seen ? blockIdx.x * len : seen;
@@ -316,29 +315,21 @@ __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
 
     int k0 = k_lo + wave * 64;
     int kp = number(k0, c16 / 4), vp = number(k0, quarter), kp2 = number(k0 + 256, c16 / 4), vp2 = number(k0 + 256, quarter);
-    bf16x8 qf[RT][FR][NT];
+    const int r = tile * 16 + c16, rr = r < sq.all ? r : sq.all - 1, rq = quotient(rr, g.group);
+    const int sees = r >= sq.all ? 0 : g.causal ? sq.first + rq + 1 : sq.held;       // a row sees the keys before this one
+    bf16x8 qf[FR][NT];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const int r = tile * ROWS + t * 16 + c16, rr = r < sq.all ? r : sq.all - 1, rq = quotient(rr, g.group);
-      sees[t] = r >= sq.all ? 0 : g.causal ? sq.first + rq + 1 : sq.held;
-#pragma unroll
-      for (int f = 0; f < FR; ++f) {
-        const int d = f < 2 * W16 ? f / 2 * 64 + quarter * 16 + f % 2 * 8 : W16 * 64 + quarter * 8;
-        float v[8];
-        load8((const T*)g.q + (sq.begin + rq) * g.ldq + (int64_t)(kvh * group + rr - rq * group) * HD + d, v);
-        to_terms(v, qf[t][f]);
-      }
+    for (int f = 0; f < FR; ++f) {
+      const int d = f < 2 * W16 ? f / 2 * 64 + quarter * 16 + f % 2 * 8 : W16 * 64 + quarter * 8;
+      float v[8];
+      load8((const T*)g.q + (sq.begin + rq) * g.ldq + (int64_t)(kvh * group + rr - rq * group) * HD + d, v);
+      to_terms(v, qf[f]);
     }
     load_keys(offset(k0, c16 / 4, kp, g.cache.stride_page, kBlock * HD));
-    f32x4 o[RT][DT];
-    float m[RT], l[RT];
+    f32x4 o[DT];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      m[t] = -INFINITY;
-      l[t] = 0.f;
-#pragma unroll
-      for (int d = 0; d < DT; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
 
     for (; k0 < k_hi; k0 += 256) {
       const int64_t va = offset(k0, quarter, vp, g.cache.stride_page, kBlock * HD);
@@ -349,72 +340,60 @@ __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
       const float ks = sa >= 0 ? g.cache.k_scale[sa + kvh * blocks] * g.scale : 0.f, vs = sa >= 0 ? g.cache.v_scale[sa + kvh * blocks] : 0.f;
       const int kp3 = number(k0 + 512, c16 / 4), vp3 = number(k0 + 512, quarter);
 
-      f32x4 s[RT][4];
+      f32x4 s[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-#pragma unroll
-        for (int t = 0; t < RT; ++t) s[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int f = 0; f < FR; ++f) {
           const bf16x8 kf = f < 2 * W16 ? codes_bf16(kw[j][f / 2][f % 2 * 2], kw[j][f / 2][f % 2 * 2 + 1]) : codes_bf16(kr[j][0], kr[j][1]);
 #pragma unroll
-          for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int u = NT - 1; u >= 0; --u) s[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][f][u], s[t][j], 0, 0, 0);
+          for (int u = NT - 1; u >= 0; --u) s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[f][u], s[j], 0, 0, 0);
         }
       }
       load_keys(offset(k0 + 256, c16 / 4, kp2, g.cache.stride_page, kBlock * HD));
       kp = kp2; vp = vp2; kp2 = kp3; vp2 = vp3;
 
       const int vb = (k0 / kBlock + quarter) * kBlock;
-      bf16x8 pf[RT][2][NT];
+      const int left = (va >= 0 ? sees : 0) - vb;        // of this lane's block, the tokens its row sees
+      float big = -INFINITY;
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        const int left = (va >= 0 ? sees[t] : 0) - vb;        // of this lane's block, the tokens its row sees
-        float big = -INFINITY;
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            s[t][j][i] = 4 * j + i < left ? s[t][j][i] * ks : -INFINITY;
-            big = fmaxf(big, s[t][j][i]);
-          }
-        big = fmaxf(big, __shfl_xor(big, 16, 64));
-        big = fmaxf(big, __shfl_xor(big, 32, 64));
-        const float m_new = fmaxf(m[t], big), ref = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m[t] - ref);
-        m[t] = m_new;
-        float p[16], sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(s[t][e / 4][e % 4] - ref);
-          sum += p[e];
+        for (int i = 0; i < 4; ++i) {
+          s[j][i] = 4 * j + i < left ? s[j][i] * ks : -INFINITY;
+          big = fmaxf(big, s[j][i]);
         }
-        l[t] = fmaf(l[t], alpha, sum);
+      big = fmaxf(big, __shfl_xor(big, 16, 64));
+      big = fmaxf(big, __shfl_xor(big, 32, 64));
+      const float m_new = fmaxf(m, big), ref = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m - ref);
+      m = m_new;
+      float p[16], sum = 0.f;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          float pv[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) pv[e] = p[8 * u + e] * vs;
-          to_terms(pv, pf[t][u]);
-        }
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
+      for (int e = 0; e < 16; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(s[e / 4][e % 4] - ref);
+        sum += p[e];
       }
+      l = fmaf(l, alpha, sum);
+      bf16x8 pf[2][NT];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float pv[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pv[e] = p[8 * u + e] * vs;
+        to_terms(pv, pf[u]);
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= alpha;
       bool poisoned = false;                                         // whether a code that not every row sees is NaN
       if (k0 + 64 > fewest) {
         uint32_t any = 0;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          // tokens past the last that the tile's rows see may hold anything
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int n = seen - vb - 4 * i;
-            vw[d][i] = n >= 4 ? vw[d][i] : n <= 0 ? 0u : vw[d][i] & (0xffffffffu >> (8 * (4 - n)));
-            any |= nan_bytes(vw[d][i]);
-          }
-        }
-        poisoned = __any(any != 0);
+          for (int i = 0; i < 4; ++i) any |= (vw[d][i] & 0x7f7f7f7fu) + 0x01010101u;     // bit 7 of a byte: it is NaN
+        poisoned = __any((any & 0x80808080u) != 0);
       }
       if (!poisoned) {
 #pragma unroll
@@ -423,71 +402,84 @@ __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
           for (int u = 0; u < 2; ++u) {
             const bf16x8 vf = codes_bf16(vw[d][2 * u], vw[d][2 * u + 1]);
 #pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-              for (int x = NT - 1; x >= 0; --x) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t][u][x], o[t][d], 0, 0, 0);
+            for (int x = NT - 1; x >= 0; --x) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[u][x], o[d], 0, 0, 0);
           }
       } else {
-        // A NaN times a probability of 0 is NaN, so NaN values are counted apart, among the tokens that a row sees.
+        // A NaN times a probability of 0 is NaN, so NaN values are counted apart, among the tokens that a row sees.  (Tokens past the last may hold
+        // anything.)
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+        for (int d = 0; d < DT; ++d) {
+          f32x4 count = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            f32x4 count = {0.f, 0.f, 0.f, 0.f};
+          for (int u = 0; u < 2; ++u) {
+            const uint32_t n0 = nan_bytes(vw[d][2 * u]), n1 = nan_bytes(vw[d][2 * u + 1]);
+            const bf16x8 vf = codes_bf16(vw[d][2 * u] & ~n0, vw[d][2 * u + 1] & ~n1);
+            const bf16x8 nf = codes_bf16(n0 & 0x38383838u, n1 & 0x38383838u);      // 0x38 is 1
+            bf16x8 seen_f;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const uint32_t n0 = nan_bytes(vw[d][2 * u]), n1 = nan_bytes(vw[d][2 * u + 1]);
-              const bf16x8 vf = codes_bf16(vw[d][2 * u] & ~n0, vw[d][2 * u + 1] & ~n1);
-              const bf16x8 nf = codes_bf16(n0 & 0x38383838u, n1 & 0x38383838u);      // 0x38 is 1
-              bf16x8 seen_f;
+            for (int e = 0; e < 8; ++e) seen_f[e] = 8 * u + e < left ? (bf16_t)1.0f : (bf16_t)0.0f;
 #pragma unroll
-              for (int e = 0; e < 8; ++e) seen_f[e] = 8 * u + e < sees[t] - vb ? (bf16_t)1.0f : (bf16_t)0.0f;
-#pragma unroll
-              for (int x = NT - 1; x >= 0; --x) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t][u][x], o[t][d], 0, 0, 0);
-              count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf, seen_f, count, 0, 0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (count[i] > 0.f) o[t][d][i] = __builtin_nanf("");
+            for (int x = NT - 1; x >= 0; --x) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[u][x], o[d], 0, 0, 0);
+            count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf, seen_f, count, 0, 0, 0);
           }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (count[i] > 0.f) o[d][i] = __builtin_nanf("");
+        }
       }
     }
 
-    // join the four waves, 16 rows at a time
-    float* ml = joined + 4 * 16 * HD;
+    // join the four waves
+    float* const ml = joined + 4 * 16 * LD;                 // [4][16][2], then each wave's factor of a row [16][4]
+    float* const factor = ml + 4 * 16 * 2;
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      l[t] += __shfl_xor(l[t], 16, 64);
-      l[t] += __shfl_xor(l[t], 32, 64);
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(&joined[(wave * 16 + c16) * LD + d * 16 + quarter * 4]) = o[d];
+    if (quarter == 0) { ml[(wave * 16 + c16) * 2] = m; ml[(wave * 16 + c16) * 2 + 1] = l; }
+    __syncthreads();
+    const int rows_left = sq.all - tile * 16;
+    if (threadIdx.x < 16 && (int)threadIdx.x < rows_left) {
+      const int rt = threadIdx.x;
+      float top = ml[rt * 2];
 #pragma unroll
-      for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(&joined[(wave * 16 + c16) * HD + d * 16 + quarter * 4]) = o[t][d];
-      if (quarter == 0) { ml[(wave * 16 + c16) * 2] = m[t]; ml[(wave * 16 + c16) * 2 + 1] = l[t]; }
-      __syncthreads();
-      for (int e = threadIdx.x; e < 16 * HD; e += 256) {
-        const int rt = e / HD, d = e % HD, ro = tile * ROWS + t * 16 + rt;
-        if (ro >= sq.all) continue;
-        float top = ml[rt * 2];
+      for (int u = 1; u < 4; ++u) top = fmaxf(top, ml[(u * 16 + rt) * 2]);
+      const float ref = top == -INFINITY ? 0.f : top;
+      float total = 0.f, f[4];
 #pragma unroll
-        for (int u = 1; u < 4; ++u) top = fmaxf(top, ml[(u * 16 + rt) * 2]);
-        const float ref = top == -INFINITY ? 0.f : top;
-        float total = 0.f, v = 0.f;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const float f = __builtin_amdgcn_exp2f(ml[(u * 16 + rt) * 2] - ref);
-          total = fmaf(f, ml[(u * 16 + rt) * 2 + 1], total);
-          v = fmaf(f, joined[(u * 16 + rt) * HD + d], v);
-        }
-        const int oq = quotient(ro, g.group), ohead = kvh * group + ro - oq * group;
-        if (g.splits == 1) {
-          Elem<T>::st((T*)g.out + (sq.begin + oq) * g.ldo + (int64_t)ohead * HD + d, total == 0.f ? 0.f : v / total);
-        } else {
-          const int64_t at = (blockIdx.x * g.rows.rows + sq.begin + oq) * g.heads + ohead;
-          g.part_o[at * HD + d] = v;
-          if (d == 0) { g.part_ml[at * 2] = top; g.part_ml[at * 2 + 1] = total; }
-        }
+      for (int u = 0; u < 4; ++u) {
+        f[u] = __builtin_amdgcn_exp2f(ml[(u * 16 + rt) * 2] - ref);
+        total = fmaf(f[u], ml[(u * 16 + rt) * 2 + 1], total);
       }
-      __syncthreads();
+      const float inv = g.splits > 1 ? 1.f : total == 0.f ? 0.f : 1.0f / total;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) factor[rt * 4 + u] = f[u] * inv;
+      if (g.splits > 1) {
+        const int oq = quotient(tile * 16 + rt, g.group);
+        const int64_t at = (blockIdx.x * g.rows.rows + sq.begin + oq) * g.heads + kvh * group + tile * 16 + rt - oq * group;
+        g.part_ml[at * 2] = top;
+        g.part_ml[at * 2 + 1] = total;
+      }
     }
+    __syncthreads();
+    for (int e = threadIdx.x; e < 4 * HD; e += 256) {
+      const int rt = e / (HD / 4), d = e % (HD / 4) * 4, ro = tile * 16 + rt;
+      if (rt >= rows_left) break;
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(&joined[(u * 16 + rt) * LD + d]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = fmaf(factor[rt * 4 + u], x[i], v[i]);
+      }
+      const int oq = quotient(ro, g.group), ohead = kvh * group + ro - oq * group;
+      if (g.splits == 1) {
+        store4((T*)g.out + (sq.begin + oq) * g.ldo + (int64_t)ohead * HD + d, v);
+      } else {
+        store4(g.part_o + ((blockIdx.x * g.rows.rows + sq.begin + oq) * g.heads + ohead) * HD + d, v);
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -536,21 +528,29 @@ __global__ void __launch_bounds__(256) cache_attention_join(CacheAttnArgs g) {
   store4((T*)g.out + row * g.ldo + (item - row * g.heads) * HD + lane * 4, w);
 }
 
-// How a call is computed: rows in tiles of 16 or 32, or of 128 by the kernel for prompts; and runs of keys.
-struct Shape { int rows, tiles, splits; };
+// How a call is computed: rows in tiles of 16, or of 128 by the kernel for prompts; and runs of keys.
+struct Shape { bool prompt; int tiles, splits; };
 
-// Runs of keys: as many as fill the chip, and no longer than kLongRun, so that sequences of all lengths, of which the host knows only the longest,
-// keep it filled to the end.
-constexpr int kMostSplits = 128, kLeastRun = 256, kLongRun = 2048, kPlaces = 1024, kPromptPlaces = 256, kPromptRows = 64;
+// Tiles of 128 read the keys once where tiles of 16 read them eight times, but take longer for each step of keys: they are taken where the call is large, by heads x rows
+// x tokens (us, 16 and 128 rows a tile).  Heads of 128: eight times 256 rows of 32 heads over 8192 tokens (5 * 10^8) 124 and 64; eight times 300 rows of 32 heads over 900 (7 * 10^7)
+// 120 and 74; four times 64 rows of 16 heads over 4096 (1.7 * 10^7) 35 and 29; 512 rows of 32 heads over 512 (8 * 10^6) 19 and 24; 128 rows of 16 heads over 2048 (4 * 10^6) 17 and
+// 22.  Heads of 64: 64 rows of 16 heads over 65536 (7 * 10^7) 71 and 59; 700 rows of 16 heads over 700 (8 * 10^6) 12 and 19.  32 rows a key head and fewer leave three quarters of a
+// large tile empty: eight times 8 rows of 32 heads over 8192 tokens 39 and 47.
+constexpr int kPromptRows = 32, kPromptWork = 1 << 24;
+// Runs of keys: as many as fill the chip's places, two blocks of 256 threads a CU (64k tokens, 16 heads of 64: 57 us, with twice as many 60) or one of 512, and, of
+// several sequences, none longer than kLongRun, so that sequences of all lengths, of which the host knows only the longest, keep the chip filled to the end (64
+// sequences of up to 8190 tokens, 8 key heads of 128: 127 us, with runs of 1024 131, of 4096 133).
+constexpr int kMostSplits = 128, kLeastRun = 256, kLongRun = 2048, kPlaces = 512, kPromptPlaces = 256;
 Shape shape(int heads, const ac_kv_cache& c, const CacheRows& r, int dtype) {
-  const int64_t rows = (r.max_rows < r.rows ? r.max_rows : r.rows) * (heads / c.heads);
-  const bool prompt = dtype == AC_BF16 && c.pages > 0 && rows > kPromptRows;
+  const int64_t rows_of = r.max_rows < r.rows ? r.max_rows : r.rows, rows = rows_of * (heads / c.heads);
+  const int64_t all = rows_of < r.rows / (r.batch > 0 ? r.batch : 1) ? rows_of * r.batch : r.rows;
   Shape s;
-  s.rows = prompt ? 128 : rows > 16 && c.head_dim <= 128 ? 32 : 16;      // (two tiles of 16, where the registers allow, read the keys once for both)
-  s.tiles = rows < 1 ? 1 : (int)((rows + s.rows - 1) / s.rows);
+  s.prompt = dtype == AC_BF16 && c.pages > 0 && rows > kPromptRows && all * heads * (double)r.max_length >= kPromptWork;
+  const int each = s.prompt ? 128 : 16;
+  s.tiles = rows < 1 ? 1 : (int)((rows + each - 1) / each);
   const int64_t blocks = (int64_t)s.tiles * c.heads * r.batch;
-  int64_t n = blocks > 0 ? (prompt ? kPromptPlaces : kPlaces) / blocks : 1;
-  if (!prompt && r.batch > 1 && n < r.max_length / kLongRun) n = r.max_length / kLongRun;
+  int64_t n = blocks > 0 ? (s.prompt ? kPromptPlaces : kPlaces) / blocks : 1;
+  if (!s.prompt && r.batch > 1 && n < r.max_length / kLongRun) n = r.max_length / kLongRun;
   const int64_t most = (r.max_length + kLeastRun - 1) / kLeastRun;
   if (n > most) n = most;
   if (n > kMostSplits) n = kMostSplits;
@@ -558,25 +558,22 @@ Shape shape(int heads, const ac_kv_cache& c, const CacheRows& r, int dtype) {
   return s;
 }
 
-template <typename T, int HD, int RT>
+template <typename T, int HD>
 hipError_t attention_rows_launch(const CacheAttnArgs& a, int tiles, hipStream_t s) {
   const int most = 65535 / a.cache.heads;
   if (tiles > most) tiles = most;
   const dim3 grid((unsigned)a.splits, (unsigned)(tiles * a.cache.heads), (unsigned)a.rows.batch);
-  constexpr size_t lds = (size_t)(4 * 16 * HD + 4 * 16 * 2) * sizeof(float);
-  static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(cache_attention<T, HD, RT>),
+  constexpr size_t lds = (size_t)(4 * 16 * (HD + 4) + 4 * 16 * 2 + 16 * 4) * sizeof(float);
+  static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(cache_attention<T, HD>),
                                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (attr_status != hipSuccess) return attr_status;
-  hipLaunchKernelGGL((cache_attention<T, HD, RT>), grid, dim3(256), lds, s, a);
+  hipLaunchKernelGGL((cache_attention<T, HD>), grid, dim3(256), lds, s, a);
   return hipGetLastError();
 }
 
 template <typename T, int HD>
 hipError_t attention_launch(CacheAttnArgs a, const Shape& shape, hipStream_t s) {
-  hipError_t e;
-  if (shape.rows == 128) e = launch_cache_prefill(a, shape.tiles, s);
-  else if (shape.rows == 32) e = attention_rows_launch<T, HD, HD <= 128 ? 2 : 1>(a, shape.tiles, s);
-  else e = attention_rows_launch<T, HD, 1>(a, shape.tiles, s);
+  const hipError_t e = shape.prompt ? launch_cache_prefill(a, shape.tiles, s) : attention_rows_launch<T, HD>(a, shape.tiles, s);
   if (e != hipSuccess || a.splits == 1) return e;
   constexpr int TEAMS = 256 / (HD / 4);
   a.teams = a.splits / 4 < 1 ? 1 : a.splits / 4 > TEAMS ? TEAMS : a.splits / 4;

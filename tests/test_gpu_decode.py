@@ -279,7 +279,7 @@ def test_append_of_zeros_and_what_is_dropped(B):
 # ---- attention -------------------------------------------------------------------------------------------------------------------
 
 def attention_case(B, dtype, counts, lengths, heads, heads_kv, d, page, causal=True, scale=None, seed=0, gap=0, lie=False, pad=0, alter=None,
-                   std=1.0, pages_of_a_sequence=None, fill=0x7f):
+                   std=1.0, pages_of_a_sequence=None, fill=0x7f, longest=None):
     """What lies behind a sequence's last token, and in pages that no sequence has, is NaN, codes and scales."""
     import torch
     cache = D.Cache(lengths, heads_kv, d, page, seed, pages_of_a_sequence, fill=fill)
@@ -294,7 +294,7 @@ def attention_case(B, dtype, counts, lengths, heads, heads_kv, d, page, causal=T
         spread[:, :heads * d] = qt
         qt = spread[:, :heads * d]
     dev = Device(B, cache, gap)
-    rows = dev.rows(counts, lengths, *((1, 1) if lie else (None, None)))
+    rows = dev.rows(counts, lengths, *((1, 1) if lie else (None, longest)))
     out = torch.full((total, heads * d + pad), float("nan"), dtype=qt.dtype, device="cuda")[:, :heads * d]
     need = B.ac_cache_attention_workspace_bytes(qt, dev.desc, rows, causal)
     ws = torch.full((max(need, 16),), 0xff, dtype=torch.uint8, device="cuda")
@@ -338,6 +338,22 @@ def test_attention_prompts(B, d, counts, lengths, heads, heads_kv, page, causal)
     attention_case(B, "bf16", counts, lengths, heads, heads_kv, d, page, causal, seed=d)
 
 
+@pytest.mark.parametrize("d", [32, 64, 96, 128, 192, 256])
+@pytest.mark.parametrize("counts,lengths,heads,heads_kv,page,causal", [
+    ([65], [65], 1, 1, 16, True), ([150], [700], 2, 1, 48, True), ([128], [333], 1, 1, 32, False), ([257, 3, 0, 90], [257, 1400, 0, 95], 2, 2, 64, True),
+    ([31], [1029], 9, 3, 16, True), ([33, 5] + [0, 34] * 34, [40, 100] + [0, 34] * 34, 2, 2, 16, True)])
+def test_attention_prompts_of_long_caches(B, d, counts, lengths, heads, heads_kv, page, causal):
+    """Where the host knows of the lengths only that they are no more than 2^19, work is laid out for these."""
+    attention_case(B, "bf16", counts, lengths, heads, heads_kv, d, page, causal, seed=d, longest=1 << 19)
+
+
+@pytest.mark.parametrize("longest", [None, 1 << 19])
+@pytest.mark.parametrize("counts,lengths", [([400], [900]), ([90, 0, 300], [2000, 7, 301])])
+def test_attention_prompts_forms(B, counts, lengths, longest):
+    for i, more in enumerate((dict(gap=48), dict(pad=8), dict(scale=0.37), dict(std=30.0), dict(pages_of_a_sequence=160), dict(causal=False))):
+        attention_case(B, "bf16", counts, lengths, 4, 2, 64, 32, seed=i, longest=longest, **more)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_attention_forms(B, dtype):
     attention_case(B, dtype, [3, 20], [90, 50], 4, 2, 64, 32, seed=1, gap=48)                           # pages apart
@@ -378,6 +394,26 @@ def test_attention_nan_reaches_only_the_rows_that_see_it(B, dtype, d, counts, le
     got = attention_case(B, dtype, counts, [length], 4, 2, d, 16, seed=10, alter=alter)
     if counts[0] == 30:
         assert np.isnan(got[25:, :2]).all() and not np.isnan(got[:25, :2]).any() and np.isnan(got[10:, 2:, 5]).all() and not np.isnan(got[:10, 2:, 5]).any()
+
+
+def test_attention_prompts_with_nan_and_missing_pages(B):
+    def nan(cache):
+        for name, token, head, e in (("k", 95, 0, 3), ("v", 80, 1, 5), ("v", 199, 0, 2), ("v", 40, 1, 31), ("v", 199, 1, 63)):
+            where = cache.block(0, token // 16)
+            codes, s = cache.get(name, where, head)
+            codes = codes.copy()
+            codes[token % 16, e] = 0xff
+            cache.put(name, where, head, codes, s, 200 - token // 16 * 16)
+    got = attention_case(B, "bf16", [130], [200], 4, 2, 64, 16, seed=10, alter=nan, longest=1 << 19)
+    assert np.isnan(got[25:, :2]).all() and not np.isnan(got[:25, :2]).any() and np.isnan(got[10:, 2:, 5]).all() and np.isnan(got[:, 2:, 31]).all()
+
+    def missing(cache):
+        cache.table[0, 0], cache.table[0, 3] = -1, cache.pages
+        cache.table[1] = -7
+    got = attention_case(B, "bf16", [70, 4], [100, 9], 4, 2, 64, 16, seed=8, alter=missing, longest=1 << 19)
+    assert (got[70:] == 0).all()
+    got = attention_case(B, "bf16", [90, 1], [60, 0], 4, 2, 64, 16, seed=9, longest=1 << 19)
+    assert (got[:30] == 0).all() and (got[90] == 0).all() and (got[30:90] != 0).any()
 
 
 def test_far_pages(B):

@@ -12,18 +12,25 @@ namespace {
 
 // ---- append ----------------------------------------------------------------------------------------------------------
 
-// The least power of two s >= 2^-100 with v <= 448 s, for 0 <= v < inf: 448 = 1.75 * 2^8.
-__device__ __forceinline__ float scale_of(float v) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+__device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+
+// The least power of two s >= 2^-100 with v <= 448 s, for the bits of 0 <= v < inf: 448 = 1.75 * 2^8.
+__device__ __forceinline__ float scale_of(uint32_t u) {
   int e = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
   if (e < 27) e = 27;
   return __builtin_bit_cast(float, (uint32_t)e << 23);
 }
 
 // Four numbers as e4m3, to nearest, ties to even; what is not finite becomes NaN.
-__device__ __forceinline__ uint32_t to_e4m3(const float (&v)[4]) {
+__device__ __forceinline__ uint32_t to_e4m3(const float (&v)[4], bool finite) {
   uint32_t r = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
   r = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], r, true);
+  if (finite) return r;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (!(fabsf(v[i]) < INFINITY)) r |= 0x7fu << (8 * i);
@@ -38,7 +45,7 @@ __device__ __forceinline__ uint32_t move_codes(uint32_t c, float ratio) {
   from_e4m3(c, v);
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] *= ratio;
-  return to_e4m3(v);
+  return to_e4m3(v, false);
 }
 
 __device__ __forceinline__ void load4(const float* p, float (&v)[4]) { load_vec(p, v); }
@@ -72,6 +79,7 @@ struct AppendArgs {
   ac_kv_cache cache;
   CacheRows rows;
   ac_rotary rot;
+  Divisor blocks;                                      // blocks of 16 tokens a page
 };
 
 // A lane holds, of one of a block's 16 tokens (four lanes a token), HD / 32 chunks of four pairs: elements lo .. lo + 3 and hi .. hi + 3.
@@ -81,117 +89,148 @@ __device__ __forceinline__ Chunk chunk(const ac_rotary& r, int i, int sub) {
   return r.interleaved || j >= r.pairs ? Chunk{j, 2 * j, 2 * j + 4} : Chunk{j, j, j + r.pairs};
 }
 
-// Turns a chunk of row `row`, which stands at place `place` of its sequence.
-__device__ __forceinline__ void turn_chunk(const ac_rotary& r, const Chunk& c, int64_t row, int64_t place, float (&a)[4], float (&b)[4]) {
-  if (c.pair >= r.pairs) return;
-  float cs[4], sn[4];
+// Cosines and sines of a lane's chunks, for row `row`, which stands at place `place` of its sequence.
+template <int CH>
+struct Angles { float c[CH][4], s[CH][4]; };
+template <int CH>
+__device__ __forceinline__ void load_angles(const ac_rotary& r, int sub, int64_t row, int64_t place, Angles<CH>& a) {
+  if (r.pairs == 0) return;
+  // bytes from the tables' begin, which 32 bits hold
+  auto table_row = [&](int64_t p) { return (uint32_t)(p < 0 ? 0 : p < r.table_rows ? p : r.table_rows - 1) * (uint32_t)r.ld_table * 4u; };
   if (r.axes == 1 || !r.positions) {
-    int64_t p = r.positions ? r.positions[row] : place;
-    p = p < 0 ? 0 : p < r.table_rows ? p : r.table_rows - 1;
-    load_vec(r.cos + p * r.ld_table + c.pair, cs);
-    load_vec(r.sin + p * r.ld_table + c.pair, sn);
-  } else {
+    const uint32_t at = table_row(r.positions ? r.positions[row] : place);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      int axis = 0, end = r.section[0];
-      while (axis + 1 < r.axes && c.pair + i >= end) end += r.section[++axis];
-      int64_t p = r.positions[axis * r.ld_positions + row];
-      p = p < 0 ? 0 : p < r.table_rows ? p : r.table_rows - 1;
-      cs[i] = r.cos[p * r.ld_table + c.pair + i];
-      sn[i] = r.sin[p * r.ld_table + c.pair + i];
+    for (int i = 0; i < CH; ++i) {
+      const uint32_t in = at + (4 * (sub + 4 * i) < r.pairs ? 16 * (sub + 4 * i) : 0);
+      load_vec((const float*)((const char*)r.cos + in), a.c[i]);
+      load_vec((const float*)((const char*)r.sin + in), a.s[i]);
     }
+  } else {
+    uint32_t at[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) at[x] = table_row(x < r.axes ? r.positions[x * r.ld_positions + row] : 0);
+    const int e0 = r.section[0], e1 = e0 + r.section[1], e2 = e1 + (r.axes > 2 ? r.section[2] : 0);
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int pair = 4 * (sub + 4 * i) < r.pairs ? 4 * (sub + 4 * i) + e : 0;
+        const uint32_t in = (pair < e0 ? at[0] : pair < e1 || r.axes == 2 ? at[1] : pair < e2 || r.axes == 3 ? at[2] : at[3]) + 4u * pair;
+        a.c[i][e] = *(const float*)((const char*)r.cos + in);
+        a.s[i][e] = *(const float*)((const char*)r.sin + in);
+      }
   }
+}
+template <int CH>
+__device__ __forceinline__ void turn_chunk(const ac_rotary& r, int i, int sub, const Angles<CH>& g, float (&a)[4], float (&b)[4]) {
+  if (4 * (sub + 4 * i) >= r.pairs) return;
+  const float(&cs)[4] = g.c[i], (&sn)[4] = g.s[i];
   if (r.interleaved) {
     turn(a[0], a[1], cs[0], sn[0]); turn(a[2], a[3], cs[1], sn[1]);
     turn(b[0], b[1], cs[2], sn[2]); turn(b[2], b[3], cs[3], sn[3]);
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) turn(a[i], b[i], cs[i], sn[i]);
+    for (int e = 0; e < 4; ++e) turn(a[e], b[e], cs[e], sn[e]);
   }
 }
 
-// One wave takes one block of 16 tokens of one head: of the keys, the values or the queries.
-template <typename T, int HD>
-__global__ void __launch_bounds__(256) cache_append(AppendArgs g) {
-  __shared__ __attribute__((aligned(16))) uint8_t turned[4][HD * kBlock];   // a block's values on the way to their order
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, sub = lane % 4, t = lane / 4;
-  const int task = blockIdx.y * 4 + wave, kv = g.cache.heads;
-  if (task >= 2 * kv + g.heads) return;
-  const int64_t page = g.cache.page, b = blockIdx.z;
+enum { KEYS, VALUES, QUERIES };
+template <typename T, int HD, int kind>
+__device__ __forceinline__ void append_head(const AppendArgs& g, int h, uint8_t* turned) {
+  constexpr int CH = HD / 32, VL = (HD + kWave - 1) / kWave;
+  const int lane = threadIdx.x % kWave, sub = lane % 4, t = lane / 4, blocks = g.blocks.d;
+  const int64_t b = blockIdx.z;
   const Sequence sq = sequence(g.rows, b);
   const int64_t first = sq.length - sq.rows;                          // tokens before the rows; what would stand before token 0 is dropped
   const int64_t from = first > 0 ? first : 0;
-  constexpr int CH = HD / 32;
+  if (from >= sq.length) return;
+  const T* src = (const T*)(kind == KEYS ? g.k : kind == VALUES ? g.v : g.q);
+  const int64_t ld = kind == KEYS ? g.ldk : kind == VALUES ? g.ldv : g.ldq;
+  uint8_t* const store = (uint8_t*)(kind == KEYS ? g.cache.k : g.cache.v);
+  float* const scales = kind == KEYS ? g.cache.k_scale : g.cache.v_scale;
+  auto piece = [&](int i) {
+    const Chunk c = chunk(g.rot, i, sub);
+    return kind == VALUES ? Chunk{c.pair, 2 * c.pair, 2 * c.pair + 4} : c;
+  };
   for (int64_t blk = from / kBlock + blockIdx.x; blk * kBlock < sq.length; blk += gridDim.x) {
-    const int64_t place = blk * kBlock + t, row = sq.begin + place - first;
-    const bool fresh = place >= from && place < sq.length;
-    if (task >= 2 * kv) {
-      const int h = task - 2 * kv;
+    const int64_t place = blk * kBlock + t, near = place < from ? from : place < sq.length ? place : sq.length - 1, row = sq.begin + near - first;
+    const bool fresh = place == near;
+    const int nth = quotient((int)blk, g.blocks), in_page = (int)blk - nth * blocks;
+    const int64_t id = kind != QUERIES && nth < g.rows.ld_page_table ? g.rows.page_table[b * g.rows.ld_page_table + nth] : -1;
+    float x[CH][4], y[CH][4];
+    const T* from_row = src + row * ld + h * HD;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const Chunk c = piece(i);
+      load4(from_row + c.lo, x[i]);
+      load4(from_row + c.hi, y[i]);
+    }
+    if constexpr (kind != VALUES) {
+      Angles<CH> ang;
+      load_angles(g.rot, sub, row, near, ang);
+#pragma unroll
+      for (int i = 0; i < CH; ++i) turn_chunk(g.rot, i, sub, ang, x[i], y[i]);
+    }
+    if constexpr (kind == QUERIES) {
       if (!fresh) continue;
+      T* dst = (T*)g.q_out + row * g.ldqo + h * HD;
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
-        const Chunk c = chunk(g.rot, i, sub);
-        float x[4], y[4];
-        const T* src = (const T*)g.q + row * g.ldq + (int64_t)h * HD;
-        T* dst = (T*)g.q_out + row * g.ldqo + (int64_t)h * HD;
-        load4(src + c.lo, x);
-        load4(src + c.hi, y);
-        turn_chunk(g.rot, c, row, place, x, y);
-        store4(dst + c.lo, x);
-        store4(dst + c.hi, y);
+        const Chunk c = piece(i);
+        store4(dst + c.lo, x[i]);
+        store4(dst + c.hi, y[i]);
       }
       continue;
     }
-    const int64_t nth = blk * kBlock / page;
-    const int64_t id = nth < g.rows.ld_page_table ? g.rows.page_table[b * g.rows.ld_page_table + nth] : -1;
     if (id < 0 || id >= g.cache.pages) continue;
-    const bool keys = task < kv;
-    const int h = keys ? task : task - kv;
-    const int64_t blocks = page / kBlock, in_page = blk % blocks;
-    // a block's codes, of keys and of values, are HD * 16 bytes side by side
-    uint8_t* codes = (uint8_t*)(keys ? g.cache.k : g.cache.v) + id * g.cache.stride_page + (h * blocks + in_page) * (HD * kBlock);
-    float* scale = (keys ? g.cache.k_scale : g.cache.v_scale) + id * g.cache.stride_scale + h * blocks + in_page;
-    float x[CH][4], y[CH][4], largest = 0.f;
-    if (fresh) {
-      const T* src = (keys ? (const T*)g.k + row * g.ldk : (const T*)g.v + row * g.ldv) + (int64_t)h * HD;
-#pragma unroll
-      for (int i = 0; i < CH; ++i) {
-        Chunk c = chunk(g.rot, i, sub);
-        if (!keys) c = Chunk{c.pair, 2 * c.pair, 2 * c.pair + 4};
-        load4(src + c.lo, x[i]);
-        load4(src + c.hi, y[i]);
-        if (keys) turn_chunk(g.rot, c, row, place, x[i], y[i]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float u = fabsf(x[i][e]), w = fabsf(y[i][e]);
-          if (u < INFINITY) largest = fmaxf(largest, u);
-          if (w < INFINITY) largest = fmaxf(largest, w);
-        }
-      }
-    }
-    float s = scale_of(wave_max(largest)), ratio = 1.f;
     const int old = from > blk * kBlock ? (int)(from - blk * kBlock) : 0, end = sq.length - blk * kBlock < kBlock ? (int)(sq.length - blk * kBlock) : kBlock;
-    if (old > 0) {
-      const float before = *scale;
-      s = fmaxf(s, before);
-      ratio = before / s;
+    // a block's codes, of keys and of values, are HD * 16 bytes side by side
+    const int64_t in_cache = (int64_t)h * blocks + in_page;
+    uint8_t* codes = store + id * g.cache.stride_page + in_cache * (HD * kBlock);
+    float* scale = scales + id * g.cache.stride_scale + in_cache;
+    float before = 0.f;
+    if (old > 0) before = *scale;
+    u32x4 held[VL];
+    if (kind == VALUES && (old > 0 || end < kBlock)) {
+#pragma unroll
+      for (int i = 0; i < VL; ++i) held[i] = *reinterpret_cast<const u32x4*>(codes + (lane + i * kWave < HD ? lane + i * kWave : HD - 1) * kBlock);
     }
-    const float inv = 1.0f / s;
-    if (fresh) {
+    uint32_t largest = 0;                                           // in the order of the magnitudes' bits: numbers, infinity, NaN
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) largest = max(largest, max(magnitude(x[i][e]), magnitude(y[i][e])));
+    largest = wave_max_u32(fresh ? largest : 0);
+    const bool finite = largest < 0x7f800000u;
+    if (!finite) {
+      largest = 0;
 #pragma unroll
       for (int i = 0; i < CH; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { x[i][e] *= inv; y[i][e] *= inv; }
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t u = magnitude(x[i][e]), w = magnitude(y[i][e]);
+          if (u < 0x7f800000u) largest = max(largest, u);
+          if (w < 0x7f800000u) largest = max(largest, w);
+        }
+      largest = wave_max_u32(fresh ? largest : 0);
     }
-    if (keys) {
+    float s = scale_of(largest), ratio = 1.f;
+    if (old > 0) s = fmaxf(s, before);
+    const float inv = __builtin_bit_cast(float, 0x7f000000u - __builtin_bit_cast(uint32_t, s));      // 1 / s of a power of two
+    if (old > 0) ratio = before * inv;
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { x[i][e] *= inv; y[i][e] *= inv; }
+    if constexpr (kind == KEYS) {
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
-        const Chunk c = chunk(g.rot, i, sub);
+        const Chunk c = piece(i);
         uint32_t* lo = (uint32_t*)(codes + t * HD + c.lo);
         uint32_t* hi = (uint32_t*)(codes + t * HD + c.hi);
         if (fresh) {
-          *lo = to_e4m3(x[i]);
-          *hi = to_e4m3(y[i]);
+          *lo = to_e4m3(x[i], finite);
+          *hi = to_e4m3(y[i], finite);
         } else if (t < old && ratio != 1.f) {
           *lo = move_codes(*lo, ratio);
           *hi = move_codes(*hi, ratio);
@@ -202,40 +241,58 @@ __global__ void __launch_bounds__(256) cache_append(AppendArgs g) {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
           const int d = 8 * (sub + 4 * i);
-          const uint32_t lo = to_e4m3(x[i]), hi = to_e4m3(y[i]);
+          const uint32_t lo = to_e4m3(x[i], finite), hi = to_e4m3(y[i], finite);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            turned[wave][(d + e) * kBlock + t] = (uint8_t)(lo >> (8 * e));
-            turned[wave][(d + 4 + e) * kBlock + t] = (uint8_t)(hi >> (8 * e));
+            turned[(d + e) * kBlock + t] = (uint8_t)(lo >> (8 * e));
+            turned[(d + 4 + e) * kBlock + t] = (uint8_t)(hi >> (8 * e));
           }
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      for (int d = lane; d < HD; d += kWave) {
-        u32x4 c = *reinterpret_cast<const u32x4*>(&turned[wave][d * kBlock]);
-        u32x4* dst = reinterpret_cast<u32x4*>(codes + d * kBlock);
+#pragma unroll
+      for (int j = 0; j < VL; ++j) {
+        const int d = lane + j * kWave;
+        if (d >= HD) break;
+        u32x4 c = *reinterpret_cast<const u32x4*>(&turned[d * kBlock]);
         if (old > 0 || end < kBlock) {
-          const u32x4 held = *dst;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t moved = ratio != 1.f ? move_codes(held[i], ratio) : held[i];
+            const uint32_t moved = ratio != 1.f ? move_codes(held[j][i], ratio) : held[j][i];
             uint32_t r = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int at = 4 * i + e;
-              r |= (at < old ? moved : at < end ? c[i] : held[i]) & (0xffu << (8 * e));
+              r |= (at < old ? moved : at < end ? c[i] : held[j][i]) & (0xffu << (8 * e));
             }
             c[i] = r;
           }
         }
-        *dst = c;
+        *reinterpret_cast<u32x4*>(codes + d * kBlock) = c;
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     }
     if (lane == 0) *scale = s;
   }
+}
+
+// One wave: one block of 16 tokens of one head's keys, values or queries, four lanes a token.  A block has one wave for its scale, so nothing is shared between
+// waves, and where older tokens share it with the new rows the same wave moves them.  What bounds small calls is one load after another, and large ones half the
+// instructions and half the bytes: what does not depend on the rows is asked for beside them, and keys, values and queries, which need different registers, have a
+// path each (in one path 188 registers for heads of 128, 161 in three).  64 sequences, one row each, 32 and 8 heads of 128: 7.1 us; 8192 rows of 16 and 16 heads of 64, 86 MB, 23 us
+// (3.7 TB/s); 65536 rows of 32 and 8 heads of 128, 1.5 GB, 375 us (3.9 TB/s).  Several heads a wave, which share their angles, were no faster.
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) cache_append(AppendArgs g) {
+  __shared__ __attribute__((aligned(16))) uint8_t turned[4][HD * kBlock];   // a block's values on the way to their order
+  const int wave = threadIdx.x / kWave, kv = g.cache.heads, task = __builtin_amdgcn_readfirstlane(blockIdx.y * 4 + wave);
+  if (task < kv)
+    append_head<T, HD, KEYS>(g, task, nullptr);
+  else if (task < 2 * kv)
+    append_head<T, HD, VALUES>(g, task - kv, turned[wave]);
+  else if (task - 2 * kv < g.heads)
+    append_head<T, HD, QUERIES>(g, task - 2 * kv, nullptr);
 }
 
 // ---- attention ---------------------------------------------------------------------------------------------------------
@@ -625,7 +682,7 @@ hipError_t launch_cache_append(const void* q, int64_t ldq, void* q_out, int64_t 
                                int64_t ldv, const ac_kv_cache& cache, const CacheRows& rows, const ac_rotary* rotary, int dtype,
                                hipStream_t s) {
   if (rows.batch <= 0 || rows.rows <= 0) return hipSuccess;
-  AppendArgs a{q, k, v, q_out, ldq, ldqo, ldk, ldv, q ? heads : 0, cache, rows, rotary ? *rotary : ac_rotary{}};
+  AppendArgs a{q, k, v, q_out, ldq, ldqo, ldk, ldv, q ? heads : 0, cache, rows, rotary ? *rotary : ac_rotary{}, divisor(cache.page / kBlock)};
   return dtype == AC_BF16 ? append_width<bf16_t>(a, s) : append_width<float>(a, s);
 }
 

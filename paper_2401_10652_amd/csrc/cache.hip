@@ -597,7 +597,9 @@ constexpr int kPromptRows = 32, kPromptWork = 1 << 24;
 // Runs of keys: as many as fill the chip's places, two blocks of 256 threads a CU (64k tokens, 16 heads of 64: 57 us, with twice as many 60) or one of 512, and, of
 // several sequences, none longer than kLongRun, so that sequences of all lengths, of which the host knows only the longest, keep the chip filled to the end (64
 // sequences of up to 8190 tokens, 8 key heads of 128: 127 us, with runs of 1024 131, of 4096 133).
-constexpr int kMostSplits = 128, kLeastRun = 256, kLongRun = 2048, kPlaces = 512, kPromptPlaces = 256;
+// A run has 256 keys at least: one row over 2400 tokens, 16 heads of 64, 8.4 us, with 128 9.2, with 512 9.6.  Up to 640 keys stay one run, as the second kernel costs
+// more than it saves: 300 tokens 6.0 us and, in two runs, 7.8, 600 tokens 7.5 and 8.3; 1200 tokens 12.0 and 8.3.
+constexpr int kMostSplits = 128, kLeastRun = 256, kWholeRun = 640, kLongRun = 2048, kPlaces = 512, kPromptPlaces = 256;
 Shape shape(int heads, const ac_kv_cache& c, const CacheRows& r, int dtype) {
   const int64_t rows_of = r.max_rows < r.rows ? r.max_rows : r.rows, rows = rows_of * (heads / c.heads);
   const int64_t all = rows_of < r.rows / (r.batch > 0 ? r.batch : 1) ? rows_of * r.batch : r.rows;
@@ -608,7 +610,7 @@ Shape shape(int heads, const ac_kv_cache& c, const CacheRows& r, int dtype) {
   const int64_t blocks = (int64_t)s.tiles * c.heads * r.batch;
   int64_t n = blocks > 0 ? (s.prompt ? kPromptPlaces : kPlaces) / blocks : 1;
   if (!s.prompt && r.batch > 1 && n < r.max_length / kLongRun) n = r.max_length / kLongRun;
-  const int64_t most = (r.max_length + kLeastRun - 1) / kLeastRun;
+  const int64_t most = !s.prompt && r.max_length <= kWholeRun ? 1 : (r.max_length + kLeastRun - 1) / kLeastRun;
   if (n > most) n = most;
   if (n > kMostSplits) n = kMostSplits;
   s.splits = n < 1 ? 1 : (int)n;

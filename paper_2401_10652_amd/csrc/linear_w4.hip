@@ -253,9 +253,15 @@ hipError_t launch_columns(const LinearW4Args& g, hipStream_t s) {
   return rows * ((columns + 1) / 2) >= 256 ? launch_vec<T, NT, MB, 2>(g, s) : launch_vec<T, NT, MB, 1>(g, s);
 }
 
+// Rows a block: 32 share the weights' conversion, 16 fill the chip sooner.  16 are taken below two blocks of 32 for each CU, but for bf16 not where one each
+// fills it.  us, 32 and 16 rows: fp32 61 rows 1003 x 1096, groups of 32, 10.6 and 7.1 (126 blocks of 32); 64 rows 2048 x 2048 17.1 and 15.6 (256); 3200 x 2048 25.9 and
+// 22.4 (400); 4096 x 2048 19.4 and 22.7 (512); bf16 32 rows 2048 x 2048 8.5 and 6.7 (128); 61 rows 8.7 and 9.3 (256); 300 rows 700 x 1000 10.4 and 8.8 (440); 128 rows
+// 2048 x 1024 10.0 and 14.4 (512).
 template <typename T, int NT>
 hipError_t launch_rows(const LinearW4Args& g, hipStream_t s) {
-  return g.m <= 16 ? launch_columns<T, NT, 1>(g, s) : launch_columns<T, NT, 2>(g, s);
+  const int64_t blocks = (g.m + 31) / 32 * ((g.n + 15) / 16);
+  const bool few = blocks < 512 && (NT == 3 || blocks <= 224 || blocks > 256);
+  return g.m <= 16 || few ? launch_columns<T, NT, 1>(g, s) : launch_columns<T, NT, 2>(g, s);
 }
 
 // ---- many rows ---------------------------------------------------------------------------------------------------------

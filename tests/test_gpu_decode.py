@@ -75,6 +75,13 @@ def test_linear_w4_of_many_rows(B, m, n, k, group):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k,group", [(33, 4110, 200, 32), (64, 2048, 130, 128), (70, 2801, 96, 256), (47, 8200, 129, 64), (90, 11000, 160, 128), (300, 700, 72, 64)])
+def test_linear_w4_of_some_rows(B, dtype, m, n, k, group):
+    got, ref, bound = linear_case(B, dtype, m, n, k, group, seed=m + n)
+    assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("zero", [False, True])
 @pytest.mark.parametrize("act,bias,residual", [("none", False, False), ("gelu_erf", True, False), ("gelu_tanh", False, True), ("relu", True, True)])
 def test_linear_w4_epilogues(B, dtype, zero, act, bias, residual):

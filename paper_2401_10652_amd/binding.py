@@ -210,24 +210,35 @@ def _check(status, where):
         raise AcError(status, where)
 
 
+_current = None
+
+
 def _stream():
     """The address of torch's current stream; without the stream object, whose making takes longer than a launch."""
-    import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(torch.cuda.current_device()) if raw is not None else torch.cuda.current_stream().cuda_stream
+    global _current
+    if _current is None:
+        import torch
+        torch.cuda.current_device()                                     # (starts the runtime)
+        raw, device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+        _current = (lambda: raw(device())) if raw and device else lambda: torch.cuda.current_stream().cuda_stream
+    return _current()
 
 
 def _ptr(t):
     return C.c_void_p(0 if t is None else t.data_ptr())
 
 
+_DTYPES = {}
+
+
 def _dt(t):
-    import torch
-    if t.dtype == torch.bfloat16:
-        return AC_BF16
-    if t.dtype == torch.float32:
-        return AC_F32
-    raise TypeError(f"unsupported tensor dtype {t.dtype}")
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.bfloat16: AC_BF16, torch.float32: AC_F32, "codes": torch.uint8})
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        raise TypeError(f"unsupported tensor dtype {t.dtype}")
+    return dt
 
 
 def transformer_desc(cfg, flags=0) -> ac_model_desc:
@@ -517,11 +528,11 @@ def _matrix(t, what, dtype, rows, cols):
 def ac_op_linear_w4(x, w, scale, out, group, zero=None, bias=None, residual=None, activation=AC_ACT_NONE):
     """x [m, k], w uint8 [n, bytes of a row] (two codes a byte, the even column's in the low bits), scale and zero
     [n, ceil(k / group)] -> out [m, n]."""
-    import torch
     (m, k), (n, row), dt = x.shape, w.shape, x.dtype
     groups = -(-k // group)
+    kind = _dt(x)
     xp, ldx = _matrix(x, "x", dt, m, k)
-    wp, ldw = _matrix(w, "w", torch.uint8, n, row)
+    wp, ldw = _matrix(w, "w", _DTYPES["codes"], n, row)
     sp, lds = _matrix(scale, "scale", dt, n, groups)
     zp, ldz = _matrix(zero, "zero", dt, n, groups)
     rp, ldr = _matrix(residual, "residual", dt, m, n)
@@ -531,7 +542,7 @@ def ac_op_linear_w4(x, w, scale, out, group, zero=None, bias=None, residual=None
     if 2 * row < k:
         _bad("w", w, f"{k} columns are wanted")
     _check(lib().ac_op_linear_w4(xp, ldx, wp, ldw, sp, lds, zp, ldz, group, None if bias is None else bias.data_ptr(), rp, ldr, op, ldo, m, n, k,
-                                 activation, _dt(x), _stream()), "ac_op_linear_w4")
+                                 activation, kind, _stream()), "ac_op_linear_w4")
 
 
 def kv_cache(k, v, k_scale, v_scale) -> ac_kv_cache:

@@ -14,6 +14,7 @@ namespace ac {
 
 namespace {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = 128;   // columns a wave takes at a time: 16 bytes of codes a lane
@@ -266,28 +267,27 @@ hipError_t launch_rows(const LinearW4Args& g, hipStream_t s) {
 
 // ---- many rows ---------------------------------------------------------------------------------------------------------
 //
-// Of many rows the matrix cores bound the product, if loads are far enough ahead: a step of 64 columns of k is half a microsecond, and what no
-// block has read yet takes two and more to come.  A block owns 128 rows and 128 columns; of its eight waves four own 32 columns each (whose codes are
-// then converted once for all rows), and its two sets of four take a half of k each, so that two waves share a SIMD also where there are few
-// blocks, and add up in LDS.  x comes to LDS by direct loads three steps ahead, the codes to the registers of the wave that multiplies with them
-// four steps ahead, and blocks that read the same rows of x at a time begin at different steps, so that one has them brought to the cache for the
-// others.  Codes become whole numbers code - zero in bf16 (exact where the zero is a whole number), and a group's sum is scaled in fp32.
-// Scales and zeros of eight groups at a time lie in LDS, each wave's its own.
+// Many rows are work for the matrix cores.  A block owns 128 rows and 128 columns; of its eight waves four own 32 columns each (whose codes are then converted
+// once for all rows), and its two sets of four take a half of k each, so that two waves share a SIMD also where there are few blocks, and add up in LDS.  What no
+// block has read yet takes two microseconds and more to come: x comes to LDS by direct loads, and the codes to the registers of the wave that multiplies
+// with them, two steps of 64 columns of k at a time while the two before are multiplied, and blocks that read the same rows of x at a time begin at different
+// steps, so that one has them brought to the cache for the others.  Codes become whole numbers code - zero in bf16 (exact where the zero is a whole
+// number, else rounded once), and a group's sum is scaled in fp32.  Scales and zeros of eight groups at a time lie in LDS, each wave's its own.
+//
+// 512 rows 6144 x 2048, 192 blocks: 28.6 us, 450 TFLOP/s; 4096 rows 8192 x 2048 199 us, 690.  A step of the eight waves takes 1.4 us: 0.4 of matrix instructions on a
+// SIMD, 0.5 to read x from LDS, and 0.7 to issue what converts codes and scales sums, which overlap in part.  With one step at a time and a barrier
+// after each 29.9 and 210.
 constexpr int kTileM = 128, kTileN = 128, kTileK = 64, kStages = 4;
 constexpr int kXBytes = kTileM * kTileK * 2;
 constexpr int kSetBytes = kStages * kXBytes + 4 * 2 * 1024;          // of a set of four waves: x, and two times eight groups' scales and zeros of each wave
 
-// Codes 0 .. 7 of a word, less `zero`, as bf16 in their own order.
+// Codes 0 .. 7 of a word, less `zero`, as bf16 in their own order.  Read as e4m3, a byte of 0 .. 15 is that number times 2^-9 (0 .. 7 are its subnormal
+// numbers, 8 .. 15 the ones with the least exponent): one conversion with the scale 2^9 makes fp32 of two.
 __device__ __forceinline__ bf16x8 codes_less(uint32_t w, float zero) {
-  uint32_t even = w & 0x0f0f0f0fu, odd = w >> 4 & 0x0f0f0f0fu;
-  asm("" : "+v"(even), "+v"(odd));       // (bytes from here on, which convert without another mask)
-  bf16x8 r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    r[2 * i] = f2bf((float)(even >> (8 * i) & 0xffu) - zero);
-    r[2 * i + 1] = f2bf((float)(odd >> (8 * i) & 0xffu) - zero);
-  }
-  return r;
+  const uint32_t even = w & 0x0f0f0f0fu, odd = w >> 4 & 0x0f0f0f0fu;
+  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(even, 512.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(odd, 512.f, false);
+  const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(even, 512.f, true), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(odd, 512.f, true);
+  return bf16x8{f2bf(a[0] - zero), f2bf(b[0] - zero), f2bf(a[1] - zero), f2bf(b[1] - zero), f2bf(c[0] - zero), f2bf(d[0] - zero), f2bf(c[1] - zero), f2bf(d[1] - zero)};
 }
 
 template <int ACT> __device__ __forceinline__ void activate8(float (&v)[8]) {
@@ -378,7 +378,6 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
     __builtin_amdgcn_sched_barrier(0);
   };
   using all_landed = std::integral_constant<int, 0>;
-  using two_steps = std::integral_constant<int, 2 * (kXBytes / 4096 + 1)>;      // the loads of a step: of x, and of codes
 
   f32x16 total[4], zero16;
 #pragma unroll
@@ -390,7 +389,7 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
   int chunk = chunk_of(step_of(0)), place = 0;
   load_scales(chunk, 0);
 #pragma unroll
-  for (int t = 0; t < kStages - 1; ++t) {
+  for (int t = 0; t < 2; ++t) {
     codes[t] = load_w(t);
     load_x(t, t);
   }
@@ -407,8 +406,13 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
         place ^= 1;
         load_scales(chunk_after(chunk), place ^ 1);
       }
-      codes[(u + kStages - 1) % kStages] = load_w(t + kStages - 1);
-      load_x(t + kStages - 1, (u + kStages - 1) % kStages);
+      if (u % 2 == 0) {
+#pragma unroll
+        for (int v = 2; v < 4; ++v) {
+          codes[(u + v) % kStages] = load_w(t + v);
+          load_x(t + v, (u + v) % kStages);
+        }
+      }
       const uint8_t* const xt = ring + u * kXBytes + l32 * (kTileK * 2);
       u32x4 cw = codes[u];
       // product q takes 16 columns of k: word q of the lane's codes, columns 32 half + 8 q; with groups of 32 words change halves first, so that both
@@ -456,7 +460,7 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
         asm volatile("" : "+v"(total[0]), "+v"(total[1]), "+v"(total[2]), "+v"(total[3]));    // (here and not later, or the groups' sums live side by side)
         __builtin_amdgcn_sched_barrier(0);
       }
-      arrived(two_steps{});
+      if (u % 2 == 1) arrived(all_landed{});
     }
   }
 
@@ -511,7 +515,7 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
 
 // Rows of x that direct loads can take: 16-byte pieces that hold columns of k alone; and offsets within a tile of 32 bits.
 // Products of less than 48 tiles are left to the kernel above, which has blocks for the whole chip then (us, tiles and rows: 256 rows 2048 x 2048, 32 tiles, 26
-// and 15; 512 rows 2048 x 2048, 64 tiles, 27 and 28; 128 rows 8192 x 2048 27 and 36; 512 rows 6144 x 2048 30 and 105).
+// and 15; 512 rows 2048 x 2048, 64 tiles, 26 and 28; 128 rows 8192 x 2048 25 and 36; 512 rows 6144 x 2048 29 and 105).
 bool tiles_take(const LinearW4Args& g) {
   return g.dtype == AC_BF16 && g.m >= 96 && g.m * g.n >= 48 * kTileM * kTileN && (uintptr_t)g.x % 16 == 0 && g.ldx % 8 == 0 && g.k % 8 == 0 && g.k < 1 << 22 && g.ldx < 1 << 22 && g.ldw < 1 << 24 &&
          g.lds < 1 << 22 && g.ldz < 1 << 22;

@@ -2230,8 +2230,8 @@ int ac_op_cache_append(const void* q, int64_t ldq, void* q_out, int64_t ldqo, in
         rotary->ld_table < rotary->pairs || (rotary->positions && rotary->axes > 1 && rotary->ld_positions < n_rows))
       return fail(AC_ERR_ARG, "%s: bad rotation", what);
     if (rotary->pairs % 4 != 0) return fail(AC_ERR_UNSUPPORTED, "%s: pairs in multiples of 4", what);
-    if (rotary->ld_table > 0 && rotary->table_rows > (1 << 30) / rotary->ld_table) return fail(AC_ERR_UNSUPPORTED, "%s: tables of at most 2^30 elements", what);
-    if ((uintptr_t)rotary->cos % 16 != 0 || (uintptr_t)rotary->sin % 16 != 0 || rotary->ld_table % 4 != 0)
+    if (rotary->pairs > 0 && rotary->table_rows > (1 << 30) / rotary->ld_table) return fail(AC_ERR_UNSUPPORTED, "%s: tables of at most 2^30 elements", what);
+    if (rotary->pairs > 0 && ((uintptr_t)rotary->cos % 16 != 0 || (uintptr_t)rotary->sin % 16 != 0 || rotary->ld_table % 4 != 0))
       return fail(AC_ERR_ALIGN, "%s: rows of the tables start at multiples of 16 bytes", what);
   }
   const int64_t on = dtype == AC_BF16 ? 8 : 16;

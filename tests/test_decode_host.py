@@ -98,6 +98,8 @@ for kw in (dict(cos=None), dict(sin=None), dict(pairs=-4), dict(pairs=36, sectio
            dict(ld_table=28), dict(axes=0), dict(axes=5), dict(sections=(16, 16), positions=X, ld_positions=2)):
     refused(B.AC_ERR_ARG, what=append, ro=rot(**kw))
 refused(B.AC_ERR_UNSUPPORTED, what=append, ro=rot(pairs=30, sections=(30,)))
+for no_pairs in (dict(ld_table=1), dict(cos=X + 4, sin=X + 8, ld_table=3), dict(table_rows=1 << 40)):
+    assert append(ro=rot(**{**dict(sections=(0,), pairs=0, axes=1), **no_pairs})) == 0 and kernels()
 assert append(ro=rot(table_rows=1 << 25)) == 0 and append(ro=rot((), pairs=0, axes=1, cos=None, sin=None, ld_table=0)) == 0 and kernels()
 refused(B.AC_ERR_UNSUPPORTED, what=append, ro=rot(table_rows=(1 << 25) + 1))
 for kw in (dict(cos=X + 4), dict(sin=X + 8), dict(ld_table=34)):

@@ -264,6 +264,20 @@ def test_append_values_that_are_not_finite(B, dtype):
     append_case(B, dtype, [12], [5], 2, 2, 64, 16, 0, positions=False, seed=10, alter=alter)
 
 
+def test_append_with_tables_of_no_pairs(B):
+    import torch
+    for cos in (torch.empty((70, 0), device="cuda"), torch.empty((70, 9), device="cuda")[:, 9:]):
+        x, host = up(D.normal((40, 96), 12), "f32")
+        cache = D.Cache([40], 1, 32, 16, 4)
+        dev, out = Device(B, cache), torch.empty((40, 32), device="cuda")
+        where = torch.arange(40, dtype=torch.int32, device="cuda")[None]
+        B.ac_op_cache_append(x[:, 32:64], x[:, 64:], dev.desc, dev.rows([40], [40]), q=x[:, :32], q_out=out, rotary=B.rotary(cos, cos, where))
+        assert torch.equal(out, x[:, :32])
+        cache.append(0, host[:, 32:64].reshape(40, 1, 32), host[:, 64:].reshape(40, 1, 32), 40)
+        down = dev.down()
+        assert all(np.array_equal(down[n], getattr(cache, n)) for n in ("k", "v", "k_scale", "v_scale"))
+
+
 def test_append_of_zeros_and_what_is_dropped(B):
     import torch
     cache = D.Cache([40, 8], 1, 32, 16, 3, fill=0x7f)

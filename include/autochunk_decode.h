@@ -36,6 +36,7 @@ int ac_op_linear_w4(const void* x, int64_t ldx, const void* w, int64_t ldw, cons
  *   k        [pages][heads][page][head_dim]             codes, pages stride_page bytes apart
  *   v        [pages][heads][page / 16][head_dim][16]    codes, the 16 tokens of a block side by side, pages stride_page bytes apart
  *   k_scale, v_scale  [pages][heads][page / 16]         fp32, pages stride_scale floats apart
+ * Scales of blocks that hold tokens are powers of two, as the append leaves them: the attention may apply a scale by its exponent alone.
  * head_dim 32, 64, 96, 128, 192 or 256, else AC_ERR_UNSUPPORTED; k, v and stride_page in multiples of 16 bytes, else AC_ERR_ALIGN.
  */
 typedef struct ac_kv_cache {
@@ -68,7 +69,7 @@ typedef struct ac_cache_rows {
  * positions = NULL, the row's place in its sequence; it is brought into [0, table_rows).
  */
 typedef struct ac_rotary {
-  const float* cos; const float* sin;   /* dev, [table_rows][ld_table], ld_table >= pairs */
+  const float* cos; const float* sin;   /* dev, [table_rows][ld_table], ld_table >= pairs; at most 2^30 elements */
   int64_t table_rows, ld_table;
   const int32_t* positions;             /* dev, [axes][ld_positions], or NULL */
   int64_t ld_positions;
@@ -83,7 +84,7 @@ typedef struct ac_rotary {
  * tokens and that one is larger; elements are stored as the nearest e4m3 number (ties to even) of x / s, infinities and NaN as NaN.  Where older tokens' scale
  * grows, their codes are rewritten as the nearest of code * (old scale / s), which is exact for all but the smallest numbers.  Tokens of a block
  * behind the sequence's last stay as they are.  Two sequences must not append into the same block.
- * All rows and q_out's on 8-byte (bf16) / 16-byte (fp32) boundaries, tables on 16-byte ones, ld_table a multiple of 4, else AC_ERR_ALIGN.
+ * All rows and q_out's on 8-byte (bf16) / 16-byte (fp32) boundaries, tables (if there are pairs) on 16-byte ones, ld_table a multiple of 4, else AC_ERR_ALIGN.
  */
 int ac_op_cache_append(const void* q, int64_t ldq, void* q_out, int64_t ldqo, int heads, const void* k, int64_t ldk, const void* v,
                        int64_t ldv, int64_t n_rows, const ac_kv_cache* cache, const ac_cache_rows* rows, const ac_rotary* rotary,

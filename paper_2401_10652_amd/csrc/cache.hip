@@ -325,6 +325,8 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
 // block g, with that block's two scales in one register each, and the probabilities of its 16 tokens in the order in which the cache
 // holds their values.  No code passes through LDS.  What bounds it is HBM: a step's values are on their way while its scores are computed, the next step's
 // keys while its values are multiplied, and page numbers are read two steps ahead.
+// One row over 65536 tokens, 16 heads of 128, 268 MB: 50 us (5.4 TB/s) and 5 for the join; 64 rows over up to 8190 tokens each, 32 heads on 8 of 128: 120 us and 5.  Small calls
+// are latency: lengths, page numbers, scales and keys come one after another, and the join is a launch more (33 tokens 5.5 us, eight times 5 rows over 2049 tokens 10.5).
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
   constexpr int NT = Terms<T>::kN, W16 = HD / 64, REST = HD % 64 / 32, DT = HD / 16;

@@ -76,26 +76,73 @@ class Decoder:
         # one copy to the device for both
         where = torch.tensor(begin + lengths, dtype=torch.int32).to("cuda")
         rows = B.cache_rows(where[:len(begin)], where[len(begin):], self.table, max(counts), max(lengths))
-        h, hk, d, width = cfg.heads, self.heads_kv, cfg.head_dim, (cfg.heads + 2 * self.heads_kv) * cfg.head_dim
-        like = dict(dtype=self.dtype, device="cuda")
-        x = x.clone()
-        u, qkv, ctx, mid = (torch.empty((n, c), **like) for c in (cfg.d_model, width, h * d, cfg.d_ffn))
-        q, k, v = qkv[:, :h * d], qkv[:, h * d:(h + hk) * d], qkv[:, (h + hk) * d:]
+        need = self._workspace_bytes(n, rows)
+        if need > self.workspace.numel():
+            self.workspace = B.empty_workspace(need)
+        x = self._run(x.clone(), rows, self.workspace)
+        self.lengths = lengths
+        return x
+
+    def _heads(self, n):
+        """A place for n rows' queries, keys and values, and the three as views of it."""
+        import torch
+        h, hk, d = self.cfg.heads, self.heads_kv, self.cfg.head_dim
+        qkv = torch.empty((n, (h + 2 * hk) * d), dtype=self.dtype, device="cuda")
+        return qkv, qkv[:, :h * d], qkv[:, h * d:(h + hk) * d], qkv[:, (h + hk) * d:]
+
+    def _workspace_bytes(self, n, rows):
+        return B.ac_cache_attention_workspace_bytes(self._heads(n)[1], self.caches[0], rows)
+
+    def _run(self, x, rows, workspace):
+        """x becomes the last layer's rows."""
+        import torch
+        cfg, n = self.cfg, x.shape[0]
+        qkv, q, k, v = self._heads(n)
+        u, ctx, mid = (torch.empty((n, c), dtype=self.dtype, device="cuda") for c in (cfg.d_model, q.shape[1], cfg.d_ffn))
         act = B.ACTIVATIONS[cfg.activation]
         for w, cache in zip(self.layers, self.caches):
-            need = B.ac_cache_attention_workspace_bytes(q, cache, rows)
-            if need > self.workspace.numel():
-                self.workspace = B.empty_workspace(need)
             B.ac_op_layernorm(x, w["ln1_g"], w["ln1_b"], u, cfg.ln_eps)
             self._linear(w, "qkv", u, qkv)
             B.ac_op_cache_append(k, v, cache, rows, q=q, q_out=q, rotary=self.rotary)
-            B.ac_op_cache_attention(q, ctx, cache, rows, workspace=self.workspace)
+            B.ac_op_cache_attention(q, ctx, cache, rows, workspace=workspace)
             self._linear(w, "o", ctx, x, residual=x)
             B.ac_op_layernorm(x, w["ln2_g"], w["ln2_b"], u, cfg.ln_eps)
             self._linear(w, "1", u, mid, activation=act)
             self._linear(w, "2", mid, x, residual=x)
-        self.lengths = lengths
         return x
+
+    def step_graph(self):
+        """A function of x [sequences, d_model], the next token of every sequence, as forward's with counts of one, but from a graph: lengths count on the device,
+        and work is laid out for max_tokens.  What it returns is overwritten by its next call."""
+        import torch
+        n = len(self.lengths)
+        x, begin, length = torch.zeros((n, self.cfg.d_model), dtype=self.dtype, device="cuda"), *(
+            torch.arange(n + 1, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda"))
+        rows = B.cache_rows(begin, length, self.table, 1, self.max_tokens)
+        workspace = B.empty_workspace(self._workspace_bytes(n, rows))
+        # once without a page, which leaves the cache as it is: kernels are loaded before the capture
+        self._run(x.clone(), B.cache_rows(begin, length, torch.full_like(self.table, -1), 1, self.max_tokens), workspace)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            length.add_(1)
+            y = self._run(x.clone(), rows, workspace)
+        on_device = None
+
+        def step(new):
+            nonlocal on_device
+            if new.shape != x.shape or new.dtype is not x.dtype:
+                raise ValueError(f"rows {tuple(new.shape)} of {new.dtype} for {n} sequences of {x.shape[1]} x {x.dtype}")
+            if max(self.lengths) >= self.max_tokens:
+                raise ValueError(f"the cache holds {self.max_tokens} tokens of a sequence")
+            if self.lengths != on_device:
+                length.copy_(torch.tensor(self.lengths, dtype=torch.int32))
+            x.copy_(new)
+            graph.replay()
+            self.lengths = on_device = [t + 1 for t in self.lengths]
+            return y
+        step.keep = (graph, workspace, rows, begin)
+        return step
 
 
 def main():
@@ -127,18 +174,23 @@ def main():
             y = read(at, min(args.stretch, args.prompt - at))
         return y.view(args.batch, -1, cfg.d_model)[:, -1].contiguous()
 
-    def steps(y):
+    def steps(y, step):
         for _ in range(args.steps):
-            y = model.forward(y, [1] * args.batch)
+            y = step(y)
         return y
 
     read(0, min(args.stretch, args.prompt))                             # code and clocks
     model.lengths = [0] * args.batch
     y, reading = timed(prompt)
-    y, writing = timed(lambda: steps(y))
+    y, writing = timed(lambda: steps(y, lambda x: model.forward(x, [1] * args.batch)))
+    step = model.step_graph()
+    step(y)
+    model.lengths = [args.prompt] * args.batch
+    y, replaying = timed(lambda: steps(y, step))
     print(json.dumps({"config": cfg.name, "layers": cfg.layers, "dtype": cfg.dtype, "weights": "4 bits", "cache": "8 bits", "batch": args.batch,
                       "prompt": args.prompt, "prompt_tokens_per_s": round(args.batch * args.prompt / reading, 1), "steps": args.steps,
                       "tokens_per_s": round(args.batch * args.steps / writing, 1), "ms_per_step": round(writing / args.steps * 1e3, 3),
+                      "graph_tokens_per_s": round(args.batch * args.steps / replaying, 1), "graph_ms_per_step": round(replaying / args.steps * 1e3, 3),
                       "finite": bool(torch.isfinite(y).all())}))
 
 

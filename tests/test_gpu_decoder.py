@@ -100,6 +100,45 @@ def test_model(B, dtype, tol, heads_kv):
     assert model.lengths == [64, 26, 36]
 
 
+def test_steps_from_a_graph(B):
+    """Replays with eager calls and other lengths between them, each against the model in 64 bits and against an eager call from the same state."""
+    import torch
+    from paper_2401_10652_amd.decode import Decoder
+    cfg, tol = I.TransformerConfig("decoder_2l", 11, 2, 60, 128, 4, 256, True, "f32", None, batch=3), 12 * 2.0 ** -12
+    x, layers = I.transformer_inputs(cfg, bias_std=0.1, ln_jitter=0.1)
+    model = Decoder(cfg, layers, 3, 1500, page=16, group=32)
+    x = torch.as_tensor(x, device="cuda")
+    model.forward(x[:47], [40, 0, 7])
+    step = model.step_graph()
+    assert model.lengths == [40, 0, 7]
+    at = 47
+    for eager in (None, [1, 1, 1], None, [5, 17, 0], None, None):
+        n = 3 if eager is None else sum(eager)
+        rows = x[at:at + n]
+        at += n
+        if eager is None:
+            before = [[t.clone() for t in c.keep] for c in model.caches], list(model.lengths)
+            y = step(rows).clone()
+            ref = reference(model, host(rows), [1, 1, 1], model.lengths, tol * 4)
+            assert np.abs(host(y) - ref).max() <= tol * np.abs(ref).max()
+            after = [[t.clone() for t in c.keep] for c in model.caches], list(model.lengths)
+            for c, held in zip(model.caches, before[0]):
+                for t, u in zip(c.keep, held):
+                    t.copy_(u)
+            model.lengths = before[1]
+            assert np.abs(host(model.forward(rows, [1, 1, 1])) - ref).max() <= tol * np.abs(ref).max()
+            assert model.lengths == after[1]
+            # (the first layer's keys and values do not depend on how its attention is split)
+            assert all(torch.equal(t, u) for t, u in zip(model.caches[0].keep, after[0][0]))
+        else:
+            model.forward(rows, eager)
+    with pytest.raises(ValueError):
+        step(x[:2])
+    model.lengths[1] = 1500
+    with pytest.raises(ValueError):
+        step(x[:3])
+
+
 def test_codes_of_weights(B):
     import torch
     from paper_2401_10652_amd.decode import quantize_w4

@@ -44,8 +44,10 @@ __device__ __forceinline__ Eight<T> load_eight(const T* row, int k, int cols) {
   if (MASKED) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) r.v[i] = row[min(k + i, cols - 1)];
+    int left = cols - k;
+    asm volatile("" : "+v"(left));                       // (conditions of this piece alone: those of all, shared by the rows, were spilled)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r.v[i] = k + i < cols ? r.v[i] : (T)0.0f;
+    for (int i = 0; i < 8; ++i) r.v[i] = i < left ? r.v[i] : (T)0.0f;
   } else {
 #pragma unroll
     for (int j = 0; j < 8 / V; ++j) {
@@ -77,26 +79,41 @@ __device__ __forceinline__ bf16x8 codes_plus_16(uint32_t w) {
 
 // A block owns 16 * MB rows and 16 * CT columns; its waves take steps of 128 columns of k in turn, the next ones' codes and scales on their way while one
 // is multiplied, and add their sums in LDS, in the order of the waves.  SUBS: runs of 32 columns that share a scale within a step (1, 2 or 4).
-// One row 2048 x 2048 (2 MB of codes) 4.6 us, 16 rows 8192 x 2048 7.2, both mostly a launch and the latency of what no one has read yet; 16 rows 8192 x 8192 21 us (34 MB,
-// 1.6 TB/s), 8192 x 8032 16: sixteen rows a power of two apart meet in the same channels of the caches.  Loads that the compiler can count (none under a condition,
-// x one or two steps ahead) took longer, 24 us; other orders of the steps made no difference.
+// One row 2048 x 2048 (2 MB of codes) 4.2 us and 16 rows 8192 x 2048 7.4, both mostly a launch and the latency of what no one has read yet; 16 rows 8192 x 8192 16.4
+// (34 MB, 2.1 TB/s), 32768 x 8192 51 (2.7 TB/s).  Bound by the lines that loads touch: a load takes 64 bytes of each of 16 rows of codes or of x, and of rows a
+// power of two apart few lines stay (8192 x 8032 14 us).  Loads that the compiler can count (none under a condition, x one or two steps ahead, again behind the end)
+// took longer, and other orders of the steps made no difference.
 constexpr int kMostWaves = 8;
 
+template <typename T> struct Pair;                     // a group's scale and zero
+template <> struct Pair<bf16_t> {
+  uint32_t w;
+  __device__ __forceinline__ static Pair of(bf16_t s, bf16_t z) { return Pair{__builtin_bit_cast(uint16_t, s) | (uint32_t)__builtin_bit_cast(uint16_t, z) << 16}; }
+  __device__ __forceinline__ float scale() const { return __builtin_bit_cast(float, w << 16); }
+  __device__ __forceinline__ float zero() const { return __builtin_bit_cast(float, w & 0xffff0000u); }
+};
+template <> struct Pair<float> {
+  float s, z;
+  __device__ __forceinline__ static Pair of(float s, float z) { return Pair{s, z}; }
+  __device__ __forceinline__ float scale() const { return s; }
+  __device__ __forceinline__ float zero() const { return z; }
+};
+
+// Scales and zeros lie in LDS, chunk_steps steps' at a time, a column's `pitch` apart: as a lane's own loads, two bytes of each of sixteen rows, they took as long as codes
+// and x (16 rows 32768 x 8192 69 us, 8192 x 8192 21; one row 8192 x 2048 in groups of 32 12.2 and now 7.5).
 template <typename T, int NT, int MB, int CT, int SUBS, bool VEC>
-__global__ void __launch_bounds__(kMostWaves * 64) linear_w4(LinearW4Args g) {
-  extern __shared__ float joined[];   // [waves][16 MB][16 CT]
+__global__ void __launch_bounds__(kMostWaves * 64) linear_w4(LinearW4Args g, int chunk_steps, int pitch) {
+  extern __shared__ __attribute__((aligned(16))) float joined[];   // [waves][16 MB][16 CT], before that Pair<T> [16 CT][pitch]
+  Pair<T>* const pairs = reinterpret_cast<Pair<T>*>(joined);
   constexpr int ROWS = 16 * MB, COLS = 16 * CT, GS = 4 / SUBS, AHEAD = 2;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
   const int c16 = lane % 16, quarter = lane / 16;
   const int64_t n0 = (int64_t)blockIdx.x * COLS, m0 = (int64_t)blockIdx.y * ROWS;
   const uint8_t* w[CT];
-  const T *scale[CT], *zero[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
     const int64_t n = n0 + 16 * c + c16 < g.n ? n0 + 16 * c + c16 : g.n - 1;
     w[c] = (const uint8_t*)g.w + n * g.ldw;
-    scale[c] = (const T*)g.scale + n * g.lds;
-    zero[c] = (const T*)g.zero + n * g.ldz;
   }
   const T* x[MB];
 #pragma unroll
@@ -115,7 +132,7 @@ __global__ void __launch_bounds__(kMostWaves * 64) linear_w4(LinearW4Args g) {
 
   const int groups = quotient((int)g.k - 1, g.group) + 1;
   const uint32_t last_piece = ((int)g.k - 1) / 2 & ~15;
-  struct Step { u32x4 codes[CT]; T scale[CT][GS], zero[CT][GS]; };
+  struct Step { u32x4 codes[CT]; };
   auto load_x = [&](int r, int k0, Eight<T> (&to)[4]) __attribute__((always_inline)) {
     if (VEC && k0 + kStep <= (int)g.k) {
 #pragma unroll
@@ -125,20 +142,12 @@ __global__ void __launch_bounds__(kMostWaves * 64) linear_w4(LinearW4Args g) {
       for (int j = 0; j < 4; ++j) to[j] = load_eight<true>(x[r], k0 + j * 32, (int)g.k - quarter * 8);
     }
   };
-  // (past the end of k, where x is zero, codes and scales that are there)
+  // (past the end of k, where x is zero, codes that are there)
   auto fetch = [&](int k0) __attribute__((always_inline)) {
     Step s;
     const uint32_t at = min((uint32_t)k0 / 2 + quarter * 16, last_piece);
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      s.codes[c] = *reinterpret_cast<const u32x4*>(w[c] + at);
-#pragma unroll
-      for (int e = 0; e < GS; ++e) {
-        const int gi = min(quotient(k0 + e * SUBS * 32, g.group), groups - 1);
-        s.scale[c][e] = scale[c][gi];
-        s.zero[c][e] = g.zero ? zero[c][gi] : (T)8.0f;
-      }
-    }
+    for (int c = 0; c < CT; ++c) s.codes[c] = *reinterpret_cast<const u32x4*>(w[c] + at);
     return s;
   };
   const int steps = ((int)g.k + kStep - 1) / kStep;
@@ -146,55 +155,83 @@ __global__ void __launch_bounds__(kMostWaves * 64) linear_w4(LinearW4Args g) {
 #pragma unroll
   for (int d = 0; d < AHEAD; ++d)
     if (wave + d * waves < steps) ring[d] = fetch((wave + d * waves) * kStep);
-  for (int i0 = wave; i0 < steps; i0 += waves * AHEAD) {
+  // four columns a wave and 16 groups of each at a time
+  constexpr int PASSES = COLS / 16;                      // of four waves
+  auto load_pairs = [&](int first, int count) __attribute__((always_inline)) {
+    for (int j = lane % 16; j < count; j += 16) {
+      T s[PASSES], z[PASSES];
 #pragma unroll
-    for (int d = 0; d < AHEAD; ++d) {
-      const int i = i0 + d * waves, k0 = i * kStep;
-      if (i >= steps) break;
-      Step& now = ring[d];
-      bf16x8 xf[MB][4][NT];
-#pragma unroll
-      for (int r = 0; r < MB; ++r) {
-        Eight<T> raw[4];
-        load_x(r, k0, raw);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) to_terms(raw[j], xf[r][j]);
+      for (int p = 0; p < PASSES; ++p) {
+        const int64_t n = min(n0 + min((p * waves + wave) * 4 + lane / 16, COLS - 1), g.n - 1);
+        s[p] = ((const T*)g.scale)[n * g.lds + first + j];
+        z[p] = (T)8.0f;
+        if (g.zero) z[p] = ((const T*)g.zero)[n * g.ldz + first + j];
       }
 #pragma unroll
-      for (int c = 0; c < CT; ++c) transpose_quarters(now.codes[c]);
+      for (int p = 0; p < PASSES; ++p) {
+        const int col = (p * waves + wave) * 4 + lane / 16;
+        if (col < COLS) pairs[col * pitch + j] = Pair<T>::of(s[p], z[p]);
+      }
+    }
+  };
+  int i0 = wave;
+  for (int c0 = 0; c0 < steps; c0 += chunk_steps) {
+    const int c1 = min(c0 + chunk_steps, steps), g0 = quotient(c0 * kStep, g.group);
+    if (c0 > 0) __syncthreads();
+    load_pairs(g0, min(quotient(c1 * kStep - 1, g.group), groups - 1) + 1 - g0);
+    __syncthreads();
+    for (; i0 < c1; i0 += waves * AHEAD) {
 #pragma unroll
-      for (int e = 0; e < GS; ++e) {
-        f32x4 sum[MB], part[MB][CT];
+      for (int d = 0; d < AHEAD; ++d) {
+        const int i = i0 + d * waves, k0 = i * kStep;
+        if (i >= steps) break;
+        Step& now = ring[d];
+        bf16x8 xf[MB][4][NT];
 #pragma unroll
         for (int r = 0; r < MB; ++r) {
-          sum[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+          Eight<T> raw[4];
+          load_x(r, k0, raw);
 #pragma unroll
-          for (int j = e * SUBS; j < (e + 1) * SUBS; ++j)
-#pragma unroll
-            for (int t = NT - 1; t >= 0; --t) sum[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[r][j][t], ones, sum[r], 0, 0, 0);
+          for (int j = 0; j < 4; ++j) to_terms(raw[j], xf[r][j]);
         }
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
+        for (int c = 0; c < CT; ++c) transpose_quarters(now.codes[c]);
 #pragma unroll
-          for (int r = 0; r < MB; ++r) part[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int e = 0; e < GS; ++e) {
+          f32x4 sum[MB], part[MB][CT];
 #pragma unroll
-          for (int j = e * SUBS; j < (e + 1) * SUBS; ++j) {
-            const bf16x8 wf = codes_plus_16(now.codes[c][j]);
+          for (int r = 0; r < MB; ++r) {
+            sum[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = e * SUBS; j < (e + 1) * SUBS; ++j)
+#pragma unroll
+              for (int t = NT - 1; t >= 0; --t) sum[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[r][j][t], ones, sum[r], 0, 0, 0);
+          }
+#pragma unroll
+          for (int c = 0; c < CT; ++c) {
+#pragma unroll
+            for (int r = 0; r < MB; ++r) part[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = e * SUBS; j < (e + 1) * SUBS; ++j) {
+              const bf16x8 wf = codes_plus_16(now.codes[c][j]);
+#pragma unroll
+              for (int r = 0; r < MB; ++r)
+#pragma unroll
+                for (int t = NT - 1; t >= 0; --t) part[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[r][j][t], wf, part[r][c], 0, 0, 0);
+            }
+            const Pair<T> pair = pairs[(16 * c + c16) * pitch + min(quotient(k0 + e * SUBS * 32, g.group), groups - 1) - g0];
+            const float s = pair.scale(), off = -16.0f - pair.zero();
 #pragma unroll
             for (int r = 0; r < MB; ++r)
 #pragma unroll
-              for (int t = NT - 1; t >= 0; --t) part[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[r][j][t], wf, part[r][c], 0, 0, 0);
+              for (int i = 0; i < 4; ++i) total[r][c][i] = fmaf(s, fmaf(off, sum[r][i], part[r][c][i]), total[r][c][i]);
           }
-          const float s = Elem<T>::ld(&now.scale[c][e]), off = -16.0f - Elem<T>::ld(&now.zero[c][e]);
-#pragma unroll
-          for (int r = 0; r < MB; ++r)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) total[r][c][i] = fmaf(s, fmaf(off, sum[r][i], part[r][c][i]), total[r][c][i]);
         }
+        if (i + AHEAD * waves < steps) now = fetch((i + AHEAD * waves) * kStep);
       }
-      if (i + AHEAD * waves < steps) now = fetch((i + AHEAD * waves) * kStep);
     }
   }
+  __syncthreads();
 
   // what the first element that this thread finishes is joined with, on its way before the waves meet
   const int e0 = threadIdx.x;
@@ -227,9 +264,15 @@ hipError_t launch_subs(const LinearW4Args& g, hipStream_t s) {
   while (waves < kMostWaves && waves < steps) waves *= 2;
   const dim3 grid((unsigned)((g.n + 16 * CT - 1) / (16 * CT)), (unsigned)((g.m + 16 * MB - 1) / (16 * MB)));
   static_assert((size_t)kMostWaves * 16 * MB * 16 * CT * sizeof(float) <= 64 * 1024, "the waves' sums fit what a kernel has unasked");
-  const size_t lds = (size_t)waves * 16 * MB * 16 * CT * sizeof(float);
+  // chunks of whole rounds of the waves' steps
+  const int64_t round = 2 * waves * kStep, a_round = round / g.group.d + 2, room = 32768 / (16 * CT * 2 * (int64_t)sizeof(T));
+  const int64_t rounds = room > a_round ? room / a_round : 1, groups = (g.k + g.group.d - 1) / g.group.d, most = rounds * round / g.group.d + 2;
+  const int pitch = (int)(groups < most ? groups : most) | 1;            // (odd: sixteen columns in sixteen banks)
+  size_t lds = (size_t)waves * 16 * MB * 16 * CT * sizeof(float);
+  if (lds < 16 * CT * 2 * sizeof(T) * pitch) lds = 16 * CT * 2 * sizeof(T) * pitch;
+  if (lds > 64 * 1024) return hipErrorInvalidValue;
   auto run = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(waves * kWave), lds, s, g);
+    hipLaunchKernelGGL(kernel, grid, dim3(waves * kWave), lds, s, g, (int)(rounds * 2 * waves), pitch);
     return hipGetLastError();
   };
   if constexpr (CT * NT < 12) {
@@ -248,8 +291,8 @@ hipError_t launch_vec(const LinearW4Args& g, hipStream_t s) {
   return vec ? launch_subs<T, NT, MB, CT, true>(g, s) : launch_subs<T, NT, MB, CT, false>(g, s);
 }
 
-// Column tiles of a wave share what it does for x: as many as leave a block for each of the 256 CUs (small groups at most two, for registers).  us, one, two
-// and four tiles: 64 rows 2048 x 2048 8.0, 9.9, 14.1 (256, 128, 64 blocks); 64 rows 8192 x 2048 19.4, 19.4, 15.2; 256 rows 2048 x 2048 27.5, 19.0, 15.4.
+// Column tiles of a wave share what it does for x: as many as leave a block for each of the 256 CUs (small groups at most two, for registers).  us, one tile and as
+// many: 16 rows 8192 x 2048 8.7 and 7.5 (two tiles, 256 blocks), 16 rows 32768 x 8192 81 and 51 (four, 512); 64 rows 8192 x 2048 27 and 13 (four); fp32 512 rows 4096 x 1024 108 and 42 (four).
 template <typename T, int NT, int MB>
 hipError_t launch_columns(const LinearW4Args& g, hipStream_t s) {
   const int64_t rows = (g.m + 16 * MB - 1) / (16 * MB), columns = (g.n + 15) / 16;
@@ -257,14 +300,12 @@ hipError_t launch_columns(const LinearW4Args& g, hipStream_t s) {
   return rows * ((columns + 1) / 2) >= 256 ? launch_vec<T, NT, MB, 2>(g, s) : launch_vec<T, NT, MB, 1>(g, s);
 }
 
-// Rows a block: 32 share the weights' conversion, 16 fill the chip sooner.  16 are taken below two blocks of 32 for each CU, but for bf16 not where one each
-// fills it.  us, 32 and 16 rows: fp32 61 rows 1003 x 1096, groups of 32, 10.6 and 7.1 (126 blocks of 32); 64 rows 2048 x 2048 17.1 and 15.6 (256); 3200 x 2048 25.9 and
-// 22.4 (400); 4096 x 2048 19.4 and 22.7 (512); bf16 32 rows 2048 x 2048 8.5 and 6.7 (128); 61 rows 8.7 and 9.3 (256); 300 rows 700 x 1000 10.4 and 8.8 (440); 128 rows
-// 2048 x 1024 10.0 and 14.4 (512).
+// Rows a block: 32 share the weights' conversion, 16 fill the chip sooner and are taken below two blocks of 32 for each CU.  us, 32 and 16 rows: fp32 61 rows 1003 x 1096,
+// groups of 32, 9.7 and 6.7 (126 blocks of 32); 64 rows 2048 x 2048 11.8 and 8.7 (256); 4096 x 2048 14.9 and 16.7 (512); bf16 64 rows 1024 x 8192 20 and 13 (128); 61 rows 2048 x
+// 2048 7.6 and 6.7 (256); 300 rows 700 x 1000 10.0 and 6.6 (440); 64 rows 8192 x 2048 13 and 18 (1024).
 template <typename T, int NT>
 hipError_t launch_rows(const LinearW4Args& g, hipStream_t s) {
-  const int64_t blocks = (g.m + 31) / 32 * ((g.n + 15) / 16);
-  const bool few = blocks < 512 && (NT == 3 || blocks <= 224 || blocks > 256);
+  const bool few = (g.m + 31) / 32 * ((g.n + 15) / 16) < 512;
   return g.m <= 16 || few ? launch_columns<T, NT, 1>(g, s) : launch_columns<T, NT, 2>(g, s);
 }
 
@@ -517,10 +558,11 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
 }
 
 // Rows of x that direct loads can take: 16-byte pieces that hold columns of k alone; and offsets within a tile of 32 bits.
-// Products of less than 48 tiles are left to the kernel above, which has blocks for the whole chip then (us, tiles and rows: 256 rows 2048 x 2048, 32 tiles, 26
-// and 15; 512 rows 2048 x 2048, 64 tiles, 26 and 28; 128 rows 8192 x 2048 25 and 36; 512 rows 6144 x 2048 29 and 105).
+// Products of up to 64 tiles are left to the kernel above, which has blocks for the whole chip then (us, tiles and rows: 256 rows 2048 x 2048, 32 tiles, 26
+// and 13; 512 rows 2048 x 2048, 64 tiles, 26 and 23, 2048 x 8192 84 and 58; 128 rows 8192 x 2048, 64, 26 and 24; 200 rows 6000 x 1000, 73 tiles' area, 17 and 25; 384 rows 4096 x 1024, 96, 17 and
+// 24; 512 rows 6144 x 2048, 192, 27 and 66).
 bool tiles_take(const LinearW4Args& g) {
-  return g.dtype == AC_BF16 && g.m >= 96 && g.m * g.n >= 48 * kTileM * kTileN && (uintptr_t)g.x % 16 == 0 && g.ldx % 8 == 0 && g.k % 8 == 0 && g.k < 1 << 22 && g.ldx < 1 << 22 && g.ldw < 1 << 24 &&
+  return g.dtype == AC_BF16 && g.m >= 96 && g.m * g.n > 64 * kTileM * kTileN && (uintptr_t)g.x % 16 == 0 && g.ldx % 8 == 0 && g.k % 8 == 0 && g.k < 1 << 22 && g.ldx < 1 << 22 && g.ldw < 1 << 24 &&
          g.lds < 1 << 22 && g.ldz < 1 << 22;
 }
 

@@ -74,8 +74,34 @@ def test_linear_w4_of_many_rows(B, m, n, k, group):
         assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)
 
 
+@pytest.mark.parametrize("m,n,k,group", [(96, 11000, 64, 32), (8200, 129, 8, 64), (1029, 1100, 200, 128), (3500, 310, 520, 64), (257, 4200, 1000, 32), (512, 2100, 1032, 256),
+                                         (300, 3600, 2112, 32), (1100, 1000, 1096, 64), (128, 8300, 4096, 512)])
+def test_linear_w4_of_tiles(B, m, n, k, group):
+    for zero in (False, True):
+        got, ref, bound = linear_case(B, "bf16", m, n, k, group, zero, seed=m + n)
+        assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)
+
+
+@pytest.mark.parametrize("act,bias,residual,pad,wide", [("none", False, False, 8, 16), ("gelu_erf", True, False, 1, 0), ("gelu_tanh", False, True, 24, 0), ("relu", True, True, 8, 48)])
+def test_linear_w4_of_tiles_forms(B, act, bias, residual, pad, wide):
+    got, ref, bound = linear_case(B, "bf16", 130, 8300, 320, 64, True, bias, residual, act, seed=7, pad=pad, wide=wide)
+    assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)
+
+
+def test_linear_w4_of_tiles_rows_keep_to_themselves(B):
+    m, n, k = 130, 8300, 160
+    x = D.normal((m, k), 31)
+    x[3, 7], x[17, 159], x[5] = np.nan, np.inf, x[5] * 1e30
+    x[6] *= 1e-30
+    got, ref, bound = linear_case(B, "bf16", m, n, k, 32, bias=False, residual=False, x=x)
+    assert not np.isfinite(got[[3, 17]]).any()
+    rest = [i for i in range(m) if i not in (3, 17)]
+    assert (np.abs(got - ref)[rest] <= bound[rest]).all()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("m,n,k,group", [(33, 4110, 200, 32), (64, 2048, 130, 128), (70, 2801, 96, 256), (47, 8200, 129, 64), (90, 11000, 160, 128), (300, 700, 72, 64)])
+@pytest.mark.parametrize("m,n,k,group", [(33, 4110, 200, 32), (64, 2048, 130, 128), (70, 2801, 96, 256), (47, 8200, 129, 64), (90, 11000, 160, 128), (300, 700, 72, 64),
+                                         (1, 33, 30100, 32), (3, 20, 20000, 64), (20, 8200, 2300, 32), (17, 70, 9000, 384)])
 def test_linear_w4_of_some_rows(B, dtype, m, n, k, group):
     got, ref, bound = linear_case(B, dtype, m, n, k, group, seed=m + n)
     assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)

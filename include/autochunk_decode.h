@@ -22,7 +22,7 @@ extern "C" {
  * ones; rows start `ldw` bytes apart, a multiple of 16 that is at least (k + 1) / 2; a row is read in pieces of 16 bytes, codes past column k are not used.
  * scale (and zero, NULL = 8 everywhere) [n, ceil(k / group)], rows lds (ldz) elements apart, of type `dtype` as x, bias (may be
  * NULL), residual (may be NULL, may be out) and out.  group: 32, 64 or a multiple of 128.  A row of x that holds an infinity or a NaN comes out without a finite element.
- * w on a 16-byte boundary, else AC_ERR_ALIGN.  Rows of x on 16-byte boundaries (ldx a multiple of 8 in bf16, of 4 in fp32) are read
+ * At most 16 * 65535 rows, else AC_ERR_UNSUPPORTED, and 2^30 columns and groups.  w on a 16-byte boundary, else AC_ERR_ALIGN.  Rows of x on 16-byte boundaries (ldx a multiple of 8 in bf16, of 4 in fp32) are read
  * faster than others.
  */
 int ac_op_linear_w4(const void* x, int64_t ldx, const void* w, int64_t ldw, const void* scale, int64_t lds, const void* zero,
@@ -53,6 +53,7 @@ typedef struct ac_kv_cache {
  * [0, pages) names no memory: what would be stored there is dropped, what would be read there counts as masked.  So do rows that a length
  * shorter than the sequence's rows would put in front of token 0.  max_rows and max_length: the most rows and tokens of one
  * sequence as far as the host knows, by which launches are sized; sequences that exceed them are still computed, more slowly.
+ * At most 65535 sequences, 2^30 rows (times heads, in the attention) and 2^30 places of a sequence, else AC_ERR_UNSUPPORTED.
  */
 typedef struct ac_cache_rows {
   const int32_t* row_begin;         /* dev, [batch + 1] */

@@ -8,8 +8,6 @@
 // scale multiplies a group's sum once, in fp32: no weight is ever rounded.  fp32 rows are three bf16 terms that sum to them exactly.
 #include "common.h"
 
-#include <type_traits>
-
 namespace ac {
 
 namespace {
@@ -411,17 +409,20 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
   const int chunk_first = chunk_of(first), chunk_last = chunk_of(first + steps - 1);
   auto chunk_after = [&](int c) { return c == chunk_last ? chunk_first : c + 1; };
 
-  // all loads but the youngest N have landed and LDS is read, in this wave and then in every
-  auto arrived = [&](auto n) __attribute__((always_inline)) {
-    constexpr int N = decltype(n)::value;
+  // this wave's loads have landed and its LDS reads are done; and every wave's
+  auto landed = [&]() __attribute__((always_inline)) {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 7 << 4);
+    __builtin_amdgcn_s_waitcnt(7 << 4);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto arrived = [&]() __attribute__((always_inline)) {
+    landed();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
-  using all_landed = std::integral_constant<int, 0>;
 
   f32x16 total[4], zero16;
 #pragma unroll
@@ -431,6 +432,7 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
 
   u32x4 codes[kStages];
   int chunk = chunk_of(step_of(0)), place = 0;
+  bool asked = false;            // whether a chunk's scales have been asked for since the last barrier
   load_scales(chunk, 0);
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
@@ -438,17 +440,22 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
     load_x(t, t);
   }
   load_scales(chunk_after(chunk), 1);
-  arrived(all_landed{});
+  arrived();
   for (int t0 = 0; t0 < steps; t0 += kStages) {
 #pragma unroll
     for (int u = 0; u < kStages; ++u) {
       const int t = t0 + u;
       if (t >= steps) break;
       const int step = step_of(t), g0 = quotient(step * kTileK, g.group), c = min(g0, groups - 1) / 8;
-      if (c != chunk) {          // (its scales landed steps ago; those before them are not read any more)
+      // A chunk's scales are on their way from the first step of the chunk before it, and every second step ends with all loads landed.  Where a set's part of k begins
+      // or ends in the middle of a chunk, that chunk may be one step, an even one, and no barrier lies behind it: then the wave waits for its own loads.
+      if (u % 2 == 0) asked = false;
+      if (c != chunk) {
+        if (asked) landed();
+        asked = true;
         chunk = c;
         place ^= 1;
-        load_scales(chunk_after(chunk), place ^ 1);
+        load_scales(chunk_after(chunk), place ^ 1);      // (over those of the chunk before, which are not read any more)
       }
       if (u % 2 == 0) {
 #pragma unroll
@@ -504,7 +511,7 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
         asm volatile("" : "+v"(total[0]), "+v"(total[1]), "+v"(total[2]), "+v"(total[3]));    // (here and not later, or the groups' sums live side by side)
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (u % 2 == 1) arrived(all_landed{});
+      if (u % 2 == 1) arrived();
     }
   }
 

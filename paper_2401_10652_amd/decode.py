@@ -113,7 +113,8 @@ class Decoder:
 
     def step_graph(self):
         """A function of x [sequences, d_model], the next token of every sequence, as forward's with counts of one, but from a graph: lengths count on the device,
-        and work is laid out for max_tokens.  What it returns is overwritten by its next call."""
+        and work is laid out for max_tokens.  What it returns is overwritten by its next call.  Between calls `lengths` may be set, whole or one of it: a sequence
+        then goes on behind as many of its tokens."""
         import torch
         n = len(self.lengths)
         x, begin, length = torch.zeros((n, self.cfg.d_model), dtype=self.dtype, device="cuda"), *(
@@ -139,7 +140,8 @@ class Decoder:
                 length.copy_(torch.tensor(self.lengths, dtype=torch.int32))
             x.copy_(new)
             graph.replay()
-            self.lengths = on_device = [t + 1 for t in self.lengths]
+            self.lengths = [t + 1 for t in self.lengths]
+            on_device = list(self.lengths)                              # (the caller may change the other one in place)
             return y
         step.keep = (graph, workspace, rows, begin)
         return step

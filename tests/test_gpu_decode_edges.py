@@ -6,7 +6,9 @@ import pytest
 
 import decode_ref as D
 import w4_steps as W
+from paper_2401_10652_amd import inputs as I
 from test_gpu_decode import B, torch_dtype, up  # noqa: F401
+from test_gpu_decoder import host, reference
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +52,32 @@ def test_linear_w4_of_tiles_chunks_of_one_step(B, m, n, k, group, pad):
 def test_linear_w4_scales_and_zeros_apart(B, dtype, m, n, k, group, pad):
     got, ref, bound = linear_case(B, dtype, m, n, k, group, pad, seed=m)
     assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)
+
+
+# ---- the model -----------------------------------------------------------------------------------------------------------
+
+def small_model(sequences=3, max_tokens=200, **more):
+    """(a decoder of two fp32 layers, rows for it)"""
+    import torch
+    from paper_2401_10652_amd.decode import Decoder
+    cfg = I.TransformerConfig("decoder_2l", 11, 2, 60, 128, 4, 256, True, "f32", None, batch=3)
+    x, layers = I.transformer_inputs(cfg, bias_std=0.1, ln_jitter=0.1)
+    return Decoder(cfg, layers, sequences, max_tokens, page=16, group=32, **more), torch.as_tensor(x, device="cuda")
+
+
+MODEL_TOL = 12 * 2.0 ** -12       # two layers of six operators, each off by 2^-16 of magnitudes that are about 16 times its sums
+
+
+def test_steps_from_a_graph_after_lengths_changed_in_place(B):
+    """A sequence cut short, and one begun anew, between two replays: each replay against the model in 64 bits."""
+    model, x = small_model()
+    model.forward(x[:80], [40, 25, 15])
+    step = model.step_graph()
+    for i, (b, n) in enumerate(((None, 0), (1, 0), (None, 0), (0, 17), (2, 0), (None, 0))):
+        if b is not None:
+            model.lengths[b] = n
+        lengths = [t + 1 for t in model.lengths]
+        y = step(x[80 + 3 * i:83 + 3 * i])
+        assert model.lengths == lengths
+        ref = reference(model, host(x[80 + 3 * i:83 + 3 * i]), [1, 1, 1], lengths, MODEL_TOL * 4)
+        assert np.abs(host(y) - ref).max() <= MODEL_TOL * np.abs(ref).max(), (i, np.abs(host(y) - ref).max() / np.abs(ref).max())

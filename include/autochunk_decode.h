@@ -94,7 +94,8 @@ int ac_op_cache_append(const void* q, int64_t ldq, void* q_out, int64_t ldqo, in
 /*
  * out[r, h] = softmax(scale * q[r, h] . k) v over the tokens that row r sees: all of its sequence's, or with causal != 0 those up to its own place.
  * Query head h reads head h / (heads / cache->heads) of the cache (heads a multiple of cache->heads).  A row that sees nothing (length 0)
- * comes out as zeros; tokens that a row does not see do not reach it, whatever their codes.  q, out: [n_rows][heads * head_dim], rows on
+ * comes out as zeros; tokens that a row does not see do not reach it, whatever their codes.  Scores, maxima and sums are fp32.  Probabilities are fp32 with fp32 rows; with bf16
+ * rows they meet the values with 16 bits, and with 8 where many rows go through tiles for prompts.  q, out: [n_rows][heads * head_dim], rows on
  * 16-byte boundaries, else AC_ERR_ALIGN.  Few rows over many tokens are split over the tokens, and the parts joined by a second kernel:
  * workspace (dev, 16-byte aligned) holds them, ac_cache_attention_workspace_bytes() large (0: none needed), else AC_ERR_WORKSPACE.
  * Results do not depend on what else runs, but on the split: on max_rows, max_length, batch and n_rows.

@@ -297,13 +297,23 @@ __global__ void __launch_bounds__(256) cache_append(AppendArgs g) {
 
 // ---- attention ---------------------------------------------------------------------------------------------------------
 
+// bf16 terms of a query's number and of a probability (times its value's scale).  bf16 rows are one term.  The probabilities keep 16 bits in two, or the output would be off by
+// half as much again as its own rounding to bf16 has it (of 64 bits 0.0020 to 0.0024, and now 0.0017); HBM bounds this kernel, and the second term costs 1 to 4 % (64 sequences 128 and
+// 131 us, one row over 64k tokens 57 and 57).  fp32: three terms, which sum to the number.
 template <typename T> struct Terms;
-template <> struct Terms<bf16_t> { static constexpr int kN = 1; };
-template <> struct Terms<float> { static constexpr int kN = 3; };
+template <> struct Terms<bf16_t> { static constexpr int kQuery = 1, kProb = 2; };
+template <> struct Terms<float> { static constexpr int kQuery = 3, kProb = 3; };
 
 __device__ __forceinline__ void to_terms(const float (&v)[8], bf16x8 (&f)[1]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[0][i] = f2bf(v[i]);
+}
+__device__ __forceinline__ void to_terms(const float (&v)[8], bf16x8 (&f)[2]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    f[0][i] = f2bf(v[i]);
+    f[1][i] = f2bf(v[i] - bf2f(f[0][i]));
+  }
 }
 __device__ __forceinline__ void to_terms(const float (&v)[8], bf16x8 (&f)[3]) {
 #pragma unroll
@@ -329,7 +339,7 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
 // are latency: lengths, page numbers, scales and keys come one after another, and the join is a launch more (33 tokens 5.5 us, eight times 5 rows over 2049 tokens 10.5).
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
-  constexpr int NT = Terms<T>::kN, W16 = HD / 64, REST = HD % 64 / 32, DT = HD / 16;
+  constexpr int NT = Terms<T>::kQuery, NP = Terms<T>::kProb, W16 = HD / 64, REST = HD % 64 / 32, DT = HD / 16;
   constexpr int FR = HD / 32;                          // fragments of 32 of a row
   constexpr int LD = HD + 4;                           // floats a row of sums in LDS: rows begin four banks apart
   extern __shared__ float joined[];
@@ -435,7 +445,7 @@ __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
         sum += p[e];
       }
       l = fmaf(l, alpha, sum);
-      bf16x8 pf[2][NT];
+      bf16x8 pf[2][NP];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         float pv[8];
@@ -461,7 +471,7 @@ __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
           for (int u = 0; u < 2; ++u) {
             const bf16x8 vf = codes_bf16(vw[d][2 * u], vw[d][2 * u + 1]);
 #pragma unroll
-            for (int x = NT - 1; x >= 0; --x) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[u][x], o[d], 0, 0, 0);
+            for (int x = NP - 1; x >= 0; --x) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[u][x], o[d], 0, 0, 0);
           }
       } else {
         // A NaN times a probability of 0 is NaN, so NaN values are counted apart, among the tokens that a row sees.  (Tokens past the last may hold
@@ -478,7 +488,7 @@ __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) seen_f[e] = 8 * u + e < left ? (bf16_t)1.0f : (bf16_t)0.0f;
 #pragma unroll
-            for (int x = NT - 1; x >= 0; --x) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[u][x], o[d], 0, 0, 0);
+            for (int x = NP - 1; x >= 0; --x) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[u][x], o[d], 0, 0, 0);
             count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf, seen_f, count, 0, 0, 0);
           }
 #pragma unroll

@@ -8,7 +8,8 @@
 // O^T = V^T P^T by v_mfma_f32_32x32x16_bf16 with a row to a column.  Row x of a tile of 32 keys is token 4 (x / 8) + x mod 4 of block
 // (x / 4) mod 2: lane half h then holds the scores of block h of the tile, in the order in which the cache holds the values of its 16 tokens, and the
 // probabilities are the second product's operand as they stand.  Scales are powers of two: the conversion from e4m3 to bf16 multiplies by
-// them, and nothing is rounded.
+// them, and nothing is rounded.  Probabilities are: to bf16, one term, with their sum taken before it, which puts outputs 0.0023 (in 2-norm) from 64 bits where their own rounding
+// has them at 0.0017.  With a second term, as where rows are few, half as many matrix instructions again: 2048 rows behind 14336 tokens 425 us for 281, heads of 64 254 for 196.
 //
 // 2048 rows behind 14336 tokens, 16 heads of 128: 280 us, 0.92 PFLOP/s, of 1.25 that a large library product reaches.  What is left is issued beside the matrix
 // instructions: 32 exponentials, their scaling and packing, and as many conversions of codes for every 32 of them.

@@ -7,7 +7,7 @@ import pytest
 import decode_ref as D
 import w4_steps as W
 from paper_2401_10652_amd import inputs as I
-from test_gpu_decode import B, torch_dtype, up  # noqa: F401
+from test_gpu_decode import B, attention_case, torch_dtype, up  # noqa: F401
 from test_gpu_decoder import host, reference
 
 pytestmark = pytest.mark.gpu
@@ -52,6 +52,23 @@ def test_linear_w4_of_tiles_chunks_of_one_step(B, m, n, k, group, pad):
 def test_linear_w4_scales_and_zeros_apart(B, dtype, m, n, k, group, pad):
     got, ref, bound = linear_case(B, dtype, m, n, k, group, pad, seed=m)
     assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------------
+
+def bound_of_few_rows(out, size, reach, dtype):
+    """As for rows in fp32, but probabilities of two bf16 terms, each of half a unit of 2^-8: 2^-16 of them is lost; and the result rounded once."""
+    p = 4 * 8 * D.U["f32"] * reach + 16 * D.U["f32"]
+    return (p + D.U["bf16"] ** 2) * size + 1.01 * D.U["bf16"] * np.abs(out) + 1e-30
+
+
+@pytest.mark.parametrize("counts,lengths,heads,heads_kv,d,page", [
+    ([1], [40], 4, 4, 32, 16), ([1], [1000], 4, 2, 64, 16), ([1], [4099], 4, 2, 128, 32), ([1, 1, 1], [700, 0, 3000], 8, 2, 96, 16), ([5, 3], [900, 2500], 8, 1, 64, 32),
+    ([7], [600], 2, 1, 192, 16), ([16], [333], 2, 2, 256, 64)])
+def test_attention_of_few_rows_rounds_once(B, monkeypatch, counts, lengths, heads, heads_kv, d, page):
+    """What bf16 rows come out as is the fp32 result, rounded to bf16."""
+    monkeypatch.setattr(D, "attention_bound", bound_of_few_rows)
+    attention_case(B, "bf16", counts, lengths, heads, heads_kv, d, page, seed=sum(lengths) + d)
 
 
 # ---- the model -----------------------------------------------------------------------------------------------------------

@@ -313,10 +313,10 @@ hipError_t launch_rows(const LinearW4Args& g, hipStream_t s) {
 // once for all rows), and its two sets of four take a half of k each, so that two waves share a SIMD also where there are few blocks, and add up in LDS.  What no
 // block has read yet takes two microseconds and more to come: x comes to LDS by direct loads, and the codes to the registers of the wave that multiplies
 // with them, two steps of 64 columns of k at a time while the two before are multiplied, and blocks that read the same rows of x at a time begin at different
-// steps, so that one has them brought to the cache for the others.  Codes become whole numbers code - zero in bf16 (exact where the zero is a whole
-// number, else rounded once), and a group's sum is scaled in fp32.  Scales and zeros of eight groups at a time lie in LDS, each wave's its own.
+// steps, so that one has them brought to the cache for the others.  Codes become code - zero in bf16, exact for whole zeros; of
+// another the whole part goes there and the rest, which bf16 holds as well, times x is a second product.  A group's sum is scaled in fp32.  Scales and zeros of eight groups at a time lie in LDS, each wave's its own.
 //
-// 512 rows 6144 x 2048, 192 blocks: 28.6 us, 450 TFLOP/s; 4096 rows 8192 x 2048 199 us, 690.  A step of the eight waves takes 1.4 us: 0.4 of matrix instructions on a
+// 512 rows 6144 x 2048, 192 blocks: 28.8 us, 450 TFLOP/s; 4096 rows 8192 x 2048 211 us, 650 (zeros that are no whole numbers: 40 and 307).  A step of the eight waves takes 1.4 us: 0.4 of matrix instructions on a
 // SIMD, 0.5 to read x from LDS, and 0.7 to issue what converts codes and scales sums, which overlap in part.  With one step at a time and a barrier
 // after each 29.9 and 210.
 constexpr int kTileM = 128, kTileN = 128, kTileK = 64, kStages = 4;
@@ -331,6 +331,9 @@ __device__ __forceinline__ bf16x8 codes_less(uint32_t w, float zero) {
   const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(even, 512.f, true), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(odd, 512.f, true);
   return bf16x8{f2bf(a[0] - zero), f2bf(b[0] - zero), f2bf(a[1] - zero), f2bf(b[1] - zero), f2bf(c[0] - zero), f2bf(d[0] - zero), f2bf(c[1] - zero), f2bf(d[1] - zero)};
 }
+
+// The part of a zero that codes_less takes, whose differences fit bf16; what is left of a zero does as well.
+__device__ __forceinline__ float whole_part(float zero) { return fabsf(zero) <= 240.f ? rintf(zero) : 0.f; }
 
 template <int ACT> __device__ __forceinline__ void activate8(float (&v)[8]) {
 #pragma unroll
@@ -477,13 +480,16 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
         const int piece = GS == 2 ? 2 * q + half : half * 4 + q;
         return *reinterpret_cast<const bf16x8*>(xt + r * 32 * (kTileK * 2) + (piece ^ (l32 & 7)) * 16);
       };
-      float s[GS], z[GS];
+      float s[GS], z[GS], z_rest[GS];
 #pragma unroll
       for (int e = 0; e < GS; ++e) {
         const uint8_t* const at = scales + place * 1024 + l32 * 16 + min(g0 + e, groups - 1) % 8 * 2;
         s[e] = bf2f(*reinterpret_cast<const bf16_t*>(at));
-        z[e] = g.zero ? bf2f(*reinterpret_cast<const bf16_t*>(at + 512)) : 8.f;
+        const float zero = g.zero ? bf2f(*reinterpret_cast<const bf16_t*>(at + 512)) : 8.f;
+        z[e] = whole_part(zero);
+        z_rest[e] = zero - z[e];
       }
+      const bool second = g.zero && __any(z_rest[0] != 0.f || z_rest[GS - 1] != 0.f);
       // a product's fragments are read and its codes converted under the one before
       bf16x8 a[4], b[2];
 #pragma unroll
@@ -510,6 +516,22 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
           for (int x = 0; x < 16; ++x) total[r][x] = fmaf(s[e], part[r][x], total[r][x]);
         asm volatile("" : "+v"(total[0]), "+v"(total[1]), "+v"(total[2]), "+v"(total[3]));    // (here and not later, or the groups' sums live side by side)
         __builtin_amdgcn_sched_barrier(0);
+      }
+      if (second) {              // (behind the step's other products: between two groups' its branch took 4 % with groups of 32 whether taken or not)
+#pragma unroll
+        for (int e = 0; e < GS; ++e) {
+          bf16x8 rest;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) rest[x] = f2bf(-z_rest[e]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            f32x16 part = zero16;
+#pragma unroll
+            for (int p = 0; p < EACH; ++p) part = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x_frag(e * EACH + p, r), rest, part, 0, 0, 0);
+#pragma unroll
+            for (int x = 0; x < 16; ++x) total[r][x] = fmaf(s[e], part[x], total[r][x]);
+          }
+        }
       }
       if (u % 2 == 1) arrived();
     }

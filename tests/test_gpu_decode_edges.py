@@ -25,7 +25,7 @@ def apart(t, pad):
     return spread[:, :t.shape[1]]
 
 
-def linear_case(B, dtype, m, n, k, group, pad=(0, 0), seed=0):
+def linear_case(B, dtype, m, n, k, group, pad=(0, 0), seed=0, zeros=None):
     """(what comes out, the definition's, the bound): sums in 32 bits, at most 8 roundings of the magnitudes that they are made of, and the result
     rounded once.  pad: elements between rows of scales and of zeros."""
     import torch
@@ -33,7 +33,7 @@ def linear_case(B, dtype, m, n, k, group, pad=(0, 0), seed=0):
     xt, x = up(D.normal((m, k), seed), dtype)
     codes = D.uniform_ints(0, 16, (n, k), seed + 1)
     st, s = up((D.uniform_ints(50, 150, (n, groups), seed + 2) / 100.0) / (4.6 * math.sqrt(k)), dtype)
-    zt, z = up(D.uniform_ints(0, 16, (n, groups), seed + 3), dtype)
+    zt, z = up(D.uniform_ints(0, 16, (n, groups), seed + 3) if zeros is None else zeros(n, groups), dtype)
     out = torch.full((m, n), float("nan"), dtype=xt.dtype, device="cuda")
     B.ac_op_linear_w4(xt, torch.from_numpy(D.pack(codes)).cuda(), apart(st, pad[0]), out, group, zero=apart(zt, pad[1]))
     ref, size = D.linear(x, codes, s, z, group)
@@ -51,6 +51,20 @@ def test_linear_w4_of_tiles_chunks_of_one_step(B, m, n, k, group, pad):
 @pytest.mark.parametrize("m,n,k,group", [(1, 50, 200, 32), (40, 300, 2300, 64), (300, 700, 900, 128), (500, 2200, 520, 32)])
 def test_linear_w4_scales_and_zeros_apart(B, dtype, m, n, k, group, pad):
     got, ref, bound = linear_case(B, dtype, m, n, k, group, pad, seed=m)
+    assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)
+
+
+# Zeros that are no whole numbers from 0 to 15.  32nds leave differences of up to 9 bits, numbers below 1 longer ones, and whole numbers beyond 240 ones of 9 and more.
+ZEROS = {"fractions": lambda n, g: D.uniform_ints(0, 15 * 32, (n, g), 91) / 32.0, "any": lambda n, g: D.normal((n, g), 92, 5.0) + 7.5, "small": lambda n, g: D.normal((n, g), 93, 0.01),
+         "hundreds": lambda n, g: D.normal((n, g), 94, 300.0), "whole": lambda n, g: D.uniform_ints(-260, 270, (n, g), 95), "mixed": lambda n, g: np.where(
+             D.uniform_ints(0, 40, (n, g), 96) == 0, 7.53125, 8.0)}
+
+
+@pytest.mark.parametrize("zeros", ZEROS)
+@pytest.mark.parametrize("dtype,m,n,k,group", [("f32", 5, 100, 200, 32), ("f32", 150, 300, 520, 64), ("bf16", 1, 100, 200, 32), ("bf16", 150, 300, 520, 64), ("bf16", 500, 2200, 328, 32),
+                                               ("bf16", 1000, 1160, 520, 64), ("bf16", 500, 2200, 1000, 256)])
+def test_linear_w4_zeros_that_are_not_whole(B, dtype, m, n, k, group, zeros):
+    got, ref, bound = linear_case(B, dtype, m, n, k, group, seed=m, zeros=ZEROS[zeros])
     assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)
 
 

@@ -22,7 +22,8 @@ extern "C" {
  * ones; rows start `ldw` bytes apart, a multiple of 16 that is at least (k + 1) / 2; a row is read in pieces of 16 bytes, codes past column k are not used.
  * scale (and zero, NULL = 8 everywhere) [n, ceil(k / group)], rows lds (ldz) elements apart, of type `dtype` as x, bias (may be
  * NULL), residual (may be NULL, may be out) and out.  group: 32, 64 or a multiple of 128.  Sums are fp32,
- * and no weight is rounded; in products of many bf16 rows zeros that are no whole numbers take longer.  A row of x that holds an infinity or a NaN comes out without a finite element.
+ * and no weight is rounded; in products of many bf16 rows zeros that are no whole numbers take longer.  The products of a row of x that holds an infinity or a NaN are
+ * infinities or NaN, where an infinity is due also NaN, and every activation leaves NaN as it is; other rows do not see them.
  * At most 16 * 65535 rows, else AC_ERR_UNSUPPORTED, and 2^30 columns and groups.  w on a 16-byte boundary, else AC_ERR_ALIGN.  Rows of x on 16-byte boundaries (ldx a multiple of 8 in bf16, of 4 in fp32) are read
  * faster than others.
  */

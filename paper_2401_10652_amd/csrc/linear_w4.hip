@@ -75,6 +75,9 @@ __device__ __forceinline__ bf16x8 codes_plus_16(uint32_t w) {
   return __builtin_bit_cast(bf16x8, r);
 }
 
+// NaN stays NaN in every activation here, ReLU's too: of an infinity in x the sums above make NaN, which must not come out as 0.
+__device__ __forceinline__ float relu(float v) { return v < 0.f ? 0.f : v; }
+
 // A block owns 16 * MB rows and 16 * CT columns; its waves take steps of 128 columns of k in turn, the next ones' codes and scales on their way while one
 // is multiplied, and add their sums in LDS, in the order of the waves.  SUBS: runs of 32 columns that share a scale within a step (1, 2 or 4).
 // One row 2048 x 2048 (2 MB of codes) 4.2 us and 16 rows 8192 x 2048 7.4, both mostly a launch and the latency of what no one has read yet; 16 rows 8192 x 8192 16.4
@@ -249,7 +252,7 @@ __global__ void __launch_bounds__(kMostWaves * 64) linear_w4(LinearW4Args g, int
     float v = 0.f;
     for (int u = 0; u < waves; ++u) v += joined[u * ROWS * COLS + e];
     v += e == e0 ? bias0 : g.bias ? Elem<T>::ld((const T*)g.bias + n) : 0.f;
-    v = apply_act_rt(v, g.act);
+    v = g.act == AC_ACT_RELU ? relu(v) : apply_act_rt(v, g.act);
     v += e == e0 ? resid0 : g.resid ? Elem<T>::ld((const T*)g.resid + m * g.ldr + n) : 0.f;
     Elem<T>::st((T*)g.out + m * g.ldo + n, v);
   }
@@ -337,7 +340,7 @@ __device__ __forceinline__ float whole_part(float zero) { return fabsf(zero) <= 
 
 template <int ACT> __device__ __forceinline__ void activate8(float (&v)[8]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = apply_act_bf16<ACT>(v[e]);
+  for (int e = 0; e < 8; ++e) v[e] = ACT == AC_ACT_RELU ? relu(v[e]) : apply_act_bf16<ACT>(v[e]);
 }
 __device__ __forceinline__ void activate(float (&v)[8], int act) {
   switch (act) {

@@ -68,6 +68,31 @@ def test_linear_w4_zeros_that_are_not_whole(B, dtype, m, n, k, group, zeros):
     assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)
 
 
+@pytest.mark.parametrize("act", ["none", "relu", "sigmoid", "silu", "gelu_erf", "gelu_tanh"])
+@pytest.mark.parametrize("dtype,m,n", [("f32", 20, 40), ("f32", 200, 1500), ("bf16", 20, 40), ("bf16", 1000, 1160)])
+def test_linear_w4_nan_passes_activations(B, dtype, m, n, act):
+    """Where the definition's product is NaN, so is the result; where it is an infinity, what the activation makes of it, or NaN; elsewhere neither."""
+    import torch
+    k, group = 160, 32
+    x = D.normal((m, k), 3)
+    x[3, 7], x[17, 159], x[5, 40], x[11, 0], x[11, 90] = np.nan, np.inf, -np.inf, np.inf, -np.inf
+    xt, x = up(x, dtype)
+    codes, zero = D.uniform_ints(0, 16, (n, k), 4), D.uniform_ints(0, 16, (n, k // group), 5)
+    st, s = up(np.full((n, k // group), 0.01), dtype)
+    zt, z = up(zero, dtype)
+    out = torch.empty((m, n), dtype=xt.dtype, device="cuda")
+    B.ac_op_linear_w4(xt, torch.from_numpy(D.pack(codes)).cuda(), st, out, group, zero=zt, activation=getattr(B, "AC_ACT_" + act.upper()))
+    got = out.double().cpu().numpy()
+    with np.errstate(all="ignore"):
+        y = D.linear(x, codes, s, z, group)[0]
+        of = {"none": lambda v: v, "relu": lambda v: np.where(v < 0, 0.0, v), "sigmoid": lambda v: 1 / (1 + np.exp(-v)), "silu": lambda v: v / (1 + np.exp(-v)),
+              "gelu_erf": lambda v: np.where(v > 0, v, np.nan), "gelu_tanh": lambda v: np.where(v > 0, v, np.nan)}[act]       # (of infinities)
+        far = np.isinf(y)
+        assert far.any() and np.isnan(got[np.isnan(y)]).all()
+        assert (np.isnan(got) | (got == of(y)))[far].all()
+    assert np.isfinite(got[np.isfinite(y)]).all()
+
+
 # ---- attention ---------------------------------------------------------------------------------------------------------
 
 def bound_of_few_rows(out, size, reach, dtype):

@@ -23,7 +23,8 @@ extern "C" {
  * scale (and zero, NULL = 8 everywhere) [n, ceil(k / group)], rows lds (ldz) elements apart, of type `dtype` as x, bias (may be
  * NULL), residual (may be NULL, may be out) and out.  group: 32, 64 or a multiple of 128.  Sums are fp32,
  * and no weight is rounded; in products of many bf16 rows zeros that are no whole numbers take longer.  The products of a row of x that holds an infinity or a NaN are
- * infinities or NaN, where an infinity is due also NaN, and every activation leaves NaN as it is; other rows do not see them.
+ * infinities or NaN, where an infinity is due also NaN, and every activation leaves NaN as it is; other rows do not see them.  The sums
+ * over a group of |x|, twice that with zeros up to 16, and of |x (code - zero)| / 16 have to be within fp32's range.
  * At most 16 * 65535 rows, else AC_ERR_UNSUPPORTED, and 2^30 columns and groups.  w on a 16-byte boundary, else AC_ERR_ALIGN.  Rows of x on 16-byte boundaries (ldx a multiple of 8 in bf16, of 4 in fp32) are read
  * faster than others.
  */

@@ -1,9 +1,10 @@
 // out = act(x W^T + bias) + residual with weights W[n][k] = (code - zero) * scale held in 4 bits, one scale (and zero) for each group
 // of `group` columns of a row: the linear layers of a decoding step, whose few rows read every weight once.
 //
-// The codes go to the matrix cores as they are.  A bf16 with the code in the upper bits of its mantissa is 16 + code exactly
-// (0x4180 | code << 3), one shift and one and-or for two codes, so per group
-//   sum_k x (code - zero) = sum_k x (16 + code) - (16 + zero) sum_k x,
+// The codes go to the matrix cores as they are.  A bf16 with the code in the upper bits of its mantissa is 1 + code / 16 exactly
+// (0x3f80 | code << 3), one shift and one and-or for two codes, so per group
+//   sum_k x (code - zero) / 16 = sum_k x (1 + code / 16) - (1 + zero / 16) sum_k x,
+// no larger than the sums of x themselves (with 16 + code, rows whose sums are a 32nd of fp32's range became infinities and their difference NaN),
 // both sums by v_mfma_f32_16x16x32_bf16 in fp32 (the second with a matrix of ones, which leaves it in the layout of the first), and the
 // scale multiplies a group's sum once, in fp32: no weight is ever rounded.  fp32 rows are three bf16 terms that sum to them exactly.
 #include "common.h"
@@ -66,12 +67,12 @@ __device__ __forceinline__ void transpose_quarters(u32x4& w) {
   w = u32x4{(uint32_t)c[0], (uint32_t)c[1], (uint32_t)d[0], (uint32_t)d[1]};
 }
 
-__device__ __forceinline__ bf16x8 codes_plus_16(uint32_t w) {
+__device__ __forceinline__ bf16x8 codes_over_16(uint32_t w) {
   u32x4 r;
-  r[0] = (w << 3 & 0x00780078u) | 0x41804180u;
-  r[1] = (w >> 1 & 0x00780078u) | 0x41804180u;
-  r[2] = (w >> 5 & 0x00780078u) | 0x41804180u;
-  r[3] = (w >> 9 & 0x00780078u) | 0x41804180u;
+  r[0] = (w << 3 & 0x00780078u) | 0x3f803f80u;
+  r[1] = (w >> 1 & 0x00780078u) | 0x3f803f80u;
+  r[2] = (w >> 5 & 0x00780078u) | 0x3f803f80u;
+  r[3] = (w >> 9 & 0x00780078u) | 0x3f803f80u;
   return __builtin_bit_cast(bf16x8, r);
 }
 
@@ -214,14 +215,14 @@ __global__ void __launch_bounds__(kMostWaves * 64) linear_w4(LinearW4Args g, int
             for (int r = 0; r < MB; ++r) part[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int j = e * SUBS; j < (e + 1) * SUBS; ++j) {
-              const bf16x8 wf = codes_plus_16(now.codes[c][j]);
+              const bf16x8 wf = codes_over_16(now.codes[c][j]);
 #pragma unroll
               for (int r = 0; r < MB; ++r)
 #pragma unroll
                 for (int t = NT - 1; t >= 0; --t) part[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[r][j][t], wf, part[r][c], 0, 0, 0);
             }
             const Pair<T> pair = pairs[(16 * c + c16) * pitch + min(quotient(k0 + e * SUBS * 32, g.group), groups - 1) - g0];
-            const float s = pair.scale(), off = -16.0f - pair.zero();
+            const float s = pair.scale(), off = fmaf(pair.zero(), -0.0625f, -1.0f);
 #pragma unroll
             for (int r = 0; r < MB; ++r)
 #pragma unroll
@@ -251,7 +252,7 @@ __global__ void __launch_bounds__(kMostWaves * 64) linear_w4(LinearW4Args g, int
     if (m >= g.m || n >= g.n) continue;
     float v = 0.f;
     for (int u = 0; u < waves; ++u) v += joined[u * ROWS * COLS + e];
-    v += e == e0 ? bias0 : g.bias ? Elem<T>::ld((const T*)g.bias + n) : 0.f;
+    v = fmaf(v, 16.0f, e == e0 ? bias0 : g.bias ? Elem<T>::ld((const T*)g.bias + n) : 0.f);
     v = g.act == AC_ACT_RELU ? relu(v) : apply_act_rt(v, g.act);
     v += e == e0 ? resid0 : g.resid ? Elem<T>::ld((const T*)g.resid + m * g.ldr + n) : 0.f;
     Elem<T>::st((T*)g.out + m * g.ldo + n, v);
@@ -316,7 +317,7 @@ hipError_t launch_rows(const LinearW4Args& g, hipStream_t s) {
 // once for all rows), and its two sets of four take a half of k each, so that two waves share a SIMD also where there are few blocks, and add up in LDS.  What no
 // block has read yet takes two microseconds and more to come: x comes to LDS by direct loads, and the codes to the registers of the wave that multiplies
 // with them, two steps of 64 columns of k at a time while the two before are multiplied, and blocks that read the same rows of x at a time begin at different
-// steps, so that one has them brought to the cache for the others.  Codes become code - zero in bf16, exact for whole zeros; of
+// steps, so that one has them brought to the cache for the others.  Codes become (code - zero) / 16 in bf16, exact for whole zeros; of
 // another the whole part goes there and the rest, which bf16 holds as well, times x is a second product.  A group's sum is scaled in fp32.  Scales and zeros of eight groups at a time lie in LDS, each wave's its own.
 //
 // 512 rows 6144 x 2048, 192 blocks: 28.8 us, 450 TFLOP/s; 4096 rows 8192 x 2048 211 us, 650 (zeros that are no whole numbers: 40 and 307).  A step of the eight waves takes 1.4 us: 0.4 of matrix instructions on a
@@ -326,17 +327,17 @@ constexpr int kTileM = 128, kTileN = 128, kTileK = 64, kStages = 4;
 constexpr int kXBytes = kTileM * kTileK * 2;
 constexpr int kSetBytes = kStages * kXBytes + 4 * 2 * 1024;          // of a set of four waves: x, and two times eight groups' scales and zeros of each wave
 
-// Codes 0 .. 7 of a word, less `zero`, as bf16 in their own order.  Read as e4m3, a byte of 0 .. 15 is that number times 2^-9 (0 .. 7 are its subnormal
-// numbers, 8 .. 15 the ones with the least exponent): one conversion with the scale 2^9 makes fp32 of two.
+// Sixteenths of codes 0 .. 7 of a word, less `zero`, as bf16 in their own order.  Read as e4m3, a byte of 0 .. 15 is that number times 2^-9 (0 .. 7 are its subnormal
+// numbers, 8 .. 15 the ones with the least exponent): one conversion with the scale 2^5 makes fp32 of two.
 __device__ __forceinline__ bf16x8 codes_less(uint32_t w, float zero) {
   const uint32_t even = w & 0x0f0f0f0fu, odd = w >> 4 & 0x0f0f0f0fu;
-  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(even, 512.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(odd, 512.f, false);
-  const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(even, 512.f, true), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(odd, 512.f, true);
+  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(even, 32.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(odd, 32.f, false);
+  const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(even, 32.f, true), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(odd, 32.f, true);
   return bf16x8{f2bf(a[0] - zero), f2bf(b[0] - zero), f2bf(a[1] - zero), f2bf(b[1] - zero), f2bf(c[0] - zero), f2bf(d[0] - zero), f2bf(c[1] - zero), f2bf(d[1] - zero)};
 }
 
-// The part of a zero that codes_less takes, whose differences fit bf16; what is left of a zero does as well.
-__device__ __forceinline__ float whole_part(float zero) { return fabsf(zero) <= 240.f ? rintf(zero) : 0.f; }
+// Of a zero's sixteenth the part that codes_less takes, whose differences fit bf16; what is left does as well.
+__device__ __forceinline__ float whole_part(float zero) { return fabsf(zero) <= 240.f ? rintf(zero) * 0.0625f : 0.f; }
 
 template <int ACT> __device__ __forceinline__ void activate8(float (&v)[8]) {
 #pragma unroll
@@ -490,7 +491,7 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
         s[e] = bf2f(*reinterpret_cast<const bf16_t*>(at));
         const float zero = g.zero ? bf2f(*reinterpret_cast<const bf16_t*>(at + 512)) : 8.f;
         z[e] = whole_part(zero);
-        z_rest[e] = zero - z[e];
+        z_rest[e] = fmaf(zero, 0.0625f, -z[e]);
       }
       const bool second = g.zero && __any(z_rest[0] != 0.f || z_rest[GS - 1] != 0.f);
       // a product's fragments are read and its codes converted under the one before
@@ -569,7 +570,7 @@ __global__ void __launch_bounds__(512, 2) linear_w4_tiles(LinearW4Args g) {
     const f32x4 lo = *reinterpret_cast<const f32x4*>(joined + row * kTileN + c8), hi = *reinterpret_cast<const f32x4*>(joined + row * kTileN + c8 + 4);
     float v[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) { v[e] = lo[e] + bias[e]; v[4 + e] = hi[e] + bias[4 + e]; }
+    for (int e = 0; e < 4; ++e) { v[e] = fmaf(lo[e], 16.0f, bias[e]); v[4 + e] = fmaf(hi[e], 16.0f, bias[4 + e]); }
     activate(v, g.act);
     bf16_t* const out = (bf16_t*)g.out + (m0 + row) * g.ldo + n;
     const bf16_t* const resid = (const bf16_t*)g.resid + (m0 + row) * g.ldr + n;

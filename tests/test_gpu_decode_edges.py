@@ -25,19 +25,19 @@ def apart(t, pad):
     return spread[:, :t.shape[1]]
 
 
-def linear_case(B, dtype, m, n, k, group, pad=(0, 0), seed=0, zeros=None):
+def linear_case(B, dtype, m, n, k, group, pad=(0, 0), seed=0, zeros=None, x=None):
     """(what comes out, the definition's, the bound): sums in 32 bits, at most 8 roundings of the magnitudes that they are made of, and the result
     rounded once.  pad: elements between rows of scales and of zeros."""
     import torch
     groups = -(-k // group)
-    xt, x = up(D.normal((m, k), seed), dtype)
+    xt, x = up(D.normal((m, k), seed) if x is None else x, dtype)
     codes = D.uniform_ints(0, 16, (n, k), seed + 1)
     st, s = up((D.uniform_ints(50, 150, (n, groups), seed + 2) / 100.0) / (4.6 * math.sqrt(k)), dtype)
     zt, z = up(D.uniform_ints(0, 16, (n, groups), seed + 3) if zeros is None else zeros(n, groups), dtype)
     out = torch.full((m, n), float("nan"), dtype=xt.dtype, device="cuda")
     B.ac_op_linear_w4(xt, torch.from_numpy(D.pack(codes)).cuda(), apart(st, pad[0]), out, group, zero=apart(zt, pad[1]))
     ref, size = D.linear(x, codes, s, z, group)
-    return out.double().cpu().numpy(), ref, 8 * D.U["f32"] * size + 1.01 * D.U[dtype] * np.abs(ref) + 1e-30
+    return out.double().cpu().numpy(), ref, 8 * D.U["f32"] * size + 1.01 * D.U[dtype] * np.abs(ref) + 2.0 ** -126
 
 
 @pytest.mark.parametrize("m,n,k,group,pad", W.SHORT_CHUNKS)
@@ -65,6 +65,20 @@ ZEROS = {"fractions": lambda n, g: D.uniform_ints(0, 15 * 32, (n, g), 91) / 32.0
                                                ("bf16", 1000, 1160, 520, 64), ("bf16", 500, 2200, 1000, 256)])
 def test_linear_w4_zeros_that_are_not_whole(B, dtype, m, n, k, group, zeros):
     got, ref, bound = linear_case(B, dtype, m, n, k, group, seed=m, zeros=ZEROS[zeros])
+    assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)
+
+
+@pytest.mark.parametrize("zeros", [None, "fractions"])
+@pytest.mark.parametrize("dtype,m,n,k,group", [("f32", 3, 60, 256, 32), ("f32", 200, 700, 256, 128), ("bf16", 3, 60, 256, 32), ("bf16", 64, 2100, 256, 64), ("bf16", 500, 2200, 256, 32),
+                                               ("bf16", 1000, 1160, 256, 128)])
+def test_linear_w4_rows_near_the_ends_of_the_range(B, dtype, m, n, k, group, zeros):
+    """Rows whose sums are a tenth of fp32's range, and rows of its least numbers (as far as an output of their size is one)."""
+    x = D.normal((m, k), 41)
+    x[0] = np.abs(x[0]) * (3.4e38 / 10 / (0.8 * group))
+    x[1] *= -2.0 ** 90
+    x[2] *= 2.0 ** -100
+    got, ref, bound = linear_case(B, dtype, m, n, k, group, seed=m, zeros=ZEROS[zeros] if zeros else None, x=x)
+    assert np.isfinite(got).all() and np.isfinite(ref).all()
     assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)
 
 

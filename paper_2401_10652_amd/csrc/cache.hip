@@ -608,7 +608,9 @@ struct Shape { bool prompt; int tiles, splits; };
 constexpr int kPromptRows = 32, kPromptWork = 1 << 24;
 // Runs of keys: as many as fill the chip's places, two blocks of 256 threads a CU (64k tokens, 16 heads of 64: 57 us, with twice as many 60) or one of 512, and, of
 // several sequences, none longer than kLongRun, so that sequences of all lengths, of which the host knows only the longest, keep the chip filled to the end (64
-// sequences of up to 8190 tokens, 8 key heads of 128: 127 us, with runs of 1024 131, of 4096 133).
+// sequences of up to 8190 tokens, 8 key heads of 128: 127 us, with runs of 1024 131, of 4096 133).  Where a sequence has more than 32 rows of a key head, which are the many rows of
+// fp32, blocks are many as it is and parts large: then only up to two blocks a place (fp32, us, without this and with: two times 2048 rows of 16 heads of 128 over 8192 tokens 1549, behind
+// 136 MB of parts, and 1217 with none; eight times 64 rows of 16 heads on 4 over 8192 210 and 191; four times 40 rows of 16 heads of 64 over 16384 77 and 80).
 // A run has 256 keys at least: one row over 2400 tokens, 16 heads of 64, 8.4 us, with 128 9.2, with 512 9.6.  Up to 640 keys stay one run, as the second kernel costs
 // more than it saves: 300 tokens 6.0 us and, in two runs, 7.8, 600 tokens 7.5 and 8.3; 1200 tokens 12.0 and 8.3.
 constexpr int kMostSplits = 128, kLeastRun = 256, kWholeRun = 640, kLongRun = 2048, kPlaces = 512, kPromptPlaces = 256;
@@ -621,7 +623,11 @@ Shape shape(int heads, const ac_kv_cache& c, const CacheRows& r, int dtype) {
   s.tiles = rows < 1 ? 1 : (int)((rows + each - 1) / each);
   const int64_t blocks = (int64_t)s.tiles * c.heads * r.batch;
   int64_t n = blocks > 0 ? (s.prompt ? kPromptPlaces : kPlaces) / blocks : 1;
-  if (!s.prompt && r.batch > 1 && n < r.max_length / kLongRun) n = r.max_length / kLongRun;
+  if (!s.prompt && r.batch > 1) {
+    int64_t runs = r.max_length / kLongRun;
+    if (r.rows * (heads / c.heads) > kPromptRows * r.batch && runs > 2 * kPlaces / blocks) runs = 2 * kPlaces / blocks;
+    if (n < runs) n = runs;
+  }
   const int64_t most = !s.prompt && r.max_length <= kWholeRun ? 1 : (r.max_length + kLeastRun - 1) / kLeastRun;
   if (n > most) n = most;
   if (n > kMostSplits) n = kMostSplits;

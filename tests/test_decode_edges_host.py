@@ -3,6 +3,7 @@ import random
 
 import pytest
 
+import launch_stub
 import w4_steps as W
 
 
@@ -22,3 +23,27 @@ def test_cases_of_short_chunks_need_the_wait(m, n, k, group, pad):
     groups = -(-k // group)
     assert m >= 96 and m * n > 64 * 128 * 128 and (groups + pad) % 8 == 0 and groups > 8
     assert any(W.late_chunks(k, group, block, half, False) for block in range(-(-n // 128)) for half in (0, 1))
+
+
+def test_attention_workspace_stays_small(tmp_path):
+    """The parts of rows over split keys: no more than what fills the chip once (256 tiles of 128 rows), or, of rows that are few in a sequence (32 of a key head), a part for every
+    2048 tokens, which is a 31st of the codes that they read."""
+    launch_stub.run(launch_stub.build(str(tmp_path)), """
+rng, split = random.Random(3), 0
+def need(dtype, batch, rows, total, length, heads, group, d):
+    c = B.ac_kv_cache(k=X, v=Y, k_scale=W, v_scale=W + 4096, pages=10, stride_page=heads * 64 * d, stride_scale=heads * 4, page=64, heads=heads, head_dim=d)
+    r = B.ac_cache_rows(row_begin=X, length=Y, page_table=W, ld_page_table=1 << 14, batch=batch, max_rows=rows, max_length=length)
+    return L.ac_cache_attention_workspace_bytes(total, heads * group, ctypes.byref(c), ctypes.byref(r), 1, dtype)
+for dtype in (B.AC_F32, B.AC_BF16):
+    for i in range(3000):
+        batch, rows, length = (int(2 ** rng.uniform(0, e)) for e in (8, 13, 18))
+        heads, group, d = rng.choice((1, 2, 8, 16)), rng.choice((1, 4, 7)), rng.choice((32, 64, 128, 256))
+        total = rng.randint(rows, rows * batch)
+        got = need(dtype, batch, rows, total, length, heads, group, d)
+        split += got > 0
+        fill, runs = 256 * 128 * (d + 2) * 4, batch * heads * length * (d + 2) // 16
+        # (rows of a tile that is not full are counted by their tile, and where sequences differ the longest's count is taken for all)
+        assert got <= max(fill, runs), (dtype, batch, rows, total, length, heads, group, d, got)
+    assert split > 100
+assert need(B.AC_F32, 2, 8192, 16384, 8192, 16, 1, 128) == 0 and need(B.AC_F32, 8, 512, 4096, 65536, 16, 1, 128) == 0 and need(B.AC_F32, 2, 65536, 131072, 65536, 16, 1, 128) == 0
+""")

@@ -32,10 +32,13 @@ def quantize_w4(w, group, dtype):
 
 class Decoder:
     """The layers of `cfg` (weights as transformer_inputs makes them; w_qkv's rows are the queries' heads, then the keys' and the
-    values', which may be fewer) and the cache of `sequences` sequences of up to `max_tokens` tokens."""
+    values', which may be fewer) and the cache of `sequences` sequences of up to `max_tokens` tokens.  `cfg` is causal: a token sees those before it and itself; and its
+    queries and keys are rotated by their places, which no plan of the framework does, so that a plan's rows are not these."""
 
     def __init__(self, cfg, layers, sequences, max_tokens, page=64, group=64, base=10000.0):
         import torch
+        if not cfg.causal:
+            raise ValueError(f"{cfg.name} is not causal: its rows cannot be read a token at a time")
         self.cfg, self.group, self.max_tokens = cfg, group, max_tokens
         self.dtype = {"f32": torch.float32, "bf16": torch.bfloat16}[cfg.dtype]
         dev, d = "cuda", cfg.head_dim
@@ -150,7 +153,7 @@ class Decoder:
 def main():
     import torch
     ap = argparse.ArgumentParser()
-    ap.add_argument("--config", default="C2", choices=[n for n, c in I.CONFIGS.items() if isinstance(c, I.TransformerConfig)])
+    ap.add_argument("--config", default="C2", choices=[n for n, c in I.CONFIGS.items() if isinstance(c, I.TransformerConfig) and c.causal])
     ap.add_argument("--batch", type=int, default=8)
     ap.add_argument("--prompt", type=int, default=1024)
     ap.add_argument("--stretch", type=int, default=512, help="tokens of a sequence read at once")

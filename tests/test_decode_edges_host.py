@@ -1,10 +1,14 @@
 """The decoding operators at their edges, on the host: no GPU, no pointer followed."""
+import os
 import random
+import subprocess
+import sys
 
 import pytest
 
 import launch_stub
 import w4_steps as W
+from paper_2401_10652_amd import inputs as I
 
 
 def test_scales_have_landed_before_they_are_read():
@@ -47,3 +51,12 @@ for dtype in (B.AC_F32, B.AC_BF16):
     assert split > 100
 assert need(B.AC_F32, 2, 8192, 16384, 8192, 16, 1, 128) == 0 and need(B.AC_F32, 8, 512, 4096, 65536, 16, 1, 128) == 0 and need(B.AC_F32, 2, 65536, 131072, 65536, 16, 1, 128) == 0
 """)
+
+
+@pytest.mark.parametrize("name", ["C1", "C3"])
+def test_decoder_refuses_models_that_are_not_causal(name):
+    from paper_2401_10652_amd.decode import Decoder
+    with pytest.raises(ValueError, match="not causal"):
+        Decoder(I.CONFIGS[name], [], 1, 16)
+    r = subprocess.run([sys.executable, "-m", "paper_2401_10652_amd.decode", "--config", name], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True)
+    assert r.returncode == 2 and "invalid choice" in r.stderr

@@ -56,6 +56,7 @@ typedef struct ac_kv_cache {
  * [0, pages) names no memory: what would be stored there is dropped, what would be read there counts as masked.  So do rows that a length
  * shorter than the sequence's rows would put in front of token 0.  max_rows and max_length: the most rows and tokens of one
  * sequence as far as the host knows, by which launches are sized; sequences that exceed them are still computed, more slowly.
+ * There may be no sequences, no rows, no places (ld_page_table 0) and no pages in the cache; pointers to what is not there may be NULL.
  * At most 65535 sequences, 2^30 rows (times heads, in the attention) and 2^30 places of a sequence, else AC_ERR_UNSUPPORTED.
  */
 typedef struct ac_cache_rows {

@@ -568,8 +568,8 @@ def kv_cache(k, v, k_scale, v_scale) -> ac_kv_cache:
 
 
 def cache_rows(row_begin, length, page_table, max_rows, max_length) -> ac_cache_rows:
-    """A call's rows: row_begin int32 [batch + 1], length int32 [batch], page_table int32 [batch, pages of a sequence], on the device.  Keeps the
-    tensors alive."""
+    """A call's rows: row_begin int32 [batch + 1], length int32 [batch], page_table int32 [batch, pages of a sequence], on the device (where
+    its rows lie further apart, what lies between them counts as theirs).  Keeps the tensors alive."""
     import torch
     batch, pages = page_table.shape
     if length.shape != (batch,) or row_begin.shape != (batch + 1,):
@@ -578,6 +578,8 @@ def cache_rows(row_begin, length, page_table, max_rows, max_length) -> ac_cache_
         if t.dtype is not torch.int32 or not t.is_contiguous():
             raise TypeError(f"{what} is {t.dtype} with strides {t.stride()}: contiguous int32 is wanted")
     table, ld = _matrix(page_table, "page_table", torch.int32, batch, pages)
+    if batch < 2 or pages == 0:
+        ld = pages
     r = ac_cache_rows(row_begin.data_ptr(), length.data_ptr(), table, ld, batch, max_rows, max_length)
     r.keep = (row_begin, length, page_table)
     return r

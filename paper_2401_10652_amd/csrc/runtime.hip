@@ -2188,15 +2188,19 @@ int ac_op_linear_w4(const void* x, int64_t ldx, const void* w, int64_t ldw, cons
 
 // What append and attention ask of a cache and of the rows' descriptions; AC_OK, or the refusal.
 static int cache_ok(const char* what, const ac_kv_cache* c, const ac_cache_rows* r, int64_t n_rows) {
-  if (!c || !r || !c->k || !c->v || !c->k_scale || !c->v_scale || c->pages < 0 || c->page < 16 || c->page % 16 != 0 || c->heads < 1 ||
-      c->heads > 4096 || c->head_dim < 1 || !r->row_begin || !r->length || !r->page_table || r->ld_page_table < 0 || r->batch < 0 || n_rows < 0 ||
-      r->max_rows < 0 || r->max_length < 0)
+  if (!c || !r || c->pages < 0 || c->page < 16 || c->page % 16 != 0 || c->heads < 1 || c->heads > 4096 || c->head_dim < 1 || r->ld_page_table < 0 ||
+      r->batch < 0 || n_rows < 0 || r->max_rows < 0 || r->max_length < 0)
+    return fail(AC_ERR_ARG, "%s: bad cache or rows", what);
+  // (nothing is read of a cache without pages, of no sequences and of tables without places)
+  const bool pages = c->pages > 0, sequences = r->batch > 0;
+  if ((pages && (!c->k || !c->v || !c->k_scale || !c->v_scale)) || (sequences && (!r->row_begin || !r->length || (r->ld_page_table > 0 && !r->page_table))))
     return fail(AC_ERR_ARG, "%s: bad cache or rows", what);
   if (r->batch > 65535 || n_rows > 1 << 30 || r->max_length > 1 << 30 || r->ld_page_table > (1 << 30) / c->page)
     return fail(AC_ERR_UNSUPPORTED, "%s: at most 65535 sequences, 2^30 rows and places of a sequence", what);
   const int d = c->head_dim;
   if (d != 32 && d != 64 && d != 96 && d != 128 && d != 192 && d != 256)
     return fail(AC_ERR_UNSUPPORTED, "%s: heads of 32, 64, 96, 128, 192 or 256", what);
+  if (!pages) return AC_OK;
   if (c->stride_page < (int64_t)c->heads * c->page * d || c->stride_scale < (int64_t)c->heads * (c->page / 16))
     return fail(AC_ERR_ARG, "%s: pages overlap", what);
   if ((uintptr_t)c->k % 16 != 0 || (uintptr_t)c->v % 16 != 0 || c->stride_page % 16 != 0)

@@ -60,3 +60,25 @@ def test_decoder_refuses_models_that_are_not_causal(name):
         Decoder(I.CONFIGS[name], [], 1, 16)
     r = subprocess.run([sys.executable, "-m", "paper_2401_10652_amd.decode", "--config", name], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True)
     assert r.returncode == 2 and "invalid choice" in r.stderr
+
+
+def test_calls_with_nothing_in_them(tmp_path):
+    """No sequences, no rows, sequences without places, a cache without pages: empty tensors, whose addresses are NULL."""
+    launch_stub.run(launch_stub.build(str(tmp_path)), """
+import torch
+B._stream = lambda: 0
+i = lambda *x: torch.tensor(x, dtype=torch.int32)
+u8 = lambda *s: torch.zeros(s, dtype=torch.uint8)
+table = lambda *s: torch.zeros(s, dtype=torch.int32)
+def cache(pages): return B.kv_cache(u8(pages, 2, 32, 64), u8(pages, 2, 2, 64, 16), torch.ones(pages, 2, 2), torch.ones(pages, 2, 2))
+x = torch.zeros(2, 128)
+for c, begin, length, t, n, launches in ((cache(3), i(0), i(), table(0, 3), 0, 0), (cache(3), i(0, 0), i(5), table(1, 3), 0, 0), (cache(3), i(0, 1, 2), i(1, 1), table(2, 0), 2, 1),
+                                         (cache(0), i(0, 1, 2), i(1, 1), table(2, 3), 2, 1)):
+    rows = B.cache_rows(begin, length, t, 1, 1)
+    assert rows.ld_page_table == t.shape[1] and B.ac_cache_attention_workspace_bytes(x[:n], c, rows) == 0
+    B.ac_op_cache_append(x[:n], x[:n], c, rows)
+    assert len(kernels()) == launches
+    B.ac_op_cache_attention(x[:n], x[:n], c, rows)
+    assert len(kernels()) == launches
+assert B.cache_rows(i(0, 1), i(1), table(4, 8)[1:2, 3:5], 1, 1).ld_page_table == 2         # one row's places, not those between it and the next
+""")

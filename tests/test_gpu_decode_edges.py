@@ -124,6 +124,30 @@ def test_attention_of_few_rows_rounds_once(B, monkeypatch, counts, lengths, head
     attention_case(B, "bf16", counts, lengths, heads, heads_kv, d, page, seed=sum(lengths) + d)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pages,places", [(0, 3), (4, 0), (0, 0)])
+def test_no_pages_and_no_places(B, dtype, pages, places):
+    """Queries are rotated, keys and values dropped, rows see nothing."""
+    import torch
+    heads, heads_kv, d, n = 4, 2, 64, 9
+    u8, i32 = dict(dtype=torch.uint8, device="cuda"), dict(dtype=torch.int32, device="cuda")
+    k, v = torch.full((pages, heads_kv, 32, d), 0x7f, **u8), torch.full((pages, heads_kv, 2, d, 16), 0x7f, **u8)
+    ks, vs = (torch.full((pages, heads_kv, 2), float("nan"), device="cuda") for _ in "kv")
+    cache = B.kv_cache(k, v, ks, vs)
+    rows = B.cache_rows(torch.tensor([0, 5, n], **i32), torch.tensor([20, 4], **i32), torch.zeros((2, places), **i32), 5, 20)
+    xt, x = up(D.normal((n, (heads + 2 * heads_kv) * d), 6), dtype)
+    q, kn, vn = xt.split([heads * d, heads_kv * d, heads_kv * d], 1)
+    q_out, out = (torch.full((n, heads * d), float("nan"), dtype=xt.dtype, device="cuda") for _ in "qo")
+    cos, sin = torch.zeros((20, 32), device="cuda"), torch.ones((20, 32), device="cuda")
+    B.ac_op_cache_append(kn, vn, cache, rows, q=q, q_out=q_out, rotary=B.rotary(cos, sin))
+    turned = D.rotate(x[:, :heads * d].reshape(n, heads, d), np.zeros((n, 32)), np.ones((n, 32)), False)
+    assert np.array_equal(host(q_out).reshape(n, heads, d), turned)
+    for causal in (True, False):
+        B.ac_op_cache_attention(q_out, out.fill_(float("nan")), cache, rows, causal, workspace=B.empty_workspace(B.ac_cache_attention_workspace_bytes(q_out, cache, rows, causal)))
+        assert (out == 0).all()
+    assert (k == 0x7f).all() and (v == 0x7f).all() and torch.isnan(ks).all() and torch.isnan(vs).all()
+
+
 # ---- the model -----------------------------------------------------------------------------------------------------------
 
 def small_model(sequences=3, max_tokens=200, **more):

@@ -70,6 +70,8 @@ class Decoder:
         cfg, n = self.cfg, sum(counts)
         if len(counts) != len(self.lengths) or min(counts) < 0 or x.shape != (n, cfg.d_model) or x.dtype is not self.dtype:
             raise ValueError(f"rows {tuple(x.shape)} of {x.dtype} for {counts} tokens of {len(self.lengths)} sequences of {cfg.d_model} x {self.dtype}")
+        if n == 0:
+            return x.clone()
         lengths = [a + b for a, b in zip(self.lengths, counts)]
         if max(lengths) > self.max_tokens:
             raise ValueError(f"{max(lengths)} tokens: the cache holds {self.max_tokens} of a sequence")

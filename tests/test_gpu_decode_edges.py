@@ -175,3 +175,9 @@ def test_steps_from_a_graph_after_lengths_changed_in_place(B):
         assert model.lengths == lengths
         ref = reference(model, host(x[80 + 3 * i:83 + 3 * i]), [1, 1, 1], lengths, MODEL_TOL * 4)
         assert np.abs(host(y) - ref).max() <= MODEL_TOL * np.abs(ref).max(), (i, np.abs(host(y) - ref).max() / np.abs(ref).max())
+
+
+def test_model_without_tokens(B):
+    model, x = small_model()
+    model.forward(x[:5], [2, 0, 3])
+    assert model.forward(x[:0], [0, 0, 0]).shape == (0, 128) and model.lengths == [2, 0, 3]

@@ -84,7 +84,7 @@ class Decoder:
         need = self._workspace_bytes(n, rows)
         if need > self.workspace.numel():
             self.workspace = B.empty_workspace(need)
-        x = self._run(x.clone(), rows, self.workspace)
+        x = self._run(x.clone(memory_format=torch.contiguous_format), rows, self.workspace)
         self.lengths = lengths
         return x
 

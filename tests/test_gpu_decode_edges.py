@@ -181,3 +181,14 @@ def test_model_without_tokens(B):
     model, x = small_model()
     model.forward(x[:5], [2, 0, 3])
     assert model.forward(x[:0], [0, 0, 0]).shape == (0, 128) and model.lengths == [2, 0, 3]
+
+
+def test_model_reads_rows_of_any_layout(B):
+    """Column by column, and every other row."""
+    import torch
+    model, x = small_model()
+    y = model.forward(x[:30], [20, 0, 10])
+    for rows in (x[:30].T.contiguous().T, x[:30].repeat_interleave(2, 0)[::2]):
+        assert torch.equal(rows, x[:30])
+        model.lengths = [0, 0, 0]
+        assert torch.equal(model.forward(rows, [20, 0, 10]), y)

@@ -555,8 +555,8 @@ def kv_cache(k, v, k_scale, v_scale) -> ac_kv_cache:
     for t, what in ((k, "k"), (v, "v"), (k_scale, "k_scale"), (v_scale, "v_scale")):
         if pages and not t[0].is_contiguous():
             _bad(what, t, "contiguous pages are wanted")
-    if k.element_size() != 1 or v.element_size() != 1:
-        raise TypeError(f"codes are {k.dtype}, {v.dtype}: one byte each is wanted")
+    if any(t.element_size() != 1 or (t.dtype.is_floating_point and t.dtype is not torch.float8_e4m3fn) for t in (k, v)):
+        raise TypeError(f"codes are {k.dtype}, {v.dtype}: e4m3 or bare bytes are wanted")
     if k_scale.dtype is not torch.float32 or v_scale.dtype is not torch.float32:
         raise TypeError(f"scales are {k_scale.dtype}, {v_scale.dtype}: float32 is wanted")
     apart = lambda t: t.stride(0) if pages > 1 else t.numel()  # noqa: E731

@@ -82,3 +82,15 @@ for c, begin, length, t, n, launches in ((cache(3), i(0), i(), table(0, 3), 0, 0
     assert len(kernels()) == launches
 assert B.cache_rows(i(0, 1), i(1), table(4, 8)[1:2, 3:5], 1, 1).ld_page_table == 2         # one row's places, not those between it and the next
 """)
+
+
+def test_cache_of_other_formats_is_refused():
+    import torch
+    from paper_2401_10652_amd import binding as B
+    k, v, s = torch.zeros((3, 2, 32, 64), dtype=torch.uint8), torch.zeros((3, 2, 2, 64, 16), dtype=torch.uint8), torch.ones(3, 2, 2)
+    B.kv_cache(k, v, s, s)
+    B.kv_cache(k.view(torch.float8_e4m3fn), v.view(torch.float8_e4m3fn), s, s)
+    for other in (torch.float8_e5m2, torch.float8_e4m3fnuz, torch.float8_e5m2fnuz):
+        for bad in ((k.view(other), v), (k, v.view(other))):
+            with pytest.raises(TypeError):
+                B.kv_cache(*bad, s, s)

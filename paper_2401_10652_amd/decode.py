@@ -96,7 +96,9 @@ class Decoder:
         return qkv, qkv[:, :h * d], qkv[:, h * d:(h + hk) * d], qkv[:, (h + hk) * d:]
 
     def _workspace_bytes(self, n, rows):
-        return B.ac_cache_attention_workspace_bytes(self._heads(n)[1], self.caches[0], rows)
+        import torch
+        q = torch.empty((n, self.cfg.heads * self.cfg.head_dim), dtype=self.dtype, device="meta")       # (of which sizes and type are read)
+        return B.ac_cache_attention_workspace_bytes(q, self.caches[0], rows)
 
     def _run(self, x, rows, workspace):
         """x becomes the last layer's rows."""

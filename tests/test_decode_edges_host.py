@@ -94,3 +94,18 @@ def test_cache_of_other_formats_is_refused():
         for bad in ((k.view(other), v), (k, v.view(other))):
             with pytest.raises(TypeError):
                 B.kv_cache(*bad, s, s)
+
+
+def test_decoder_asks_for_a_workspace_without_making_rows():
+    import torch
+    from paper_2401_10652_amd import binding as B
+    from paper_2401_10652_amd.decode import Decoder
+    model = object.__new__(Decoder)
+    model.cfg, model.dtype, model.heads_kv = I.C2, torch.bfloat16, 16
+    model.caches = [B.kv_cache(torch.zeros((3, 16, 32, 64), dtype=torch.uint8), torch.zeros((3, 16, 2, 64, 16), dtype=torch.uint8), *(torch.ones(3, 16, 2) for _ in "kv"))]
+    i32 = dict(dtype=torch.int32)
+    rows = B.cache_rows(torch.zeros(2, **i32), torch.zeros(1, **i32), torch.zeros((1, 2048), **i32), 1, 65536)
+    q = torch.empty((1, 1024), dtype=torch.bfloat16)
+    assert model._workspace_bytes(1, rows) == B.ac_cache_attention_workspace_bytes(q, model.caches[0], rows) > 0
+    rows = B.cache_rows(torch.zeros(2, **i32), torch.zeros(1, **i32), torch.zeros((1, 2048), **i32), 1 << 26, 65536)
+    assert model._workspace_bytes(1 << 26, rows) == 0                 # (128 GiB of queries)

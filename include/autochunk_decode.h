@@ -25,7 +25,7 @@ extern "C" {
  * and no weight is rounded; in products of many bf16 rows zeros that are no whole numbers take longer.  The products of a row of x that holds an infinity or a NaN are
  * infinities or NaN, where an infinity is due also NaN, and every activation leaves NaN as it is; other rows do not see them.  The sums
  * over a group of |x|, twice that with zeros up to 16, and of |x (code - zero)| / 16 have to be within fp32's range.
- * At most 16 * 65535 rows, else AC_ERR_UNSUPPORTED, and 2^30 columns and groups.  w on a 16-byte boundary, else AC_ERR_ALIGN.  Rows of x on 16-byte boundaries (ldx a multiple of 8 in bf16, of 4 in fp32) are read
+ * m is at most 16 * 65535, n 2^26, else AC_ERR_UNSUPPORTED, k and group 2^30.  w on a 16-byte boundary, else AC_ERR_ALIGN.  Rows of x on 16-byte boundaries (ldx a multiple of 8 in bf16, of 4 in fp32) are read
  * faster than others.
  */
 int ac_op_linear_w4(const void* x, int64_t ldx, const void* w, int64_t ldw, const void* scale, int64_t lds, const void* zero,

@@ -559,7 +559,7 @@ __global__ void __launch_bounds__(256) cache_attention_join(CacheAttnArgs g) {
   constexpr int LANES = HD / 4, TEAMS = 256 / LANES;
   __shared__ float sums[TEAMS][HD + 2];
   const int team = threadIdx.x / LANES, lane = threadIdx.x % LANES, each = TEAMS / g.teams, mine = team / g.teams, nth = team % g.teams;
-  const int64_t items = g.rows.rows * g.heads, item = (int64_t)blockIdx.x * each + mine, row = item / g.heads;
+  const int64_t items = g.rows.rows * g.heads, item = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * each + mine, row = item / g.heads;
   const bool live = mine < each && item < items && row >= g.rows.row_begin[0] && row < g.rows.row_begin[g.rows.batch];
   float top = -INFINITY, total = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
   if (live) {
@@ -655,7 +655,8 @@ hipError_t attention_launch(CacheAttnArgs a, const Shape& shape, hipStream_t s) 
   constexpr int TEAMS = 256 / (HD / 4);
   a.teams = a.splits / 4 < 1 ? 1 : a.splits / 4 > TEAMS ? TEAMS : a.splits / 4;
   const int64_t items = a.rows.rows * a.heads, each = TEAMS / a.teams;
-  hipLaunchKernelGGL((cache_attention_join<T, HD>), dim3((unsigned)((items + each - 1) / each)), dim3(256), 0, s, a);
+  const int64_t blocks = (items + each - 1) / each, in_row = blocks < 1 << 20 ? blocks : 1 << 20;      // (a launch has less than 2^32 threads in a row)
+  hipLaunchKernelGGL((cache_attention_join<T, HD>), dim3((unsigned)in_row, (unsigned)((blocks + in_row - 1) / in_row)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -676,7 +677,8 @@ template <typename T, int HD>
 hipError_t append_launch(const AppendArgs& a, hipStream_t s) {
   int64_t n = a.rows.max_rows < a.rows.rows ? a.rows.max_rows : a.rows.rows;
   if (n < 1) n = 1;
-  const int64_t blocks = (n + 14) / kBlock + 1;        // n tokens touch that many at most
+  int64_t blocks = (n + 14) / kBlock + 1;              // n tokens touch that many at most
+  if (blocks > 1 << 20) blocks = 1 << 20;              // (and more in turn: a launch has less than 2^32 threads in a row)
   const int tasks = 2 * a.cache.heads + a.heads;
   const dim3 grid((unsigned)blocks, (unsigned)((tasks + 3) / 4), (unsigned)a.rows.batch);
   hipLaunchKernelGGL((cache_append<T, HD>), grid, dim3(256), 0, s, a);

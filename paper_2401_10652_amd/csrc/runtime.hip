@@ -2179,7 +2179,7 @@ int ac_op_linear_w4(const void* x, int64_t ldx, const void* w, int64_t ldw, cons
     return fail(AC_ERR_ARG, "ac_op_linear_w4: bad argument");
   if (group != 32 && group != 64 && group % 128 != 0)
     return fail(AC_ERR_UNSUPPORTED, "ac_op_linear_w4: groups of 32, 64 or a multiple of 128 columns");
-  if (m > 16 * 65535ll) return fail(AC_ERR_UNSUPPORTED, "ac_op_linear_w4: at most %lld rows", 16 * 65535ll);
+  if (m > 16 * 65535ll || n > 1 << 26) return fail(AC_ERR_UNSUPPORTED, "ac_op_linear_w4: at most %lld rows and 2^26 columns", 16 * 65535ll);
   if (ldw < ceil_div(k, 2)) return fail(AC_ERR_ARG, "ac_op_linear_w4: rows of codes overlap");
   if (ldw % 16 != 0 || (uintptr_t)w % 16 != 0) return fail(AC_ERR_ALIGN, "ac_op_linear_w4: rows of codes start at multiples of 16 bytes");
   return hip_status(launch_linear_w4(LinearW4Args{x, ldx, w, ldw, scale, lds, zero, ldz, divisor((uint32_t)group), bias, residual, ldr, out, ldo, m, n, k,

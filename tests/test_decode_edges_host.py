@@ -109,3 +109,38 @@ def test_decoder_asks_for_a_workspace_without_making_rows():
     assert model._workspace_bytes(1, rows) == B.ac_cache_attention_workspace_bytes(q, model.caches[0], rows) > 0
     rows = B.cache_rows(torch.zeros(2, **i32), torch.zeros(1, **i32), torch.zeros((1, 2048), **i32), 1 << 26, 65536)
     assert model._workspace_bytes(1 << 26, rows) == 0                 # (128 GiB of queries)
+
+
+def test_launches_of_the_largest_calls(tmp_path, monkeypatch):
+    """A launch has less than 2^32 threads along each side: the stub refuses others, as the runtime does."""
+    source = launch_stub.SOURCE
+    for old, new in (("__hipPushCallConfiguration(grid3 g, grid3 b, size_t lds, void* stream) { return 0; }",
+                      "__hipPushCallConfiguration(grid3 g, grid3 b, size_t lds, void* stream) { grid = g; block = b; return 0; }"),
+                     ("__hipPopCallConfiguration(grid3* g, grid3* b, size_t* lds, void** stream) { return 0; }",
+                      "__hipPopCallConfiguration(grid3* g, grid3* b, size_t* lds, void** stream) { *g = grid; *b = block; return 0; }"),
+                     ("  int i = 0;\n", "  int i = 0;\n  if ((unsigned long long)g.x * b.x >> 32 || g.y > 65535 || g.z > 65535) return error = 9;\n"),
+                     ("static int n_known", "static int error;\nstatic grid3 grid, block;\nstatic int n_known"),
+                     ("int hipGetLastError(void) { return 0; }", "int hipGetLastError(void) { int e = error; error = 0; return e; }")):
+        assert source.count(old) == 1
+        source = source.replace(old, new)
+    monkeypatch.setattr(launch_stub, "SOURCE", source)
+    launch_stub.run(launch_stub.build(str(tmp_path)), """
+N = 1 << 30
+def cache(d): return B.ac_kv_cache(k=X, v=Y, k_scale=W, v_scale=W + 4096, pages=1 << 24, stride_page=16 * d, stride_scale=1, page=16, heads=1, head_dim=d)
+def rows(batch, most, length): return B.ac_cache_rows(row_begin=X, length=Y, page_table=W, ld_page_table=1 << 26, batch=batch, max_rows=most, max_length=length)
+for d in (32, 256):
+    for batch, most in ((1, N), (2, N), (65535, 1 << 15)):
+        for dtype in (B.AC_BF16, B.AC_F32):
+            c, r = cache(d), rows(batch, most, N)
+            assert L.ac_op_cache_append(None, 0, None, 0, 0, X, d, Y, d, N, ctypes.byref(c), ctypes.byref(r), None, dtype, None) == 0, L.ac_last_error()
+            for most in (most, 1):                                 # few rows of a sequence, many of the matrices
+                r = rows(batch, most, N)
+                need = L.ac_cache_attention_workspace_bytes(N, 1, ctypes.byref(c), ctypes.byref(r), 1, dtype)
+                assert L.ac_op_cache_attention(X, d, Y, d, N, 1, ctypes.byref(c), ctypes.byref(r), 1, 0.1, W, need, dtype, None) == 0, L.ac_last_error()
+for m, n in ((1, 1 << 26), (16 * 65535, 1 << 26), (200, 1 << 26), (16 * 65535, 16)):
+    for dtype in (B.AC_BF16, B.AC_F32):
+        for group in (32, 128):
+            assert L.ac_op_linear_w4(X, 64, Y, 32, W, 2, None, 0, group, None, None, 0, W + 4096, 1 << 26, m, n, 64, 0, dtype, None) == 0, L.ac_last_error()
+assert L.ac_op_linear_w4(X, 64, Y, 32, W, 2, None, 0, 32, None, None, 0, W + 4096, 1 << 27, 1, (1 << 26) + 1, 64, 0, B.AC_BF16, None) == B.AC_ERR_UNSUPPORTED
+assert kernels()
+""")

@@ -2247,7 +2247,9 @@ int ac_op_cache_append(const void* q, int64_t ldq, void* q_out, int64_t ldqo, in
 
 uint64_t ac_cache_attention_workspace_bytes(int64_t n_rows, int heads, const ac_kv_cache* cache, const ac_cache_rows* rows, int causal,
                                             int dtype) {
-  if (cache_ok("ac_cache_attention_workspace_bytes", cache, rows, n_rows) || heads < 1 || heads % cache->heads != 0 || !dtype_ok(dtype)) return 0;
+  if (cache_ok("ac_cache_attention_workspace_bytes", cache, rows, n_rows) || heads < 1 || heads > 65536 || heads % cache->heads != 0 ||
+      n_rows * heads > 1 << 30 || !dtype_ok(dtype))
+    return 0;
   return cache_attention_workspace_bytes(heads, *cache, CacheRows{*rows, n_rows}, causal != 0, dtype);
 }
 

@@ -144,3 +144,15 @@ for m, n in ((1, 1 << 26), (16 * 65535, 1 << 26), (200, 1 << 26), (16 * 65535, 1
 assert L.ac_op_linear_w4(X, 64, Y, 32, W, 2, None, 0, 32, None, None, 0, W + 4096, 1 << 27, 1, (1 << 26) + 1, 64, 0, B.AC_BF16, None) == B.AC_ERR_UNSUPPORTED
 assert kernels()
 """)
+
+
+def test_workspace_of_calls_that_are_refused(tmp_path):
+    """Rows times heads past what a call takes: no size, as no launch could use it."""
+    launch_stub.run(launch_stub.build(str(tmp_path)), """
+c = B.ac_kv_cache(k=X, v=Y, k_scale=W, v_scale=W + 4096, pages=10, stride_page=64 * 64, stride_scale=4, page=64, heads=1, head_dim=64)
+for rows, heads in ((1 << 30, 64), (1 << 30, 2), (1 << 20, 1 << 11), (1 << 16, 1 << 17)):
+    for dtype in (B.AC_F32, B.AC_BF16):
+        r = B.ac_cache_rows(row_begin=X, length=Y, page_table=W, ld_page_table=1 << 14, batch=2, max_rows=rows, max_length=1 << 20)
+        assert L.ac_cache_attention_workspace_bytes(rows, heads, ctypes.byref(c), ctypes.byref(r), 1, dtype) == 0
+        assert L.ac_op_cache_attention(X, heads * 64, Y, heads * 64, rows, heads, ctypes.byref(c), ctypes.byref(r), 1, 0.1, W, 1 << 62, dtype, None) < 0
+""")

@@ -29,3 +29,11 @@ def pytest_collection_modifyitems(config, items):
     skip = pytest.mark.skip(reason="no GPU visible")
     for it in need_gpu:
         it.add_marker(skip)
+
+
+@pytest.fixture(autouse=True, scope="module")
+def _cycles_of_other_modules_are_gone():
+    """Tensors that an earlier module's tests left in reference cycles (a refusal's traceback holds its frame) are freed here, and not by chance while a test
+    reads how much memory is allocated."""
+    import gc
+    gc.collect()

@@ -335,8 +335,8 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
 // block g, with that block's two scales in one register each, and the probabilities of its 16 tokens in the order in which the cache
 // holds their values.  No code passes through LDS.  What bounds it is HBM: a step's values are on their way while its scores are computed, the next step's
 // keys while its values are multiplied, and page numbers are read two steps ahead.
-// One row over 65536 tokens, 16 heads of 128, 268 MB: 50 us (5.4 TB/s) and 5 for the join; 64 rows over up to 8190 tokens each, 32 heads on 8 of 128: 120 us and 5.  Small calls
-// are latency: lengths, page numbers, scales and keys come one after another, and the join is a launch more (33 tokens 5.5 us, eight times 5 rows over 2049 tokens 10.5).
+// One row over 65536 tokens, 16 heads of 128, 268 MB: 49 us (5.5 TB/s) and 5 for the join; 64 rows over up to 8190 tokens each, 32 heads on 8 of 128: 121 us and 5.  Small calls
+// are latency: lengths, page numbers, scales and keys come one after another, and the join is a launch more (33 tokens 5.5 us, eight times 5 rows over 2049 tokens 10.9).
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
   constexpr int NT = Terms<T>::kQuery, NP = Terms<T>::kProb, W16 = HD / 64, REST = HD % 64 / 32, DT = HD / 16;
@@ -601,18 +601,18 @@ __global__ void __launch_bounds__(256) cache_attention_join(CacheAttnArgs g) {
 struct Shape { bool prompt; int tiles, splits; };
 
 // Tiles of 128 read the keys once where tiles of 16 read them eight times, but take longer for each step of keys: they are taken where the call is large, by heads x rows
-// x tokens (us, 16 and 128 rows a tile).  Heads of 128: eight times 256 rows of 32 heads over 8192 tokens (5 * 10^8) 124 and 64; eight times 300 rows of 32 heads over 900 (7 * 10^7)
-// 120 and 74; four times 64 rows of 16 heads over 4096 (1.7 * 10^7) 35 and 29; 512 rows of 32 heads over 512 (8 * 10^6) 19 and 24; 128 rows of 16 heads over 2048 (4 * 10^6) 17 and
-// 22.  Heads of 64: 64 rows of 16 heads over 65536 (7 * 10^7) 71 and 59; 700 rows of 16 heads over 700 (8 * 10^6) 12 and 19.  32 rows a key head and fewer leave three quarters of a
-// large tile empty: eight times 8 rows of 32 heads over 8192 tokens 39 and 47.
+// x tokens (us, 16 and 128 rows a tile).  Heads of 128: eight times 256 rows of 32 heads on 8 over 8192 tokens (5 * 10^8) 752 and 302; eight times 300 rows of 32 heads on 8 over 900
+// (7 * 10^7) 127 and 73; four times 64 rows of 16 heads over 4096 (1.7 * 10^7) 37 and 34; 512 rows of 32 heads on 8 over 512 (8 * 10^6) 19 and 24; 128 rows of 16 heads over 2048 (4 * 10^6)
+// 18 and 22.  Heads of 64: 64 rows of 16 heads over 65536 (7 * 10^7) 77 and 59; 700 rows of 16 heads over 700 (8 * 10^6) 12 and 18.  32 rows a key head and fewer leave three quarters
+// of a large tile empty: eight times 8 rows of 32 heads on 8 over 8192 tokens 41 and 47.
 constexpr int kPromptRows = 32, kPromptWork = 1 << 24;
-// Runs of keys: as many as fill the chip's places, two blocks of 256 threads a CU (64k tokens, 16 heads of 64: 57 us, with twice as many 60) or one of 512, and, of
+// Runs of keys: as many as fill the chip's places, two blocks of 256 threads a CU (64k tokens, 16 heads of 128: 57 us, with twice as many 61) or one of 512, and, of
 // several sequences, none longer than kLongRun, so that sequences of all lengths, of which the host knows only the longest, keep the chip filled to the end (64
-// sequences of up to 8190 tokens, 8 key heads of 128: 127 us, with runs of 1024 131, of 4096 133).  Where a sequence has more than 32 rows of a key head, which are the many rows of
+// sequences of up to 8190 tokens, 8 key heads of 128: 131 us, with runs of 1024 135, of 4096 138).  Where a sequence has more than 32 rows of a key head, which are the many rows of
 // fp32, blocks are many as it is and parts large: then only up to two blocks a place (fp32, us, without this and with: two times 2048 rows of 16 heads of 128 over 8192 tokens 1549, behind
 // 136 MB of parts, and 1217 with none; eight times 64 rows of 16 heads on 4 over 8192 210 and 191; four times 40 rows of 16 heads of 64 over 16384 77 and 80).
-// A run has 256 keys at least: one row over 2400 tokens, 16 heads of 64, 8.4 us, with 128 9.2, with 512 9.6.  Up to 640 keys stay one run, as the second kernel costs
-// more than it saves: 300 tokens 6.0 us and, in two runs, 7.8, 600 tokens 7.5 and 8.3; 1200 tokens 12.0 and 8.3.
+// A run has 256 keys at least, a step of each wave: one row over 2400 tokens, 16 heads of 64, 8.5 us, with 512 9.9.  Up to 640 keys stay one run, as the second kernel costs
+// more than it saves: 300 tokens 6.3 us and, in two runs, 7.9, 600 tokens 7.9 and 8.4; 1200 tokens 10.9 and 8.5.
 constexpr int kMostSplits = 128, kLeastRun = 256, kWholeRun = 640, kLongRun = 2048, kPlaces = 512, kPromptPlaces = 256;
 Shape shape(int heads, const ac_kv_cache& c, const CacheRows& r, int dtype) {
   const int64_t rows_of = r.max_rows < r.rows ? r.max_rows : r.rows, rows = rows_of * (heads / c.heads);

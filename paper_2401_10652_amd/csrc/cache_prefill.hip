@@ -11,8 +11,9 @@
 // them, and nothing is rounded.  Probabilities are: to bf16, one term, with their sum taken before it, which puts outputs 0.0023 (in 2-norm) from 64 bits where their own rounding
 // has them at 0.0017.  With a second term, as where rows are few, half as many matrix instructions again: 2048 rows behind 14336 tokens 425 us for 281, heads of 64 254 for 196.
 //
-// 2048 rows behind 14336 tokens, 16 heads of 128: 280 us, 0.92 PFLOP/s, of 1.25 that a large library product reaches.  What is left is issued beside the matrix
-// instructions: 32 exponentials, their scaling and packing, and as many conversions of codes for every 32 of them.
+// 2048 rows behind 14336 tokens, 16 heads of 128: 280 us, 0.92 PFLOP/s, of 1.27 that a large library product reaches.  What is left is issued beside the matrix
+// instructions: 32 exponentials, their scaling and packing, and as many conversions of codes for every 32 of them.  The matrix cores are busy 37 % of the time, the vector units 58 %.  Heads of 128 spill 15
+// registers, 64 bytes a lane (of 96 two): half of the 16 MB that this call writes, 8 being the output.
 #include "cache.h"
 
 namespace ac {

@@ -320,9 +320,9 @@ hipError_t launch_rows(const LinearW4Args& g, hipStream_t s) {
 // steps, so that one has them brought to the cache for the others.  Codes become (code - zero) / 16 in bf16, exact for whole zeros; of
 // another the whole part goes there and the rest, which bf16 holds as well, times x is a second product.  A group's sum is scaled in fp32.  Scales and zeros of eight groups at a time lie in LDS, each wave's its own.
 //
-// 512 rows 6144 x 2048, 192 blocks: 28.8 us, 450 TFLOP/s; 4096 rows 8192 x 2048 211 us, 650 (zeros that are no whole numbers: 40 and 307).  A step of the eight waves takes 1.4 us: 0.4 of matrix instructions on a
+// 512 rows 6144 x 2048, 192 blocks: 28.8 us, 450 TFLOP/s; 4096 rows 8192 x 2048 208 us, 660 (zeros that are no whole numbers: 39 and 304).  A step of the eight waves takes 1.4 us: 0.4 of matrix instructions on a
 // SIMD, 0.5 to read x from LDS, and 0.7 to issue what converts codes and scales sums, which overlap in part.  With one step at a time and a barrier
-// after each 29.9 and 210.
+// after each a twentieth more.
 constexpr int kTileM = 128, kTileN = 128, kTileK = 64, kStages = 4;
 constexpr int kXBytes = kTileM * kTileK * 2;
 constexpr int kSetBytes = kStages * kXBytes + 4 * 2 * 1024;          // of a set of four waves: x, and two times eight groups' scales and zeros of each wave

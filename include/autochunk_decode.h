@@ -110,6 +110,19 @@ int ac_op_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, in
 uint64_t ac_cache_attention_workspace_bytes(int64_t n_rows, int heads, const ac_kv_cache* cache, const ac_cache_rows* rows, int causal,
                                             int dtype);
 
+/*
+ * The same through a sliding window: row r, at place p of its sequence, sees the tokens t <= p with p - t < window or t < sinks: the last `window` ones,
+ * itself among them, and the first `sinks` ones, which stay visible.  Places count from the sequence's first token however long it is, and rotations
+ * (ac_rotary) by place are those of the whole text.  Pages of which no row sees a token are not read: their numbers in the page table may
+ * name no memory, so that a sequence holds no more pages than its window and sinks need (ac_op_pages_update frees the others).  window and sinks: 0 to
+ * 2^30, else AC_ERR_ARG; with both 0 rows see nothing.  Work goes by what the rows see, and so do splits and workspace.
+ */
+int ac_op_cache_attention_window(const void* q, int64_t ldq, void* out, int64_t ldo, int64_t n_rows, int heads, const ac_kv_cache* cache,
+                                 const ac_cache_rows* rows, int64_t window, int64_t sinks, float scale, void* workspace, uint64_t workspace_bytes,
+                                 int dtype, void* stream);
+uint64_t ac_cache_attention_window_workspace_bytes(int64_t n_rows, int heads, const ac_kv_cache* cache, const ac_cache_rows* rows, int64_t window,
+                                                   int64_t sinks, int dtype);
+
 #ifdef __cplusplus
 }
 #endif

@@ -166,6 +166,9 @@ SIGNATURES = {
     "ac_op_cache_attention": (INT, [VP, I64, VP, I64, I64, INT, C.POINTER(ac_kv_cache), C.POINTER(ac_cache_rows), INT, F32, VP, U64,
                                     INT, VP]),
     "ac_cache_attention_workspace_bytes": (U64, [I64, INT, C.POINTER(ac_kv_cache), C.POINTER(ac_cache_rows), INT, INT]),
+    "ac_op_cache_attention_window": (INT, [VP, I64, VP, I64, I64, INT, C.POINTER(ac_kv_cache), C.POINTER(ac_cache_rows), I64, I64, F32, VP, U64,
+                                           INT, VP]),
+    "ac_cache_attention_window_workspace_bytes": (U64, [I64, INT, C.POINTER(ac_kv_cache), C.POINTER(ac_cache_rows), I64, I64, INT]),
     "ac_chunk_trace": (INT, [C.POINTER(ac_graph_node), INT, INT, INT, INT, INT, I32P, U8P, INTP]),
     "ac_chunk_search": (INT, [C.POINTER(ac_graph_node), INT, INT, INT, INT, C.POINTER(ac_chunk_candidate), I32P, U8P,
                               INT, INTP, INTP, INTP]),
@@ -638,6 +641,23 @@ def ac_op_cache_attention(q, out, cache, rows, causal=True, scale=None, workspac
     ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     _check(lib().ac_op_cache_attention(qp, ldq, op, ldo, n, width // d, C.byref(cache), C.byref(rows), int(causal),
                                        d ** -0.5 if scale is None else scale, ws, size, _dt(q), _stream()), "ac_op_cache_attention")
+
+
+def ac_cache_attention_window_workspace_bytes(q, cache, rows, window, sinks=0):
+    n, width = q.shape
+    return int(lib().ac_cache_attention_window_workspace_bytes(n, width // cache.head_dim, C.byref(cache), C.byref(rows), window, sinks, _dt(q)))
+
+
+def ac_op_cache_attention_window(q, out, cache, rows, window, sinks=0, scale=None, workspace=None):
+    """q, out [rows, heads * head_dim]: each row over the last `window` tokens up to its own and the first `sinks` ones."""
+    (n, width), d = q.shape, cache.head_dim
+    if width % d:
+        _bad("q", q, f"heads of {d} are wanted")
+    qp, ldq = _matrix(q, "q", q.dtype, n, width)
+    op, ldo = _matrix(out, "out", q.dtype, n, width)
+    ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _check(lib().ac_op_cache_attention_window(qp, ldq, op, ldo, n, width // d, C.byref(cache), C.byref(rows), window, sinks,
+                                              d ** -0.5 if scale is None else scale, ws, size, _dt(q), _stream()), "ac_op_cache_attention_window")
 
 
 # ---- helpers for callers (buffers only) ------------------------------------------------------

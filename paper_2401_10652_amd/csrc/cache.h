@@ -37,6 +37,7 @@ struct CacheAttnArgs {
   ac_kv_cache cache;
   CacheRows rows;
   int causal;
+  int window, sinks;                // of a windowed call
   float scale;                      // times log2 e
   Divisor group, blocks;            // query heads of a key head, blocks of a page
   int splits, least;                // runs of keys, and the fewest keys of one (a multiple of 256)
@@ -65,7 +66,25 @@ struct Sight {
   }
 };
 
+// What the rows of a tile read of a windowed call: the sinks' blocks and those from the first row's window on, numbered one after another.  Runs and steps
+// count these blocks (and 16 tokens for each); where windows reach the sinks nothing is left out, and they are the sequence's own.
+struct Reach {
+  int sinks, gap;                        // blocks with sinks, blocks left out behind them
+  // seen: tokens up to the last row's place; first: the first row's place
+  __device__ Reach(const CacheAttnArgs& g, int first, int seen) {
+    const int low = min(first - g.window + 1, seen), begin = low > 0 ? low / kBlock : 0;
+    sinks = (min(g.sinks, seen) + kBlock - 1) / kBlock;
+    gap = begin > sinks ? begin - sinks : 0;
+  }
+  __device__ int block(int b) const { return b < sinks ? b : b + gap; }
+};
+// The first n of 16 tokens, as bits; and those of the block at token `at` that a row at `place` sees, of `seen` tokens that there are up to it.
+__device__ __forceinline__ uint32_t first_of_16(int n) { return n <= 0 ? 0u : n >= 16 ? 0xffffu : (1u << n) - 1; }
+__device__ __forceinline__ uint32_t seen_of_block(const CacheAttnArgs& g, int at, int place, int seen) {
+  return first_of_16(seen - at) & (~first_of_16(place - g.window + 1 - at) | first_of_16(g.sinks - at));
+}
+
 // Rows in tiles of 128, for prompts: bf16, at least one page.
-hipError_t launch_cache_prefill(const CacheAttnArgs& a, int64_t tiles, hipStream_t s);
+hipError_t launch_cache_prefill(const CacheAttnArgs& a, int64_t tiles, bool windowed, hipStream_t s);
 
 }  // namespace ac

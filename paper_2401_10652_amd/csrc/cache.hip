@@ -337,7 +337,9 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
 // keys while its values are multiplied, and page numbers are read two steps ahead.
 // One row over 65536 tokens, 16 heads of 128, 268 MB: 49 us (5.5 TB/s) and 5 for the join; 64 rows over up to 8190 tokens each, 32 heads on 8 of 128: 121 us and 5.  Small calls
 // are latency: lengths, page numbers, scales and keys come one after another, and the join is a launch more (33 tokens 5.5 us, eight times 5 rows over 2049 tokens 10.9).
-template <typename T, int HD>
+//
+// WINDOWED: steps go over the blocks of a tile's Reach, the sinks' and then the window's; a lane has the tokens of its block that its row sees as bits.
+template <typename T, int HD, bool WINDOWED>
 __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
   constexpr int NT = Terms<T>::kQuery, NP = Terms<T>::kProb, W16 = HD / 64, REST = HD % 64 / 32, DT = HD / 16;
   constexpr int FR = HD / 32;                          // fragments of 32 of a row
@@ -358,16 +360,19 @@ __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
       fewest = sq.first + quotient(tile * 16, g.group) + 1;
     }
     if (seen < 0) seen = 0;
+    const Reach reach(g, WINDOWED ? sq.first + quotient(tile * 16, g.group) : 0, WINDOWED ? seen : 0);
+    if (WINDOWED) seen -= reach.gap * kBlock;
+    auto block_of = [&](int b) { return WINDOWED ? reach.block(b) : b; };
     const int len = run_length(seen, g.splits, g.least), k_lo = (int)blockIdx.x * len < seen ? blockIdx.x * len : seen;
     const int k_hi = seen - k_lo < len ? seen : k_lo + len;
 
     // page numbers of the step at key k0 (-1 behind the run's end), and where its codes lie
     auto number = [&](int k0, int block) {
       const int b = k0 / kBlock + block;
-      return b * kBlock < k_hi ? table[quotient(b, g.blocks)] : -1;
+      return b * kBlock < k_hi ? table[quotient(block_of(b), g.blocks)] : -1;
     };
     auto offset = [&](int k0, int block, int page, int64_t stride, int in_block) {
-      const int b = k0 / kBlock + block, in_page = b - quotient(b, g.blocks) * blocks;
+      const int b = block_of(k0 / kBlock + block), in_page = b - quotient(b, g.blocks) * blocks;
       return page >= 0 && page < g.cache.pages ? page * stride + in_page * in_block : (int64_t)-1;
     };
     u32x4 kw[4][W16 + 1];
@@ -385,7 +390,8 @@ __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
     int k0 = k_lo + wave * 64;
     int kp = number(k0, c16 / 4), vp = number(k0, quarter), kp2 = number(k0 + 256, c16 / 4), vp2 = number(k0 + 256, quarter);
     const int r = tile * 16 + c16, rr = r < sq.all ? r : sq.all - 1, rq = quotient(rr, g.group);
-    const int sees = r >= sq.all ? 0 : g.causal ? sq.first + rq + 1 : sq.held;       // a row sees the keys before this one
+    // a row sees the keys before this one (windowed, rows past the last are as the last: nothing of theirs is stored)
+    const int sees = WINDOWED ? min(sq.first + rq + 1, sq.held) : r >= sq.all ? 0 : g.causal ? sq.first + rq + 1 : sq.held;
     bf16x8 qf[FR][NT];
 #pragma unroll
     for (int f = 0; f < FR; ++f) {
@@ -423,16 +429,25 @@ __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
       load_keys(offset(k0 + 256, c16 / 4, kp2, g.cache.stride_page, kBlock * HD));
       kp = kp2; vp = vp2; kp2 = kp3; vp2 = vp3;
 
-      const int vb = (k0 / kBlock + quarter) * kBlock;
+      const int vb = block_of(k0 / kBlock + quarter) * kBlock;
       const int left = (va >= 0 ? sees : 0) - vb;        // of this lane's block, the tokens its row sees
+      const uint32_t bits = !WINDOWED || va < 0 ? 0u : seen_of_block(g, vb, sq.first + rq, sees);
+      const bool whole = WINDOWED && __all(bits == 0xffffu);           // every row sees every key
+      auto visible = [&](int e) { return WINDOWED ? (bits >> e & 1) != 0 : e < left; };
       float big = -INFINITY;
+      if (whole) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] *= ks;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[j][i] = visible(4 * j + i) ? s[j][i] * ks : -INFINITY;
+      }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[j][i] = 4 * j + i < left ? s[j][i] * ks : -INFINITY;
-          big = fmaxf(big, s[j][i]);
-        }
+        for (int i = 0; i < 4; ++i) big = fmaxf(big, s[j][i]);
       big = fmaxf(big, __shfl_xor(big, 16, 64));
       big = fmaxf(big, __shfl_xor(big, 32, 64));
       const float m_new = fmaxf(m, big), ref = m_new == -INFINITY ? 0.f : m_new;
@@ -456,7 +471,7 @@ __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] *= alpha;
       bool poisoned = false;                                         // whether a code that not every row sees is NaN
-      if (k0 + 64 > fewest) {
+      if (WINDOWED ? !whole : k0 + 64 > fewest) {
         uint32_t any = 0;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -486,7 +501,7 @@ __global__ void __launch_bounds__(256) cache_attention(CacheAttnArgs g) {
             const bf16x8 nf = codes_bf16(n0 & 0x38383838u, n1 & 0x38383838u);      // 0x38 is 1
             bf16x8 seen_f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) seen_f[e] = 8 * u + e < left ? (bf16_t)1.0f : (bf16_t)0.0f;
+            for (int e = 0; e < 8; ++e) seen_f[e] = visible(8 * u + e) ? (bf16_t)1.0f : (bf16_t)0.0f;
 #pragma unroll
             for (int x = NP - 1; x >= 0; --x) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[u][x], o[d], 0, 0, 0);
             count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf, seen_f, count, 0, 0, 0);
@@ -614,43 +629,53 @@ constexpr int kPromptRows = 32, kPromptWork = 1 << 24;
 // A run has 256 keys at least, a step of each wave: one row over 2400 tokens, 16 heads of 64, 8.5 us, with 512 9.9.  Up to 640 keys stay one run, as the second kernel costs
 // more than it saves: 300 tokens 6.3 us and, in two runs, 7.9, 600 tokens 7.9 and 8.4; 1200 tokens 10.9 and 8.5.
 constexpr int kMostSplits = 128, kLeastRun = 256, kWholeRun = 640, kLongRun = 2048, kPlaces = 512, kPromptPlaces = 256;
-Shape shape(int heads, const ac_kv_cache& c, const CacheRows& r, int dtype) {
+// tokens: the most that a row or a tile reads.
+Shape shape(int heads, const ac_kv_cache& c, const CacheRows& r, int64_t tokens, int dtype) {
   const int64_t rows_of = r.max_rows < r.rows ? r.max_rows : r.rows, rows = rows_of * (heads / c.heads);
   const int64_t all = rows_of < r.rows / (r.batch > 0 ? r.batch : 1) ? rows_of * r.batch : r.rows;
   Shape s;
-  s.prompt = dtype == AC_BF16 && c.pages > 0 && rows > kPromptRows && all * heads * (double)r.max_length >= kPromptWork;
+  s.prompt = dtype == AC_BF16 && c.pages > 0 && rows > kPromptRows && all * heads * (double)tokens >= kPromptWork;
   const int each = s.prompt ? 128 : 16;
   s.tiles = rows < 1 ? 1 : (int)((rows + each - 1) / each);
   const int64_t blocks = (int64_t)s.tiles * c.heads * r.batch;
   int64_t n = blocks > 0 ? (s.prompt ? kPromptPlaces : kPlaces) / blocks : 1;
   if (!s.prompt && r.batch > 1) {
-    int64_t runs = r.max_length / kLongRun;
+    int64_t runs = tokens / kLongRun;
     if (r.rows * (heads / c.heads) > kPromptRows * r.batch && runs > 2 * kPlaces / blocks) runs = 2 * kPlaces / blocks;
     if (n < runs) n = runs;
   }
-  const int64_t most = !s.prompt && r.max_length <= kWholeRun ? 1 : (r.max_length + kLeastRun - 1) / kLeastRun;
+  const int64_t most = !s.prompt && tokens <= kWholeRun ? 1 : (tokens + kLeastRun - 1) / kLeastRun;
   if (n > most) n = most;
   if (n > kMostSplits) n = kMostSplits;
   s.splits = n < 1 ? 1 : (int)n;
   return s;
 }
 
-template <typename T, int HD>
+// The most tokens of a windowed call's tile: the sinks' blocks, the first row's window with its first block, and the rows behind that one.
+int64_t window_tokens(int heads, const ac_kv_cache& c, const CacheRows& r, int window, int sinks) {
+  const int64_t rows_of = r.max_rows < r.rows ? r.max_rows : r.rows, group = heads / c.heads, tile = (128 + group - 1) / group + 1;
+  const int64_t n = (sinks + (int64_t)kBlock - 1) / kBlock * kBlock + window + kBlock + (rows_of < tile ? rows_of : tile);
+  return n < r.max_length ? n : r.max_length;
+}
+
+template <typename T, int HD, bool WINDOWED>
 hipError_t attention_rows_launch(const CacheAttnArgs& a, int tiles, hipStream_t s) {
   const int most = 65535 / a.cache.heads;
   if (tiles > most) tiles = most;
   const dim3 grid((unsigned)a.splits, (unsigned)(tiles * a.cache.heads), (unsigned)a.rows.batch);
   constexpr size_t lds = (size_t)(4 * 16 * (HD + 4) + 4 * 16 * 2 + 16 * 4) * sizeof(float);
-  static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(cache_attention<T, HD>),
+  static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(cache_attention<T, HD, WINDOWED>),
                                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (attr_status != hipSuccess) return attr_status;
-  hipLaunchKernelGGL((cache_attention<T, HD>), grid, dim3(256), lds, s, a);
+  hipLaunchKernelGGL((cache_attention<T, HD, WINDOWED>), grid, dim3(256), lds, s, a);
   return hipGetLastError();
 }
 
 template <typename T, int HD>
-hipError_t attention_launch(CacheAttnArgs a, const Shape& shape, hipStream_t s) {
-  const hipError_t e = shape.prompt ? launch_cache_prefill(a, shape.tiles, s) : attention_rows_launch<T, HD>(a, shape.tiles, s);
+hipError_t attention_launch(CacheAttnArgs a, const Shape& shape, bool windowed, hipStream_t s) {
+  const hipError_t e = shape.prompt ? launch_cache_prefill(a, shape.tiles, windowed, s)
+                       : windowed   ? attention_rows_launch<T, HD, true>(a, shape.tiles, s)
+                                    : attention_rows_launch<T, HD, false>(a, shape.tiles, s);
   if (e != hipSuccess || a.splits == 1) return e;
   constexpr int TEAMS = 256 / (HD / 4);
   a.teams = a.splits / 4 < 1 ? 1 : a.splits / 4 > TEAMS ? TEAMS : a.splits / 4;
@@ -661,14 +686,14 @@ hipError_t attention_launch(CacheAttnArgs a, const Shape& shape, hipStream_t s) 
 }
 
 template <typename T>
-hipError_t attention_width(const CacheAttnArgs& a, const Shape& shape, hipStream_t s) {
+hipError_t attention_width(const CacheAttnArgs& a, const Shape& shape, bool windowed, hipStream_t s) {
   switch (a.cache.head_dim) {
-    case 32: return attention_launch<T, 32>(a, shape, s);
-    case 64: return attention_launch<T, 64>(a, shape, s);
-    case 96: return attention_launch<T, 96>(a, shape, s);
-    case 128: return attention_launch<T, 128>(a, shape, s);
-    case 192: return attention_launch<T, 192>(a, shape, s);
-    case 256: return attention_launch<T, 256>(a, shape, s);
+    case 32: return attention_launch<T, 32>(a, shape, windowed, s);
+    case 64: return attention_launch<T, 64>(a, shape, windowed, s);
+    case 96: return attention_launch<T, 96>(a, shape, windowed, s);
+    case 128: return attention_launch<T, 128>(a, shape, windowed, s);
+    case 192: return attention_launch<T, 192>(a, shape, windowed, s);
+    case 256: return attention_launch<T, 256>(a, shape, windowed, s);
     default: return hipErrorNotSupported;
   }
 }
@@ -708,20 +733,20 @@ hipError_t launch_cache_append(const void* q, int64_t ldq, void* q_out, int64_t 
   return dtype == AC_BF16 ? append_width<bf16_t>(a, s) : append_width<float>(a, s);
 }
 
-uint64_t cache_attention_workspace_bytes(int heads, const ac_kv_cache& cache, const CacheRows& rows, int causal, int dtype) {
-  const int n = shape(heads, cache, rows, dtype).splits;
+uint64_t cache_attention_workspace_bytes(int heads, const ac_kv_cache& cache, const CacheRows& rows, const CacheSight& sight, int dtype) {
+  const int n = shape(heads, cache, rows, sight.windowed ? window_tokens(heads, cache, rows, sight.window, sight.sinks) : rows.max_length, dtype).splits;
   return n == 1 ? 0 : (uint64_t)n * rows.rows * heads * (cache.head_dim + 2) * sizeof(float);
 }
 
 hipError_t launch_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int heads, const ac_kv_cache& cache,
-                                  const CacheRows& rows, int causal, float scale, void* workspace, int dtype, hipStream_t s) {
+                                  const CacheRows& rows, const CacheSight& sight, float scale, void* workspace, int dtype, hipStream_t s) {
   if (rows.batch <= 0 || rows.rows <= 0) return hipSuccess;
-  const Shape sh = shape(heads, cache, rows, dtype);
+  const Shape sh = shape(heads, cache, rows, sight.windowed ? window_tokens(heads, cache, rows, sight.window, sight.sinks) : rows.max_length, dtype);
   const int n = sh.splits;
   float* parts = (float*)workspace;
-  CacheAttnArgs a{q, out, ldq, ldo, heads, cache, rows, causal, scale * kLog2e, divisor(heads / cache.heads), divisor(cache.page / kBlock),
-                  n, kLeastRun, parts, n > 1 ? parts + (uint64_t)n * rows.rows * heads * cache.head_dim : nullptr, 1};
-  return dtype == AC_BF16 ? attention_width<bf16_t>(a, sh, s) : attention_width<float>(a, sh, s);
+  CacheAttnArgs a{q, out, ldq, ldo, heads, cache, rows, sight.causal, sight.window, sight.sinks, scale * kLog2e, divisor(heads / cache.heads),
+                  divisor(cache.page / kBlock), n, kLeastRun, parts, n > 1 ? parts + (uint64_t)n * rows.rows * heads * cache.head_dim : nullptr, 1};
+  return dtype == AC_BF16 ? attention_width<bf16_t>(a, sh, sight.windowed, s) : attention_width<float>(a, sh, sight.windowed, s);
 }
 
 }  // namespace ac

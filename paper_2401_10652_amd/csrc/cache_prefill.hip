@@ -39,11 +39,12 @@ __device__ __forceinline__ bf16x8 scaled_bf16(uint32_t lo, uint32_t hi, float s)
 // Two waves of 256 registers share a SIMD where that is enough for the sums of a row, else one has it alone.
 template <int HD> constexpr int sides() { return HD <= 128 ? 2 : 1; }
 template <int HD> constexpr size_t lds_bytes() {
-  constexpr size_t ring = (size_t)sides<HD>() * (4 * kTile * HD + 64) + (HD + 1) * sizeof(int), join = sides<HD>() == 2 ? (size_t)kRowsOfBlock * (HD + 2) * sizeof(float) : 0;
+  constexpr size_t ring = (size_t)sides<HD>() * (4 * kTile * HD + 64) + 2 * (HD + 1) * sizeof(int), join = sides<HD>() == 2 ? (size_t)kRowsOfBlock * (HD + 2) * sizeof(float) : 0;
   return ring > join ? ring : join;
 }
 
-template <int HD>
+// WINDOWED: tiles of keys are made of the blocks of the block's Reach, the sinks' and then the window's; key numbers count these blocks.
+template <int HD, bool WINDOWED>
 __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(CacheAttnArgs g) {
   constexpr int TILE = kTile * HD, BLOCK = kBlock * HD, CHUNKS = TILE / 1024;   // bytes of a tile's keys or values and of a block; KB of the former
   constexpr int C = HD / 32, DT = HD / 32, SIDES = sides<HD>();
@@ -61,15 +62,23 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
   uint8_t* const ring = smem + side * 4 * TILE;        // two tiles of keys, two of values
   float* const scales = reinterpret_cast<float*>(smem + SIDES * 4 * TILE) + side * 16;
   int* const nan_at = reinterpret_cast<int*>(smem + SIDES * (4 * TILE + 64));    // of each element the first token with a NaN value; [HD]: of all
+  int* const nan_to = nan_at + HD + 1;                                           // (windowed) of each element the last
   const int k_block = lane >> 2 & 1, k_token = 4 * (l32 >> 3) + (lane & 3);      // what row l32 of a tile of 32 keys is
 
   for (int nth = blockIdx.y; nth < tiles; nth += gridDim.y) {
     const int tile = tiles - 1 - nth, row0 = tile * kRowsOfBlock + rowset * 32;
     // keys that the block's rows see at most; that this wave's see at most and at least
     auto sees_of = [&](int r) { return g.causal ? min(max(sq.first + quotient(min(r, sq.all - 1), g.group) + 1, 0), sq.held) : sq.held; };
-    const int seen = sees_of(tile * kRowsOfBlock + kRowsOfBlock - 1);
+    auto place_of_row = [&](int r) { return sq.first + quotient(min(r, sq.all - 1), g.group); };
+    const int tokens = sees_of(tile * kRowsOfBlock + kRowsOfBlock - 1);
+    const Reach reach(g, WINDOWED ? place_of_row(tile * kRowsOfBlock) : 0, WINDOWED ? tokens : 0);
+    const int gap = WINDOWED ? reach.gap * kBlock : 0, seen = tokens - gap;
+    auto block_of = [&](int b) { return WINDOWED ? reach.block(b) : b; };
     const bool active = row0 < sq.all;
-    const int wave_seen = active ? sees_of(row0 + 31) : 0, fewest = sees_of(row0);
+    const int wave_seen = active ? sees_of(row0 + 31) - gap : 0, fewest = sees_of(row0) - gap;
+    // windowed: keys before this one are hidden from some row of the wave (of the block), unless they are sinks
+    const int hidden = WINDOWED ? place_of_row(row0 + 31) - g.window + 1 - gap : 0, hidden_all = WINDOWED ? place_of_row(tile * kRowsOfBlock + kRowsOfBlock - 1) - g.window + 1 - gap : 0;
+    auto behind = [&](int key, int from) { return WINDOWED && key < from && key + kTile > g.sinks; };
     const int len = run_length(seen, g.splits, g.least), k_lo = min(split * len, seen), k_hi = min(k_lo + len, seen);
     const int steps = ((k_hi - k_lo + kTile - 1) / kTile + SIDES - 1) / SIDES;      // of a side
     const int r = row0 + l32, rr = min(r, sq.all - 1), rq = quotient(rr, g.group), head = kvh * group + rr - rq * group;
@@ -82,11 +91,11 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
     // block that is not there is read from the first page, and its scores are masked.
     auto number = [&](int step) __attribute__((always_inline)) {
       const int b = key_of(step) / kBlock + (lane & 3);
-      return b * kBlock < k_hi ? table[quotient(b, g.blocks)] : -1;
+      return b * kBlock < k_hi ? table[quotient(block_of(b), g.blocks)] : -1;
     };
     struct Place { int64_t codes, scale; int there; };     // bytes and floats from the key head's first; there: bit i, block i (the same for all lanes)
     auto place_of = [&](int step, int page) __attribute__((always_inline)) {
-      const int b = key_of(step) / kBlock + (lane & 3), in_page = b - quotient(b, g.blocks) * blocks;
+      const int b = block_of(key_of(step) / kBlock + (lane & 3)), in_page = b - quotient(b, g.blocks) * blocks;
       const bool have = (uint32_t)page < n_pages;
       const int64_t p = have ? page : 0, i = have ? in_page : 0;
       return Place{p * g.cache.stride_page + i * BLOCK, p * g.cache.stride_scale + i, (int)(__ballot(have) & 15)};
@@ -126,7 +135,7 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
     // This wave's loads have landed and its LDS reads are done, then every wave's.  In between, of the values of tile `step` if not every row of
     // the block sees all its keys: a NaN value times a probability of 0 is NaN, so each wave takes NaN values among those that it loaded as zeros and notes
     // the first token of each element that has one, for the end.
-    const int first_seen = sees_of(tile * kRowsOfBlock);
+    const int first_seen = sees_of(tile * kRowsOfBlock) - gap;
     auto landed = [&]() __attribute__((always_inline)) {
       asm volatile("" ::: "memory");
       __builtin_amdgcn_sched_barrier(0);
@@ -139,7 +148,7 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
     };
     auto arrived = [&](int step, int there) __attribute__((always_inline)) {
       landed();
-      if (key_of(step) < k_hi && (key_of(step) + kTile > first_seen || there != 15)) {
+      if (key_of(step) < k_hi && (key_of(step) + kTile > first_seen || there != 15 || behind(key_of(step), hidden_all))) {
         for (int n = 0; n < (CHUNKS + 3) / 4; ++n) {
           const int at = (n * 4 + rowset) * 1024 + lane * 16;
           if (CHUNKS % 4 != 0 && at >= TILE) break;
@@ -148,10 +157,12 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
           if ((x[0] | x[1] | x[2] | x[3]) != 0) {
             *mine = w & ~x;
             const int word = x[0] ? 0 : x[1] ? 1 : x[2] ? 2 : 3;
-            const int token = key_of(step) + at / BLOCK * kBlock + 4 * word + __builtin_ctz(x[0] ? x[0] : x[1] ? x[1] : x[2] ? x[2] : x[3]) / 8;
+            const int block = block_of(key_of(step) / kBlock + at / BLOCK);
+            const int token = block * kBlock + 4 * word + __builtin_ctz(x[0] ? x[0] : x[1] ? x[1] : x[2] ? x[2] : x[3]) / 8;
             if (there >> (at / BLOCK) & 1) {
               atomicMin(&nan_at[at % BLOCK / kBlock], token);
               atomicMin(&nan_at[HD], token);
+              if (WINDOWED) atomicMax(&nan_to[at % BLOCK / kBlock], block * kBlock + kBlock - 1);
             }
           }
         }
@@ -171,7 +182,10 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
     float m = -INFINITY, l = 0.f;
-    for (int e = threadIdx.x; e <= HD; e += blockDim.x) nan_at[e] = 0x7fffffff;
+    for (int e = threadIdx.x; e <= HD; e += blockDim.x) {
+      nan_at[e] = 0x7fffffff;
+      if (WINDOWED) nan_to[e] = -1;
+    }
 
     auto key_frag = [&](int step, int t, int c) __attribute__((always_inline)) {
       const uint8_t* at = ring + step % 2 * TILE + (2 * t + k_block) * BLOCK + k_token * HD;
@@ -190,11 +204,20 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
       const float s = scales[(step & 1) * 8 + 4 + 2 * t + half];
       return there >> (2 * t + half) & 1 ? s : 1.f;
     };
-    auto bounded = [&](int step, int there) { return key_of(step) + kTile > fewest || there != 15; };   // not every row sees every key
+    // not every row sees every key
+    auto bounded = [&](int step, int there) { return key_of(step) + kTile > fewest || there != 15 || behind(key_of(step), hidden); };
     auto mask = [&](f32x16 (&s)[2], int step, int there) __attribute__((always_inline)) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const int n = (there >> (2 * t + half) & 1 ? sees : 0) - key_of(step) - (2 * t + half) * kBlock;
+        const bool here = there >> (2 * t + half) & 1;
+        if (WINDOWED) {
+          const uint32_t bits = here ? seen_of_block(g, block_of(key_of(step) / kBlock + 2 * t + half) * kBlock, sq.first + rq, sees) : 0u;
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (!(bits >> i & 1)) s[t][i] = -INFINITY;
+          continue;
+        }
+        const int n = (here ? sees : 0) - key_of(step) - (2 * t + half) * kBlock;
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (i >= n) s[t][i] = -INFINITY;
@@ -320,13 +343,24 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
       if (step + 1 < steps) iteration(s_b, s_a, step + 1);
     }
 
-    // elements whose row sees a NaN value that was taken as zero
+    // elements whose row sees a NaN value that was taken as zero (windowed: first and last such token do not say whether one is in a row's window, so
+    // what lies between them is looked through)
+    auto meets_nan = [&](int e) {
+      const int from = nan_at[e], to = min(nan_to[e], sees - 1), low = sq.first + rq - g.window + 1;
+      for (int t = from; t <= to; ++t) {
+        if (t >= g.sinks && t < low) { t = low - 1; continue; }
+        const int b = t / kBlock, nth = quotient(b, g.blocks);
+        const uint32_t page = (uint32_t)table[nth];
+        if (page < n_pages && (vbase[page * g.cache.stride_page + (int64_t)(b - nth * blocks) * BLOCK + e * kBlock + t % kBlock] & 0x7f) == 0x7f) return true;
+      }
+      return false;
+    };
     if (nan_at[HD] != 0x7fffffff) {
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (nan_at[d * 32 + 8 * (i / 4) + 4 * half + i % 4] < sees) o[d][i] = __builtin_nanf("");
+          if (WINDOWED ? meets_nan(d * 32 + 8 * (i / 4) + 4 * half + i % 4) : nan_at[d * 32 + 8 * (i / 4) + 4 * half + i % 4] < sees) o[d][i] = __builtin_nanf("");
     }
 
     // the second half of the keys to LDS (pieces of four elements turned by the row, against bank conflicts), the first joins
@@ -377,27 +411,32 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
   }
 }
 
-template <int HD>
+template <int HD, bool WINDOWED>
 hipError_t prefill_launch(const CacheAttnArgs& a, int64_t tiles, hipStream_t s) {
   constexpr size_t lds = lds_bytes<HD>();
-  static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(cache_prefill<HD>),
+  static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(cache_prefill<HD, WINDOWED>),
                                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (attr_status != hipSuccess) return attr_status;
   const dim3 grid((unsigned)(a.splits * a.cache.heads), (unsigned)(tiles < 65535 ? tiles : 65535), (unsigned)a.rows.batch);
-  hipLaunchKernelGGL((cache_prefill<HD>), grid, dim3(256 * sides<HD>()), lds, s, a);
+  hipLaunchKernelGGL((cache_prefill<HD, WINDOWED>), grid, dim3(256 * sides<HD>()), lds, s, a);
   return hipGetLastError();
+}
+
+template <int HD>
+hipError_t prefill_width(const CacheAttnArgs& a, int64_t tiles, bool windowed, hipStream_t s) {
+  return windowed ? prefill_launch<HD, true>(a, tiles, s) : prefill_launch<HD, false>(a, tiles, s);
 }
 
 }  // namespace
 
-hipError_t launch_cache_prefill(const CacheAttnArgs& a, int64_t tiles, hipStream_t s) {
+hipError_t launch_cache_prefill(const CacheAttnArgs& a, int64_t tiles, bool windowed, hipStream_t s) {
   switch (a.cache.head_dim) {
-    case 32: return prefill_launch<32>(a, tiles, s);
-    case 64: return prefill_launch<64>(a, tiles, s);
-    case 96: return prefill_launch<96>(a, tiles, s);
-    case 128: return prefill_launch<128>(a, tiles, s);
-    case 192: return prefill_launch<192>(a, tiles, s);
-    case 256: return prefill_launch<256>(a, tiles, s);
+    case 32: return prefill_width<32>(a, tiles, windowed, s);
+    case 64: return prefill_width<64>(a, tiles, windowed, s);
+    case 96: return prefill_width<96>(a, tiles, windowed, s);
+    case 128: return prefill_width<128>(a, tiles, windowed, s);
+    case 192: return prefill_width<192>(a, tiles, windowed, s);
+    case 256: return prefill_width<256>(a, tiles, windowed, s);
     default: return hipErrorNotSupported;
   }
 }

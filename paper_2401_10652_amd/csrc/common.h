@@ -377,9 +377,10 @@ struct CacheRows : ac_cache_rows { int64_t rows; };   // with the rows of the ca
 hipError_t launch_cache_append(const void* q, int64_t ldq, void* q_out, int64_t ldqo, int heads, const void* k, int64_t ldk, const void* v,
                                int64_t ldv, const ac_kv_cache& cache, const CacheRows& rows, const ac_rotary* rotary, int dtype,
                                hipStream_t s);
+struct CacheSight { int causal, windowed, window, sinks; };   // what a row sees; windowed: causal too
 hipError_t launch_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int heads, const ac_kv_cache& cache,
-                                  const CacheRows& rows, int causal, float scale, void* workspace, int dtype, hipStream_t s);
-uint64_t cache_attention_workspace_bytes(int heads, const ac_kv_cache& cache, const CacheRows& rows, int causal, int dtype);
+                                  const CacheRows& rows, const CacheSight& sight, float scale, void* workspace, int dtype, hipStream_t s);
+uint64_t cache_attention_workspace_bytes(int heads, const ac_kv_cache& cache, const CacheRows& rows, const CacheSight& sight, int dtype);
 
 // hipErrorInvalidValue-style refusal with a message for ac_last_error().
 void set_error(const char* fmt, ...);

@@ -2245,18 +2245,15 @@ int ac_op_cache_append(const void* q, int64_t ldq, void* q_out, int64_t ldqo, in
                     "cache_append");
 }
 
-uint64_t ac_cache_attention_workspace_bytes(int64_t n_rows, int heads, const ac_kv_cache* cache, const ac_cache_rows* rows, int causal,
-                                            int dtype) {
-  if (cache_ok("ac_cache_attention_workspace_bytes", cache, rows, n_rows) || heads < 1 || heads > 65536 || heads % cache->heads != 0 ||
-      n_rows * heads > 1 << 30 || !dtype_ok(dtype))
+// The attention over a cache, causal or not or through a window.
+static uint64_t cache_attention_bytes(const char* what, int64_t n_rows, int heads, const ac_kv_cache* cache, const ac_cache_rows* rows, const CacheSight& sight,
+                                      int dtype) {
+  if (cache_ok(what, cache, rows, n_rows) || heads < 1 || heads > 65536 || heads % cache->heads != 0 || n_rows * heads > 1 << 30 || !dtype_ok(dtype))
     return 0;
-  return cache_attention_workspace_bytes(heads, *cache, CacheRows{*rows, n_rows}, causal != 0, dtype);
+  return cache_attention_workspace_bytes(heads, *cache, CacheRows{*rows, n_rows}, sight, dtype);
 }
-
-int ac_op_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int64_t n_rows, int heads, const ac_kv_cache* cache,
-                          const ac_cache_rows* rows, int causal, float scale, void* workspace, uint64_t workspace_bytes, int dtype,
-                          void* stream) {
-  const char* const what = "ac_op_cache_attention";
+static int cache_attention(const char* what, const void* q, int64_t ldq, void* out, int64_t ldo, int64_t n_rows, int heads, const ac_kv_cache* cache,
+                           const ac_cache_rows* rows, const CacheSight& sight, float scale, void* workspace, uint64_t workspace_bytes, int dtype, void* stream) {
   if (const int st = cache_ok(what, cache, rows, n_rows)) return st;
   if (n_rows == 0 || rows->batch == 0) return AC_OK;
   if (!q || !out || heads < 1 || heads > 65536 || heads % cache->heads != 0 || ldq < (int64_t)heads * cache->head_dim ||
@@ -2266,11 +2263,39 @@ int ac_op_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, in
   if (!rows_on(q, ldq, 16, dtype) || !rows_on(out, ldo, 16, dtype))
     return fail(AC_ERR_ALIGN, "%s: rows start at multiples of 16 bytes", what);
   const CacheRows all{*rows, n_rows};
-  const uint64_t need = cache_attention_workspace_bytes(heads, *cache, all, causal != 0, dtype);
+  const uint64_t need = cache_attention_workspace_bytes(heads, *cache, all, sight, dtype);
   if (need > 0 && (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0))
     return fail(AC_ERR_WORKSPACE, "%s: workspace of %llu bytes, %llu needed", what, (unsigned long long)workspace_bytes, (unsigned long long)need);
-  return hip_status(launch_cache_attention(q, ldq, out, ldo, heads, *cache, all, causal != 0, scale, workspace, dtype, (hipStream_t)stream),
-                    "cache_attention");
+  return hip_status(launch_cache_attention(q, ldq, out, ldo, heads, *cache, all, sight, scale, workspace, dtype, (hipStream_t)stream), what + 6);
+}
+
+uint64_t ac_cache_attention_workspace_bytes(int64_t n_rows, int heads, const ac_kv_cache* cache, const ac_cache_rows* rows, int causal,
+                                            int dtype) {
+  return cache_attention_bytes("ac_cache_attention_workspace_bytes", n_rows, heads, cache, rows, CacheSight{causal != 0, 0, 0, 0}, dtype);
+}
+
+int ac_op_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int64_t n_rows, int heads, const ac_kv_cache* cache,
+                          const ac_cache_rows* rows, int causal, float scale, void* workspace, uint64_t workspace_bytes, int dtype,
+                          void* stream) {
+  return cache_attention("ac_op_cache_attention", q, ldq, out, ldo, n_rows, heads, cache, rows, CacheSight{causal != 0, 0, 0, 0}, scale, workspace,
+                         workspace_bytes, dtype, stream);
+}
+
+static bool window_ok(int64_t window, int64_t sinks) { return window >= 0 && sinks >= 0 && window <= 1 << 30 && sinks <= 1 << 30; }
+
+uint64_t ac_cache_attention_window_workspace_bytes(int64_t n_rows, int heads, const ac_kv_cache* cache, const ac_cache_rows* rows, int64_t window,
+                                                   int64_t sinks, int dtype) {
+  return window_ok(window, sinks) ? cache_attention_bytes("ac_cache_attention_window_workspace_bytes", n_rows, heads, cache, rows,
+                                                          CacheSight{1, 1, (int)window, (int)sinks}, dtype) : 0;
+}
+
+int ac_op_cache_attention_window(const void* q, int64_t ldq, void* out, int64_t ldo, int64_t n_rows, int heads, const ac_kv_cache* cache,
+                                 const ac_cache_rows* rows, int64_t window, int64_t sinks, float scale, void* workspace, uint64_t workspace_bytes,
+                                 int dtype, void* stream) {
+  const char* const what = "ac_op_cache_attention_window";
+  if (!window_ok(window, sinks)) return fail(AC_ERR_ARG, "%s: windows and sinks of 0 to 2^30 tokens", what);
+  return cache_attention(what, q, ldq, out, ldo, n_rows, heads, cache, rows, CacheSight{1, 1, (int)window, (int)sinks}, scale, workspace, workspace_bytes,
+                         dtype, stream);
 }
 
 }  // extern "C"

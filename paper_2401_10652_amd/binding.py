@@ -98,6 +98,11 @@ class ac_rotary(C.Structure):
                 ("axes", C.c_int32), ("section", C.c_int32 * 4)]
 
 
+class ac_page_books(C.Structure):
+    _fields_ = [("uses", C.c_void_p), ("page_table", C.c_void_p), ("pages", C.c_int64), ("ld_page_table", C.c_int64), ("batch", C.c_int64),
+                ("page", C.c_int32)]
+
+
 AC_GRAPH_MAX_RANK, AC_GRAPH_MAX_INPUTS = 6, 3
 (AC_OP_INPUT, AC_OP_PARAM, AC_OP_LINEAR, AC_OP_MATMUL_NT, AC_OP_MATMUL_NN, AC_OP_ELEMENTWISE, AC_OP_NORM_LAST,
  AC_OP_SOFTMAX_LAST, AC_OP_TRANSPOSE, AC_OP_SPLIT_DIM, AC_OP_MERGE_DIMS, AC_OP_SLICE_LAST, AC_OP_CONTRACT_IKC_JKC,
@@ -169,6 +174,11 @@ SIGNATURES = {
     "ac_op_cache_attention_window": (INT, [VP, I64, VP, I64, I64, INT, C.POINTER(ac_kv_cache), C.POINTER(ac_cache_rows), I64, I64, F32, VP, U64,
                                            INT, VP]),
     "ac_cache_attention_window_workspace_bytes": (U64, [I64, INT, C.POINTER(ac_kv_cache), C.POINTER(ac_cache_rows), I64, I64, INT]),
+    "ac_pages_workspace_bytes": (U64, [C.POINTER(ac_page_books)]),
+    "ac_op_pages_update": (INT, [C.POINTER(ac_page_books), C.POINTER(ac_page_books), VP, VP, VP, VP, VP, VP, U64, VP]),
+    "ac_op_cache_fork": (INT, [C.POINTER(ac_kv_cache), INT, C.POINTER(ac_page_books), C.POINTER(ac_page_books), VP, VP, VP, VP, VP, U64, VP]),
+    "ac_op_cache_compact": (INT, [C.POINTER(ac_kv_cache), INT, C.POINTER(ac_page_books), C.POINTER(ac_page_books), VP, VP, U64, VP]),
+    "ac_op_cache_copy_pages": (INT, [C.POINTER(ac_kv_cache), INT, VP, VP, VP, I64, VP]),
     "ac_chunk_trace": (INT, [C.POINTER(ac_graph_node), INT, INT, INT, INT, INT, I32P, U8P, INTP]),
     "ac_chunk_search": (INT, [C.POINTER(ac_graph_node), INT, INT, INT, INT, C.POINTER(ac_chunk_candidate), I32P, U8P,
                               INT, INTP, INTP, INTP]),
@@ -658,6 +668,77 @@ def ac_op_cache_attention_window(q, out, cache, rows, window, sinks=0, scale=Non
     ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     _check(lib().ac_op_cache_attention_window(qp, ldq, op, ldo, n, width // d, C.byref(cache), C.byref(rows), window, sinks,
                                               d ** -0.5 if scale is None else scale, ws, size, _dt(q), _stream()), "ac_op_cache_attention_window")
+
+
+# ---- pages ------------------------------------------------------------------------------------
+
+def _ints(t, what, *shape):
+    """The address of a contiguous int32 tensor of this shape; None of None."""
+    if t is None:
+        return None
+    if _INT32 is None:
+        import torch
+        globals()["_INT32"] = torch.int32
+    if t.dtype is not _INT32:
+        raise TypeError(f"{what} is {t.dtype}, not int32")
+    if t.shape != shape or not t.is_contiguous():
+        _bad(what, t, f"{shape}, contiguous, is wanted")
+    return t.data_ptr()
+
+
+_INT32 = None
+
+
+def kv_caches(caches):
+    """The layers' caches (kv_cache) for calls that go over all of them.  Keeps them alive."""
+    array = (ac_kv_cache * len(caches))(*caches)
+    array.keep = list(caches)
+    return array
+
+
+def page_books(uses, page_table, page) -> ac_page_books:
+    """uses int32 [pages], page_table int32 [batch, places of a sequence], on the device, of pages of `page` tokens.  Keeps the tensors alive."""
+    (pages,), (batch, places) = uses.shape, page_table.shape
+    b = ac_page_books(_ints(uses, "uses", pages), _ints(page_table, "page_table", batch, places), pages, places, batch, page)
+    b.keep = (uses, page_table)
+    return b
+
+
+def ac_pages_workspace_bytes(books):
+    return int(lib().ac_pages_workspace_bytes(C.byref(books)))
+
+
+def _space(workspace):
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def ac_op_pages_update(books, out, workspace, drop=None, take=None, missing=None):
+    """drop, take: (begin, end), each int32 [batch], of tokens; out may be books; missing int32 [1]."""
+    n = books.batch
+    db, de = (None, None) if drop is None else (_ints(t, "drop", n) for t in drop)
+    tb, te = (None, None) if take is None else (_ints(t, "take", n) for t in take)
+    _check(lib().ac_op_pages_update(C.byref(books), C.byref(out), db, de, tb, te, _ints(missing, "missing", 1), *_space(workspace), _stream()),
+           "ac_op_pages_update")
+
+
+def ac_op_cache_fork(caches, books, out, parent, length, length_out, workspace, missing=None):
+    """caches: kv_caches; parent, length, length_out int32 [batch]; out's table and length_out are not those of books."""
+    n = books.batch
+    _check(lib().ac_op_cache_fork(caches, len(caches), C.byref(books), C.byref(out), _ints(parent, "parent", n), _ints(length, "length", n),
+                                  _ints(length_out, "length_out", n), _ints(missing, "missing", 1), *_space(workspace), _stream()), "ac_op_cache_fork")
+
+
+def ac_op_cache_compact(caches, books, out, workspace, used=None):
+    """caches: kv_caches; out may be books; used int32 [1]."""
+    _check(lib().ac_op_cache_compact(caches, len(caches), C.byref(books), C.byref(out), _ints(used, "used", 1), *_space(workspace), _stream()),
+           "ac_op_cache_compact")
+
+
+def ac_op_cache_copy_pages(caches, source, target, tokens=None):
+    """caches: kv_caches; source, target (and tokens) int32 [n]."""
+    n = source.shape[0]
+    _check(lib().ac_op_cache_copy_pages(caches, len(caches), _ints(source, "source", n), _ints(target, "target", n), _ints(tokens, "tokens", n), n,
+                                        _stream()), "ac_op_cache_copy_pages")
 
 
 # ---- helpers for callers (buffers only) ------------------------------------------------------

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "../../include/autochunk_decode.h"
+#include "../../include/autochunk_pages.h"
 #include "../../include/autochunk_rt.h"
 
 namespace ac {
@@ -381,6 +382,17 @@ struct CacheSight { int causal, windowed, window, sinks; };   // what a row sees
 hipError_t launch_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int heads, const ac_kv_cache& cache,
                                   const CacheRows& rows, const CacheSight& sight, float scale, void* workspace, int dtype, hipStream_t s);
 uint64_t cache_attention_workspace_bytes(int heads, const ac_kv_cache& cache, const CacheRows& rows, const CacheSight& sight, int dtype);
+
+// The books of a cache's pages: see autochunk_pages.h.
+uint64_t pages_workspace_bytes(const ac_page_books& books);
+hipError_t launch_pages_update(const ac_page_books& from, const ac_page_books& to, const int32_t* drop_begin, const int32_t* drop_end, const int32_t* take_begin,
+                               const int32_t* take_end, int32_t* missing, void* workspace, hipStream_t s);
+hipError_t launch_cache_fork(const ac_kv_cache* caches, int n_caches, const ac_page_books& from, const ac_page_books& to, const int32_t* parent,
+                             const int32_t* length, int32_t* length_to, int32_t* missing, void* workspace, hipStream_t s);
+hipError_t launch_cache_compact(const ac_kv_cache* caches, int n_caches, const ac_page_books& from, const ac_page_books& to, int32_t* used, void* workspace,
+                                hipStream_t s);
+hipError_t launch_cache_copy_pages(const ac_kv_cache* caches, int n_caches, const int32_t* source, const int32_t* target, const int32_t* tokens, int64_t n,
+                                   hipStream_t s);
 
 // hipErrorInvalidValue-style refusal with a message for ac_last_error().
 void set_error(const char* fmt, ...);

@@ -1,0 +1,456 @@
+// The books of a paged cache: pages freed and taken, sequences that go on as others, pages moved to the front, and the copies that follow.
+//
+// Free pages are taken by number, the lowest first, and places that want one stand in the order of the table, so that what a call leaves does not depend on
+// which thread came first: numbers of free pages and of wants are counted before them (prefix sums), and a want's rank finds the page of that rank.  uses is
+// changed by integer atomics, whose order does not matter.  Pages are copied by one kernel, 16 bytes a lane.
+#include "common.h"
+
+namespace ac {
+
+namespace {
+
+constexpr int kChunk = 4096, kEach = kChunk / 256;      // pages that a block counts, and a thread of it
+constexpr int kBlockTokens = 16;
+
+struct PagesArgs {
+  const int32_t* uses_from; const int32_t* table_from;
+  int32_t* uses; int32_t* table;
+  int pages, page, batch, chunks;
+  int64_t places;
+  const int32_t *drop_begin, *drop_end, *take_begin, *take_end;     // update
+  const int32_t *parent, *length; int32_t* length_to;               // fork
+  int32_t* count;                                                   // missing or used, or null
+  int32_t *total, *need, *counts, *list, *source, *target, *tokens; // workspace: [0] pages of the list, [1] wants; need [batch]; counts [chunks]; the others [pages] or [batch]
+};
+
+__device__ __forceinline__ bool names(const PagesArgs& g, int e) { return (uint32_t)e < (uint32_t)g.pages; }
+__device__ __forceinline__ int uses_now(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }   // (behind atomics of other lanes)
+__device__ __forceinline__ void add_use(const PagesArgs& g, int e, int n) {
+  if (names(g, e)) __hip_atomic_fetch_add(g.uses + e, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Sum over the block's threads before this one; `sum`: over all of them.  n waves.
+template <int WAVES>
+__device__ __forceinline__ int sum_before(int v, int* of_wave, int& sum) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int y = __shfl_up(x, o, kWave);
+    if (lane >= o) x += y;
+  }
+  if (lane == kWave - 1) of_wave[wave] = x;
+  __syncthreads();
+  int before = 0;
+  sum = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    before += w < wave ? of_wave[w] : 0;
+    sum += of_wave[w];
+  }
+  __syncthreads();
+  return before + x - v;
+}
+
+// ---- rows of the table, a wave each ------------------------------------------------------------------------------------
+
+struct Range { int64_t from, to; };     // places
+__device__ __forceinline__ Range places_in(const PagesArgs& g, const int32_t* begin, const int32_t* end, int b, bool whole) {
+  if (!begin) return Range{0, 0};
+  const int64_t lo = begin[b] > 0 ? begin[b] : 0, hi = end[b] > 0 ? end[b] : 0;
+  if (hi <= lo) return Range{0, 0};
+  Range r = whole ? Range{(lo + g.page - 1) / g.page, hi / g.page} : Range{lo / g.page, (hi + g.page - 1) / g.page};
+  if (r.to > g.places) r.to = g.places;
+  return r;
+}
+
+// Frees what row b drops; the number of its places that want a page.
+__device__ __forceinline__ int update_row(const PagesArgs& g, int b, int lane) {
+  const int32_t* from = g.table_from + b * g.places;
+  int32_t* to = g.table + b * g.places;
+  const Range drop = places_in(g, g.drop_begin, g.drop_end, b, true), take = places_in(g, g.take_begin, g.take_end, b, false);
+  const bool apart = from != to;
+  const int64_t end = apart ? g.places : drop.to;
+  int wants = 0;
+  for (int64_t i = (apart ? 0 : drop.from) + lane; i < end; i += kWave) {
+    int e = from[i];
+    if (i >= drop.from && i < drop.to && names(g, e)) {
+      add_use(g, e, -1);
+      e = -1;
+      if (!apart) to[i] = e;
+    }
+    if (apart) to[i] = e;
+  }
+  // (in place a dropped entry may or may not be seen as it was: it wants a page either way)
+  for (int64_t i = take.from + lane; i < take.to; i += kWave) wants += !names(g, from[i]) || (i >= drop.from && i < drop.to);
+#pragma unroll
+  for (int o = kWave / 2; o > 0; o >>= 1) wants += __shfl_xor(wants, o, kWave);
+  return wants;
+}
+
+// Gives row b's places their pages, the first of them that of rank `rank`.
+__device__ __forceinline__ void give_row(const PagesArgs& g, int b, int lane, int rank) {
+  const int32_t* from = g.table_from + b * g.places;
+  int32_t* to = g.table + b * g.places;
+  const Range drop = places_in(g, g.drop_begin, g.drop_end, b, true), take = places_in(g, g.take_begin, g.take_end, b, false);
+  const int have = uses_now(g.total);
+  for (int64_t i0 = take.from; i0 < take.to; i0 += kWave) {
+    const int64_t i = i0 + lane;
+    const bool wants = i < take.to && (!names(g, from[i]) || (i >= drop.from && i < drop.to));
+    const uint64_t all = __ballot(wants);
+    const int mine = rank + __popcll(all & ((1ull << lane) - 1));
+    if (wants) {
+      const int e = mine < have ? uses_now(g.list + mine) : -1;
+      to[i] = e;
+      if (e >= 0) g.uses[e] = 1;
+    }
+    rank += __popcll(all);
+  }
+}
+
+// Row j goes on as its parent; whether it wants a page for a copy of the partly filled one.
+__device__ __forceinline__ int fork_row(const PagesArgs& g, int j, int lane) {
+  const int p = g.parent[j];
+  const bool none = (uint32_t)p >= (uint32_t)g.batch;
+  bool first = true;
+  if (!none) {
+    for (int i = lane; __any(i < j) && first; i += kWave) first = !__any(i < j && g.parent[i] == p);
+  }
+  const int length = none ? 0 : max(g.length[p], 0), rest = length % g.page;
+  const int64_t whole = length / g.page;
+  const int32_t* old = g.table_from + j * g.places;
+  const int32_t* from = g.table_from + (none ? 0 : p) * g.places;
+  int32_t* to = g.table + j * g.places;
+  for (int64_t i = lane; i < g.places; i += kWave) {
+    const int o = old[i], n = !none && (i < whole || first) ? from[i] : -1;
+    if (n != o) {
+      add_use(g, o, -1);
+      add_use(g, n, 1);
+    }
+    to[i] = n;
+  }
+  const int source = !none && !first && rest > 0 && whole < g.places ? from[whole] : -1;
+  const bool wants = names(g, source);
+  if (lane == 0) {
+    g.length_to[j] = length;
+    g.source[j] = source;
+    g.tokens[j] = rest;
+  }
+  return wants;
+}
+__device__ __forceinline__ void give_copy(const PagesArgs& g, int j, int rank) {
+  const int source = uses_now(g.source + j);
+  int target = -1;
+  if (names(g, source)) {
+    if (rank < uses_now(g.total)) target = uses_now(g.list + rank);
+    const int32_t length = max(g.length[g.parent[j]], 0);
+    g.table[j * g.places + length / g.page] = target;
+    if (target >= 0) g.uses[target] = 1;
+  }
+  g.target[j] = target;
+}
+
+// ---- pages, a chunk a block ------------------------------------------------------------------------------------------------
+
+enum { FREE, USED };
+__device__ __forceinline__ int count_chunk(const int32_t* uses, int pages, int first, int kind) {
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) n += first + i < pages && (uses[first + i] > 0) == (kind == USED);
+  return n;
+}
+
+__global__ void __launch_bounds__(256) pages_copy_uses(PagesArgs g) {
+  for (int p = blockIdx.x * 256 + threadIdx.x; p < g.pages; p += gridDim.x * 256) g.uses[p] = g.uses_from[p];
+}
+
+template <bool FORK>
+__global__ void __launch_bounds__(256) pages_rows(PagesArgs g) {
+  const int lane = threadIdx.x % kWave, b = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / kWave);
+  if (!FORK && !g.take_begin && b == 0 && lane == 0 && g.count) *g.count = 0;
+  if (b >= g.batch) return;
+  const int wants = FORK ? fork_row(g, b, lane) : update_row(g, b, lane);
+  if (lane == 0) g.need[b] = wants;
+}
+
+// Free pages of each chunk; the last block: the wants before each row.
+__global__ void __launch_bounds__(256) pages_count(PagesArgs g) {
+  __shared__ int of_wave[4];
+  int sum;
+  if ((int)blockIdx.x < g.chunks) {
+    sum_before<4>(count_chunk(g.uses, g.pages, blockIdx.x * kChunk + threadIdx.x * kEach, FREE), of_wave, sum);
+    if (threadIdx.x == 0) g.counts[blockIdx.x] = sum;
+    return;
+  }
+  int before = 0;
+  for (int b0 = 0; b0 < g.batch; b0 += kChunk) {
+    const int b = b0 + threadIdx.x * kEach;
+    int v[kEach], mine = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) mine += v[i] = b + i < g.batch ? g.need[b + i] : 0;
+    int at = before + sum_before<4>(mine, of_wave, sum);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (b + i < g.batch) g.need[b + i] = at;
+      at += v[i];
+    }
+    before += sum;
+  }
+  if (threadIdx.x == 0) g.total[1] = before;
+}
+
+// Pages of the chunks before this block's, of `kind`; all: of all chunks.
+__device__ __forceinline__ int chunks_before(const PagesArgs& g, int* of_wave, int& all) {
+  int mine = 0, total = 0, sum;
+  for (int c = threadIdx.x; c < g.chunks; c += 256) {
+    const int n = g.counts[c];
+    mine += c < (int)blockIdx.x ? n : 0;
+    total += n;
+  }
+  sum_before<4>(total, of_wave, all);
+  sum_before<4>(mine, of_wave, sum);
+  return sum;
+}
+
+// The free pages' numbers, in order.
+__global__ void __launch_bounds__(256) pages_list(PagesArgs g) {
+  __shared__ int of_wave[4];
+  int all, sum;
+  const int before = chunks_before(g, of_wave, all), first = blockIdx.x * kChunk + threadIdx.x * kEach;
+  int at = before + sum_before<4>(count_chunk(g.uses, g.pages, first, FREE), of_wave, sum);
+#pragma unroll
+  for (int i = 0; i < kEach; ++i)
+    if (first + i < g.pages && g.uses[first + i] <= 0) g.list[at++] = first + i;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    g.total[0] = all;
+    if (g.count) *g.count = g.total[1] > all ? g.total[1] - all : 0;
+  }
+}
+
+template <bool FORK>
+__global__ void __launch_bounds__(256) pages_give(PagesArgs g) {
+  if (FORK) {
+    const int j = blockIdx.x * 256 + threadIdx.x;
+    if (j < g.batch) give_copy(g, j, g.need[j]);
+  } else {
+    const int b = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / kWave);
+    if (b < g.batch) give_row(g, b, threadIdx.x % kWave, g.need[b]);
+  }
+}
+
+// ---- compaction ------------------------------------------------------------------------------------------------------------
+
+// Pages in use of each chunk, and uses to where it goes.
+__global__ void __launch_bounds__(256) compact_count(PagesArgs g) {
+  __shared__ int of_wave[4];
+  const int first = blockIdx.x * kChunk + threadIdx.x * kEach;
+  int n = 0, sum;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i)
+    if (first + i < g.pages) {
+      const int u = g.uses_from[first + i];
+      n += u > 0;
+      if (g.uses != g.uses_from) g.uses[first + i] = u;
+    }
+  sum_before<4>(n, of_wave, sum);
+  if (threadIdx.x == 0 && (int)blockIdx.x < g.chunks) g.counts[blockIdx.x] = sum;      // (without pages there is one block, and no chunk)
+}
+
+// With n pages in use: a free page p < n is the target of rank p minus the pages in use before it, and a page p >= n in use the source whose rank is
+// the number of pages in use behind it; both ranks run from 0 to the number of moves.  need[p]: the rank of a source.
+__global__ void __launch_bounds__(256) compact_list(PagesArgs g) {
+  __shared__ int of_wave[4];
+  int n, sum;
+  const int before = chunks_before(g, of_wave, n), first = blockIdx.x * kChunk + threadIdx.x * kEach;
+  int at = before + sum_before<4>(count_chunk(g.uses_from, g.pages, first, USED), of_wave, sum);
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int p = first + i;
+    if (p >= g.pages) break;
+    const bool used = g.uses_from[p] > 0;
+    if (!used && p < n) g.target[p - at] = p;
+    if (used && p >= n) {
+      g.source[n - 1 - at] = p;
+      g.list[p] = n - 1 - at;
+    }
+    at += used;
+    if (p == (n > 0 ? n - 1 : 0)) g.total[0] = n > 0 ? n - at : 0;           // moves: free pages among the first n
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (g.pages == 0) g.total[0] = 0;
+    g.total[1] = n;
+    if (g.count) *g.count = n;
+  }
+}
+
+// The table's entries and uses follow the pages.
+__global__ void __launch_bounds__(256) compact_follow(PagesArgs g) {
+  const int n = g.total[1], moves = g.total[0];
+  const int64_t all = g.batch * g.places, step = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all || i < moves; i += step) {
+    if (i < all) {
+      int e = g.table_from[i];
+      // (an entry that uses does not know of stays as it is: list has a rank for pages in use alone)
+      if (names(g, e) && e >= n) {
+        const int r = g.list[e];
+        if ((uint32_t)r < (uint32_t)moves && g.source[r] == e) e = g.target[r];
+      }
+      if (g.table != g.table_from || e != g.table_from[i]) g.table[i] = e;
+    }
+    if (i < moves) {
+      const int from = g.source[i], to = g.target[i];
+      g.uses[to] = g.uses_from[from];
+      g.uses[from] = 0;
+    }
+  }
+}
+
+// ---- copies -------------------------------------------------------------------------------------------------------------------
+
+constexpr int kCaches = 16, kUnits = 1024;       // caches of a launch, 16-byte units of a block
+struct CopyArgs {
+  struct { uint8_t *k, *v; float *ks, *vs; int64_t stride_page, stride_scale; uint32_t half; int heads; Divisor head; } cache[kCaches];   // units of a page's keys and of one head's
+  const int32_t *source, *target, *tokens;
+  const int32_t* n_dev;                                  // null: n
+  int n, pages, page;
+};
+
+// One block: 16 KB of a page's codes, keys before values.  A head's blocks lie one after another, so the first ones are its first units.
+__global__ void __launch_bounds__(256) pages_copy(CopyArgs g) {
+  const auto& c = g.cache[blockIdx.y];
+  const int n = g.n_dev ? *g.n_dev : g.n;
+  for (int pair = blockIdx.z; pair < n; pair += gridDim.z) {
+    const int from = g.source[pair], to = g.target[pair];
+    if ((uint32_t)from >= (uint32_t)g.pages || (uint32_t)to >= (uint32_t)g.pages || from == to) continue;
+    const int tokens = g.tokens ? min(max(g.tokens[pair], 0), g.page) : g.page, blocks = (tokens + kBlockTokens - 1) / kBlockTokens, of_page = g.page / kBlockTokens;
+    const uint32_t most = c.head.d / of_page * blocks;
+    const int64_t src = from * c.stride_page, dst = to * c.stride_page;
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    for (uint32_t u0 = blockIdx.x * kUnits; u0 < 2 * c.half; u0 += gridDim.x * kUnits) {
+      u32x4 x[4];
+      uint8_t* at[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t u = u0 + i * 256 + threadIdx.x;
+        const bool values = u >= c.half;
+        const uint32_t in = values ? u - c.half : u, in_head = in - quotient((int)in, c.head) * c.head.d;
+        uint8_t* const base = values ? c.v : c.k;
+        at[i] = u < 2 * c.half && in_head < most ? base + dst + (int64_t)in * 16 : nullptr;
+        if (at[i]) x[i] = *reinterpret_cast<const u32x4*>(base + src + (int64_t)in * 16);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (at[i]) *reinterpret_cast<u32x4*>(at[i]) = x[i];
+    }
+    if (blockIdx.x == 0)
+      for (int i = threadIdx.x; i < c.heads * of_page; i += 256)
+        if (i % of_page < blocks) {
+          c.ks[to * c.stride_scale + i] = c.ks[from * c.stride_scale + i];
+          c.vs[to * c.stride_scale + i] = c.vs[from * c.stride_scale + i];
+        }
+  }
+}
+
+hipError_t copy_launch(const ac_kv_cache* caches, int n_caches, CopyArgs a, int64_t most, hipStream_t s) {
+  if (most <= 0) return hipSuccess;
+  for (int first = 0; first < n_caches; first += kCaches) {
+    const int n = n_caches - first < kCaches ? n_caches - first : kCaches;
+    int64_t units = 0;
+    for (int i = 0; i < n; ++i) {
+      const ac_kv_cache& c = caches[first + i];
+      const uint32_t head = (uint32_t)c.page * c.head_dim / 16, half = head * c.heads;
+      a.cache[i] = {(uint8_t*)c.k, (uint8_t*)c.v, c.k_scale, c.v_scale, c.stride_page, c.stride_scale, half, c.heads, divisor(head)};
+      if (2 * (int64_t)half > units) units = 2 * (int64_t)half;
+    }
+    const int64_t pieces = (units + kUnits - 1) / kUnits;
+    const dim3 grid((unsigned)(pieces < 4096 ? pieces : 4096), (unsigned)n, (unsigned)(most < 2048 ? most : 2048));
+    hipLaunchKernelGGL(pages_copy, grid, dim3(256), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+PagesArgs pages_args(const ac_page_books& from, const ac_page_books& to, void* workspace) {
+  PagesArgs g{};
+  g.uses_from = from.uses; g.table_from = from.page_table;
+  g.uses = to.uses; g.table = to.page_table;
+  g.pages = (int)from.pages; g.page = from.page; g.batch = (int)from.batch; g.places = from.ld_page_table;
+  g.chunks = (g.pages + kChunk - 1) / kChunk;
+  int32_t* w = (int32_t*)workspace;
+  g.total = w; w += 64;
+  g.counts = w; w += g.chunks;
+  g.list = w; w += g.pages;
+  const int most = g.pages > g.batch ? g.pages : g.batch;
+  g.source = w; w += most;
+  g.target = w; w += most;
+  g.tokens = w; w += g.batch;
+  g.need = w;
+  return g;
+}
+
+template <bool FORK>
+hipError_t rows_launch(const PagesArgs& g, hipStream_t s) {
+  if (g.uses != g.uses_from && g.pages > 0)
+    hipLaunchKernelGGL(pages_copy_uses, dim3((unsigned)(g.chunks < 1024 ? 4 * g.chunks : 4096)), dim3(256), 0, s, g);
+  hipLaunchKernelGGL((pages_rows<FORK>), dim3((unsigned)(g.batch / 4 + 1)), dim3(256), 0, s, g);
+  if (FORK || g.take_begin) {
+    hipLaunchKernelGGL(pages_count, dim3((unsigned)g.chunks + 1), dim3(256), 0, s, g);
+    hipLaunchKernelGGL(pages_list, dim3((unsigned)(g.chunks > 0 ? g.chunks : 1)), dim3(256), 0, s, g);
+    hipLaunchKernelGGL((pages_give<FORK>), dim3((unsigned)(g.batch / (FORK ? 256 : 4) + 1)), dim3(256), 0, s, g);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+uint64_t pages_workspace_bytes(const ac_page_books& b) {
+  const uint64_t most = b.pages > b.batch ? b.pages : b.batch;
+  return (64 + (b.pages + kChunk - 1) / kChunk + b.pages + 2 * most + 2 * b.batch) * sizeof(int32_t);
+}
+
+hipError_t launch_pages_update(const ac_page_books& from, const ac_page_books& to, const int32_t* drop_begin, const int32_t* drop_end, const int32_t* take_begin,
+                               const int32_t* take_end, int32_t* missing, void* workspace, hipStream_t s) {
+  PagesArgs g = pages_args(from, to, workspace);
+  g.drop_begin = drop_begin; g.drop_end = drop_end; g.take_begin = take_begin; g.take_end = take_end;
+  g.count = missing;
+  return rows_launch<false>(g, s);
+}
+
+hipError_t launch_cache_fork(const ac_kv_cache* caches, int n_caches, const ac_page_books& from, const ac_page_books& to, const int32_t* parent,
+                             const int32_t* length, int32_t* length_to, int32_t* missing, void* workspace, hipStream_t s) {
+  PagesArgs g = pages_args(from, to, workspace);
+  g.parent = parent; g.length = length; g.length_to = length_to;
+  g.count = missing;
+  const hipError_t e = rows_launch<true>(g, s);
+  if (e != hipSuccess) return e;
+  CopyArgs c{};
+  c.source = g.source; c.target = g.target; c.tokens = g.tokens; c.n = g.batch; c.pages = g.pages; c.page = g.page;
+  return copy_launch(caches, n_caches, c, g.batch, s);
+}
+
+hipError_t launch_cache_compact(const ac_kv_cache* caches, int n_caches, const ac_page_books& from, const ac_page_books& to, int32_t* used, void* workspace,
+                                hipStream_t s) {
+  PagesArgs g = pages_args(from, to, workspace);
+  g.count = used;
+  const int blocks = g.chunks > 0 ? g.chunks : 1;
+  hipLaunchKernelGGL(compact_count, dim3((unsigned)blocks), dim3(256), 0, s, g);
+  hipLaunchKernelGGL(compact_list, dim3((unsigned)blocks), dim3(256), 0, s, g);
+  const int64_t all = g.batch * g.places > g.pages ? g.batch * g.places : g.pages, follow = (all + 1023) / 1024;
+  hipLaunchKernelGGL(compact_follow, dim3((unsigned)(follow < 1 ? 1 : follow < 4096 ? follow : 4096)), dim3(256), 0, s, g);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  CopyArgs c{};
+  c.source = g.source; c.target = g.target; c.n_dev = g.total; c.pages = g.pages; c.page = g.page;
+  return copy_launch(caches, n_caches, c, g.pages / 2, s);
+}
+
+hipError_t launch_cache_copy_pages(const ac_kv_cache* caches, int n_caches, const int32_t* source, const int32_t* target, const int32_t* tokens, int64_t n,
+                                   hipStream_t s) {
+  if (n <= 0 || n_caches <= 0 || caches[0].pages <= 0) return hipSuccess;
+  CopyArgs c{};
+  c.source = source; c.target = target; c.tokens = tokens; c.n = (int)n; c.pages = (int)caches[0].pages; c.page = caches[0].page;
+  return copy_launch(caches, n_caches, c, n, s);
+}
+
+}  // namespace ac

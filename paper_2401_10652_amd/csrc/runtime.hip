@@ -2186,17 +2186,13 @@ int ac_op_linear_w4(const void* x, int64_t ldx, const void* w, int64_t ldw, cons
                                                   activation, dtype}, (hipStream_t)stream), "linear_w4");
 }
 
-// What append and attention ask of a cache and of the rows' descriptions; AC_OK, or the refusal.
-static int cache_ok(const char* what, const ac_kv_cache* c, const ac_cache_rows* r, int64_t n_rows) {
-  if (!c || !r || c->pages < 0 || c->page < 16 || c->page % 16 != 0 || c->heads < 1 || c->heads > 4096 || c->head_dim < 1 || r->ld_page_table < 0 ||
-      r->batch < 0 || n_rows < 0 || r->max_rows < 0 || r->max_length < 0)
+// What every call asks of a cache; AC_OK, or the refusal.
+static int cache_alone_ok(const char* what, const ac_kv_cache* c) {
+  if (!c || c->pages < 0 || c->page < 16 || c->page % 16 != 0 || c->heads < 1 || c->heads > 4096 || c->head_dim < 1)
     return fail(AC_ERR_ARG, "%s: bad cache or rows", what);
-  // (nothing is read of a cache without pages, of no sequences and of tables without places)
-  const bool pages = c->pages > 0, sequences = r->batch > 0;
-  if ((pages && (!c->k || !c->v || !c->k_scale || !c->v_scale)) || (sequences && (!r->row_begin || !r->length || (r->ld_page_table > 0 && !r->page_table))))
-    return fail(AC_ERR_ARG, "%s: bad cache or rows", what);
-  if (r->batch > 65535 || n_rows > 1 << 30 || r->max_length > 1 << 30 || r->ld_page_table > (1 << 30) / c->page)
-    return fail(AC_ERR_UNSUPPORTED, "%s: at most 65535 sequences, 2^30 rows and places of a sequence", what);
+  // (nothing is read of a cache without pages)
+  const bool pages = c->pages > 0;
+  if (pages && (!c->k || !c->v || !c->k_scale || !c->v_scale)) return fail(AC_ERR_ARG, "%s: bad cache or rows", what);
   const int d = c->head_dim;
   if (d != 32 && d != 64 && d != 96 && d != 128 && d != 192 && d != 256)
     return fail(AC_ERR_UNSUPPORTED, "%s: heads of 32, 64, 96, 128, 192 or 256", what);
@@ -2205,6 +2201,18 @@ static int cache_ok(const char* what, const ac_kv_cache* c, const ac_cache_rows*
     return fail(AC_ERR_ARG, "%s: pages overlap", what);
   if ((uintptr_t)c->k % 16 != 0 || (uintptr_t)c->v % 16 != 0 || c->stride_page % 16 != 0)
     return fail(AC_ERR_ALIGN, "%s: codes and pages start at multiples of 16 bytes", what);
+  return AC_OK;
+}
+// What append and attention ask of a cache and of the rows' descriptions.
+static int cache_ok(const char* what, const ac_kv_cache* c, const ac_cache_rows* r, int64_t n_rows) {
+  if (!c || !r || r->ld_page_table < 0 || r->batch < 0 || n_rows < 0 || r->max_rows < 0 || r->max_length < 0)
+    return fail(AC_ERR_ARG, "%s: bad cache or rows", what);
+  // (nor of no sequences and of tables without places)
+  if (r->batch > 0 && (!r->row_begin || !r->length || (r->ld_page_table > 0 && !r->page_table)))
+    return fail(AC_ERR_ARG, "%s: bad cache or rows", what);
+  if (const int st = cache_alone_ok(what, c)) return st;
+  if (r->batch > 65535 || n_rows > 1 << 30 || r->max_length > 1 << 30 || r->ld_page_table > (1 << 30) / c->page)
+    return fail(AC_ERR_UNSUPPORTED, "%s: at most 65535 sequences, 2^30 rows and places of a sequence", what);
   return AC_OK;
 }
 
@@ -2296,6 +2304,88 @@ int ac_op_cache_attention_window(const void* q, int64_t ldq, void* out, int64_t 
   if (!window_ok(window, sinks)) return fail(AC_ERR_ARG, "%s: windows and sinks of 0 to 2^30 tokens", what);
   return cache_attention(what, q, ldq, out, ldo, n_rows, heads, cache, rows, CacheSight{1, 1, (int)window, (int)sinks}, scale, workspace, workspace_bytes,
                          dtype, stream);
+}
+
+// ---- pages ---------------------------------------------------------------------------------
+
+constexpr int64_t kMostPages = 1 << 24;
+static int caches_ok(const char* what, const ac_kv_cache* caches, int n) {
+  if (n < 0 || n > 4096 || (n > 0 && !caches)) return fail(AC_ERR_ARG, "%s: bad caches", what);
+  for (int i = 0; i < n; ++i) {
+    const ac_kv_cache& c = caches[i];
+    if (const int st = cache_alone_ok(what, &c)) return st;
+    if (c.pages != caches[0].pages || c.page != caches[0].page) return fail(AC_ERR_ARG, "%s: caches of different pages", what);
+    if (c.pages > kMostPages || (int64_t)c.heads * c.page * c.head_dim >= 1ll << 34)
+      return fail(AC_ERR_UNSUPPORTED, "%s: at most 2^24 pages, of less than 2^34 codes", what);
+  }
+  return AC_OK;
+}
+static int book_ok(const char* what, const ac_page_books* b) {
+  if (!b || b->pages < 0 || b->ld_page_table < 0 || b->batch < 0 || b->page < 16 || b->page % 16 != 0 || (b->pages > 0 && !b->uses) ||
+      (b->batch > 0 && b->ld_page_table > 0 && !b->page_table))
+    return fail(AC_ERR_ARG, "%s: bad books", what);
+  if (b->pages > kMostPages || b->batch > 65535 || b->ld_page_table > (1 << 30) / b->page)
+    return fail(AC_ERR_UNSUPPORTED, "%s: at most 2^24 pages, 65535 sequences and 2^30 places of a sequence", what);
+  if ((uintptr_t)b->uses % 4 != 0 || (uintptr_t)b->page_table % 4 != 0) return fail(AC_ERR_ALIGN, "%s: books start at multiples of 4 bytes", what);
+  return AC_OK;
+}
+// Whether arrays of n elements of 4 bytes overlap.
+static bool overlap(const void* a, const void* b, int64_t n) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return n > 0 && x < y + 4 * n && y < x + 4 * n;
+}
+static int books_ok(const char* what, const ac_kv_cache* caches, int n_caches, const ac_page_books* from, const ac_page_books* to, void* workspace,
+                    uint64_t workspace_bytes) {
+  if (const int st = caches_ok(what, caches, n_caches)) return st;
+  if (const int st = book_ok(what, from)) return st;
+  if (const int st = book_ok(what, to)) return st;
+  if (from->pages != to->pages || from->ld_page_table != to->ld_page_table || from->batch != to->batch || from->page != to->page)
+    return fail(AC_ERR_ARG, "%s: books of different sizes", what);
+  const int64_t table = from->batch * from->ld_page_table;
+  if ((from->uses != to->uses && overlap(from->uses, to->uses, from->pages)) || (from->page_table != to->page_table && overlap(from->page_table, to->page_table, table)))
+    return fail(AC_ERR_ARG, "%s: books that overlap in part", what);
+  if (n_caches > 0 && (caches[0].pages != from->pages || caches[0].page != from->page)) return fail(AC_ERR_ARG, "%s: books of other pages than the caches'", what);
+  const uint64_t need = pages_workspace_bytes(*from);
+  if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0)
+    return fail(AC_ERR_WORKSPACE, "%s: workspace of %llu bytes, %llu needed", what, (unsigned long long)workspace_bytes, (unsigned long long)need);
+  return AC_OK;
+}
+
+uint64_t ac_pages_workspace_bytes(const ac_page_books* books) {
+  return book_ok("ac_pages_workspace_bytes", books) ? 0 : pages_workspace_bytes(*books);
+}
+
+int ac_op_pages_update(const ac_page_books* from, const ac_page_books* to, const int32_t* drop_begin, const int32_t* drop_end, const int32_t* take_begin,
+                       const int32_t* take_end, int32_t* missing, void* workspace, uint64_t workspace_bytes, void* stream) {
+  const char* const what = "ac_op_pages_update";
+  if (const int st = books_ok(what, nullptr, 0, from, to, workspace, workspace_bytes)) return st;
+  if (!drop_begin != !drop_end || !take_begin != !take_end) return fail(AC_ERR_ARG, "%s: ranges with one end", what);
+  return hip_status(launch_pages_update(*from, *to, drop_begin, drop_end, take_begin, take_end, missing, workspace, (hipStream_t)stream), what + 6);
+}
+
+int ac_op_cache_fork(const ac_kv_cache* caches, int n_caches, const ac_page_books* from, const ac_page_books* to, const int32_t* parent, const int32_t* length,
+                     int32_t* length_to, int32_t* missing, void* workspace, uint64_t workspace_bytes, void* stream) {
+  const char* const what = "ac_op_cache_fork";
+  if (const int st = books_ok(what, caches, n_caches, from, to, workspace, workspace_bytes)) return st;
+  if (from->batch > 0 && (!parent || !length || !length_to || overlap(length, length_to, from->batch) || overlap(parent, length_to, from->batch) || (from->ld_page_table > 0 && from->page_table == to->page_table)))
+    return fail(AC_ERR_ARG, "%s: parents, lengths, and a table and lengths apart from them are wanted", what);
+  return hip_status(launch_cache_fork(caches, n_caches, *from, *to, parent, length, length_to, missing, workspace, (hipStream_t)stream), what + 6);
+}
+
+int ac_op_cache_compact(const ac_kv_cache* caches, int n_caches, const ac_page_books* from, const ac_page_books* to, int32_t* used, void* workspace,
+                        uint64_t workspace_bytes, void* stream) {
+  const char* const what = "ac_op_cache_compact";
+  if (const int st = books_ok(what, caches, n_caches, from, to, workspace, workspace_bytes)) return st;
+  return hip_status(launch_cache_compact(caches, n_caches, *from, *to, used, workspace, (hipStream_t)stream), what + 6);
+}
+
+int ac_op_cache_copy_pages(const ac_kv_cache* caches, int n_caches, const int32_t* source, const int32_t* target, const int32_t* tokens, int64_t n,
+                           void* stream) {
+  const char* const what = "ac_op_cache_copy_pages";
+  if (const int st = caches_ok(what, caches, n_caches)) return st;
+  if (n < 0 || (n > 0 && (!source || !target))) return fail(AC_ERR_ARG, "%s: bad argument", what);
+  if (n > 1 << 24) return fail(AC_ERR_UNSUPPORTED, "%s: at most 2^24 pairs", what);
+  return hip_status(launch_cache_copy_pages(caches, n_caches, source, target, tokens, n, (hipStream_t)stream), what + 6);
 }
 
 }  // extern "C"

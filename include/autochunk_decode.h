@@ -123,6 +123,23 @@ int ac_op_cache_attention_window(const void* q, int64_t ldq, void* out, int64_t 
 uint64_t ac_cache_attention_window_workspace_bytes(int64_t n_rows, int heads, const ac_kv_cache* cache, const ac_cache_rows* rows, int64_t window,
                                                    int64_t sinks, int dtype);
 
+/*
+ * Beam search's selection.  Of each of `batch` prompts `beams` sequences go on; sequence r = b * beams + i has the sum of logarithms scores[r] and, over the tokens that may come next, the
+ * logits x[r, 0 .. vocab - 1], rows ld elements apart.  A candidate is a beam with a token, with
+ *     total(i, t) = scores[r] + x[r, t] - log(sum_u exp x[r, u]).
+ * A sequence with ended[r] != 0 has ended: its one candidate is (i, end) with scores[r] as it is, and its logits are not read.  The `keep` candidates with the largest totals come out, largest first, of
+ * equal ones the lower i, then the lower t: scores_out, parent (r, the sequence it goes on from) and token, each [batch][keep], and ended_out (may be NULL): 1 where the parent had ended or the token is end, else 0.
+ * Logits of -inf (tokens that may not come) and scores of -inf (a beam that is none yet) give no candidates, and none comes from a row that holds a NaN; logits of +inf
+ * share the probability among them.  Where candidates are fewer than `keep` the others come out as score -inf, parent -1, token -1, ended 0.
+ * Totals are compared in 64 bits, from maxima and sums of exponentials held in 32; within a beam the order is that of the logits.
+ * ended: NULL = none; end: a token, with ended NULL also -1 = none.  beams and keep at most 64, batch 65535, vocab 2^24, else AC_ERR_UNSUPPORTED.  Rows may start at any element.  Outputs lie apart from scores and ended.
+ * workspace: dev, 16-byte aligned, ac_beam_select_workspace_bytes() large, else AC_ERR_WORKSPACE.
+ */
+int ac_op_beam_select(const void* logits, int64_t ld, int64_t batch, int beams, int64_t vocab, const float* scores, const int32_t* ended, int keep,
+                      int end, float* scores_out, int32_t* parent, int32_t* token, int32_t* ended_out, void* workspace, uint64_t workspace_bytes,
+                      int dtype, void* stream);
+uint64_t ac_beam_select_workspace_bytes(int64_t batch, int beams, int64_t vocab, int keep, int dtype);
+
 #ifdef __cplusplus
 }
 #endif

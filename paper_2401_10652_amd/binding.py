@@ -174,6 +174,8 @@ SIGNATURES = {
     "ac_op_cache_attention_window": (INT, [VP, I64, VP, I64, I64, INT, C.POINTER(ac_kv_cache), C.POINTER(ac_cache_rows), I64, I64, F32, VP, U64,
                                            INT, VP]),
     "ac_cache_attention_window_workspace_bytes": (U64, [I64, INT, C.POINTER(ac_kv_cache), C.POINTER(ac_cache_rows), I64, I64, INT]),
+    "ac_op_beam_select": (INT, [VP, I64, I64, INT, I64, VP, VP, INT, INT, VP, VP, VP, VP, VP, U64, INT, VP]),
+    "ac_beam_select_workspace_bytes": (U64, [I64, INT, I64, INT, INT]),
     "ac_pages_workspace_bytes": (U64, [C.POINTER(ac_page_books)]),
     "ac_op_pages_update": (INT, [C.POINTER(ac_page_books), C.POINTER(ac_page_books), VP, VP, VP, VP, VP, VP, U64, VP]),
     "ac_op_cache_fork": (INT, [C.POINTER(ac_kv_cache), INT, C.POINTER(ac_page_books), C.POINTER(ac_page_books), VP, VP, VP, VP, VP, U64, VP]),
@@ -244,11 +246,15 @@ def _ptr(t):
 _DTYPES = {}
 
 
-def _dt(t):
+def _types():
     if not _DTYPES:
         import torch
-        _DTYPES.update({torch.bfloat16: AC_BF16, torch.float32: AC_F32, "codes": torch.uint8})
-    dt = _DTYPES.get(t.dtype)
+        _DTYPES.update({torch.bfloat16: AC_BF16, torch.float32: AC_F32, "codes": torch.uint8, "i32": torch.int32, "f32": torch.float32})
+    return _DTYPES
+
+
+def _dt(t):
+    dt = _types().get(t.dtype)
     if dt is None:
         raise TypeError(f"unsupported tensor dtype {t.dtype}")
     return dt
@@ -676,17 +682,11 @@ def _ints(t, what, *shape):
     """The address of a contiguous int32 tensor of this shape; None of None."""
     if t is None:
         return None
-    if _INT32 is None:
-        import torch
-        globals()["_INT32"] = torch.int32
-    if t.dtype is not _INT32:
+    if t.dtype is not _types()["i32"]:
         raise TypeError(f"{what} is {t.dtype}, not int32")
     if t.shape != shape or not t.is_contiguous():
         _bad(what, t, f"{shape}, contiguous, is wanted")
     return t.data_ptr()
-
-
-_INT32 = None
 
 
 def kv_caches(caches):
@@ -739,6 +739,27 @@ def ac_op_cache_copy_pages(caches, source, target, tokens=None):
     n = source.shape[0]
     _check(lib().ac_op_cache_copy_pages(caches, len(caches), _ints(source, "source", n), _ints(target, "target", n), _ints(tokens, "tokens", n), n,
                                         _stream()), "ac_op_cache_copy_pages")
+
+
+# ---- beam search ------------------------------------------------------------------------------
+
+def ac_beam_select_workspace_bytes(logits, beams, keep):
+    rows, vocab = logits.shape
+    return int(lib().ac_beam_select_workspace_bytes(rows // beams, beams, vocab, keep, _dt(logits)))
+
+
+def ac_op_beam_select(logits, scores, scores_out, parent, token, workspace, ended=None, ended_out=None, end=-1):
+    """logits [batch * beams, vocab], scores fp32 and ended int32 [batch, beams] -> scores_out fp32, parent, token and ended_out int32 [batch, keep]."""
+    (rows, vocab), (batch, beams), keep = logits.shape, scores.shape, scores_out.shape[-1]
+    lp, ld = _matrix(logits, "logits", logits.dtype, batch * beams, vocab)
+    for t, what, n in ((scores, "scores", beams), (scores_out, "scores_out", keep)):
+        if t.dtype is not _types()["f32"]:
+            raise TypeError(f"{what} is {t.dtype}, not float32")
+        if t.shape != (batch, n) or not t.is_contiguous():
+            _bad(what, t, f"({batch}, {n}), contiguous, is wanted")
+    _check(lib().ac_op_beam_select(lp, ld, batch, beams, vocab, scores.data_ptr(), _ints(ended, "ended", batch, beams), keep, end, scores_out.data_ptr(),
+                                   _ints(parent, "parent", batch, keep), _ints(token, "token", batch, keep), _ints(ended_out, "ended_out", batch, keep),
+                                   *_space(workspace), _dt(logits), _stream()), "ac_op_beam_select")
 
 
 # ---- helpers for callers (buffers only) ------------------------------------------------------

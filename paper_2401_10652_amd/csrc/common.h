@@ -383,6 +383,17 @@ hipError_t launch_cache_attention(const void* q, int64_t ldq, void* out, int64_t
                                   const CacheRows& rows, const CacheSight& sight, float scale, void* workspace, int dtype, hipStream_t s);
 uint64_t cache_attention_workspace_bytes(int heads, const ac_kv_cache& cache, const CacheRows& rows, const CacheSight& sight, int dtype);
 
+// Beam search's selection: see autochunk_decode.h.
+struct BeamSelectArgs {
+  const void* logits; int64_t ld;
+  int64_t batch; int beams; int64_t vocab;
+  const float* scores; const int32_t* ended;
+  int keep, end;
+  float* scores_out; int32_t *parent, *token, *ended_out;
+  void* workspace; int dtype;
+};
+uint64_t beam_select_workspace_bytes(int64_t batch, int beams, int64_t vocab, int keep, int dtype);
+hipError_t launch_beam_select(const BeamSelectArgs& b, hipStream_t s);
 // The books of a cache's pages: see autochunk_pages.h.
 uint64_t pages_workspace_bytes(const ac_page_books& books);
 hipError_t launch_pages_update(const ac_page_books& from, const ac_page_books& to, const int32_t* drop_begin, const int32_t* drop_end, const int32_t* take_begin,

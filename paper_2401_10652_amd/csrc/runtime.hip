@@ -2306,6 +2306,47 @@ int ac_op_cache_attention_window(const void* q, int64_t ldq, void* out, int64_t 
                          dtype, stream);
 }
 
+// Whether arrays of n and m elements of 4 bytes overlap.
+static bool overlap(const void* a, int64_t n, const void* b, int64_t m) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return a && b && n > 0 && m > 0 && x < y + 4 * m && y < x + 4 * n;
+}
+
+static int beam_sizes_ok(const char* what, int64_t batch, int beams, int64_t vocab, int keep, int dtype) {
+  if (batch < 0 || beams < 1 || vocab < 1 || keep < 1 || !dtype_ok(dtype)) return fail(AC_ERR_ARG, "%s: bad argument", what);
+  if (batch > 65535 || beams > 64 || keep > 64 || vocab > 1 << 24)
+    return fail(AC_ERR_UNSUPPORTED, "%s: at most 65535 prompts, 64 beams, 64 kept and 2^24 tokens", what);
+  return AC_OK;
+}
+
+uint64_t ac_beam_select_workspace_bytes(int64_t batch, int beams, int64_t vocab, int keep, int dtype) {
+  return beam_sizes_ok("ac_beam_select_workspace_bytes", batch, beams, vocab, keep, dtype) ? 0 : beam_select_workspace_bytes(batch, beams, vocab, keep, dtype);
+}
+
+int ac_op_beam_select(const void* logits, int64_t ld, int64_t batch, int beams, int64_t vocab, const float* scores, const int32_t* ended, int keep,
+                      int end, float* scores_out, int32_t* parent, int32_t* token, int32_t* ended_out, void* workspace, uint64_t workspace_bytes,
+                      int dtype, void* stream) {
+  const char* const what = "ac_op_beam_select";
+  if (const int st = beam_sizes_ok(what, batch, beams, vocab, keep, dtype)) return st;
+  if (batch == 0) return AC_OK;
+  if (!logits || !scores || !scores_out || !parent || !token || ld < vocab || end >= vocab || end < (ended ? 0 : -1)) return fail(AC_ERR_ARG, "%s: bad argument", what);
+  const int64_t in = batch * beams, out = batch * keep;
+  const void* const outs[] = {scores_out, parent, token, ended_out};
+  for (int i = 0; i < 4; ++i) {
+    if ((uintptr_t)outs[i] % 4 != 0) return fail(AC_ERR_ALIGN, "%s: outputs start at multiples of 4 bytes", what);
+    bool apart = !overlap(outs[i], out, scores, in) && !overlap(outs[i], out, ended, in);
+    for (int j = 0; j < i; ++j) apart = apart && !overlap(outs[i], out, outs[j], out);
+    if (!apart) return fail(AC_ERR_ARG, "%s: outputs that overlap", what);
+  }
+  if ((uintptr_t)scores % 4 != 0 || (uintptr_t)ended % 4 != 0 || (uintptr_t)logits % (dtype == AC_BF16 ? 2 : 4) != 0)
+    return fail(AC_ERR_ALIGN, "%s: arrays start at their elements' multiples", what);
+  const uint64_t need = beam_select_workspace_bytes(batch, beams, vocab, keep, dtype);
+  if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0)
+    return fail(AC_ERR_WORKSPACE, "%s: workspace of %llu bytes, %llu needed", what, (unsigned long long)workspace_bytes, (unsigned long long)need);
+  return hip_status(launch_beam_select(BeamSelectArgs{logits, ld, batch, beams, vocab, scores, ended, keep, end, scores_out, parent, token, ended_out, workspace, dtype},
+                                       (hipStream_t)stream), what + 6);
+}
+
 // ---- pages ---------------------------------------------------------------------------------
 
 constexpr int64_t kMostPages = 1 << 24;
@@ -2329,11 +2370,6 @@ static int book_ok(const char* what, const ac_page_books* b) {
   if ((uintptr_t)b->uses % 4 != 0 || (uintptr_t)b->page_table % 4 != 0) return fail(AC_ERR_ALIGN, "%s: books start at multiples of 4 bytes", what);
   return AC_OK;
 }
-// Whether arrays of n elements of 4 bytes overlap.
-static bool overlap(const void* a, const void* b, int64_t n) {
-  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return n > 0 && x < y + 4 * n && y < x + 4 * n;
-}
 static int books_ok(const char* what, const ac_kv_cache* caches, int n_caches, const ac_page_books* from, const ac_page_books* to, void* workspace,
                     uint64_t workspace_bytes) {
   if (const int st = caches_ok(what, caches, n_caches)) return st;
@@ -2342,7 +2378,7 @@ static int books_ok(const char* what, const ac_kv_cache* caches, int n_caches, c
   if (from->pages != to->pages || from->ld_page_table != to->ld_page_table || from->batch != to->batch || from->page != to->page)
     return fail(AC_ERR_ARG, "%s: books of different sizes", what);
   const int64_t table = from->batch * from->ld_page_table;
-  if ((from->uses != to->uses && overlap(from->uses, to->uses, from->pages)) || (from->page_table != to->page_table && overlap(from->page_table, to->page_table, table)))
+  if ((from->uses != to->uses && overlap(from->uses, from->pages, to->uses, from->pages)) || (from->page_table != to->page_table && overlap(from->page_table, table, to->page_table, table)))
     return fail(AC_ERR_ARG, "%s: books that overlap in part", what);
   if (n_caches > 0 && (caches[0].pages != from->pages || caches[0].page != from->page)) return fail(AC_ERR_ARG, "%s: books of other pages than the caches'", what);
   const uint64_t need = pages_workspace_bytes(*from);
@@ -2367,7 +2403,7 @@ int ac_op_cache_fork(const ac_kv_cache* caches, int n_caches, const ac_page_book
                      int32_t* length_to, int32_t* missing, void* workspace, uint64_t workspace_bytes, void* stream) {
   const char* const what = "ac_op_cache_fork";
   if (const int st = books_ok(what, caches, n_caches, from, to, workspace, workspace_bytes)) return st;
-  if (from->batch > 0 && (!parent || !length || !length_to || overlap(length, length_to, from->batch) || overlap(parent, length_to, from->batch) || (from->ld_page_table > 0 && from->page_table == to->page_table)))
+  if (from->batch > 0 && (!parent || !length || !length_to || overlap(length, from->batch, length_to, from->batch) || overlap(parent, from->batch, length_to, from->batch) || (from->ld_page_table > 0 && from->page_table == to->page_table)))
     return fail(AC_ERR_ARG, "%s: parents, lengths, and a table and lengths apart from them are wanted", what);
   return hip_status(launch_cache_fork(caches, n_caches, *from, *to, parent, length, length_to, missing, workspace, (hipStream_t)stream), what + 6);
 }

@@ -1,9 +1,10 @@
 """A pre-norm transformer that reads and writes token by token: linear layers with 4-bit weights, keys and values in a paged 8-bit cache.
 
-    python -m paper_2401_10652_amd.decode [--config C2] [--batch 8] [--prompt 1024] [--stretch 512] [--steps 32]
+    python -m paper_2401_10652_amd.decode [--config C2] [--batch 8] [--prompt 1024] [--stretch 512] [--steps 32] [--window 512 --sinks 4] [--beams 4 --vocab 32768]
 
 reads a prompt for each sequence of a batch in stretches, then single tokens (each step's output is the next one's input: there is no
-vocabulary here, as in the framework's other workloads), and prints one JSON line with both rates.
+vocabulary here, as in the framework's other workloads), and prints one JSON line with both rates.  With a window rows see the last tokens and the first few (sinks), and pages
+that no row sees any more are used again.  With beams, a beam search from each prompt over a random vocabulary is timed too.
 """
 from __future__ import annotations
 
@@ -33,9 +34,14 @@ def quantize_w4(w, group, dtype):
 class Decoder:
     """The layers of `cfg` (weights as transformer_inputs makes them; w_qkv's rows are the queries' heads, then the keys' and the
     values', which may be fewer) and the cache of `sequences` sequences of up to `max_tokens` tokens.  `cfg` is causal: a token sees those before it and itself; and its
-    queries and keys are rotated by their places, which no plan of the framework does, so that a plan's rows are not these."""
+    queries and keys are rotated by their places, which no plan of the framework does, so that a plan's rows are not these.
 
-    def __init__(self, cfg, layers, sequences, max_tokens, page=64, group=64, base=10000.0):
+    window, sinks: a token sees the last `window` ones, itself among them, and the first `sinks` ones.  pages: the cache has so many, which sequences take as they grow, give
+    up as their windows leave them, and share when one goes on as several (fork); without it, and without a window, each sequence has its own, enough for max_tokens."""
+
+    window, sinks, shares = None, 0, False
+
+    def __init__(self, cfg, layers, sequences, max_tokens, page=64, group=64, base=10000.0, window=None, sinks=0, pages=None):
         import torch
         if not cfg.causal:
             raise ValueError(f"{cfg.name} is not causal: its rows cannot be read a token at a time")
@@ -48,12 +54,26 @@ class Decoder:
             t = {n: torch.as_tensor(x, device=dev) for n, x in w.items()}
             self.layers.append({n: quantize_w4(x, group, self.dtype) if n.startswith("w_") else x.to(self.dtype) for n, x in t.items()})
         each = -(-max_tokens // page)
-        pages = sequences * each
-        self.table = torch.arange(pages, dtype=torch.int32, device=dev).view(sequences, each)
+        self.window, self.sinks, self.page = window, sinks, page
+        self.shares = pages is not None or window is not None
+        if pages is None:
+            pages = sequences * each
+        if self.shares:
+            self.table = torch.full((sequences, each), -1, dtype=torch.int32, device=dev)
+            self.uses = torch.zeros(pages, dtype=torch.int32, device=dev)
+            self.books = B.page_books(self.uses, self.table, page)
+            self.next_table, self.next_uses = torch.empty_like(self.table), torch.empty_like(self.uses)      # after a fork
+            self.next_books = B.page_books(self.next_uses, self.next_table, page)
+            self.books_workspace = B.empty_workspace(B.ac_pages_workspace_bytes(self.books))
+            self.missing = torch.zeros(1, dtype=torch.int32, device=dev)
+            self.held = [0] * sequences
+        else:
+            self.table = torch.arange(pages, dtype=torch.int32, device=dev).view(sequences, each)
         codes = dict(dtype=torch.uint8, device=dev)
         self.caches = [B.kv_cache(torch.zeros((pages, self.heads_kv, page, d), **codes), torch.zeros((pages, self.heads_kv, page // 16, d, 16), **codes),
                                   torch.ones((pages, self.heads_kv, page // 16), device=dev), torch.ones((pages, self.heads_kv, page // 16), device=dev))
                        for _ in layers]
+        self.all_caches = B.kv_caches(self.caches)
         angle = torch.arange(max_tokens, dtype=torch.float64)[:, None] * base ** (-torch.arange(d // 2, dtype=torch.float64) / (d // 2))
         self.rotary = B.rotary(angle.cos().float().to(dev), angle.sin().float().to(dev))
         self.lengths = [0] * sequences
@@ -78,15 +98,88 @@ class Decoder:
         begin = [0]
         for c in counts:
             begin.append(begin[-1] + c)
-        # one copy to the device for both
-        where = torch.tensor(begin + lengths, dtype=torch.int32).to("cuda")
-        rows = B.cache_rows(where[:len(begin)], where[len(begin):], self.table, max(counts), max(lengths))
+        # one copy to the device for all
+        seqs = len(lengths)
+        where = begin + lengths
+        if self.shares:
+            where += self.lengths + [self.sinks] * seqs + [n - self.window + 1 if self.window is not None else 0 for n in self.lengths]
+        where = torch.tensor(where, dtype=torch.int32).to("cuda")
+        length = where[seqs + 1:2 * seqs + 1]
+        if self.shares:
+            before, drop_begin, drop_end = where[2 * seqs + 1:].view(3, seqs)
+            B.ac_op_pages_update(self.books, self.books, self.books_workspace, (drop_begin, drop_end), (before, length), self.missing)
+            self._enough(self._places(lengths))
+        rows = B.cache_rows(where[:seqs + 1], length, self.table, max(counts), max(lengths))
         need = self._workspace_bytes(n, rows)
         if need > self.workspace.numel():
             self.workspace = B.empty_workspace(need)
         x = self._run(x.clone(memory_format=torch.contiguous_format), rows, self.workspace)
         self.lengths = lengths
         return x
+
+    def _places(self, lengths):
+        """The most places that name a page, of each sequence after its update to these lengths."""
+        if self.window is None:
+            return [-(-n // self.page) for n in lengths]
+        p = self.page
+        return [min(-(-n // p), -(-self.sinks // p) + (self.window + n - before + p - 2) // p + 1) for n, before in zip(lengths, self.lengths)]
+
+    def _enough(self, held):
+        """Raises where pages ran out in the last call, after which sequences have up to `held` places.  The device is asked only where there are fewer pages."""
+        if sum(held) > self.uses.shape[0]:
+            missing = self.missing.item()
+            if missing:
+                raise RuntimeError(f"{missing} pages are missing: the cache has {self.uses.shape[0]}")
+        self.held = held
+
+    def _sharing(self):
+        if not self.shares:
+            raise ValueError("sequences of this cache have their own pages: give it a number of `pages` to share")
+
+    def release(self, sequences):
+        """The sequences have no tokens any more; their pages are free, but for those that others share."""
+        import torch
+        self._sharing()
+        n, gone = len(self.lengths), set(sequences)
+        if not gone <= set(range(n)):
+            raise ValueError(f"sequences {sorted(gone)} of {n}")
+        ends = torch.tensor([0] * n + [(1 << 31) - 1 if b in gone else 0 for b in range(n)], dtype=torch.int32).to("cuda").view(2, n)
+        B.ac_op_pages_update(self.books, self.books, self.books_workspace, drop=(ends[0], ends[1]))
+        for b in gone:
+            self.lengths[b] = self.held[b] = 0
+
+    def fork(self, parents, lengths=None):
+        """Sequence j goes on as sequence parents[j] (or, -1, has no tokens).  parents may be on the device (int32), with the lengths, that it does not tell, by the caller."""
+        import torch
+        self._sharing()
+        n = len(self.lengths)
+        if lengths is None:
+            parents = [int(p) for p in parents]
+            if len(parents) != n or not all(-1 <= p < n for p in parents):
+                raise ValueError(f"parents {parents} of {n} sequences")
+            lengths = [self.lengths[p] if p >= 0 else 0 for p in parents]
+            held = [self.held[p] if p >= 0 else 0 for p in parents]
+        else:
+            held = [max(self.held)] * n
+        if len(lengths) != n:
+            raise ValueError(f"{len(lengths)} lengths of {n} sequences")
+        if not torch.is_tensor(parents):
+            parents = torch.tensor(parents, dtype=torch.int32).to("cuda")
+        now = torch.tensor(self.lengths, dtype=torch.int32).to("cuda")
+        B.ac_op_cache_fork(self.all_caches, self.books, self.next_books, parents, now, torch.empty_like(now), self.books_workspace, self.missing)
+        self._enough(held)
+        # (the graph of a step knows the table by its address)
+        self.table.copy_(self.next_table)
+        self.uses.copy_(self.next_uses)
+        self.lengths = list(lengths)
+
+    def compact(self):
+        """Moves the pages in use to the front of the cache; how many they are, on the device."""
+        import torch
+        self._sharing()
+        used = torch.empty(1, dtype=torch.int32, device="cuda")
+        B.ac_op_cache_compact(self.all_caches, self.books, self.books, self.books_workspace, used)
+        return used
 
     def _heads(self, n):
         """A place for n rows' queries, keys and values, and the three as views of it."""
@@ -98,6 +191,8 @@ class Decoder:
     def _workspace_bytes(self, n, rows):
         import torch
         q = torch.empty((n, self.cfg.heads * self.cfg.head_dim), dtype=self.dtype, device="meta")       # (of which sizes and type are read)
+        if self.window is not None:
+            return B.ac_cache_attention_window_workspace_bytes(q, self.caches[0], rows, self.window, self.sinks)
         return B.ac_cache_attention_workspace_bytes(q, self.caches[0], rows)
 
     def _run(self, x, rows, workspace):
@@ -111,7 +206,10 @@ class Decoder:
             B.ac_op_layernorm(x, w["ln1_g"], w["ln1_b"], u, cfg.ln_eps)
             self._linear(w, "qkv", u, qkv)
             B.ac_op_cache_append(k, v, cache, rows, q=q, q_out=q, rotary=self.rotary)
-            B.ac_op_cache_attention(q, ctx, cache, rows, workspace=workspace)
+            if self.window is None:
+                B.ac_op_cache_attention(q, ctx, cache, rows, workspace=workspace)
+            else:
+                B.ac_op_cache_attention_window(q, ctx, cache, rows, self.window, self.sinks, workspace=workspace)
             self._linear(w, "o", ctx, x, residual=x)
             B.ac_op_layernorm(x, w["ln2_g"], w["ln2_b"], u, cfg.ln_eps)
             self._linear(w, "1", u, mid, activation=act)
@@ -131,9 +229,19 @@ class Decoder:
         # once without a page, which leaves the cache as it is: kernels are loaded before the capture
         self._run(x.clone(), B.cache_rows(begin, length, torch.full_like(self.table, -1), 1, self.max_tokens), workspace)
         torch.cuda.synchronize()
+        if self.shares:
+            before, drop_begin, drop_end = torch.empty_like(length), torch.full_like(length, self.sinks), torch.zeros_like(length)
+            B.ac_op_pages_update(self.books, self.books, self.books_workspace, (drop_end, drop_end), (drop_end, drop_end), self.missing)
+        torch.cuda.synchronize()
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
+            if self.shares:
+                torch.add(length, 0, out=before)
+                if self.window is not None:
+                    torch.sub(length, self.window - 1, out=drop_end)
             length.add_(1)
+            if self.shares:
+                B.ac_op_pages_update(self.books, self.books, self.books_workspace, (drop_begin, drop_end), (before, length), self.missing)
             y = self._run(x.clone(), rows, workspace)
         on_device = None
 
@@ -147,11 +255,99 @@ class Decoder:
                 length.copy_(torch.tensor(self.lengths, dtype=torch.int32))
             x.copy_(new)
             graph.replay()
+            if self.shares:
+                on_device = None                                        # (where pages are missing lengths are copied again)
+                self._enough(self._places([t + 1 for t in self.lengths]))
             self.lengths = [t + 1 for t in self.lengths]
             on_device = list(self.lengths)                              # (the caller may change the other one in place)
             return y
-        step.keep = (graph, workspace, rows, begin)
+        step.keep = (graph, workspace, rows, begin) + ((before, drop_begin, drop_end) if self.shares else ())
         return step
+
+
+class BeamSearch:
+    """Beam search with a Decoder whose sequences share pages: sequences p * beams .. (p + 1) * beams - 1 are prompt p's.  embedding [vocab, d_model] makes rows of tokens; the logits of a row y are head y (+
+    bias), head [vocab, d_model] in 4 bits.  end: the token that ends a sequence (-1: none does); one that ended stays among the beams with the sum that it has."""
+
+    def __init__(self, model, embedding, head, beams, bias=None, end=-1):
+        import torch
+        model._sharing()
+        self.model, self.beams, self.end = model, beams, end
+        self.prompts, left = divmod(len(model.lengths), beams)
+        vocab, d = embedding.shape
+        if left or d != model.cfg.d_model or head.shape != (vocab, d) or not -1 <= end < vocab:
+            raise ValueError(f"{len(model.lengths)} sequences, {beams} beams, embedding {tuple(embedding.shape)}, head {tuple(head.shape)}, end {end}")
+        dev = lambda t: torch.as_tensor(t, device="cuda")  # noqa: E731
+        self.embedding, self.head = dev(embedding).to(model.dtype).contiguous(), quantize_w4(dev(head), model.group, model.dtype)
+        self.bias = None if bias is None else dev(bias).to(model.dtype)
+        n = len(model.lengths)
+        self.logits = torch.empty((n, vocab), dtype=model.dtype, device="cuda")
+        self.workspace = B.empty_workspace(B.ac_beam_select_workspace_bytes(self.logits, beams, beams))
+        self.scores, self.ended = None, None
+
+    def _logits(self, y):
+        codes, scale, zero = self.head
+        B.ac_op_linear_w4(y, codes, scale, self.logits, self.model.group, zero=zero, bias=self.bias)
+
+    def start(self, prompts, stretch=512):
+        """Reads the prompts, lists of tokens, each into its first beam, `stretch` tokens at a time."""
+        import torch
+        m, k = self.model, self.beams
+        if len(prompts) != self.prompts or not all(prompts):
+            raise ValueError(f"{self.prompts} prompts of one token at least are wanted")
+        m.release(range(len(m.lengths)))
+        y = torch.zeros((self.prompts * k, m.cfg.d_model), dtype=m.dtype, device="cuda")
+        for at in range(0, max(len(p) for p in prompts), stretch):
+            now = [p[at:at + stretch] for p in prompts]
+            rows = self.embedding[torch.tensor(sum(now, []), device="cuda")]
+            out = m.forward(rows, [len(now[b // k]) if b % k == 0 else 0 for b in range(len(m.lengths))])
+            row = 0
+            for p, part in enumerate(now):
+                row += len(part)
+                if part:
+                    y[p * k] = out[row - 1]
+        self._logits(y)
+        self.scores = torch.full((self.prompts, k), float("-inf"), device="cuda")
+        self.scores[:, 0] = 0
+        self.ended = None if self.end < 0 else torch.zeros((self.prompts, k), dtype=torch.int32, device="cuda")
+        self.steps = []
+
+    def step(self):
+        """Chooses the beams' next tokens and reads them: (parent, token), int32 [prompts, beams] on the device."""
+        import torch
+        m, k = self.model, self.beams
+        i32 = dict(dtype=torch.int32, device="cuda")
+        scores, parent, token = torch.empty_like(self.scores), torch.empty((self.prompts, k), **i32), torch.empty((self.prompts, k), **i32)
+        ended = None if self.ended is None else torch.empty_like(self.ended)
+        B.ac_op_beam_select(self.logits, self.scores, scores, parent, token, self.workspace, ended=self.ended, ended_out=ended, end=self.end)
+        # all beams of a prompt have its length (a beam that is none, too: what it reads has no weight)
+        m.fork(parent.view(-1), [m.lengths[b // k * k] for b in range(len(m.lengths))])
+        y = m.forward(self.embedding[token.view(-1).clamp(min=0).long()], [1] * len(m.lengths))
+        self._logits(y)
+        self.scores, self.ended = scores, ended
+        self.steps.append((parent, token))
+        return parent, token
+
+    def found(self):
+        """[[(sum of logarithms, tokens)]] of each prompt, best first; tokens up to and with the end."""
+        scores = self.scores.tolist()
+        steps = [(p.view(-1).tolist(), t.view(-1).tolist()) for p, t in self.steps]
+        result = []
+        for p in range(self.prompts):
+            beams = []
+            for i in range(self.beams):
+                b, tokens = p * self.beams + i, []
+                for parent, token in reversed(steps):
+                    if b >= 0:
+                        tokens.append(token[b])
+                        b = parent[b]
+                tokens.reverse()
+                if self.end in tokens:
+                    tokens = tokens[:tokens.index(self.end) + 1]
+                if scores[p][i] > float("-inf"):
+                    beams.append((scores[p][i], tokens))
+            result.append(beams)
+        return result
 
 
 def main():
@@ -162,10 +358,17 @@ def main():
     ap.add_argument("--prompt", type=int, default=1024)
     ap.add_argument("--stretch", type=int, default=512, help="tokens of a sequence read at once")
     ap.add_argument("--steps", type=int, default=32)
+    ap.add_argument("--window", type=int, help="tokens that a row sees, besides the sinks")
+    ap.add_argument("--sinks", type=int, default=0)
+    ap.add_argument("--beams", type=int, default=0, help="time a beam search, too")
+    ap.add_argument("--vocab", type=int, default=32768)
     args = ap.parse_args()
     cfg = I.CONFIGS[args.config]
     x, layers = I.transformer_inputs(dataclasses.replace(cfg, batch=1, seq=args.batch * args.prompt))
-    model = Decoder(cfg, layers, args.batch, args.prompt + args.steps + 2 * args.stretch)
+    most, page = args.prompt + args.steps + 2 * args.stretch + (0 if args.window is None else args.steps + 1), 64
+    # behind a window a sequence holds its sinks, its window and a stretch
+    pages = None if args.window is None else args.batch * (-(-args.sinks // page) + -(-(args.window + args.stretch) // page) + 2)
+    model = Decoder(cfg, layers, args.batch, most, page, window=args.window, sinks=args.sinks, pages=pages)
     x = torch.as_tensor(x, device="cuda").to(model.dtype).view(args.batch, args.prompt, -1)
 
     def read(first, n):
@@ -188,15 +391,37 @@ def main():
             y = step(y)
         return y
 
+    def anew(lengths):
+        if model.shares and not any(lengths):
+            model.release(range(args.batch))
+        model.lengths = lengths
+
     read(0, min(args.stretch, args.prompt))                             # code and clocks
-    model.lengths = [0] * args.batch
+    anew([0] * args.batch)
     y, reading = timed(prompt)
     y, writing = timed(lambda: steps(y, lambda x: model.forward(x, [1] * args.batch)))
     step = model.step_graph()
     step(y)
-    model.lengths = [args.prompt] * args.batch
+    if not model.shares:
+        anew([args.prompt] * args.batch)
     y, replaying = timed(lambda: steps(y, step))
-    print(json.dumps({"config": cfg.name, "layers": cfg.layers, "dtype": cfg.dtype, "weights": "4 bits", "cache": "8 bits", "batch": args.batch,
+    found = {}
+    if args.beams:
+        each = -(-(args.prompt + args.steps) // page)
+        shared = Decoder(cfg, layers, args.batch * args.beams, args.prompt + args.steps, page, window=args.window, sinks=args.sinks,
+                         pages=args.batch * (each + 2 * args.beams * (2 + args.steps // page)))
+        g = torch.Generator(device="cuda")
+        g.manual_seed(1)
+        embedding, head = (torch.randn((args.vocab, cfg.d_model), generator=g, device="cuda") * s for s in (1.0, cfg.d_model ** -0.5))
+        search = BeamSearch(shared, embedding, head, args.beams)
+        prompts = torch.randint(0, args.vocab, (args.batch, args.prompt), generator=g, device="cuda").tolist()
+        search.start(prompts, args.stretch)
+        search.step()
+        _, searching = timed(lambda: [search.step() for _ in range(args.steps - 1)])
+        best = search.found()
+        found = {"beams": args.beams, "vocab": args.vocab, "beam_ms_per_step": round(searching / max(1, args.steps - 1) * 1e3, 3),
+                 "beam_tokens": [len(best[0][0][1]), min(len(b) for b in best)]}
+    print(json.dumps(found | {"config": cfg.name, "layers": cfg.layers, "dtype": cfg.dtype, "weights": "4 bits", "cache": "8 bits", "batch": args.batch,
                       "prompt": args.prompt, "prompt_tokens_per_s": round(args.batch * args.prompt / reading, 1), "steps": args.steps,
                       "tokens_per_s": round(args.batch * args.steps / writing, 1), "ms_per_step": round(writing / args.steps * 1e3, 3),
                       "graph_tokens_per_s": round(args.batch * args.steps / replaying, 1), "graph_ms_per_step": round(replaying / args.steps * 1e3, 3),

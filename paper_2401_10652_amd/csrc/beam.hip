@@ -1,6 +1,8 @@
 // Beam search's selection.  A candidate is (beam i, token t) with total = score[i] + x[i, t] - log sum_t exp x[i, t]; within a beam totals are in the order of the logits, so a
 // run of a row needs its `keep` largest logits and, for the sum, its maximum and the sum of exponentials behind it: one pass over the logits, which HBM bounds.  A second
 // kernel puts a prompt's runs together and ranks their candidates by totals in 64 bits: of two beams' candidates the larger is wanted, however close they are.
+#include <float.h>
+
 #include "common.h"
 
 namespace ac {
@@ -8,235 +10,364 @@ namespace ac {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kThreads = 256, kWaves = kThreads / kWave, kMostCandidates = 512;
+constexpr int kThreads = 256, kWaves = kThreads / kWave, kRoom = 128, kMostCandidates = 512;
 
 struct BeamArgs {
   const void* logits; int64_t ld;
   const float* scores; const int32_t* ended;
   float* scores_out; int32_t *parent, *token, *ended_out;
-  int beams, vocab, keep, end, splits;
-  int group;                          // lanes that share a maximum when the border is looked for
-  float* sums;                        // [rows][splits][2]: maximum, sum of exponentials
-  float* value; int32_t* index;       // [rows][splits][keep], largest first; -inf where there are no more
+  int beams, vocab, keep, end;
+  int runs, steps;                    // runs of a row, and steps of a run
+  Divisor of_beam, of_keep;           // runs, keep
+  float* sums;                        // [rows][runs][2]: maximum, sum of exponentials
+  float* value; int32_t* index;       // [rows][runs][keep], largest first; -inf where there are no more
 };
 
-// (a, i) before (b, j): the larger, of equal ones the lower index
-template <typename V> __device__ __forceinline__ bool before(V a, int i, V b, int j) { return a > b || (a == b && i < j); }
+// (a, i) before (b, j): the larger, of equal ones the lower index.  (Without a branch: one for each comparison takes 80 cycles of a candidate's count.)
+__device__ __forceinline__ bool before(double a, int i, double b, int j) { return (a > b) | ((a == b) & (i < j)); }
+// The same of a logit and its index as one number: the larger comes first.  0: none.
+typedef unsigned long long Key;
+__device__ __forceinline__ Key key_of(float v, int index) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, v + 0.f);               // (one zero)
+  return (Key)(u ^ ((int)u < 0 ? 0xffffffffu : 0x80000000u)) << 32 | ~(uint32_t)index;
+}
+__device__ __forceinline__ float value_of_key(Key k) {
+  const uint32_t u = (uint32_t)(k >> 32);
+  return __builtin_bit_cast(float, u ^ ((int)u < 0 ? 0x80000000u : 0xffffffffu));
+}
+__device__ __forceinline__ int index_of_key(Key k) { return (int)~(uint32_t)k; }
 
-template <typename V> struct Found { V value[kMostCandidates]; int index[kMostCandidates]; V most[kThreads / 2]; V border; int count; V wave_value[kWaves]; int wave_index[kWaves]; };
-
-// The `keep` first of the block's candidates: each(f) calls f(value, index) for all of a thread's own, `most` is the largest of them (-inf without any); put(rank, value, index)
-// takes them.  The border: of the maxima over groups of lanes, twice as many as are kept, the keep-th largest; at least that many candidates reach it, and few
-// more do, of which each counts those before it.  Where more do than there is room for (as many equal ones), the first are looked for one after another.  Returns how many there are.
-template <typename V, typename Each, typename Put>
-__device__ __forceinline__ int first_ones(Found<V>& s, int keep, int group, V most, Each each, Put put) {
-  const V none = -(V)INFINITY;
-  const int tid = threadIdx.x, groups = kThreads / group;
-  V top = most;
-  for (int o = 1; o < group; o <<= 1) top = fmax(top, __shfl_xor(top, o, kWave));
-  if (tid % group == 0) s.most[tid / group] = top;
-  if (tid == 0) s.count = 0;
-  __syncthreads();
-  if (tid < groups) {
-    const V mine = s.most[tid];
-    int rank = 0;
-    for (int j = 0; j < groups; ++j) rank += before(s.most[j], j, mine, tid);
-    if (rank == keep - 1) s.border = mine;
-  }
-  __syncthreads();
-  const V border = s.border;
-  if (most >= border)
-    each([&](V v, int i) {
-      if (v >= border && v > none) {
-        const int at = atomicAdd(&s.count, 1);
-        if (at < kMostCandidates) {
-          s.value[at] = v;
-          s.index[at] = i;
-        }
-      }
-    });
-  __syncthreads();
-  const int count = s.count;
-  if (count <= kMostCandidates) {
-    for (int c = tid; c < count; c += kThreads) {
-      const V v = s.value[c];
-      const int i = s.index[c];
-      int rank = 0;
-      for (int j = 0; j < count; ++j) rank += before(s.value[j], s.index[j], v, i);
-      if (rank < keep) put(rank, v, i);
-    }
-    __syncthreads();
-    return count < keep ? count : keep;
-  }
-  V last = (V)INFINITY;
-  int last_index = -1;
-  for (int k = 0; k < keep; ++k) {
-    V v = none;
-    int i = 0x7fffffff;
-    each([&](V a, int j) {
-      if (before(last, last_index, a, j) && before(a, j, v, i)) { v = a; i = j; }
-    });
-    for (int o = kWave / 2; o > 0; o >>= 1) {
-      const V a = __shfl_xor(v, o, kWave);
-      const int j = __shfl_xor(i, o, kWave);
-      if (before(a, j, v, i)) { v = a; i = j; }
-    }
-    if (tid % kWave == 0) { s.wave_value[tid / kWave] = v; s.wave_index[tid / kWave] = i; }
-    __syncthreads();
-    v = s.wave_value[0]; i = s.wave_index[0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w)
-      if (before(s.wave_value[w], s.wave_index[w], v, i)) { v = s.wave_value[w]; i = s.wave_index[w]; }
-    __syncthreads();
-    if (!(v > none)) return k;
-    if (tid == 0) put(k, v, i);
-    last = v;
-    last_index = i;
-  }
-  return keep;
+// The next number above a finite one.
+__device__ __forceinline__ float above(float v) {
+  const int i = __builtin_bit_cast(int, v);
+  return __builtin_bit_cast(float, v == 0.f ? 1 : i < 0 ? i - 1 : i + 1);
 }
 
 // 16 bytes that may begin at any element.
-__device__ __forceinline__ void load_anywhere(const float* p, float (&v)[4]) {
+__device__ __forceinline__ void load_anywhere(const float* p, f32x4& v) {
   typedef f32x4 any_f32x4 __attribute__((aligned(4)));
-  const f32x4 t = *reinterpret_cast<const any_f32x4*>(p);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = t[i];
+  v = *reinterpret_cast<const any_f32x4*>(p);
 }
-__device__ __forceinline__ void load_anywhere(const bf16_t* p, float (&v)[8]) {
+__device__ __forceinline__ void load_anywhere(const bf16_t* p, bf16x8& v) {
   typedef bf16x8 any_bf16x8 __attribute__((aligned(2)));
-  const bf16x8 t = *reinterpret_cast<const any_bf16x8*>(p);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = bf2f(t[i]);
+  v = *reinterpret_cast<const any_bf16x8*>(p);
+}
+template <typename T> struct Vec;
+template <> struct Vec<float> { typedef f32x4 type; };
+template <> struct Vec<bf16_t> { typedef bf16x8 type; };
+
+// A run's largest logits as they are found: more than are kept, and cut down to these where room runs out.
+struct Largest { Key key[kRoom]; };
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 }
 
-// One block: 256 * NV vectors of 16 bytes of one row, in registers.  They are counted from the row's begin, wherever that lies, so that equal rows give equal sums.
-template <typename T, int NV>
+// One wave: a run of a row, `steps` steps of U vectors of 16 bytes a lane, the next step's on their way while a step's are used.  Vectors are counted from the row's begin,
+// wherever that lies, so that equal rows give equal sums; one that would pass the row's end is the row's last one, without what the lanes before have of it.  A lane's exponents have its own
+// maximum for reference.  A logit is a candidate if it reaches `least`, which lies above the keep-th largest of those that were there when they were last looked at: at first it is the
+// keep-th largest of the maxima over groups of lanes, twice as many as are kept, so that what reaches it is not much more than what is kept, and hardly anything of the later steps is.
+template <typename T, int U>
 __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
-  constexpr int VEC = Elem<T>::kVec;
-  __shared__ Found<float> found;
-  __shared__ float of_wave[kWaves][2];
-  const int64_t row = (int64_t)blockIdx.z * g.beams + blockIdx.y, part = row * g.splits + blockIdx.x;
-  if ((g.ended && g.ended[row] != 0) || !(g.scores[row] > -INFINITY)) return;       // (no candidate of its logits)
+  typedef typename Vec<T>::type V;
+  constexpr int VEC = Elem<T>::kVec, STEP = kWave * VEC * U;
+  __shared__ Largest all[kWaves];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), run = blockIdx.x * kWaves + wave;
+  const int64_t row = (int64_t)blockIdx.z * g.beams + blockIdx.y, part = row * g.runs + run;
+  if (run >= g.runs || (g.ended && g.ended[row] != 0) || !(g.scores[row] > -INFINITY)) return;       // (no candidate of its logits)
+  Largest& found = all[wave];
   const T* const from = (const T*)g.logits + row * g.ld;
-  const int tid = threadIdx.x, first = (blockIdx.x * kThreads * NV + tid) * VEC;
-  float x[NV][VEC], most = -INFINITY;
+  const int begin = run * g.steps * STEP, left = g.vocab - begin, steps = left < g.steps * STEP ? (left + STEP - 1) / STEP : g.steps, last = g.vocab - VEC;
+  auto place = [&](int step, int u) { return begin + step * STEP + (u * kWave + lane) * VEC; };
+  auto load = [&](V (&x)[U], int step) __attribute__((always_inline)) {
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int at = first + v * kThreads * VEC;
-    if (at <= g.vocab - VEC) {
-      load_anywhere(from + at, x[v]);
-    } else {
+    for (int u = 0; u < U; ++u) {
+      if (last >= 0) {
+        load_anywhere(from + min(place(step, u), last), x[u]);
+      } else {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[v][e] = at + e < g.vocab ? Elem<T>::ld(from + at + e) : -INFINITY;
+        for (int e = 0; e < VEC; ++e) x[u][e] = u == 0 && lane == 0 && e < g.vocab ? from[e] : (T)-INFINITY;
+      }
     }
+  };
+  float top = -INFINITY, sum = 0.f, border = -INFINITY;
+  int count = 0;
+  // keeps the `keep` largest, in order; the border is the last of them, if there are so many
+  auto cut = [&]() __attribute__((always_inline)) {
+    Key mine[2];
+    int rank[2] = {0, 0};
+    wave_fence();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) mine[h] = lane + h * kWave < count ? found.key[lane + h * kWave] : 0;
+#pragma unroll 4
+    for (int j = 0; j < count; ++j) {
+      const Key k = found.key[j];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) rank[h] += k > mine[h];
+    }
+    wave_fence();
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (rank[h] < g.keep && mine[h] != 0) found.key[rank[h]] = mine[h];
+    wave_fence();
+    if (count >= g.keep) {
+      count = g.keep;
+      border = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, value_of_key(found.key[g.keep - 1]))));
+    }
+  };
+  V next[U];
+  load(next, 0);
+  for (int step = 0; step < steps; ++step) {
+    float x[U][VEC], largest = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[u][e] = (float)next[u][e];
+    if (step + 1 < steps) load(next, step + 1);
+    else if (begin + steps * STEP > g.vocab && last >= 0) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int again = place(step, u) - last;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[u][e] = e < again ? -INFINITY : x[u][e];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) largest = fmaxf(largest, x[u][e]);      // (NaN is no maximum; it is in the sum)
+    if (largest > top) {
+      if (top > -INFINITY) sum *= __builtin_amdgcn_exp2f((top - largest) * kLog2e);
+      top = largest;
+    }
+    const float ref = top > -INFINITY ? top : 0.f;
+    if (!__any(top == INFINITY)) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum += __builtin_amdgcn_exp2f((x[u][e] - ref) * kLog2e);
+    } else {                                                          // infinities share the probability
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          sum += top < INFINITY ? __builtin_amdgcn_exp2f((x[u][e] - ref) * kLog2e) : x[u][e] == INFINITY ? 1.f : x[u][e] != x[u][e] ? x[u][e] : 0.f;
+    }
+    // (of equal ones the lower index comes first: what equals the border is a candidate if that may be of this step, and none if it is of one before)
+    float least;
+    if (step == 0) {
+      const int group = g.keep <= 8 ? 4 : g.keep <= 16 ? 2 : 1;
+      float m = largest;
+      if (group >= 2) m = fmaxf(m, __shfl_xor(m, 1, kWave));
+      if (group >= 4) m = fmaxf(m, __shfl_xor(m, 2, kWave));
+      int larger = 0;
+      for (int j = 0; j < kWave; j += group) larger += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, m), j)) > m;
+      least = fmaxf(-wave_max(larger < g.keep ? -m : -INFINITY), -FLT_MAX);       // (the least of those with fewer than `keep` larger ones)
+    } else {
+      least = border > -INFINITY ? above(border) : -FLT_MAX;
+    }
+    if (!__any(largest >= least)) continue;
+    const int before_step = count;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const uint64_t which = __ballot(x[u][e] >= least);
+        if (which != 0) {
+          const int at = count + __popcll(which & ((1ull << lane) - 1));
+          if ((which >> lane & 1) && at < kRoom) {
+            found.key[at] = key_of(x[u][e], min(place(step, u), max(last, 0)) + e);
+          }
+          count += __popcll(which);
+        }
+      }
+    if (count > kRoom) {
+      // more than there is room for: one number of each lane at a time, from memory
+      count = before_step;
+      for (int n = 0; n < U * VEC; ++n) {
+        const int at = place(step, n / VEC) + n % VEC;
+        const float v = at < g.vocab ? (float)from[at] : -INFINITY;
+        if (count + kWave > kRoom) {
+          cut();
+          least = fmaxf(least, border);
+        }
+        const uint64_t which = __ballot(v >= least);
+        if (which >> lane & 1) {
+          found.key[count + __popcll(which & ((1ull << lane) - 1))] = key_of(v, at);
+        }
+        count += __popcll(which);
+      }
+    }
+    cut();
   }
-#pragma unroll
-  for (int v = 0; v < NV; ++v)
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) most = fmaxf(most, x[v][e]);            // (NaN is no maximum; it is in the sum)
-  float sum = 0.f;
-  if (most < INFINITY) {
-    const float ref = most > -INFINITY ? most : 0.f;
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) sum += __builtin_amdgcn_exp2f((x[v][e] - ref) * kLog2e);
-  } else {                                                                // infinities share the probability
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) sum += x[v][e] == INFINITY ? 1.f : x[v][e] != x[v][e] ? x[v][e] : 0.f;
-  }
-  float top = wave_max(most);
-  auto scaled = [](float s, float m, float t) { return m == t ? s : s * __builtin_amdgcn_exp2f((m - t) * kLog2e); };
-  sum = wave_sum(scaled(sum, most, top));
-  if (tid % kWave == 0) { of_wave[tid / kWave][0] = top; of_wave[tid / kWave][1] = sum; }
+  // (what was found is in order since the last cut, if there was one)
   const int64_t list = part * g.keep;
-  const int n = first_ones(found, g.keep, g.group, most, [&](auto f) __attribute__((always_inline)) {
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) f(x[v][e], first + v * kThreads * VEC + e);
-  }, [&](int rank, float v, int i) {
-    g.value[list + rank] = v;
-    g.index[list + rank] = i;
-  });
-  for (int k = n + tid; k < g.keep; k += kThreads) g.value[list + k] = -INFINITY;
-  if (tid == 0) {
-    top = of_wave[0][0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, of_wave[w][0]);
-    sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) sum += scaled(of_wave[w][1], of_wave[w][0], top);
-    g.sums[part * 2] = top;
+  if (lane < g.keep) {
+    g.value[list + lane] = lane < count ? value_of_key(found.key[lane]) : -INFINITY;
+    if (lane < count) g.index[list + lane] = index_of_key(found.key[lane]);
+  }
+  const float of_all = wave_max(top);
+  sum = wave_sum(top == of_all ? sum : sum * __builtin_amdgcn_exp2f((top - of_all) * kLog2e));
+  if (lane == 0) {
+    g.sums[part * 2] = of_all;
     g.sums[part * 2 + 1] = sum;
   }
 }
 
-// One block: a prompt.
+// One block: a prompt.  What comes out is found among the entries that reach a border: the keep-th largest of the threads' largest ones, in 32 bits (as the entries compared with
+// it are, which keeps their order).  A thread has lists of runs, whose first entries are their largest, and goes down those that reach it; where fewer threads than what is kept have
+// any, it has single entries.  Each candidate then counts those before it.
 __global__ void __launch_bounds__(kThreads) beam_rank(BeamArgs g) {
-  __shared__ Found<double> found;
-  __shared__ double top[64], rest[64];      // of each beam the maximum, and score minus the logarithm of the sum behind it
-  const int tid = threadIdx.x, lane = tid % kWave, per = g.splits * g.keep, all = g.beams * per;
+  __shared__ double rest[64], done[64];     // of each beam its score minus the logarithm of its sum (behind the maximum); and the score of one that ended: -inf where there is none
+  __shared__ float top[64];
+  __shared__ __attribute__((aligned(16))) float largest[kThreads];
+  __shared__ int border_at, count_at;
+  __shared__ double value_of[kMostCandidates];
+  __shared__ int place_of[kMostCandidates];
+  __shared__ double wave_value[kWaves];
+  __shared__ int wave_place[kWaves];
+  const int tid = threadIdx.x, lane = tid % kWave, lists = g.beams * g.runs, entries = lists * g.keep;
   const int64_t row0 = (int64_t)blockIdx.x * g.beams;
+  const float* const value = g.value + row0 * g.runs * g.keep;
+  const int32_t* const index = g.index + row0 * g.runs * g.keep;
+  bool heads = lists >= 2 * g.keep;
+  const float ahead = tid < (heads ? lists : entries) ? value[heads ? tid * g.keep : tid] : 0.f;       // (on its way while the sums are looked at)
   for (int i = tid / kWave; i < g.beams; i += kWaves) {
-    const float* sums = g.sums + (row0 + i) * g.splits * 2;
+    const float* sums = g.sums + (row0 + i) * g.runs * 2;
     const float score = g.scores[row0 + i];
-    const bool dead = !(score > -INFINITY) || (g.ended && g.ended[row0 + i] != 0);
+    const bool gone = g.ended && g.ended[row0 + i] != 0, dead = gone || !(score > -INFINITY);
     float m = -INFINITY;
     double sum = 0;
     if (!dead) {
-      for (int p = lane; p < g.splits; p += kWave) m = fmaxf(m, sums[2 * p]);
+      const f32x2 near = *reinterpret_cast<const f32x2*>(sums + 2 * (lane < g.runs ? lane : 0));
+      m = near[0];
+      for (int p = lane + kWave; p < g.runs; p += kWave) m = fmaxf(m, sums[2 * p]);
       m = wave_max(m);
-      for (int p = lane; p < g.splits; p += kWave) sum += sums[2 * p] == m ? (double)sums[2 * p + 1] : (double)sums[2 * p + 1] * exp((double)sums[2 * p] - (double)m);
+      for (int p = lane; p < g.runs; p += kWave) {
+        const f32x2 part = p == lane ? near : *reinterpret_cast<const f32x2*>(sums + 2 * p);
+        sum += part[0] == m ? (double)part[1] : (double)part[1] * exp((double)part[0] - (double)m);
+      }
 #pragma unroll
       for (int o = kWave / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+      sum = (double)score - log(sum);
     }
     if (lane == 0) {
       top[i] = m;
-      rest[i] = dead ? -INFINITY : (double)score - log(sum);
+      rest[i] = dead || !(sum > -INFINITY) ? -INFINITY : sum;
+      done[i] = gone && score > -INFINITY ? score : -INFINITY;
     }
   }
+  if (tid == 0) { count_at = 0; border_at = 0x7fffffff; }
   __syncthreads();
-  // entry e of the prompt's lists
-  auto entry = [&](int e, double& total, int& place) {
-    const int i = e / per, in = e - i * per;
-    total = -INFINITY;
-    place = i * g.vocab;
-    if (g.ended && g.ended[row0 + i] != 0) {
-      if (in == 0) { total = g.scores[row0 + i]; place += g.end; }
-    } else if (rest[i] > -INFINITY) {
-      const float v = g.value[row0 * per + e];
-      if (v > -INFINITY) {
-        total = v == (float)top[i] ? rest[i] : (double)v - top[i] + rest[i];
-        place += g.index[row0 * per + e];
+  auto total_of = [&](int list, float v) {
+    const int i = quotient(list, g.of_beam);
+    const double r = rest[i];
+    return r > -INFINITY && v > -INFINITY ? v == top[i] ? r : (double)v - top[i] + r : -INFINITY;
+  };
+  const double mine = tid < g.beams ? done[tid] : -INFINITY;
+  auto most_of = [&](int items) {
+    double most = mine;
+    for (int item = tid; item < items; item += kThreads)
+      most = fmax(most, total_of(heads ? item : quotient(item, g.of_keep), item == tid && items == (lists >= 2 * g.keep ? lists : entries) ? ahead : value[heads ? item * g.keep : item]));
+    return (float)most;
+  };
+  float most = most_of(heads ? lists : entries);
+  if (heads && __syncthreads_count(most > -INFINITY) < g.keep) {
+    heads = false;
+    most = most_of(entries);
+  }
+  // f of all of the thread's own entries, down a list up to the first for which it is false
+  auto each = [&](auto f) {
+    if (mine > -INFINITY) f(mine, tid * g.vocab + g.end);
+    const int items = heads ? lists : entries, down = heads ? g.keep : 1;
+    for (int item = tid; item < items; item += kThreads) {
+      const int list = heads ? item : quotient(item, g.of_keep), at = heads ? item * g.keep : item, place = quotient(list, g.of_beam) * g.vocab;
+      for (int k = 0; k < down; ++k) {
+        const double total = total_of(list, value[at + k]);
+        if (!(total > -INFINITY) || !f(total, place + index[at + k])) break;
       }
     }
   };
-  double most = -INFINITY;
-  for (int e = tid; e < all; e += kThreads) {
-    double total;
-    int place;
-    entry(e, total, place);
-    most = fmax(most, total);
+  // the least of the groups' maxima with fewer than `keep` larger ones; as an integer in the order of the floats
+  const int all_items = heads ? lists : entries, holders = all_items < kThreads ? all_items : kThreads, group = holders >= 32 * g.keep ? 4 : holders >= 16 * g.keep ? 2 : 1, groups = (holders + group - 1) / group;
+  float most_of_group = most;
+  if (group >= 2) most_of_group = fmaxf(most_of_group, __shfl_xor(most_of_group, 1, kWave));
+  if (group >= 4) most_of_group = fmaxf(most_of_group, __shfl_xor(most_of_group, 2, kWave));
+  largest[tid] = -INFINITY;
+  __syncthreads();
+  if (tid % group == 0) largest[tid / group] = most_of_group;
+  __syncthreads();
+  int larger = 0;
+#pragma unroll 2
+  for (int j = 0; j < groups; j += 4) {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(&largest[j]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) larger += a[e] > most_of_group;
   }
+  const int bits = __builtin_bit_cast(int, most_of_group + 0.f);
+  if (larger < g.keep) atomicMin(&border_at, bits < 0 ? bits ^ 0x7fffffff : bits);
+  __syncthreads();
+  const int border_bits = border_at;
+  const float border = __builtin_bit_cast(float, border_bits < 0 ? border_bits ^ 0x7fffffff : border_bits);
+  if (most >= border)
+    each([&](double v, int place) {
+      if ((float)v < border) return false;
+      const int at = atomicAdd(&count_at, 1);
+      if (at < kMostCandidates) {
+        value_of[at] = v;
+        place_of[at] = place;
+      }
+      return true;
+    });
+  __syncthreads();
   const int64_t out = (int64_t)blockIdx.x * g.keep;
-  const int n = first_ones(found, g.keep, g.group, most, [&](auto f) {
-    for (int e = tid; e < all; e += kThreads) {
-      double total;
-      int place;
-      entry(e, total, place);
-      f(total, place);
-    }
-  }, [&](int rank, double total, int place) {
+  auto put = [&](int k, double total, int place) {
     const int i = place / g.vocab, t = place - i * g.vocab;
-    g.scores_out[out + rank] = (float)total;
-    g.parent[out + rank] = (int)(row0 + i);
-    g.token[out + rank] = t;
-    if (g.ended_out) g.ended_out[out + rank] = t == g.end || (g.ended && g.ended[row0 + i] != 0);
-  });
+    g.scores_out[out + k] = (float)total;
+    g.parent[out + k] = (int)(row0 + i);
+    g.token[out + k] = t;
+    if (g.ended_out) g.ended_out[out + k] = t == g.end || done[i] > -INFINITY;
+  };
+  const int count = count_at;
+  int n = count < g.keep ? count : g.keep;
+  if (count <= kMostCandidates) {
+    for (int c = tid; c < count; c += kThreads) {
+      const double v = value_of[c];
+      const int place = place_of[c];
+      int k = 0;
+      for (int j = 0; j < count; ++j) k += before(value_of[j], place_of[j], v, place);
+      if (k < g.keep) put(k, v, place);
+    }
+  } else {
+    // as many equal ones: the first of those that are left, again and again
+    double last = INFINITY;
+    int last_place = -1;
+    for (n = 0; n < g.keep; ++n) {
+      double v = -INFINITY;
+      int place = 0x7fffffff;
+      each([&](double a, int at) {
+        if (before(last, last_place, a, at) && before(a, at, v, place)) { v = a; place = at; }
+        return true;
+      });
+#pragma unroll
+      for (int o = kWave / 2; o > 0; o >>= 1) {
+        const double a = __shfl_xor(v, o, kWave);
+        const int at = __shfl_xor(place, o, kWave);
+        if (before(a, at, v, place)) { v = a; place = at; }
+      }
+      if (lane == 0) { wave_value[tid / kWave] = v; wave_place[tid / kWave] = place; }
+      __syncthreads();
+      v = wave_value[0]; place = wave_place[0];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w)
+        if (before(wave_value[w], wave_place[w], v, place)) { v = wave_value[w]; place = wave_place[w]; }
+      __syncthreads();
+      if (!(v > -INFINITY)) break;
+      if (tid == 0) put(n, v, place);
+      last = v;
+      last_place = place;
+    }
+  }
   for (int k = n + tid; k < g.keep; k += kThreads) {
     g.scores_out[out + k] = -INFINITY;
     g.parent[out + k] = g.token[out + k] = -1;
@@ -244,29 +375,31 @@ __global__ void __launch_bounds__(kThreads) beam_rank(BeamArgs g) {
   }
 }
 
-struct Shape { int vectors, splits; };
+// Steps of U vectors of 16 bytes a lane, and runs of so many steps that there are enough of them to fill the chip.
+struct Shape { int vectors, steps, runs; };
 Shape shape(int64_t rows, int64_t vocab, int dtype) {
-  const int vec = dtype == AC_BF16 ? 8 : 4;
-  Shape s{4, 0};
-  auto splits = [&](int v) { return (int)((vocab + kThreads * vec * v - 1) / (kThreads * vec * v)); };
-  while (s.vectors > 1 && rows * splits(s.vectors) < 1024) s.vectors /= 2;
-  s.splits = splits(s.vectors);
+  const int64_t vec = kWave * (dtype == AC_BF16 ? 8 : 4);
+  Shape s{4, 1, 0};
+  auto runs = [&]() { return (vocab + vec * s.vectors * s.steps - 1) / (vec * s.vectors * s.steps); };
+  while (s.vectors > 1 && rows * runs() < 128) s.vectors /= 2;
+  while (s.steps < 16 && rows * runs() >= 8192) s.steps *= 2;
+  s.runs = (int)runs();
   return s;
 }
 
 }  // namespace
 
 uint64_t beam_select_workspace_bytes(int64_t batch, int beams, int64_t vocab, int keep, int dtype) {
-  return (uint64_t)(batch * beams) * shape(batch * beams, vocab, dtype).splits * (2 + 2 * keep) * 4;
+  return (uint64_t)(batch * beams) * shape(batch * beams, vocab, dtype).runs * (2 + 2 * keep) * 4;
 }
 
 hipError_t launch_beam_select(const BeamSelectArgs& b, hipStream_t s) {
   const Shape sh = shape(b.batch * b.beams, b.vocab, b.dtype);
-  const int64_t parts = b.batch * b.beams * sh.splits;
+  const int64_t parts = b.batch * b.beams * sh.runs;
   float* const w = (float*)b.workspace;
-  BeamArgs g{b.logits, b.ld, b.scores, b.ended, b.scores_out, b.parent, b.token, b.ended_out, b.beams, (int)b.vocab, b.keep, b.end, sh.splits,
-             b.keep <= 8 ? 16 : b.keep <= 16 ? 8 : b.keep <= 32 ? 4 : 2, w, w + 2 * parts, (int32_t*)(w + (2 + b.keep) * parts)};
-  const dim3 grid((unsigned)sh.splits, (unsigned)b.beams, (unsigned)b.batch);
+  BeamArgs g{b.logits, b.ld, b.scores, b.ended, b.scores_out, b.parent, b.token, b.ended_out, b.beams, (int)b.vocab, b.keep, b.end, sh.runs, sh.steps,
+             divisor((uint32_t)sh.runs), divisor((uint32_t)b.keep), w, w + 2 * parts, (int32_t*)(w + (2 + b.keep) * parts)};
+  const dim3 grid((unsigned)((sh.runs + kWaves - 1) / kWaves), (unsigned)b.beams, (unsigned)b.batch);
   auto scan = [&](auto zero) {
     using T = decltype(zero);
     if (sh.vectors == 4) hipLaunchKernelGGL((beam_scan<T, 4>), grid, dim3(kThreads), 0, s, g);

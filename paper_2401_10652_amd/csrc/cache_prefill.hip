@@ -356,11 +356,20 @@ __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(
       return false;
     };
     if (nan_at[HD] != 0x7fffffff) {
+      uint64_t meets = 0, more = 0;                               // (as bits, by a loop that is not unrolled: 64 copies of it take the registers of the sums)
+      if (WINDOWED) {
+#pragma unroll 1
+        for (int n = 0; n < DT * 16; ++n) {
+          const uint64_t bit = (uint64_t)meets_nan(n / 16 * 32 + 8 * (n % 16 / 4) + 4 * half + n % 4) << n % 64;
+          if (n < 64) meets |= bit;
+          else more |= bit;
+        }
+      }
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (WINDOWED ? meets_nan(d * 32 + 8 * (i / 4) + 4 * half + i % 4) : nan_at[d * 32 + 8 * (i / 4) + 4 * half + i % 4] < sees) o[d][i] = __builtin_nanf("");
+          if (WINDOWED ? ((d < 4 ? meets : more) >> (d % 4 * 16 + i) & 1) != 0 : nan_at[d * 32 + 8 * (i / 4) + 4 * half + i % 4] < sees) o[d][i] = __builtin_nanf("");
     }
 
     // the second half of the keys to LDS (pieces of four elements turned by the row, against bank conflicts), the first joins

@@ -9,7 +9,7 @@ namespace ac {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kNear = 1e38f;
 constexpr int kThreads = 256, kWaves = kThreads / kWave, kRoom = 128, kMostCandidates = 512;
 
 struct BeamArgs {
@@ -58,6 +58,15 @@ template <> struct Vec<bf16_t> { typedef bf16x8 type; };
 
 // A run's largest logits as they are found: more than are kept, and cut down to these where room runs out.
 struct Largest { Key key[kRoom]; };
+// Over the wave, by rotations within sixteen lanes.
+__device__ __forceinline__ float max_of_wave(float v) {
+  v = fmaxf(v, rotate_row<8>(v));
+  v = fmaxf(v, rotate_row<4>(v));
+  v = fmaxf(v, rotate_row<2>(v));
+  v = fmaxf(v, rotate_row<1>(v));
+  auto of = [&](int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); };
+  return fmaxf(fmaxf(of(0), of(16)), fmaxf(of(32), of(48)));
+}
 __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
@@ -90,7 +99,8 @@ __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
       }
     }
   };
-  float top = -INFINITY, sum = 0.f, border = -INFINITY;
+  // sum: of 2^(x log2 e - c) with c = top log2 e as it is rounded, which the end makes good; or, of a maximum past kNear, of e^(x - top)
+  float top = -INFINITY, c = 0.f, sum = 0.f, border = -INFINITY;
   int count = 0;
   // keeps the `keep` largest, in order; the border is the last of them, if there are so many
   auto cut = [&]() __attribute__((always_inline)) {
@@ -99,11 +109,16 @@ __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
     wave_fence();
 #pragma unroll
     for (int h = 0; h < 2; ++h) mine[h] = lane + h * kWave < count ? found.key[lane + h * kWave] : 0;
+    if (count <= kWave) {
 #pragma unroll 4
-    for (int j = 0; j < count; ++j) {
-      const Key k = found.key[j];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) rank[h] += k > mine[h];
+      for (int j = 0; j < count; ++j) rank[0] += found.key[j] > mine[0];
+    } else {
+#pragma unroll 2
+      for (int j = 0; j < count; ++j) {
+        const Key k = found.key[j];
+        rank[0] += k > mine[0];
+        rank[1] += k > mine[1];
+      }
     }
     wave_fence();
 #pragma unroll
@@ -137,21 +152,24 @@ __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) largest = fmaxf(largest, x[u][e]);      // (NaN is no maximum; it is in the sum)
     if (largest > top) {
-      if (top > -INFINITY) sum *= __builtin_amdgcn_exp2f((top - largest) * kLog2e);
+      const bool was_near = fabsf(top) < kNear, now_near = fabsf(largest) < kNear;
+      const float now = now_near ? largest * kLog2e : 0.f;
+      if (top > -INFINITY) sum *= __builtin_amdgcn_exp2f(was_near & now_near ? c - now : (top - largest) * kLog2e);
       top = largest;
+      c = now;
     }
-    const float ref = top > -INFINITY ? top : 0.f;
-    if (!__any(top == INFINITY)) {
+    if (!__any(top > -INFINITY && !(fabsf(top) < kNear))) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum += __builtin_amdgcn_exp2f((x[u][e] - ref) * kLog2e);
-    } else {                                                          // infinities share the probability
+        for (int e = 0; e < VEC; ++e) sum += __builtin_amdgcn_exp2f(fmaf(x[u][e], kLog2e, -c));
+    } else {                                                          // (infinities share the probability)
+      const float ref = top > -INFINITY ? top : 0.f;
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
-          sum += top < INFINITY ? __builtin_amdgcn_exp2f((x[u][e] - ref) * kLog2e) : x[u][e] == INFINITY ? 1.f : x[u][e] != x[u][e] ? x[u][e] : 0.f;
+          sum += fabsf(top) < kNear ? __builtin_amdgcn_exp2f(fmaf(x[u][e], kLog2e, -c)) : x[u][e] == top ? (top > -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f((x[u][e] - ref) * kLog2e);
     }
     // (of equal ones the lower index comes first: what equals the border is a candidate if that may be of this step, and none if it is of one before)
     float least;
@@ -162,41 +180,24 @@ __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
       if (group >= 4) m = fmaxf(m, __shfl_xor(m, 2, kWave));
       int larger = 0;
       for (int j = 0; j < kWave; j += group) larger += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, m), j)) > m;
-      least = fmaxf(-wave_max(larger < g.keep ? -m : -INFINITY), -FLT_MAX);       // (the least of those with fewer than `keep` larger ones)
+      least = fmaxf(-max_of_wave(larger < g.keep ? -m : -INFINITY), -FLT_MAX);       // (the least of those with fewer than `keep` larger ones)
     } else {
       least = border > -INFINITY ? above(border) : -FLT_MAX;
     }
     if (!__any(largest >= least)) continue;
-    const int before_step = count;
+    // each lane's next one, until none has any
+    uint32_t mask = 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int n = 0; n < U * VEC; ++n) mask |= x[n / VEC][n % VEC] >= least ? 1u << n : 0u;
+    for (uint64_t which = __ballot(mask != 0); which != 0; which = __ballot(mask != 0)) {
+      if (count + __popcll(which) > kRoom) cut();
+      const int n = __builtin_ctz(mask | 1u << 31);
+      float v = x[0][0];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const uint64_t which = __ballot(x[u][e] >= least);
-        if (which != 0) {
-          const int at = count + __popcll(which & ((1ull << lane) - 1));
-          if ((which >> lane & 1) && at < kRoom) {
-            found.key[at] = key_of(x[u][e], min(place(step, u), max(last, 0)) + e);
-          }
-          count += __popcll(which);
-        }
-      }
-    if (count > kRoom) {
-      // more than there is room for: one number of each lane at a time, from memory
-      count = before_step;
-      for (int n = 0; n < U * VEC; ++n) {
-        const int at = place(step, n / VEC) + n % VEC;
-        const float v = at < g.vocab ? (float)from[at] : -INFINITY;
-        if (count + kWave > kRoom) {
-          cut();
-          least = fmaxf(least, border);
-        }
-        const uint64_t which = __ballot(v >= least);
-        if (which >> lane & 1) {
-          found.key[count + __popcll(which & ((1ull << lane) - 1))] = key_of(v, at);
-        }
-        count += __popcll(which);
-      }
+      for (int i = 1; i < U * VEC; ++i) v = n == i ? x[i / VEC][i % VEC] : v;
+      if (mask != 0) found.key[count + __popcll(which & ((1ull << lane) - 1))] = key_of(v, min(place(step, n / VEC), max(last, 0)) + n % VEC);
+      count += __popcll(which);
+      mask &= mask - 1;
     }
     cut();
   }
@@ -206,8 +207,9 @@ __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
     g.value[list + lane] = lane < count ? value_of_key(found.key[lane]) : -INFINITY;
     if (lane < count) g.index[list + lane] = index_of_key(found.key[lane]);
   }
-  const float of_all = wave_max(top);
-  sum = wave_sum(top == of_all ? sum : sum * __builtin_amdgcn_exp2f((top - of_all) * kLog2e));
+  if (fabsf(top) < kNear) sum *= __builtin_amdgcn_exp2f(-fmaf(top, kLog2e, -c));
+  const float of_all = max_of_wave(top);
+  sum = group_sum<kWave>(top == of_all ? sum : sum * __builtin_amdgcn_exp2f((top - of_all) * kLog2e));
   if (lane == 0) {
     g.sums[part * 2] = of_all;
     g.sums[part * 2 + 1] = sum;

@@ -10,7 +10,7 @@ namespace ac {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kNear = 1e38f;
-constexpr int kThreads = 256, kWaves = kThreads / kWave, kRoom = 128, kMostCandidates = 512;
+constexpr int kThreads = 512, kWaves = kThreads / kWave, kRoom = 128, kNoted = 320, kMostCandidates = 512;
 
 struct BeamArgs {
   const void* logits; int64_t ld;
@@ -43,6 +43,13 @@ __device__ __forceinline__ float above(float v) {
   return __builtin_bit_cast(float, v == 0.f ? 1 : i < 0 ? i - 1 : i + 1);
 }
 
+// Floats but NaN as integers in their order.
+__device__ __forceinline__ int in_order(float v) {
+  const int i = __builtin_bit_cast(int, v + 0.f);
+  return i < 0 ? i ^ 0x7fffffff : i;
+}
+__device__ __forceinline__ float of_order(int i) { return __builtin_bit_cast(float, i < 0 ? i ^ 0x7fffffff : i); }
+
 // 16 bytes that may begin at any element.
 __device__ __forceinline__ void load_anywhere(const float* p, f32x4& v) {
   typedef f32x4 any_f32x4 __attribute__((aligned(4)));
@@ -57,7 +64,7 @@ template <> struct Vec<float> { typedef f32x4 type; };
 template <> struct Vec<bf16_t> { typedef bf16x8 type; };
 
 // A run's largest logits as they are found: more than are kept, and cut down to these where room runs out.
-struct Largest { Key key[kRoom]; };
+struct Largest { Key key[kRoom]; int vector[kNoted]; };
 // Over the wave, by rotations within sixteen lanes.
 __device__ __forceinline__ float max_of_wave(float v) {
   v = fmaxf(v, rotate_row<8>(v));
@@ -75,15 +82,21 @@ __device__ __forceinline__ void wave_fence() {
 // One wave: a run of a row, `steps` steps of U vectors of 16 bytes a lane, the next step's on their way while a step's are used.  Vectors are counted from the row's begin,
 // wherever that lies, so that equal rows give equal sums; one that would pass the row's end is the row's last one, without what the lanes before have of it.  A lane's exponents have its own
 // maximum for reference.  A logit is a candidate if it reaches `least`, which lies above the keep-th largest of those that were there when they were last looked at: at first it is the
-// keep-th largest of the maxima over groups of lanes, twice as many as are kept, so that what reaches it is not much more than what is kept, and hardly anything of the later steps is.
+// keep-th largest of the maxima over groups of lanes, twice as many as are kept.  The block's waves, whose runs are of one row, share the highest of what they have: what lies below
+// it has enough larger ones wherever they are, and after the first step hardly anything reaches it.  (Alone a wave finds a few new ones in each of its steps: 11 us of 35 with 64 prompts of eight
+// beams over 131072 tokens.)  Which candidates a run keeps then depends on time, but not which ones come out.
 template <typename T, int U>
 __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
   typedef typename Vec<T>::type V;
   constexpr int VEC = Elem<T>::kVec, STEP = kWave * VEC * U;
   __shared__ Largest all[kWaves];
+  __shared__ int border_of_all;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), run = blockIdx.x * kWaves + wave;
   const int64_t row = (int64_t)blockIdx.z * g.beams + blockIdx.y, part = row * g.runs + run;
-  if (run >= g.runs || (g.ended && g.ended[row] != 0) || !(g.scores[row] > -INFINITY)) return;       // (no candidate of its logits)
+  if ((g.ended && g.ended[row] != 0) || !(g.scores[row] > -INFINITY)) return;                         // (no candidate of its logits)
+  if (threadIdx.x == 0) border_of_all = in_order(-FLT_MAX);
+  __syncthreads();
+  if (run >= g.runs) return;
   Largest& found = all[wave];
   const T* const from = (const T*)g.logits + row * g.ld;
   const int begin = run * g.steps * STEP, left = g.vocab - begin, steps = left < g.steps * STEP ? (left + STEP - 1) / STEP : g.steps, last = g.vocab - VEC;
@@ -101,7 +114,10 @@ __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
   };
   // sum: of 2^(x log2 e - c) with c = top log2 e as it is rounded, which the end makes good; or, of a maximum past kNear, of e^(x - top)
   float top = -INFINITY, c = 0.f, sum = 0.f, border = -INFINITY;
-  int count = 0;
+  int count = 0, noted = 0;
+  auto share = [&](float v) {
+    if (lane == 0) atomicMax(&border_of_all, in_order(v));
+  };
   // keeps the `keep` largest, in order; the border is the last of them, if there are so many
   auto cut = [&]() __attribute__((always_inline)) {
     Key mine[2];
@@ -128,12 +144,34 @@ __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
     if (count >= g.keep) {
       count = g.keep;
       border = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, value_of_key(found.key[g.keep - 1]))));
+      share(border);
     }
+  };
+  // The noted vectors' numbers once more, a lane one, those that reach `least` to the candidates.  (What was kept before lies before them: where it is cut meanwhile, equal ones may be among
+  // both.)
+  auto take = [&](float least) __attribute__((always_inline)) {
+    if (noted == 0) return;
+    wave_fence();
+    for (int r = lane / VEC; r - lane / VEC < noted; r += kWave / VEC) {
+      const int at = found.vector[min(r, noted - 1)], near = min(at, max(last, 0)) + lane % VEC;
+      const float v = r < noted && near >= at && near < g.vocab ? (float)from[near] : -INFINITY;
+      uint64_t which = __ballot(v >= least);
+      if (which == 0) continue;
+      if (count + __popcll(which) > kRoom) {
+        cut();
+        least = fmaxf(least, border);
+        which = __ballot(v >= least);
+      }
+      if (which >> lane & 1) found.key[count + __popcll(which & ((1ull << lane) - 1))] = key_of(v, near);
+      count += __popcll(which);
+    }
+    noted = 0;
+    cut();
   };
   V next[U];
   load(next, 0);
   for (int step = 0; step < steps; ++step) {
-    float x[U][VEC], largest = -INFINITY;
+    float x[U][VEC], big[U], largest = -INFINITY;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -148,9 +186,12 @@ __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
       }
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      big[u] = x[u][0];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) largest = fmaxf(largest, x[u][e]);      // (NaN is no maximum; it is in the sum)
+      for (int e = 1; e < VEC; ++e) big[u] = fmaxf(big[u], x[u][e]);        // (NaN is no maximum; it is in the sum)
+      largest = fmaxf(largest, big[u]);
+    }
     if (largest > top) {
       const bool was_near = fabsf(top) < kNear, now_near = fabsf(largest) < kNear;
       const float now = now_near ? largest * kLog2e : 0.f;
@@ -181,27 +222,23 @@ __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
       int larger = 0;
       for (int j = 0; j < kWave; j += group) larger += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, m), j)) > m;
       least = fmaxf(-max_of_wave(larger < g.keep ? -m : -INFINITY), -FLT_MAX);       // (the least of those with fewer than `keep` larger ones)
+      share(least);
     } else {
       least = border > -INFINITY ? above(border) : -FLT_MAX;
     }
+    least = fmaxf(least, of_order(__builtin_amdgcn_readfirstlane(__hip_atomic_load(&border_of_all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP))));
     if (!__any(largest >= least)) continue;
-    // each lane's next one, until none has any
-    uint32_t mask = 0;
 #pragma unroll
-    for (int n = 0; n < U * VEC; ++n) mask |= x[n / VEC][n % VEC] >= least ? 1u << n : 0u;
-    for (uint64_t which = __ballot(mask != 0); which != 0; which = __ballot(mask != 0)) {
-      if (count + __popcll(which) > kRoom) cut();
-      const int n = __builtin_ctz(mask | 1u << 31);
-      float v = x[0][0];
-#pragma unroll
-      for (int i = 1; i < U * VEC; ++i) v = n == i ? x[i / VEC][i % VEC] : v;
-      if (mask != 0) found.key[count + __popcll(which & ((1ull << lane) - 1))] = key_of(v, min(place(step, n / VEC), max(last, 0)) + n % VEC);
-      count += __popcll(which);
-      mask &= mask - 1;
+    for (int u = 0; u < U; ++u) {
+      const uint64_t which = __ballot(big[u] >= least);
+      if (which != 0) {
+        if (which >> lane & 1) found.vector[noted + __popcll(which & ((1ull << lane) - 1))] = place(step, u);
+        noted += __popcll(which);
+      }
     }
-    cut();
+    if (step == 0 || noted >= kWave / 2) take(least);
   }
-  // (what was found is in order since the last cut, if there was one)
+  take(border > -INFINITY ? above(border) : -FLT_MAX);
   const int64_t list = part * g.keep;
   if (lane < g.keep) {
     g.value[list + lane] = lane < count ? value_of_key(found.key[lane]) : -INFINITY;
@@ -244,13 +281,12 @@ __global__ void __launch_bounds__(kThreads) beam_rank(BeamArgs g) {
       const f32x2 near = *reinterpret_cast<const f32x2*>(sums + 2 * (lane < g.runs ? lane : 0));
       m = near[0];
       for (int p = lane + kWave; p < g.runs; p += kWave) m = fmaxf(m, sums[2 * p]);
-      m = wave_max(m);
+      m = max_of_wave(m);
       for (int p = lane; p < g.runs; p += kWave) {
         const f32x2 part = p == lane ? near : *reinterpret_cast<const f32x2*>(sums + 2 * p);
         sum += part[0] == m ? (double)part[1] : (double)part[1] * exp((double)part[0] - (double)m);
       }
-#pragma unroll
-      for (int o = kWave / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+      for (int o = 1; o < kWave && o < g.runs; o <<= 1) sum += __shfl_xor(sum, o, kWave);      // (lane 0's is of all; the lanes from there on have nothing)
       sum = (double)score - log(sum);
     }
     if (lane == 0) {
@@ -306,11 +342,9 @@ __global__ void __launch_bounds__(kThreads) beam_rank(BeamArgs g) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) larger += a[e] > most_of_group;
   }
-  const int bits = __builtin_bit_cast(int, most_of_group + 0.f);
-  if (larger < g.keep) atomicMin(&border_at, bits < 0 ? bits ^ 0x7fffffff : bits);
+  if (larger < g.keep) atomicMin(&border_at, in_order(most_of_group));
   __syncthreads();
-  const int border_bits = border_at;
-  const float border = __builtin_bit_cast(float, border_bits < 0 ? border_bits ^ 0x7fffffff : border_bits);
+  const float border = of_order(border_at);
   if (most >= border)
     each([&](double v, int place) {
       if ((float)v < border) return false;

@@ -200,10 +200,12 @@ __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
       c = now;
     }
     if (!__any(top > -INFINITY && !(fabsf(top) < kNear))) {
+      float part[4] = {sum, 0.f, 0.f, 0.f};                                 // (four sums: what comes next need not wait for each)
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum += __builtin_amdgcn_exp2f(fmaf(x[u][e], kLog2e, -c));
+        for (int e = 0; e < VEC; ++e) part[e % 4] += __builtin_amdgcn_exp2f(fmaf(x[u][e], kLog2e, -c));
+      sum = (part[0] + part[1]) + (part[2] + part[3]);
     } else {                                                          // (infinities share the probability)
       const float ref = top > -INFINITY ? top : 0.f;
 #pragma unroll

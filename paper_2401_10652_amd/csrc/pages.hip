@@ -24,7 +24,6 @@ struct PagesArgs {
 };
 
 __device__ __forceinline__ bool names(const PagesArgs& g, int e) { return (uint32_t)e < (uint32_t)g.pages; }
-__device__ __forceinline__ int uses_now(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }   // (behind atomics of other lanes)
 __device__ __forceinline__ void add_use(const PagesArgs& g, int e, int n) {
   if (names(g, e)) __hip_atomic_fetch_add(g.uses + e, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -89,18 +88,17 @@ __device__ __forceinline__ int update_row(const PagesArgs& g, int b, int lane) {
 }
 
 // Gives row b's places their pages, the first of them that of rank `rank`.
-__device__ __forceinline__ void give_row(const PagesArgs& g, int b, int lane, int rank) {
+__device__ __forceinline__ void give_row(const PagesArgs& g, int b, int lane, int rank, int have) {
   const int32_t* from = g.table_from + b * g.places;
   int32_t* to = g.table + b * g.places;
   const Range drop = places_in(g, g.drop_begin, g.drop_end, b, true), take = places_in(g, g.take_begin, g.take_end, b, false);
-  const int have = uses_now(g.total);
   for (int64_t i0 = take.from; i0 < take.to; i0 += kWave) {
     const int64_t i = i0 + lane;
     const bool wants = i < take.to && (!names(g, from[i]) || (i >= drop.from && i < drop.to));
     const uint64_t all = __ballot(wants);
     const int mine = rank + __popcll(all & ((1ull << lane) - 1));
     if (wants) {
-      const int e = mine < have ? uses_now(g.list + mine) : -1;
+      const int e = mine < have ? g.list[mine] : -1;
       to[i] = e;
       if (e >= 0) g.uses[e] = 1;
     }
@@ -138,11 +136,11 @@ __device__ __forceinline__ int fork_row(const PagesArgs& g, int j, int lane) {
   }
   return wants;
 }
-__device__ __forceinline__ void give_copy(const PagesArgs& g, int j, int rank) {
-  const int source = uses_now(g.source + j);
+__device__ __forceinline__ void give_copy(const PagesArgs& g, int j, int rank, int have) {
+  const int source = g.source[j];
   int target = -1;
   if (names(g, source)) {
-    if (rank < uses_now(g.total)) target = uses_now(g.list + rank);
+    if (rank < have) target = g.list[rank];
     const int32_t length = max(g.length[g.parent[j]], 0);
     g.table[j * g.places + length / g.page] = target;
     if (target >= 0) g.uses[target] = 1;
@@ -152,12 +150,22 @@ __device__ __forceinline__ void give_copy(const PagesArgs& g, int j, int rank) {
 
 // ---- pages, a chunk a block ------------------------------------------------------------------------------------------------
 
-enum { FREE, USED };
-__device__ __forceinline__ int count_chunk(const int32_t* uses, int pages, int first, int kind) {
-  int n = 0;
+// uses of the kEach pages from `first` on, as bits that are set for those in use; pages past the last are as in use in `there` alone.
+struct Bits { uint32_t used, there; };
+__device__ __forceinline__ Bits chunk_bits(const int32_t* uses, int pages, int first) {
+  typedef int32_t any_i32x4 __attribute__((ext_vector_type(4), aligned(4)));
+  Bits b{0, first >= pages ? 0u : pages - first >= kEach ? (1u << kEach) - 1 : (1u << (pages - first)) - 1};
+  if (first + kEach <= pages) {
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) n += first + i < pages && (uses[first + i] > 0) == (kind == USED);
-  return n;
+    for (int i = 0; i < kEach; i += 4) {
+      const any_i32x4 u = *reinterpret_cast<const any_i32x4*>(uses + first + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) b.used |= u[e] > 0 ? 1u << (i + e) : 0u;
+    }
+  } else {
+    for (int i = 0; first + i < pages; ++i) b.used |= uses[first + i] > 0 ? 1u << i : 0u;
+  }
+  return b;
 }
 
 __global__ void __launch_bounds__(256) pages_copy_uses(PagesArgs g) {
@@ -178,7 +186,8 @@ __global__ void __launch_bounds__(256) pages_count(PagesArgs g) {
   __shared__ int of_wave[4];
   int sum;
   if ((int)blockIdx.x < g.chunks) {
-    sum_before<4>(count_chunk(g.uses, g.pages, blockIdx.x * kChunk + threadIdx.x * kEach, FREE), of_wave, sum);
+    const Bits b = chunk_bits(g.uses, g.pages, blockIdx.x * kChunk + threadIdx.x * kEach);
+    sum_before<4>(__popc(b.there & ~b.used), of_wave, sum);
     if (threadIdx.x == 0) g.counts[blockIdx.x] = sum;
     return;
   }
@@ -217,13 +226,38 @@ __global__ void __launch_bounds__(256) pages_list(PagesArgs g) {
   __shared__ int of_wave[4];
   int all, sum;
   const int before = chunks_before(g, of_wave, all), first = blockIdx.x * kChunk + threadIdx.x * kEach;
-  int at = before + sum_before<4>(count_chunk(g.uses, g.pages, first, FREE), of_wave, sum);
-#pragma unroll
-  for (int i = 0; i < kEach; ++i)
-    if (first + i < g.pages && g.uses[first + i] <= 0) g.list[at++] = first + i;
+  const Bits b = chunk_bits(g.uses, g.pages, first);
+  uint32_t free = b.there & ~b.used;
+  int at = before + sum_before<4>(__popc(free), of_wave, sum);
+  for (; free != 0; free &= free - 1) g.list[at++] = first + __builtin_ctz(free);
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     g.total[0] = all;
     if (g.count) *g.count = g.total[1] > all ? g.total[1] - all : 0;
+  }
+}
+
+// Both by one block, which stops looking for free pages when there are enough.
+constexpr int kRankThreads = 1024, kRankPages = 1 << 16;
+__global__ void __launch_bounds__(kRankThreads) pages_rank(PagesArgs g) {
+  __shared__ int of_wave[kRankThreads / kWave];
+  const int tid = threadIdx.x;
+  int sum, wants = 0, before = 0;
+  Bits bits = chunk_bits(g.uses, g.pages, tid * kEach);            // (on their way while the wants are looked at)
+  for (int b0 = 0; b0 < g.batch; b0 += kRankThreads) {
+    const int b = b0 + tid, n = b < g.batch ? g.need[b] : 0, at = wants + sum_before<kRankThreads / kWave>(n, of_wave, sum);
+    if (b < g.batch) g.need[b] = at;
+    wants += sum;
+  }
+  for (int first = 0; first < g.pages && before < wants; first += kRankThreads * kEach) {
+    if (first > 0) bits = chunk_bits(g.uses, g.pages, first + tid * kEach);
+    uint32_t free = bits.there & ~bits.used;
+    int at = before + sum_before<kRankThreads / kWave>(__popc(free), of_wave, sum);
+    for (; free != 0; free &= free - 1) g.list[at++] = first + tid * kEach + __builtin_ctz(free);
+    before += sum;
+  }
+  if (tid == 0) {
+    g.total[0] = before;
+    if (g.count) *g.count = wants > before ? wants - before : 0;
   }
 }
 
@@ -231,51 +265,50 @@ template <bool FORK>
 __global__ void __launch_bounds__(256) pages_give(PagesArgs g) {
   if (FORK) {
     const int j = blockIdx.x * 256 + threadIdx.x;
-    if (j < g.batch) give_copy(g, j, g.need[j]);
+    if (j < g.batch) give_copy(g, j, g.need[j], *g.total);
   } else {
     const int b = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / kWave);
-    if (b < g.batch) give_row(g, b, threadIdx.x % kWave, g.need[b]);
+    if (b < g.batch) give_row(g, b, threadIdx.x % kWave, g.need[b], *g.total);
   }
 }
 
 // ---- compaction ------------------------------------------------------------------------------------------------------------
 
-// Pages in use of each chunk, and uses to where it goes.
-__global__ void __launch_bounds__(256) compact_count(PagesArgs g) {
-  __shared__ int of_wave[4];
-  const int first = blockIdx.x * kChunk + threadIdx.x * kEach;
-  int n = 0, sum;
-#pragma unroll
-  for (int i = 0; i < kEach; ++i)
-    if (first + i < g.pages) {
-      const int u = g.uses_from[first + i];
-      n += u > 0;
-      if (g.uses != g.uses_from) g.uses[first + i] = u;
-    }
-  sum_before<4>(n, of_wave, sum);
-  if (threadIdx.x == 0 && (int)blockIdx.x < g.chunks) g.counts[blockIdx.x] = sum;      // (without pages there is one block, and no chunk)
-}
-
 // With n pages in use: a free page p < n is the target of rank p minus the pages in use before it, and a page p >= n in use the source whose rank is
-// the number of pages in use behind it; both ranks run from 0 to the number of moves.  need[p]: the rank of a source.
-__global__ void __launch_bounds__(256) compact_list(PagesArgs g) {
-  __shared__ int of_wave[4];
-  int n, sum;
-  const int before = chunks_before(g, of_wave, n), first = blockIdx.x * kChunk + threadIdx.x * kEach;
-  int at = before + sum_before<4>(count_chunk(g.uses_from, g.pages, first, USED), of_wave, sum);
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int p = first + i;
-    if (p >= g.pages) break;
-    const bool used = g.uses_from[p] > 0;
+// the number of pages in use behind it; both ranks run from 0 to the number of moves, which is the number of free pages among the first n.  list[p]: the rank of a source.
+// at: pages in use before `first`.
+__device__ __forceinline__ void moves_of(const Bits& bits, int first, int at, int n, const PagesArgs& g) {
+  for (uint32_t there = bits.there; there != 0; there &= there - 1) {
+    const int i = __builtin_ctz(there), p = first + i;
+    const bool used = bits.used >> i & 1;
     if (!used && p < n) g.target[p - at] = p;
     if (used && p >= n) {
       g.source[n - 1 - at] = p;
       g.list[p] = n - 1 - at;
     }
     at += used;
-    if (p == (n > 0 ? n - 1 : 0)) g.total[0] = n > 0 ? n - at : 0;           // moves: free pages among the first n
+    if (p == (n > 0 ? n - 1 : 0)) g.total[0] = n > 0 ? n - at : 0;
   }
+}
+
+// Pages in use of each chunk, and uses to where it goes.
+__global__ void __launch_bounds__(256) compact_count(PagesArgs g) {
+  __shared__ int of_wave[4];
+  const int first = blockIdx.x * kChunk;
+  int sum;
+  sum_before<4>(__popc(chunk_bits(g.uses_from, g.pages, first + threadIdx.x * kEach).used), of_wave, sum);
+  if (g.uses != g.uses_from)
+    for (int p = first + threadIdx.x; p < g.pages && p < first + kChunk; p += 256) g.uses[p] = g.uses_from[p];
+  if (threadIdx.x == 0 && (int)blockIdx.x < g.chunks) g.counts[blockIdx.x] = sum;      // (without pages there is one block, and no chunk)
+}
+
+__global__ void __launch_bounds__(256) compact_list(PagesArgs g) {
+  __shared__ int of_wave[4];
+  int n, sum;
+  const int before = chunks_before(g, of_wave, n), first = blockIdx.x * kChunk + threadIdx.x * kEach;
+  const Bits bits = chunk_bits(g.uses_from, g.pages, first);
+  const int at = before + sum_before<4>(__popc(bits.used), of_wave, sum);
+  moves_of(bits, first, at, n, g);
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     if (g.pages == 0) g.total[0] = 0;
     g.total[1] = n;
@@ -286,23 +319,173 @@ __global__ void __launch_bounds__(256) compact_list(PagesArgs g) {
 // The table's entries and uses follow the pages.
 __global__ void __launch_bounds__(256) compact_follow(PagesArgs g) {
   const int n = g.total[1], moves = g.total[0];
-  const int64_t all = g.batch * g.places, step = (int64_t)gridDim.x * 256;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all || i < moves; i += step) {
-    if (i < all) {
-      int e = g.table_from[i];
-      // (an entry that uses does not know of stays as it is: list has a rank for pages in use alone)
-      if (names(g, e) && e >= n) {
-        const int r = g.list[e];
-        if ((uint32_t)r < (uint32_t)moves && g.source[r] == e) e = g.target[r];
-      }
-      if (g.table != g.table_from || e != g.table_from[i]) g.table[i] = e;
+  const int64_t all = g.batch * g.places, first = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+  for (int64_t i = first; i < all; i += step) {
+    const int was = g.table_from[i];
+    int e = was;
+    // (an entry that uses does not know of stays as it is: list has a rank for pages in use alone)
+    if (names(g, e) && e >= n) {
+      const int r = g.list[e];
+      if ((uint32_t)r < (uint32_t)moves && g.source[r] == e) e = g.target[r];
     }
-    if (i < moves) {
-      const int from = g.source[i], to = g.target[i];
-      g.uses[to] = g.uses_from[from];
-      g.uses[from] = 0;
+    if (g.table != g.table_from || e != was) g.table[i] = e;
+  }
+  for (int64_t i = first; i < moves; i += step) {
+    const int from = g.source[i], to = g.target[i];
+    g.uses[to] = g.uses_from[from];
+    g.uses[from] = 0;
+  }
+}
+// ---- all of it in one block -------------------------------------------------------------------------------------------------
+//
+// What the launches above do one after another, for tables of which each thread has a few entries: uses, lists and what is known of rows lie in LDS, and a barrier stands where a
+// launch does.  What bounds it is one memory latency after another.
+constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / kWave, kOnePages = 8192, kOneBatch = 1024, kOneEach = 4, kOnePlaces = kOneThreads * kOneEach;
+enum { UPDATE, FORK_ROWS, COMPACT };
+
+template <int KIND>
+__global__ void __launch_bounds__(kOneThreads) pages_at_once(PagesArgs g, Divisor of_row) {
+  extern __shared__ __attribute__((aligned(16))) int32_t lds[];
+  __shared__ int of_wave[kOneWaves];
+  const int tid = threadIdx.x, places = (int)g.places, first_entry = tid * kOneEach, entries = (int)(g.batch * g.places);
+  int32_t* const uses = lds;                                       // [pages], what it is at the end
+  int32_t* const list = uses + (g.pages + 3) / 4 * 4;              // [pages]: free ones in order; of a compaction sources' ranks
+  int32_t* const row = list + g.pages;                             // [4][batch]: of an update the ranges' ends, of a fork parent, whole pages and first; of a compaction targets [pages]
+  const int mine = tid < g.batch ? tid : -1;
+  int sum, wants = 0, before = 0, rank = 0;
+  int32_t was[kOneEach], now[kOneEach];
+#pragma unroll
+  for (int e = 0; e < kOneEach; ++e) was[e] = now[e] = first_entry + e < entries ? g.table_from[first_entry + e] : -1;
+
+  int source = -1, rest = 0, parent = -1, length = 0;              // of a fork, row `mine`
+  if (KIND == UPDATE && mine >= 0) {
+    const Range drop = places_in(g, g.drop_begin, g.drop_end, mine, true), take = places_in(g, g.take_begin, g.take_end, mine, false);
+    row[mine] = (int)drop.from; row[g.batch + mine] = (int)drop.to; row[2 * g.batch + mine] = (int)take.from; row[3 * g.batch + mine] = (int)take.to;
+  }
+  if (KIND == FORK_ROWS && mine >= 0) {
+    const int p = g.parent[mine];
+    parent = (uint32_t)p < (uint32_t)g.batch ? p : -1;
+    length = parent >= 0 ? max(g.length[parent], 0) : 0;
+    rest = length % g.page;
+    row[2 * g.batch + mine] = g.batch;
+  }
+  for (int p = tid; p < g.pages; p += kOneThreads) uses[p] = g.uses_from[p];
+  __syncthreads();
+
+  uint32_t wanting = 0;                                            // the thread's entries that want a page; of a fork whether its row does
+  if (KIND == FORK_ROWS) {
+    if (parent >= 0) atomicMin(&row[2 * g.batch + parent], mine);  // the first of a parent's
+    __syncthreads();
+    const bool first = parent >= 0 && row[2 * g.batch + parent] == mine;
+    __syncthreads();
+    if (mine >= 0) {
+      const int whole = length / g.page;
+      if (parent >= 0 && !first && rest > 0 && whole < places) source = g.table_from[parent * places + whole];
+      if (!names(g, source)) source = -1;
+      row[mine] = parent; row[g.batch + mine] = whole; row[2 * g.batch + mine] = first;
+      g.length_to[mine] = length;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kOneEach; ++e) {
+      now[e] = -1;
+      if (first_entry + e >= entries) continue;
+      const int b = quotient(first_entry + e, of_row), i = first_entry + e - b * places, p = row[b];
+      if (p >= 0 && (i < row[g.batch + b] || row[2 * g.batch + b] != 0)) now[e] = g.table_from[p * places + i];
+    }
+#pragma unroll
+    for (int e = 0; e < kOneEach; ++e)
+      if (now[e] != was[e]) {
+        if (names(g, was[e])) atomicAdd(&uses[was[e]], -1);
+        if (names(g, now[e])) atomicAdd(&uses[now[e]], 1);
+      }
+    wanting = source >= 0;
+  }
+  if (KIND == UPDATE) {
+#pragma unroll
+    for (int e = 0; e < kOneEach; ++e) {
+      if (first_entry + e >= entries) break;
+      const int b = quotient(first_entry + e, of_row), i = first_entry + e - b * places;
+      if (i >= row[b] && i < row[g.batch + b] && names(g, now[e])) {
+        atomicAdd(&uses[now[e]], -1);
+        now[e] = -1;
+      }
+      if (i >= row[2 * g.batch + b] && i < row[3 * g.batch + b] && !names(g, now[e])) wanting |= 1u << e;
     }
   }
+  if (KIND != COMPACT) rank = sum_before<kOneWaves>(__popc(wanting), of_wave, wants);        // (which is a barrier, too)
+
+  if (KIND == COMPACT) {
+    int n = 0;
+    for (int first = 0; first < g.pages; first += kOneThreads * kEach) {
+      sum_before<kOneWaves>(__popc(chunk_bits(uses, g.pages, first + tid * kEach).used), of_wave, sum);
+      n += sum;
+    }
+    PagesArgs in = g;
+    in.list = list; in.target = row;
+    for (int first = 0; first < g.pages; first += kOneThreads * kEach) {
+      const Bits bits = chunk_bits(uses, g.pages, first + tid * kEach);
+      moves_of(bits, first + tid * kEach, before + sum_before<kOneWaves>(__popc(bits.used), of_wave, sum), n, in);
+      before += sum;
+    }
+    if (tid == 0 && g.count) *g.count = n;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kOneEach; ++e)
+      if (names(g, was[e]) && was[e] >= n && uses[was[e]] > 0) now[e] = row[list[was[e]]];
+    __syncthreads();
+    for (int p = tid; p < g.pages; p += kOneThreads)
+      if (p >= n && uses[p] > 0) {
+        const int to = row[list[p]];
+        g.target[list[p]] = to;
+        uses[to] = uses[p];
+        uses[p] = 0;
+      }
+  } else if (KIND == FORK_ROWS || g.take_begin) {
+    for (int first = 0; first < g.pages && before < wants; first += kOneThreads * kEach) {
+      const Bits bits = chunk_bits(uses, g.pages, first + tid * kEach);
+      uint32_t free = bits.there & ~bits.used;
+      int at = before + sum_before<kOneWaves>(__popc(free), of_wave, sum);
+      for (; free != 0; free &= free - 1) list[at++] = first + tid * kEach + __builtin_ctz(free);
+      before += sum;
+    }
+    if (tid == 0 && g.count) *g.count = wants > before ? wants - before : 0;
+    __syncthreads();
+    auto give = [&]() {
+      const int e = rank < before ? list[rank] : -1;
+      ++rank;
+      if (e >= 0) uses[e] = 1;
+      return e;
+    };
+    if (KIND == FORK_ROWS) {
+      int32_t* const target = row;                                 // (parents are not looked at any more)
+      if (mine >= 0) {
+        target[mine] = source >= 0 ? give() : -1;
+        g.source[mine] = source;
+        g.target[mine] = target[mine];
+        g.tokens[mine] = rest;
+        row[2 * g.batch + mine] = source >= 0;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < kOneEach; ++e) {
+        if (first_entry + e >= entries) break;
+        const int b = quotient(first_entry + e, of_row);
+        if (row[2 * g.batch + b] != 0 && first_entry + e - b * places == row[g.batch + b]) now[e] = target[b];
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kOneEach; ++e)
+        if (wanting >> e & 1) now[e] = give();
+    }
+  } else if (tid == 0 && g.count) {
+    *g.count = 0;
+  }
+#pragma unroll
+  for (int e = 0; e < kOneEach; ++e)
+    if (first_entry + e < entries && (g.table != g.table_from || now[e] != was[e])) g.table[first_entry + e] = now[e];
+  __syncthreads();
+  for (int p = tid; p < g.pages; p += kOneThreads) g.uses[p] = uses[p];
 }
 
 // ---- copies -------------------------------------------------------------------------------------------------------------------
@@ -389,14 +572,31 @@ PagesArgs pages_args(const ac_page_books& from, const ac_page_books& to, void* w
   return g;
 }
 
+// Whether one block gets through it.
+bool at_once(const PagesArgs& g) { return g.pages <= kOnePages && g.batch <= kOneBatch && g.batch * g.places <= kOnePlaces; }
+template <int KIND>
+hipError_t once_launch(const PagesArgs& g, hipStream_t s) {
+  constexpr int MOST = 2 * kOnePages + 4 + (kOnePages > 4 * kOneBatch ? kOnePages : 4 * kOneBatch);
+  static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_at_once<KIND>), hipFuncAttributeMaxDynamicSharedMemorySize, MOST * (int)sizeof(int32_t));
+  if (attr_status != hipSuccess) return attr_status;
+  const int words = (g.pages + 3) / 4 * 4 + g.pages + (KIND == COMPACT ? g.pages : 4 * g.batch);
+  hipLaunchKernelGGL((pages_at_once<KIND>), dim3(1), dim3(kOneThreads), (size_t)words * sizeof(int32_t), s, g, divisor((uint32_t)(g.places > 0 ? g.places : 1)));
+  return hipGetLastError();
+}
+
 template <bool FORK>
 hipError_t rows_launch(const PagesArgs& g, hipStream_t s) {
+  if (at_once(g)) return once_launch<FORK ? FORK_ROWS : UPDATE>(g, s);
   if (g.uses != g.uses_from && g.pages > 0)
     hipLaunchKernelGGL(pages_copy_uses, dim3((unsigned)(g.chunks < 1024 ? 4 * g.chunks : 4096)), dim3(256), 0, s, g);
   hipLaunchKernelGGL((pages_rows<FORK>), dim3((unsigned)(g.batch / 4 + 1)), dim3(256), 0, s, g);
   if (FORK || g.take_begin) {
-    hipLaunchKernelGGL(pages_count, dim3((unsigned)g.chunks + 1), dim3(256), 0, s, g);
-    hipLaunchKernelGGL(pages_list, dim3((unsigned)(g.chunks > 0 ? g.chunks : 1)), dim3(256), 0, s, g);
+    if (g.pages <= kRankPages) {
+      hipLaunchKernelGGL(pages_rank, dim3(1), dim3(kRankThreads), 0, s, g);
+    } else {
+      hipLaunchKernelGGL(pages_count, dim3((unsigned)g.chunks + 1), dim3(256), 0, s, g);
+      hipLaunchKernelGGL(pages_list, dim3((unsigned)g.chunks), dim3(256), 0, s, g);
+    }
     hipLaunchKernelGGL((pages_give<FORK>), dim3((unsigned)(g.batch / (FORK ? 256 : 4) + 1)), dim3(256), 0, s, g);
   }
   return hipGetLastError();
@@ -433,12 +633,17 @@ hipError_t launch_cache_compact(const ac_kv_cache* caches, int n_caches, const a
                                 hipStream_t s) {
   PagesArgs g = pages_args(from, to, workspace);
   g.count = used;
-  const int blocks = g.chunks > 0 ? g.chunks : 1;
-  hipLaunchKernelGGL(compact_count, dim3((unsigned)blocks), dim3(256), 0, s, g);
-  hipLaunchKernelGGL(compact_list, dim3((unsigned)blocks), dim3(256), 0, s, g);
-  const int64_t all = g.batch * g.places > g.pages ? g.batch * g.places : g.pages, follow = (all + 1023) / 1024;
-  hipLaunchKernelGGL(compact_follow, dim3((unsigned)(follow < 1 ? 1 : follow < 4096 ? follow : 4096)), dim3(256), 0, s, g);
-  const hipError_t e = hipGetLastError();
+  hipError_t e;
+  if (at_once(g)) {
+    e = once_launch<COMPACT>(g, s);
+  } else {
+    const int blocks = g.chunks > 0 ? g.chunks : 1;
+    hipLaunchKernelGGL(compact_count, dim3((unsigned)blocks), dim3(256), 0, s, g);
+    hipLaunchKernelGGL(compact_list, dim3((unsigned)blocks), dim3(256), 0, s, g);
+    const int64_t all = g.batch * g.places > g.pages ? g.batch * g.places : g.pages, each = (all + 1023) / 1024;
+    hipLaunchKernelGGL(compact_follow, dim3((unsigned)(each < 1 ? 1 : each < 4096 ? each : 4096)), dim3(256), 0, s, g);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess) return e;
   CopyArgs c{};
   c.source = g.source; c.target = g.target; c.n_dev = g.total; c.pages = g.pages; c.page = g.page;

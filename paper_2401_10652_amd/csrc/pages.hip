@@ -21,6 +21,7 @@ struct PagesArgs {
   const int32_t *parent, *length; int32_t* length_to;               // fork
   int32_t* count;                                                   // missing or used, or null
   int32_t *total, *need, *counts, *list, *source, *target, *tokens; // workspace: [0] pages of the list, [1] wants; need [batch]; counts [chunks]; the others [pages] or [batch]
+  int32_t *drops, *dropped, *wanted;                                // workspace, of an update in two launches, else null: [batch] and, of each row, [places]: pages given up and places that want one
 };
 
 __device__ __forceinline__ bool names(const PagesArgs& g, int e) { return (uint32_t)e < (uint32_t)g.pages; }
@@ -63,27 +64,38 @@ __device__ __forceinline__ Range places_in(const PagesArgs& g, const int32_t* be
   return r;
 }
 
-// Frees what row b drops; the number of its places that want a page.
+// Frees what row b drops; the number of its places that want a page.  NOTED: uses stays as it is, and both are noted for the second launch.
+template <bool NOTED>
 __device__ __forceinline__ int update_row(const PagesArgs& g, int b, int lane) {
   const int32_t* from = g.table_from + b * g.places;
   int32_t* to = g.table + b * g.places;
   const Range drop = places_in(g, g.drop_begin, g.drop_end, b, true), take = places_in(g, g.take_begin, g.take_end, b, false);
   const bool apart = from != to;
   const int64_t end = apart ? g.places : drop.to;
-  int wants = 0;
-  for (int64_t i = (apart ? 0 : drop.from) + lane; i < end; i += kWave) {
-    int e = from[i];
-    if (i >= drop.from && i < drop.to && names(g, e)) {
+  int wants = 0, drops = 0;
+  const uint64_t lanes_before = (1ull << lane) - 1;
+  for (int64_t i0 = apart ? 0 : drop.from; i0 < end; i0 += kWave) {
+    const int64_t i = i0 + lane;
+    int e = i < end ? from[i] : -1;
+    const bool gone = i < end && i >= drop.from && i < drop.to && names(g, e);
+    if (NOTED) {
+      const uint64_t which = __ballot(gone);
+      if (gone) g.dropped[b * g.places + drops + __popcll(which & lanes_before)] = e;
+      drops += __popcll(which);
+    } else if (gone) {
       add_use(g, e, -1);
-      e = -1;
-      if (!apart) to[i] = e;
     }
-    if (apart) to[i] = e;
+    if (gone) e = -1;
+    if (i < end && (apart || gone)) to[i] = e;
   }
   // (in place a dropped entry may or may not be seen as it was: it wants a page either way)
-  for (int64_t i = take.from + lane; i < take.to; i += kWave) wants += !names(g, from[i]) || (i >= drop.from && i < drop.to);
-#pragma unroll
-  for (int o = kWave / 2; o > 0; o >>= 1) wants += __shfl_xor(wants, o, kWave);
+  for (int64_t i0 = take.from; i0 < take.to; i0 += kWave) {
+    const int64_t i = i0 + lane;
+    const uint64_t which = __ballot(i < take.to && (!names(g, from[i]) || (i >= drop.from && i < drop.to)));
+    if (NOTED && (which >> lane & 1)) g.wanted[b * g.places + wants + __popcll(which & lanes_before)] = (int)i;
+    wants += __popcll(which);
+  }
+  if (NOTED && lane == 0) g.drops[b] = drops;
   return wants;
 }
 
@@ -175,9 +187,9 @@ __global__ void __launch_bounds__(256) pages_copy_uses(PagesArgs g) {
 template <bool FORK>
 __global__ void __launch_bounds__(256) pages_rows(PagesArgs g) {
   const int lane = threadIdx.x % kWave, b = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / kWave);
-  if (!FORK && !g.take_begin && b == 0 && lane == 0 && g.count) *g.count = 0;
+  if (!FORK && !g.take_begin && !g.dropped && b == 0 && lane == 0 && g.count) *g.count = 0;
   if (b >= g.batch) return;
-  const int wants = FORK ? fork_row(g, b, lane) : update_row(g, b, lane);
+  const int wants = FORK ? fork_row(g, b, lane) : g.dropped ? update_row<true>(g, b, lane) : update_row<false>(g, b, lane);
   if (lane == 0) g.need[b] = wants;
 }
 
@@ -336,6 +348,59 @@ __global__ void __launch_bounds__(256) compact_follow(PagesArgs g) {
     g.uses[from] = 0;
   }
 }
+// ---- an update in two launches ---------------------------------------------------------------------------------------------
+//
+// Behind the rows, which note what they drop and want: uses in LDS, from there the free pages, and each want finds its row among the wants before each row.
+constexpr int kSecondThreads = 1024, kSecondWaves = kSecondThreads / kWave, kSecondPages = 8192, kSecondBatch = 1024;
+__device__ __forceinline__ int row_of_rank(const int32_t* before, int batch, int r) {       // the last row with before[row] <= r
+  int lo = 0;
+  for (int step = kSecondBatch / 2; step > 0; step /= 2)
+    if (lo + step < batch && before[lo + step] <= r) lo += step;
+  return lo;
+}
+__global__ void __launch_bounds__(kSecondThreads) pages_second(PagesArgs g) {
+  extern __shared__ __attribute__((aligned(16))) int32_t lds[];
+  __shared__ int of_wave[kSecondWaves];
+  const int tid = threadIdx.x, mine = tid < g.batch ? tid : -1;
+  int32_t* const uses = lds;                                       // [pages], what it is at the end
+  int32_t* const drops_before = uses + (g.pages + 3) / 4 * 4;      // [batch]
+  int32_t* const wants_before = drops_before + g.batch;            // [batch]
+  int32_t* const list = wants_before + g.batch;                    // [pages], free ones in order
+  const int drops_mine = mine >= 0 ? g.drops[mine] : 0, wants_mine = mine >= 0 ? g.need[mine] : 0;
+  for (int p = tid; p < g.pages; p += kSecondThreads) uses[p] = g.uses_from[p];
+  int drops, wants, sum, before = 0;
+  const int drops_at = sum_before<kSecondWaves>(drops_mine, of_wave, drops), wants_at = sum_before<kSecondWaves>(wants_mine, of_wave, wants);
+  if (mine >= 0) { drops_before[mine] = drops_at; wants_before[mine] = wants_at; }
+  __syncthreads();
+  auto place_of = [&](int r) {
+    const int b = row_of_rank(wants_before, g.batch, r);
+    return b * g.places + g.wanted[b * g.places + r - wants_before[b]];
+  };
+  int64_t place = tid < wants ? place_of(tid) : 0;                 // (on its way while drops and free pages are looked at)
+  for (int r = tid; r < drops; r += kSecondThreads) {
+    const int b = row_of_rank(drops_before, g.batch, r);
+    atomicAdd(&uses[g.dropped[b * g.places + r - drops_before[b]]], -1);
+  }
+  __syncthreads();
+  for (int first = 0; first < g.pages && before < wants; first += kSecondThreads * kEach) {
+    const Bits bits = chunk_bits(uses, g.pages, first + tid * kEach);
+    uint32_t free = bits.there & ~bits.used;
+    int at = before + sum_before<kSecondWaves>(__popc(free), of_wave, sum);
+    for (; free != 0; free &= free - 1) list[at++] = first + tid * kEach + __builtin_ctz(free);
+    before += sum;
+  }
+  if (tid == 0 && g.count) *g.count = wants > before ? wants - before : 0;
+  __syncthreads();
+  for (int r = tid; r < wants; r += kSecondThreads) {
+    const int e = r < before ? list[r] : -1;
+    g.table[place] = e;
+    if (e >= 0) uses[e] = 1;
+    if (r + kSecondThreads < wants) place = place_of(r + kSecondThreads);
+  }
+  __syncthreads();
+  for (int p = tid; p < g.pages; p += kSecondThreads) g.uses[p] = uses[p];
+}
+
 // ---- all of it in one block -------------------------------------------------------------------------------------------------
 //
 // What the launches above do one after another, for tables of which each thread has a few entries: uses, lists and what is known of rows lie in LDS, and a barrier stands where a
@@ -568,7 +633,8 @@ PagesArgs pages_args(const ac_page_books& from, const ac_page_books& to, void* w
   g.source = w; w += most;
   g.target = w; w += most;
   g.tokens = w; w += g.batch;
-  g.need = w;
+  g.need = w; w += g.batch;
+  g.drops = w;
   return g;
 }
 
@@ -587,6 +653,17 @@ hipError_t once_launch(const PagesArgs& g, hipStream_t s) {
 template <bool FORK>
 hipError_t rows_launch(const PagesArgs& g, hipStream_t s) {
   if (at_once(g)) return once_launch<FORK ? FORK_ROWS : UPDATE>(g, s);
+  if (!FORK && g.pages <= kSecondPages && g.batch <= kSecondBatch) {
+    static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_second), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                              (2 * kSecondPages + 2 * kSecondBatch + 4) * (int)sizeof(int32_t));
+    if (attr_status != hipSuccess) return attr_status;
+    PagesArgs n = g;
+    n.dropped = g.drops + g.batch;
+    n.wanted = n.dropped + g.batch * g.places;
+    hipLaunchKernelGGL((pages_rows<FORK>), dim3((unsigned)(g.batch / 4 + 1)), dim3(256), 0, s, n);
+    hipLaunchKernelGGL(pages_second, dim3(1), dim3(kSecondThreads), ((g.pages + 3) / 4 * 4 + g.pages + 2 * g.batch) * sizeof(int32_t), s, n);
+    return hipGetLastError();
+  }
   if (g.uses != g.uses_from && g.pages > 0)
     hipLaunchKernelGGL(pages_copy_uses, dim3((unsigned)(g.chunks < 1024 ? 4 * g.chunks : 4096)), dim3(256), 0, s, g);
   hipLaunchKernelGGL((pages_rows<FORK>), dim3((unsigned)(g.batch / 4 + 1)), dim3(256), 0, s, g);
@@ -606,7 +683,8 @@ hipError_t rows_launch(const PagesArgs& g, hipStream_t s) {
 
 uint64_t pages_workspace_bytes(const ac_page_books& b) {
   const uint64_t most = b.pages > b.batch ? b.pages : b.batch;
-  return (64 + (b.pages + kChunk - 1) / kChunk + b.pages + 2 * most + 2 * b.batch) * sizeof(int32_t);
+  const uint64_t noted = b.pages <= kSecondPages && b.batch <= kSecondBatch ? 2 * b.batch * b.ld_page_table : 0;
+  return (64 + (b.pages + kChunk - 1) / kChunk + b.pages + 2 * most + 3 * b.batch + noted) * sizeof(int32_t);
 }
 
 hipError_t launch_pages_update(const ac_page_books& from, const ac_page_books& to, const int32_t* drop_begin, const int32_t* drop_end, const int32_t* take_begin,

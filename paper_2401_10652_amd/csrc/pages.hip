@@ -351,7 +351,7 @@ __global__ void __launch_bounds__(256) compact_follow(PagesArgs g) {
 // ---- an update in two launches ---------------------------------------------------------------------------------------------
 //
 // Behind the rows, which note what they drop and want: uses in LDS, from there the free pages, and each want finds its row among the wants before each row.
-constexpr int kSecondThreads = 1024, kSecondWaves = kSecondThreads / kWave, kSecondPages = 8192, kSecondBatch = 1024;
+constexpr int kSecondThreads = 1024, kSecondWaves = kSecondThreads / kWave, kSecondPages = 8192, kSecondBatch = 1024, kSecondPlaces = 1 << 22;
 __device__ __forceinline__ int row_of_rank(const int32_t* before, int batch, int r) {       // the last row with before[row] <= r
   int lo = 0;
   for (int step = kSecondBatch / 2; step > 0; step /= 2)
@@ -650,10 +650,12 @@ hipError_t once_launch(const PagesArgs& g, hipStream_t s) {
   return hipGetLastError();
 }
 
+bool in_two(int64_t pages, int64_t batch, int64_t places) { return pages <= kSecondPages && batch <= kSecondBatch && batch * places <= kSecondPlaces; }
+
 template <bool FORK>
 hipError_t rows_launch(const PagesArgs& g, hipStream_t s) {
   if (at_once(g)) return once_launch<FORK ? FORK_ROWS : UPDATE>(g, s);
-  if (!FORK && g.pages <= kSecondPages && g.batch <= kSecondBatch) {
+  if (!FORK && in_two(g.pages, g.batch, g.places)) {
     static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_second), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                               (2 * kSecondPages + 2 * kSecondBatch + 4) * (int)sizeof(int32_t));
     if (attr_status != hipSuccess) return attr_status;
@@ -683,7 +685,7 @@ hipError_t rows_launch(const PagesArgs& g, hipStream_t s) {
 
 uint64_t pages_workspace_bytes(const ac_page_books& b) {
   const uint64_t most = b.pages > b.batch ? b.pages : b.batch;
-  const uint64_t noted = b.pages <= kSecondPages && b.batch <= kSecondBatch ? 2 * b.batch * b.ld_page_table : 0;
+  const uint64_t noted = in_two(b.pages, b.batch, b.ld_page_table) ? 2 * b.batch * b.ld_page_table : 0;
   return (64 + (b.pages + kChunk - 1) / kChunk + b.pages + 2 * most + 3 * b.batch + noted) * sizeof(int32_t);
 }
 

@@ -8,7 +8,8 @@ pytestmark = pytest.mark.gpu
 
 # pages, sequences, places, tokens of a page: nothing, single ones, around a block's and a wave's counts, several chunks of pages, many sequences
 SIZES = [(0, 0, 0, 16), (0, 3, 4, 16), (5, 0, 7, 16), (5, 2, 0, 32), (1, 1, 1, 16), (3, 1, 9, 64), (40, 3, 8, 16), (70, 5, 65, 32), (4095, 30, 64, 64), (4097, 7, 300, 16), (9000, 70, 63, 128),
-         (20000, 257, 33, 16), (70000, 64, 500, 48), (300, 1100, 3, 16)]
+         (20000, 257, 33, 16), (70000, 64, 500, 48), (300, 1100, 3, 16),
+         (4000, 60, 100, 16), (8192, 1024, 5, 16), (8192, 16, 256, 16), (50, 300, 20, 16), (8193, 200, 40, 32)]
 
 
 @pytest.fixture(scope="module")

@@ -66,7 +66,7 @@ class Decoder:
             self.next_books = B.page_books(self.next_uses, self.next_table, page)
             self.books_workspace = B.empty_workspace(B.ac_pages_workspace_bytes(self.books))
             self.missing = torch.zeros(1, dtype=torch.int32, device=dev)
-            self.held = [0] * sequences
+            self.ends = [0] * sequences
         else:
             self.table = torch.arange(pages, dtype=torch.int32, device=dev).view(sequences, each)
         codes = dict(dtype=torch.uint8, device=dev)
@@ -108,7 +108,8 @@ class Decoder:
         if self.shares:
             before, drop_begin, drop_end = where[2 * seqs + 1:].view(3, seqs)
             B.ac_op_pages_update(self.books, self.books, self.books_workspace, (drop_begin, drop_end), (before, length), self.missing)
-            self._enough(self._places(lengths))
+            self.ends = [max(e, -(-n // self.page)) for e, n in zip(self.ends, lengths)]
+            self._enough(self.ends, self.lengths)
         rows = B.cache_rows(where[:seqs + 1], length, self.table, max(counts), max(lengths))
         need = self._workspace_bytes(n, rows)
         if need > self.workspace.numel():
@@ -117,20 +118,17 @@ class Decoder:
         self.lengths = lengths
         return x
 
-    def _places(self, lengths):
-        """The most places that name a page, of each sequence after its update to these lengths."""
-        if self.window is None:
-            return [-(-n // self.page) for n in lengths]
-        p = self.page
-        return [min(-(-n // p), -(-self.sinks // p) + (self.window + n - before + p - 2) // p + 1) for n, before in zip(lengths, self.lengths)]
-
-    def _enough(self, held):
-        """Raises where pages ran out in the last call, after which sequences have up to `held` places.  The device is asked only where there are fewer pages."""
-        if sum(held) > self.uses.shape[0]:
+    def _enough(self, ends, behind=None):
+        """Raises where pages ran out in the last call.  ends: of each sequence, the places up to the last that may name a page (which a length that was set back does not tell);
+        behind: the tokens that it had before, whose window has been left.  The device is asked only where there are fewer pages than such places."""
+        most = sum(ends)
+        if self.window is not None and behind is not None:
+            sinks = -(-self.sinks // self.page)
+            most = sum(min(e, sinks + e - max(0, n - self.window + 1) // self.page) for e, n in zip(ends, behind))
+        if most > self.uses.shape[0]:
             missing = self.missing.item()
             if missing:
                 raise RuntimeError(f"{missing} pages are missing: the cache has {self.uses.shape[0]}")
-        self.held = held
 
     def _sharing(self):
         if not self.shares:
@@ -146,7 +144,7 @@ class Decoder:
         ends = torch.tensor([0] * n + [(1 << 31) - 1 if b in gone else 0 for b in range(n)], dtype=torch.int32).to("cuda").view(2, n)
         B.ac_op_pages_update(self.books, self.books, self.books_workspace, drop=(ends[0], ends[1]))
         for b in gone:
-            self.lengths[b] = self.held[b] = 0
+            self.lengths[b] = self.ends[b] = 0
 
     def fork(self, parents, lengths=None):
         """Sequence j goes on as sequence parents[j] (or, -1, has no tokens).  parents may be on the device (int32), with the lengths, that it does not tell, by the caller."""
@@ -158,20 +156,20 @@ class Decoder:
             if len(parents) != n or not all(-1 <= p < n for p in parents):
                 raise ValueError(f"parents {parents} of {n} sequences")
             lengths = [self.lengths[p] if p >= 0 else 0 for p in parents]
-            held = [self.held[p] if p >= 0 else 0 for p in parents]
+            ends = [self.ends[p] if p >= 0 else 0 for p in parents]
         else:
-            held = [max(self.held)] * n
+            ends = [max(self.ends)] * n
         if len(lengths) != n:
             raise ValueError(f"{len(lengths)} lengths of {n} sequences")
         if not torch.is_tensor(parents):
             parents = torch.tensor(parents, dtype=torch.int32).to("cuda")
         now = torch.tensor(self.lengths, dtype=torch.int32).to("cuda")
         B.ac_op_cache_fork(self.all_caches, self.books, self.next_books, parents, now, torch.empty_like(now), self.books_workspace, self.missing)
-        self._enough(held)
+        self._enough(ends)
         # (the graph of a step knows the table by its address)
         self.table.copy_(self.next_table)
         self.uses.copy_(self.next_uses)
-        self.lengths = list(lengths)
+        self.lengths, self.ends = list(lengths), ends
 
     def compact(self):
         """Moves the pages in use to the front of the cache; how many they are, on the device."""
@@ -257,7 +255,8 @@ class Decoder:
             graph.replay()
             if self.shares:
                 on_device = None                                        # (where pages are missing lengths are copied again)
-                self._enough(self._places([t + 1 for t in self.lengths]))
+                self.ends = [max(e, -(-(t + 1) // self.page)) for e, t in zip(self.ends, self.lengths)]
+                self._enough(self.ends, self.lengths)
             self.lengths = [t + 1 for t in self.lengths]
             on_device = list(self.lengths)                              # (the caller may change the other one in place)
             return y

@@ -106,6 +106,20 @@ def test_forks_read_on_as_models_of_their_own(B):
     held(m)
 
 
+def test_lengths_set_back_hold_their_pages(B):
+    """Places behind a length that was set back name pages still, which are counted where pages run out, and used again."""
+    m, x = model("f32", 2, 130, pages=6)
+    m.forward(x[:80], [80, 0])
+    m.lengths = [10, 0]
+    with pytest.raises(RuntimeError, match="1 pages are missing"):
+        m.forward(x[:30], [10, 20])
+    assert m.lengths == [10, 0] and held(m) == 6
+    m.forward(x[:40], [40, 0])
+    assert m.lengths == [50, 0] and held(m) == 6
+    m.release([0])
+    m.forward(x[:60], [30, 30])
+
+
 def test_forks_want_pages(B):
     m, x = model("f32", 4, 130, pages=5)
     m.forward(x[:40], [40, 0, 0, 0])

@@ -215,6 +215,23 @@ def test_window_that_reaches_all_is_causal_attention(B):  # noqa: F811
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype,counts,length", [("f32", [9], 350), ("bf16", [60], 345), ("bf16", [3], 900)])
+@pytest.mark.parametrize("window,sinks", [(30, 20), (500, 0), (70, 300)])
+def test_window_of_a_text_longer_than_its_table(B, dtype, counts, length, window, sinks):  # noqa: F811
+    """Tokens without a place (the table has 304) count as masked."""
+    import torch
+    cache = D.Cache([300], 2, 64, 16, 3)
+    cache.fill(0, 300, 1003)
+    dev = Device(B, cache, 0)
+    q, q64 = up(D.normal((counts[0], 4 * 64), 4), dtype)
+    rows = dev.rows(counts, [length])
+    out = torch.full_like(q, float("nan"))
+    B.ac_op_cache_attention_window(q, out, dev.desc, rows, window, sinks, workspace=B.empty_workspace(B.ac_cache_attention_window_workspace_bytes(q, dev.desc, rows, window, sinks)))
+    got = out.double().cpu().numpy().reshape(counts[0], 4, 64)
+    ref, size, reach = attention(q64.reshape(counts[0], 4, 64), cache, 0, length, 2, window, sinks, 64 ** -0.5)
+    assert (np.abs(got - ref) <= D.attention_bound(ref, size, reach, dtype)).all()
+
+
 def test_window_of_a_long_text(B):  # noqa: F811
     """Places near 2^30, of which only the pages in the window are there; launches of such tables read nothing behind them."""
     import torch

@@ -630,7 +630,8 @@ constexpr int kPromptRows = 32, kPromptWork = 1 << 24;
 // more than it saves: 300 tokens 6.3 us and, in two runs, 7.9, 600 tokens 7.9 and 8.4; 1200 tokens 10.9 and 8.5.
 constexpr int kMostSplits = 128, kLeastRun = 256, kWholeRun = 640, kLongRun = 2048, kPlaces = 512, kPromptPlaces = 256;
 // tokens: the most that a row or a tile reads.
-Shape shape(int heads, const ac_kv_cache& c, const CacheRows& r, int64_t tokens, int dtype) {
+int windowed_splits(int64_t blocks, int64_t tokens, int head_dim);
+Shape shape(int heads, const ac_kv_cache& c, const CacheRows& r, int64_t tokens, bool windowed, int dtype) {
   const int64_t rows_of = r.max_rows < r.rows ? r.max_rows : r.rows, rows = rows_of * (heads / c.heads);
   const int64_t all = rows_of < r.rows / (r.batch > 0 ? r.batch : 1) ? rows_of * r.batch : r.rows;
   Shape s;
@@ -638,6 +639,10 @@ Shape shape(int heads, const ac_kv_cache& c, const CacheRows& r, int64_t tokens,
   const int each = s.prompt ? 128 : 16;
   s.tiles = rows < 1 ? 1 : (int)((rows + each - 1) / each);
   const int64_t blocks = (int64_t)s.tiles * c.heads * r.batch;
+  if (windowed && !s.prompt) {
+    s.splits = windowed_splits(blocks, tokens, c.head_dim);
+    return s;
+  }
   int64_t n = blocks > 0 ? (s.prompt ? kPromptPlaces : kPlaces) / blocks : 1;
   if (!s.prompt && r.batch > 1) {
     int64_t runs = tokens / kLongRun;
@@ -649,6 +654,27 @@ Shape shape(int heads, const ac_kv_cache& c, const CacheRows& r, int64_t tokens,
   if (n > kMostSplits) n = kMostSplits;
   s.splits = n < 1 ? 1 : (int)n;
   return s;
+}
+
+// Behind a window the host knows how many keys a tile reads, and all sequences that are longer than it read as many: runs are chosen by what they cost, in steps of 256 keys.  Up to a block
+// a CU, blocks of fewer steps are as much faster; two blocks a CU take 1.7 times as long for a step, more in proportion; and the join takes as long as one to three steps.
+// Measured (us, runs 1, 2, 3, 4, 6, 8 and 16; * is taken): 4096 tokens, one sequence of 16 heads of 128 46, 30, 23, 20, 16, 15, 13*; 8 sequences of 32 heads on 8 47, 31, 25, 22*, 22, 23, 26;
+// 24 of them 54, 47*, 44, 46, 43, 51, 62; 64 of them 99*, 109, 110, 115, 118, 141, 177; 48 sequences of drafted tokens through 1000, fp32, 12 heads on 4 of 64 15*, 17, 18, 19, 20, 23, 38; 4 sequences of
+// 16 heads on 4 of 128 in fp32 through 8192 96, 55, 40, 34, 26, 23, 19*.
+int windowed_splits(int64_t blocks, int64_t tokens, int head_dim) {
+  double best = 0;
+  int splits = 1;
+  for (int n = 1; n <= kMostSplits && (n == 1 || (n - 1) * (int64_t)kLeastRun < tokens); ++n) {
+    const int64_t even = (tokens + n - 1) / n, steps = (even + kLeastRun - 1) / kLeastRun, runs = (tokens + steps * kLeastRun - 1) / (steps * kLeastRun);
+    if (runs < n) continue;                                              // (as with fewer)
+    const double load = (double)(blocks * runs) / kPromptPlaces;
+    const double cost = steps * (load <= 1 ? 1.0 : load <= 2 ? 1.7 : 1.2 * load) + (n == 1 ? 0.0 : head_dim <= 64 ? 2.5 : 1.5);
+    if (n == 1 || cost < best) {
+      best = cost;
+      splits = n;
+    }
+  }
+  return splits;
 }
 
 // The most tokens of a windowed call's tile: the sinks' blocks, the first row's window with its first block, and the rows behind that one.
@@ -734,14 +760,14 @@ hipError_t launch_cache_append(const void* q, int64_t ldq, void* q_out, int64_t 
 }
 
 uint64_t cache_attention_workspace_bytes(int heads, const ac_kv_cache& cache, const CacheRows& rows, const CacheSight& sight, int dtype) {
-  const int n = shape(heads, cache, rows, sight.windowed ? window_tokens(heads, cache, rows, sight.window, sight.sinks) : rows.max_length, dtype).splits;
+  const int n = shape(heads, cache, rows, sight.windowed ? window_tokens(heads, cache, rows, sight.window, sight.sinks) : rows.max_length, sight.windowed != 0, dtype).splits;
   return n == 1 ? 0 : (uint64_t)n * rows.rows * heads * (cache.head_dim + 2) * sizeof(float);
 }
 
 hipError_t launch_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int heads, const ac_kv_cache& cache,
                                   const CacheRows& rows, const CacheSight& sight, float scale, void* workspace, int dtype, hipStream_t s) {
   if (rows.batch <= 0 || rows.rows <= 0) return hipSuccess;
-  const Shape sh = shape(heads, cache, rows, sight.windowed ? window_tokens(heads, cache, rows, sight.window, sight.sinks) : rows.max_length, dtype);
+  const Shape sh = shape(heads, cache, rows, sight.windowed ? window_tokens(heads, cache, rows, sight.window, sight.sinks) : rows.max_length, sight.windowed != 0, dtype);
   const int n = sh.splits;
   float* parts = (float*)workspace;
   CacheAttnArgs a{q, out, ldq, ldo, heads, cache, rows, sight.causal, sight.window, sight.sinks, scale * kLog2e, divisor(heads / cache.heads),

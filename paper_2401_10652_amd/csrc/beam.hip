@@ -1,6 +1,10 @@
 // Beam search's selection.  A candidate is (beam i, token t) with total = score[i] + x[i, t] - log sum_t exp x[i, t]; within a beam totals are in the order of the logits, so a
 // run of a row needs its `keep` largest logits and, for the sum, its maximum and the sum of exponentials behind it: one pass over the logits, which HBM bounds.  A second
 // kernel puts a prompt's runs together and ranks their candidates by totals in 64 bits: of two beams' candidates the larger is wanted, however close they are.
+//
+// 64 prompts of eight beams over 131072 tokens in bf16, eight kept, 15 % of the beams ended, 114 MB: 32 us for the runs (3.6 TB/s; 26 without looking for candidates) and 9 for the ranks; one prompt of four over 49999 in fp32: 5.5 and 7.  What
+// bounds the runs is vector work (250 instruction slots for 32 logits a lane, of which the exponentials are half) beside HBM, and that beams which ended leave some CUs with less than others; the
+// ranks are latency: sums, their logarithm, the border, the candidates' entries.
 #include <float.h>
 
 #include "common.h"
@@ -413,7 +417,8 @@ __global__ void __launch_bounds__(kThreads) beam_rank(BeamArgs g) {
   }
 }
 
-// Steps of U vectors of 16 bytes a lane, and runs of so many steps that there are enough of them to fill the chip.
+// Steps of U vectors of 16 bytes a lane, and runs of so many steps that there are enough of them to fill the chip: four waves a SIMD.  us of both kernels: 512 rows of 131072 bf16 with
+// 8192 steps of 4 vectors in runs of 8 43.5, of 4 46, of 2 50, of 16 50; of 2 vectors in runs of 16 46; of one 52.  Four rows of 49999 fp32 in one step a run: 4 vectors 13.0, 2 13.1, one 15.3.
 struct Shape { int vectors, steps, runs; };
 Shape shape(int64_t rows, int64_t vocab, int dtype) {
   const int64_t vec = kWave * (dtype == AC_BF16 ? 8 : 4);

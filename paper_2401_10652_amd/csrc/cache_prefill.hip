@@ -43,6 +43,8 @@ template <int HD> constexpr size_t lds_bytes() {
   return ring > join ? ring : join;
 }
 
+// 2048 rows behind 14336 tokens through 4096 and 64 sinks, 16 heads of 128: 87 us, 0.80 PFLOP/s: a block has 33 steps of each side, behind a prologue and before a join that take 6 us.
+//
 // WINDOWED: tiles of keys are made of the blocks of the block's Reach, the sinks' and then the window's; key numbers count these blocks.
 template <int HD, bool WINDOWED>
 __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(CacheAttnArgs g) {

@@ -3,6 +3,12 @@
 // Free pages are taken by number, the lowest first, and places that want one stand in the order of the table, so that what a call leaves does not depend on
 // which thread came first: numbers of free pages and of wants are counted before them (prefix sums), and a want's rank finds the page of that rank.  uses is
 // changed by integer atomics, whose order does not matter.  Pages are copied by one kernel, 16 bytes a lane.
+//
+// A call is bound by launches and by one memory latency after another, not by its bytes, so small books go through in one launch and middling updates in two.  us on the GPU, and in a row of calls from
+// Python (which takes 3 to 4 us of the host a launch): an update of 16 sequences of 67 places 4.3 and 6.9 in one launch, 6.3 and 9.0 in two, 9.3 and 16 in four; 64 of 75 (4800 places, past
+// what one block takes) 8.6 and 9.4 in two, 11.6 and 16.4 in four; 64 of 534 9.8 and 11.9; 1000 of 101 10.6 and 12.8; 250 of 2048 16.1 and 17.8; with 22706 pages two take 22 (whose second launch
+// goes through uses alone) and four 16.3.  Forks of 128 sequences of 28 places 10.6 in two launches, 13.6 in five; compactions of 24 sequences 9.7 and 12.5.  One block for the ranks of wants
+// and pages instead of two launches of many: 16.3 and 17.3 with 22706 pages, 11.9 and 13.6 with 1112.
 #include "common.h"
 
 namespace ac {
@@ -54,12 +60,13 @@ __device__ __forceinline__ int sum_before(int v, int* of_wave, int& sum) {
 
 // ---- rows of the table, a wave each ------------------------------------------------------------------------------------
 
+constexpr int kAhead = 8;               // loads on their way (one by one 1024 rows of 1033 places take 7.2 us, so 6.1)
 struct Range { int64_t from, to; };     // places
 __device__ __forceinline__ Range places_in(const PagesArgs& g, const int32_t* begin, const int32_t* end, int b, bool whole) {
   if (!begin) return Range{0, 0};
-  const int64_t lo = begin[b] > 0 ? begin[b] : 0, hi = end[b] > 0 ? end[b] : 0;
+  const uint32_t lo = (uint32_t)max(begin[b], 0), hi = (uint32_t)max(end[b], 0), page = (uint32_t)g.page;
   if (hi <= lo) return Range{0, 0};
-  Range r = whole ? Range{(lo + g.page - 1) / g.page, hi / g.page} : Range{lo / g.page, (hi + g.page - 1) / g.page};
+  Range r = whole ? Range{(lo + page - 1) / page, hi / page} : Range{lo / page, (hi + page - 1) / page};
   if (r.to > g.places) r.to = g.places;
   return r;
 }
@@ -74,19 +81,24 @@ __device__ __forceinline__ int update_row(const PagesArgs& g, int b, int lane) {
   const int64_t end = apart ? g.places : drop.to;
   int wants = 0, drops = 0;
   const uint64_t lanes_before = (1ull << lane) - 1;
-  for (int64_t i0 = apart ? 0 : drop.from; i0 < end; i0 += kWave) {
-    const int64_t i = i0 + lane;
-    int e = i < end ? from[i] : -1;
-    const bool gone = i < end && i >= drop.from && i < drop.to && names(g, e);
-    if (NOTED) {
-      const uint64_t which = __ballot(gone);
-      if (gone) g.dropped[b * g.places + drops + __popcll(which & lanes_before)] = e;
-      drops += __popcll(which);
-    } else if (gone) {
-      add_use(g, e, -1);
+  for (int64_t i0 = apart ? 0 : drop.from; i0 < end; i0 += kAhead * kWave) {
+    int was[kAhead];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) was[a] = i0 + a * kWave + lane < end ? from[i0 + a * kWave + lane] : -1;
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const int64_t i = i0 + a * kWave + lane;
+      const int e = was[a];
+      const bool gone = i < end && i >= drop.from && i < drop.to && names(g, e);
+      if (NOTED) {
+        const uint64_t which = __ballot(gone);
+        if (gone) g.dropped[b * g.places + drops + __popcll(which & lanes_before)] = e;
+        drops += __popcll(which);
+      } else if (gone) {
+        add_use(g, e, -1);
+      }
+      if (i < end && (apart || gone)) to[i] = gone ? -1 : e;
     }
-    if (gone) e = -1;
-    if (i < end && (apart || gone)) to[i] = e;
   }
   // (in place a dropped entry may or may not be seen as it was: it wants a page either way)
   for (int64_t i0 = take.from; i0 < take.to; i0 += kWave) {
@@ -131,13 +143,23 @@ __device__ __forceinline__ int fork_row(const PagesArgs& g, int j, int lane) {
   const int32_t* old = g.table_from + j * g.places;
   const int32_t* from = g.table_from + (none ? 0 : p) * g.places;
   int32_t* to = g.table + j * g.places;
-  for (int64_t i = lane; i < g.places; i += kWave) {
-    const int o = old[i], n = !none && (i < whole || first) ? from[i] : -1;
-    if (n != o) {
-      add_use(g, o, -1);
-      add_use(g, n, 1);
+  for (int64_t i0 = 0; i0 < g.places; i0 += kAhead * kWave) {
+    int was[kAhead], now[kAhead];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const int64_t i = i0 + a * kWave + lane;
+      was[a] = i < g.places ? old[i] : -1;
+      now[a] = i < g.places && !none && (i < whole || first) ? from[i] : -1;
     }
-    to[i] = n;
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const int64_t i = i0 + a * kWave + lane;
+      if (now[a] != was[a]) {
+        add_use(g, was[a], -1);
+        add_use(g, now[a], 1);
+      }
+      if (i < g.places) to[i] = now[a];
+    }
   }
   const int source = !none && !first && rest > 0 && whole < g.places ? from[whole] : -1;
   const bool wants = names(g, source);
@@ -248,7 +270,7 @@ __global__ void __launch_bounds__(256) pages_list(PagesArgs g) {
   }
 }
 
-// Both by one block, which stops looking for free pages when there are enough.
+// Both by one block, which stops looking for free pages when there are enough.  (Up to kRankPages: it goes through 16384 a microsecond and a half.)
 constexpr int kRankThreads = 1024, kRankPages = 1 << 16;
 __global__ void __launch_bounds__(kRankThreads) pages_rank(PagesArgs g) {
   __shared__ int of_wave[kRankThreads / kWave];
@@ -563,7 +585,8 @@ struct CopyArgs {
   int n, pages, page;
 };
 
-// One block: 16 KB of a page's codes, keys before values.  A head's blocks lie one after another, so the first ones are its first units.
+// One block: 16 KB of a page's codes, keys before values.  A head's blocks lie one after another, so the first ones are its first units.  HBM bounds it: 504 pages of 128 KB in four layers, 265 MB
+// read and written, 55 us (4.8 TB/s, of 5.05 that a large copy reaches); 96 pages, 101 MB, 22 us (4.6).
 __global__ void __launch_bounds__(256) pages_copy(CopyArgs g) {
   const auto& c = g.cache[blockIdx.y];
   const int n = g.n_dev ? *g.n_dev : g.n;
@@ -638,7 +661,7 @@ PagesArgs pages_args(const ac_page_books& from, const ac_page_books& to, void* w
   return g;
 }
 
-// Whether one block gets through it.
+// Whether one launch does it, and an update in two: see the head of this file.
 bool at_once(const PagesArgs& g) { return g.pages <= kOnePages && g.batch <= kOneBatch && g.batch * g.places <= kOnePlaces; }
 template <int KIND>
 hipError_t once_launch(const PagesArgs& g, hipStream_t s) {

@@ -2,7 +2,7 @@
 // run of a row needs its `keep` largest logits and, for the sum, its maximum and the sum of exponentials behind it: one pass over the logits, which HBM bounds.  A second
 // kernel puts a prompt's runs together and ranks their candidates by totals in 64 bits: of two beams' candidates the larger is wanted, however close they are.
 //
-// 64 prompts of eight beams over 131072 tokens in bf16, eight kept, 15 % of the beams ended, 114 MB: 29 us for the runs (3.9 TB/s; 26 without looking for candidates) and 9 for the ranks; one prompt of four over 49999 in fp32: 5.5 and 7.  What
+// 64 prompts of eight beams over 131072 tokens in bf16, eight kept, 15 % of the beams ended, 114 MB: 29 us for the runs (3.9 TB/s; 26 without looking for candidates) and 8 for the ranks; one prompt of four over 49999 in fp32: 5.5 and 7.  What
 // bounds the runs is vector work (250 instruction slots for 32 logits a lane, of which the exponentials are half) beside HBM, and that beams which ended leave some CUs with less than others; the
 // ranks are latency: sums, their logarithm, the border, the candidates' entries.
 #include <float.h>
@@ -22,7 +22,7 @@ struct BeamArgs {
   float* scores_out; int32_t *parent, *token, *ended_out;
   int beams, vocab, keep, end;
   int runs, steps;                    // runs of a row, and steps of a run
-  Divisor of_beam, of_keep;           // runs, keep
+  Divisor of_beam, of_lists, of_keep; // runs, lists of a prompt, keep
   float* sums;                        // [rows][runs][2]: maximum, sum of exponentials
   float* value; int32_t* index;       // [rows][runs][keep], largest first; -inf where there are no more
 };
@@ -87,8 +87,8 @@ __device__ __forceinline__ void wave_fence() {
 // wherever that lies, so that equal rows give equal sums; one that would pass the row's end is the row's last one, without what the lanes before have of it.  A lane's exponents have its own
 // maximum for reference.  A logit is a candidate if it reaches `least`, which lies above the keep-th largest of those that were there when they were last looked at: at first it is the
 // keep-th largest of the maxima over groups of lanes, twice as many as are kept.  The block's waves, whose runs are of one row, share the highest of what they have: what lies below
-// it has enough larger ones wherever they are, and after the first step hardly anything reaches it.  (Alone a wave finds a few new ones in each of its steps: 11 us of 35 with 64 prompts of eight
-// beams over 131072 tokens.)  Which candidates a run keeps then depends on time, but not which ones come out.
+// it has enough larger ones wherever they are, and after the first step hardly anything reaches it.  (Alone a wave finds a few new ones in each of its steps: 37 us where 64 prompts of eight
+// beams over 131072 tokens took 34 then.)  Which candidates a run keeps then depends on time, but not which ones come out.
 template <typename T, int U>
 __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
   typedef typename Vec<T>::type V;
@@ -260,9 +260,9 @@ __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
   }
 }
 
-// One block: a prompt.  What comes out is found among the entries that reach a border: the keep-th largest of the threads' largest ones, in 32 bits (as the entries compared with
-// it are, which keeps their order).  A thread has lists of runs, whose first entries are their largest, and goes down those that reach it; where fewer threads than what is kept have
-// any, it has single entries.  Each candidate then counts those before it.
+// One block: a prompt.  What comes out is found among the entries that reach a border: the keep-th largest of the maxima over threads, or groups of them, of the lists' first
+// `levels` entries, in 32 bits (as the entries compared with it are, which keeps their order).  Below these levels a list is followed as far as it reaches the border.  Each candidate then counts
+// those before it.  Where more reach it than there is room for, all entries are looked at, and where they are too many still, as equal ones can be, the first are looked for one after another.
 __global__ void __launch_bounds__(kThreads) beam_rank(BeamArgs g) {
   __shared__ double rest[64], done[64];     // of each beam its score minus the logarithm of its sum (behind the maximum); and the score of one that ended: -inf where there is none
   __shared__ float top[64];
@@ -272,12 +272,21 @@ __global__ void __launch_bounds__(kThreads) beam_rank(BeamArgs g) {
   __shared__ int place_of[kMostCandidates];
   __shared__ double wave_value[kWaves];
   __shared__ int wave_place[kWaves];
-  const int tid = threadIdx.x, lane = tid % kWave, lists = g.beams * g.runs, entries = lists * g.keep;
+  const int tid = threadIdx.x, lane = tid % kWave, lists = g.beams * g.runs;
   const int64_t row0 = (int64_t)blockIdx.x * g.beams;
   const float* const value = g.value + row0 * g.runs * g.keep;
   const int32_t* const index = g.index + row0 * g.runs * g.keep;
-  bool heads = lists >= 2 * g.keep;
-  const float ahead = tid < (heads ? lists : entries) ? value[heads ? tid * g.keep : tid] : 0.f;       // (on its way while the sums are looked at)
+  bool by_list = false;
+  // an item: entry k of a list, all lists' first ones before all second ones; by_list: list by list, so that a list's entries are
+  // different threads' (where one list has most of what comes out)
+  auto list_of = [&](int item, int& k) {
+    const int q = quotient(item, by_list ? g.of_keep : g.of_lists), r = item - q * (by_list ? g.keep : lists);
+    k = by_list ? r : q;
+    return by_list ? q : r;
+  };
+  int levels = min(g.keep, max(1, kThreads / lists)), k_ahead;
+  const int list_ahead = list_of(tid, k_ahead);
+  const float ahead = tid < lists * levels ? value[list_ahead * g.keep + k_ahead] : 0.f;       // (on its way while the sums are looked at)
   for (int i = tid / kWave; i < g.beams; i += kWaves) {
     const float* sums = g.sums + (row0 + i) * g.runs * 2;
     const float score = g.scores[row0 + i];
@@ -302,7 +311,6 @@ __global__ void __launch_bounds__(kThreads) beam_rank(BeamArgs g) {
       done[i] = gone && score > -INFINITY ? score : -INFINITY;
     }
   }
-  if (tid == 0) { count_at = 0; border_at = 0x7fffffff; }
   __syncthreads();
   auto total_of = [&](int list, float v) {
     const int i = quotient(list, g.of_beam);
@@ -310,59 +318,60 @@ __global__ void __launch_bounds__(kThreads) beam_rank(BeamArgs g) {
     return r > -INFINITY && v > -INFINITY ? v == top[i] ? r : (double)v - top[i] + r : -INFINITY;
   };
   const double mine = tid < g.beams ? done[tid] : -INFINITY;
-  auto most_of = [&](int items) {
-    double most = mine;
-    for (int item = tid; item < items; item += kThreads)
-      most = fmax(most, total_of(heads ? item : quotient(item, g.of_keep), item == tid && items == (lists >= 2 * g.keep ? lists : entries) ? ahead : value[heads ? item * g.keep : item]));
-    return (float)most;
-  };
-  float most = most_of(heads ? lists : entries);
-  if (heads && __syncthreads_count(most > -INFINITY) < g.keep) {
-    heads = false;
-    most = most_of(entries);
-  }
-  // f of all of the thread's own entries, down a list up to the first for which it is false
+  // f of all of the thread's own entries, below the levels down a list up to the first for which it is false
   auto each = [&](auto f) {
     if (mine > -INFINITY) f(mine, tid * g.vocab + g.end);
-    const int items = heads ? lists : entries, down = heads ? g.keep : 1;
-    for (int item = tid; item < items; item += kThreads) {
-      const int list = heads ? item : quotient(item, g.of_keep), at = heads ? item * g.keep : item, place = quotient(list, g.of_beam) * g.vocab;
-      for (int k = 0; k < down; ++k) {
-        const double total = total_of(list, value[at + k]);
-        if (!(total > -INFINITY) || !f(total, place + index[at + k])) break;
+    for (int item = tid; item < lists * levels; item += kThreads) {
+      int k;
+      const int list = list_of(item, k), place = quotient(list, g.of_beam) * g.vocab, down = k == levels - 1 ? g.keep : k + 1;
+      for (; k < down; ++k) {
+        const double total = total_of(list, value[list * g.keep + k]);
+        if (!(total > -INFINITY) || !f(total, place + index[list * g.keep + k])) break;
       }
     }
   };
-  // the least of the groups' maxima with fewer than `keep` larger ones; as an integer in the order of the floats
-  const int all_items = heads ? lists : entries, holders = all_items < kThreads ? all_items : kThreads, group = holders >= 32 * g.keep ? 4 : holders >= 16 * g.keep ? 2 : 1, groups = (holders + group - 1) / group;
-  float most_of_group = most;
-  if (group >= 2) most_of_group = fmaxf(most_of_group, __shfl_xor(most_of_group, 1, kWave));
-  if (group >= 4) most_of_group = fmaxf(most_of_group, __shfl_xor(most_of_group, 2, kWave));
-  largest[tid] = -INFINITY;
-  __syncthreads();
-  if (tid % group == 0) largest[tid / group] = most_of_group;
-  __syncthreads();
-  int larger = 0;
+  for (;; levels = g.keep, by_list = true) {
+    if (tid == 0) { count_at = 0; border_at = 0x7fffffff; }
+    double largest_own = mine;
+    for (int item = tid; item < lists * levels; item += kThreads) {
+      int k;
+      const int list = list_of(item, k);
+      largest_own = fmax(largest_own, total_of(list, item == tid && !by_list ? ahead : value[list * g.keep + k]));
+    }
+    // the least of the groups' maxima with fewer than `keep` larger ones; as an integer in the order of the floats
+    const float most = (float)largest_own;
+    const int holders = lists * levels < kThreads ? lists * levels : kThreads, group = holders >= 32 * g.keep ? 4 : holders >= 16 * g.keep ? 2 : 1, groups = (holders + group - 1) / group;
+    float most_of_group = most;
+    if (group >= 2) most_of_group = fmaxf(most_of_group, __shfl_xor(most_of_group, 1, kWave));
+    if (group >= 4) most_of_group = fmaxf(most_of_group, __shfl_xor(most_of_group, 2, kWave));
+    largest[tid] = -INFINITY;
+    __syncthreads();
+    if (tid % group == 0) largest[tid / group] = most_of_group;
+    __syncthreads();
+    int larger = 0;
 #pragma unroll 2
-  for (int j = 0; j < groups; j += 4) {
-    const f32x4 a = *reinterpret_cast<const f32x4*>(&largest[j]);
+    for (int j = 0; j < groups; j += 4) {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(&largest[j]);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) larger += a[e] > most_of_group;
+      for (int e = 0; e < 4; ++e) larger += a[e] > most_of_group;
+    }
+    if (larger < g.keep) atomicMin(&border_at, in_order(most_of_group));
+    __syncthreads();
+    const float border = of_order(border_at);
+    if (most >= border)
+      each([&](double v, int place) {
+        if ((float)v < border) return false;
+        const int at = atomicAdd(&count_at, 1);
+        if (at < kMostCandidates) {
+          value_of[at] = v;
+          place_of[at] = place;
+        }
+        return true;
+      });
+    __syncthreads();
+    if (count_at <= kMostCandidates || by_list) break;
+    __syncthreads();
   }
-  if (larger < g.keep) atomicMin(&border_at, in_order(most_of_group));
-  __syncthreads();
-  const float border = of_order(border_at);
-  if (most >= border)
-    each([&](double v, int place) {
-      if ((float)v < border) return false;
-      const int at = atomicAdd(&count_at, 1);
-      if (at < kMostCandidates) {
-        value_of[at] = v;
-        place_of[at] = place;
-      }
-      return true;
-    });
-  __syncthreads();
   const int64_t out = (int64_t)blockIdx.x * g.keep;
   auto put = [&](int k, double total, int place) {
     const int i = place / g.vocab, t = place - i * g.vocab;
@@ -418,8 +427,8 @@ __global__ void __launch_bounds__(kThreads) beam_rank(BeamArgs g) {
   }
 }
 
-// Steps of U vectors of 16 bytes a lane, and runs of so many steps that there are enough of them to fill the chip: four waves a SIMD.  us of both kernels: 512 rows of 131072 bf16 with
-// 8192 steps of 4 vectors in runs of 8 43.5, of 4 46, of 2 50, of 16 50; of 2 vectors in runs of 16 46; of one 52.  Four rows of 49999 fp32 in one step a run: 4 vectors 13.0, 2 13.1, one 15.3.
+// Steps of U vectors of 16 bytes a lane, and runs of so many steps that there are enough of them to fill the chip: four waves a SIMD.  us of both kernels (before the last 6 us were gained): 512 rows of 131072 bf16
+// in steps of 4 vectors and runs of 8 43.5, of 4 46, of 2 50, of 16 50; of 2 vectors in runs of 16 46; of one 52.  Four rows of 49999 fp32 in one step a run: 4 vectors 13.0, 2 13.1, one 15.3.
 struct Shape { int vectors, steps, runs; };
 Shape shape(int64_t rows, int64_t vocab, int dtype) {
   const int64_t vec = kWave * (dtype == AC_BF16 ? 8 : 4);
@@ -442,7 +451,7 @@ hipError_t launch_beam_select(const BeamSelectArgs& b, hipStream_t s) {
   const int64_t parts = b.batch * b.beams * sh.runs;
   float* const w = (float*)b.workspace;
   BeamArgs g{b.logits, b.ld, b.scores, b.ended, b.scores_out, b.parent, b.token, b.ended_out, b.beams, (int)b.vocab, b.keep, b.end, sh.runs, sh.steps,
-             divisor((uint32_t)sh.runs), divisor((uint32_t)b.keep), w, w + 2 * parts, (int32_t*)(w + (2 + b.keep) * parts)};
+             divisor((uint32_t)sh.runs), divisor((uint32_t)(sh.runs * b.beams)), divisor((uint32_t)b.keep), w, w + 2 * parts, (int32_t*)(w + (2 + b.keep) * parts)};
   const dim3 grid((unsigned)((sh.runs + kWaves - 1) / kWaves), (unsigned)b.beams, (unsigned)b.batch);
   auto scan = [&](auto zero) {
     using T = decltype(zero);

@@ -13,7 +13,7 @@ namespace ac {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kNear = 1e38f;
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kThreads = 512, kWaves = kThreads / kWave, kRoom = 128, kNoted = 320, kMostCandidates = 512;
 
 struct BeamArgs {
@@ -116,8 +116,7 @@ __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
       }
     }
   };
-  // sum: of 2^(x log2 e - c) with c = top log2 e as it is rounded, which the end makes good; or, of a maximum past kNear, of e^(x - top)
-  float top = -INFINITY, c = 0.f, sum = 0.f, border = -INFINITY;
+  float top = -INFINITY, sum = 0.f, border = -INFINITY;
   int count = 0, noted = 0;
   auto share = [&](float v) {
     if (lane == 0) atomicMax(&border_of_all, in_order(v));
@@ -197,27 +196,24 @@ __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
       largest = fmaxf(largest, big[u]);
     }
     if (largest > top) {
-      const bool was_near = fabsf(top) < kNear, now_near = fabsf(largest) < kNear;
-      const float now = now_near ? largest * kLog2e : 0.f;
-      if (top > -INFINITY) sum *= __builtin_amdgcn_exp2f(was_near & now_near ? c - now : (top - largest) * kLog2e);
+      if (top > -INFINITY) sum *= __builtin_amdgcn_exp2f((top - largest) * kLog2e);
       top = largest;
-      c = now;
     }
-    if (!__any(top > -INFINITY && !(fabsf(top) < kNear))) {
-      float part[4] = {sum, 0.f, 0.f, 0.f};                                 // (four sums: what comes next need not wait for each)
+    // (the difference first: the maximum's own term is 1, and a row of one token has a logarithm of exactly 0)
+    const float ref = top > -INFINITY ? top : 0.f;
+    float part[4] = {sum, 0.f, 0.f, 0.f};                                 // (four sums: what comes next need not wait for each)
+    if (!__any(top == INFINITY)) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) part[e % 4] += __builtin_amdgcn_exp2f(fmaf(x[u][e], kLog2e, -c));
-      sum = (part[0] + part[1]) + (part[2] + part[3]);
-    } else {                                                          // (infinities share the probability)
-      const float ref = top > -INFINITY ? top : 0.f;
+        for (int e = 0; e < VEC; ++e) part[e % 4] += __builtin_amdgcn_exp2f((x[u][e] - ref) * kLog2e);
+    } else {                                                          // infinities share the probability
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e)
-          sum += fabsf(top) < kNear ? __builtin_amdgcn_exp2f(fmaf(x[u][e], kLog2e, -c)) : x[u][e] == top ? (top > -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f((x[u][e] - ref) * kLog2e);
+        for (int e = 0; e < VEC; ++e) part[e % 4] += x[u][e] == INFINITY ? 1.f : __builtin_amdgcn_exp2f((x[u][e] - ref) * kLog2e);
     }
+    sum = (part[0] + part[1]) + (part[2] + part[3]);
     // (of equal ones the lower index comes first: what equals the border is a candidate if that may be of this step, and none if it is of one before)
     float least;
     if (step == 0) {
@@ -251,7 +247,6 @@ __global__ void __launch_bounds__(kThreads) beam_scan(BeamArgs g) {
     g.value[list + lane] = lane < count ? value_of_key(found.key[lane]) : -INFINITY;
     if (lane < count) g.index[list + lane] = index_of_key(found.key[lane]);
   }
-  if (fabsf(top) < kNear) sum *= __builtin_amdgcn_exp2f(-fmaf(top, kLog2e, -c));
   const float of_all = max_of_wave(top);
   sum = group_sum<kWave>(top == of_all ? sum : sum * __builtin_amdgcn_exp2f((top - of_all) * kLog2e));
   if (lane == 0) {

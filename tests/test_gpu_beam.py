@@ -165,6 +165,18 @@ def test_what_is_not_finite(B, dtype):
     assert (got[1] == 1).all() and (got[0] == np.inf).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [1, 40, 3001])
+def test_one_token_that_may_come_is_certain(B, dtype, vocab):
+    """The logarithm of its probability is 0, not nearly so."""
+    x, s = np.full((3, 4, vocab), -np.inf), np.zeros((3, 4))
+    for i, v in enumerate(D.normal((12,), 5, 9.0)):
+        x[i // 4, i % 4, i * 7 % vocab] = v
+    s[1], s[2, 1:] = [-1.5, -2.25, -3.0, -11.0], -np.inf
+    got = check(B, x, s, dtype, 4)
+    assert (got[0][0] == 0).all() and (got[0][1] == s[1]).all() and (got[0][2] == [0, -np.inf, -np.inf, -np.inf]).all()
+
+
 def test_ascending_rows(B):
     """The largest logits side by side at the end of a row, and rows in order: every candidate of a run is in the last one's place."""
     for dtype in ("f32", "bf16"):

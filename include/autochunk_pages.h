@@ -18,8 +18,8 @@ extern "C" {
 /*
  * uses[p] is the number of places of page tables that name page p; a page with 0 (or less) is free.  A caller that keeps a page for itself, to share a prefix
  * for instance, adds one of its own.  Place i of sequence b, page_table[b * ld_page_table + i], is where tokens i * page up to (i + 1) * page - 1 lie; a number outside
- * [0, pages) names no page (-1 by these calls).  One set of books serves all layers: caches of the same pages.  pages at most 2^24, batch 65535, places of a sequence
- * (ld_page_table times page) 2^30, else AC_ERR_UNSUPPORTED; arrays on 4-byte boundaries, page a multiple of 16.
+ * [0, pages) names no page (-1 by these calls).  One set of books serves all layers: caches of the same pages.  pages at most 2^24, batch 65535, tokens of a sequence
+ * (ld_page_table times page) and entries of a table (batch times ld_page_table) 2^30, else AC_ERR_UNSUPPORTED; arrays on 4-byte boundaries, page a multiple of 16.
  *
  * Every call reads the books `from` and leaves those after it in `to`, of the same sizes; each of `to`'s arrays may be `from`'s own (where a call does not say
  * otherwise) or lies apart from both of them.  workspace: dev, 16-byte aligned, ac_pages_workspace_bytes() large, else AC_ERR_WORKSPACE; what it holds does not matter.

@@ -2365,8 +2365,9 @@ static int book_ok(const char* what, const ac_page_books* b) {
   if (!b || b->pages < 0 || b->ld_page_table < 0 || b->batch < 0 || b->page < 16 || b->page % 16 != 0 || (b->pages > 0 && !b->uses) ||
       (b->batch > 0 && b->ld_page_table > 0 && !b->page_table))
     return fail(AC_ERR_ARG, "%s: bad books", what);
-  if (b->pages > kMostPages || b->batch > 65535 || b->ld_page_table > (1 << 30) / b->page)
-    return fail(AC_ERR_UNSUPPORTED, "%s: at most 2^24 pages, 65535 sequences and 2^30 places of a sequence", what);
+  // (ranks of the table's entries are counted in 32 bits)
+  if (b->pages > kMostPages || b->batch > 65535 || b->ld_page_table > (1 << 30) / b->page || b->batch * b->ld_page_table > 1 << 30)
+    return fail(AC_ERR_UNSUPPORTED, "%s: at most 2^24 pages, 65535 sequences, 2^30 tokens of a sequence and 2^30 entries of a table", what);
   if ((uintptr_t)b->uses % 4 != 0 || (uintptr_t)b->page_table % 4 != 0) return fail(AC_ERR_ALIGN, "%s: books start at multiples of 4 bytes", what);
   return AC_OK;
 }
@@ -2380,6 +2381,9 @@ static int books_ok(const char* what, const ac_kv_cache* caches, int n_caches, c
   const int64_t table = from->batch * from->ld_page_table;
   if ((from->uses != to->uses && overlap(from->uses, from->pages, to->uses, from->pages)) || (from->page_table != to->page_table && overlap(from->page_table, table, to->page_table, table)))
     return fail(AC_ERR_ARG, "%s: books that overlap in part", what);
+  for (const int32_t* uses : {from->uses, to->uses})
+    if (overlap(uses, from->pages, from->page_table, table) || overlap(uses, from->pages, to->page_table, table))
+      return fail(AC_ERR_ARG, "%s: uses that overlap a table", what);
   if (n_caches > 0 && (caches[0].pages != from->pages || caches[0].page != from->page)) return fail(AC_ERR_ARG, "%s: books of other pages than the caches'", what);
   const uint64_t need = pages_workspace_bytes(*from);
   if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0)

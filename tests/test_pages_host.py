@@ -85,6 +85,21 @@ assert L.ac_pages_workspace_bytes(None) == 0 and L.ac_pages_workspace_bytes(byre
 """)
 
 
+def test_uses_and_tables_apart_and_ranks_in_32_bits(run):
+    run("""
+for what in (update, fork, compact):
+    for a, b in ((dict(), dict(uses=(1 << 45) + 68)), (dict(), dict(page_table=(1 << 44) - 68)), (dict(uses=(1 << 45) - 36), dict()), (dict(), dict(page_table=(1 << 46) + 36))):
+        refused(B.AC_ERR_ARG, what, a=books(**a), b=other(**b))
+    assert what(b=other(uses=(1 << 45) + 72, page_table=(1 << 44) - 72)) == 0 and kernels()
+    # entries of a table: 65535 x 16385 is more than 2^30, 65535 x 16384 is less
+    large, rest = dict(batch=65535, ld_page_table=16384, uses=1 << 50), dict(length_to=P + (1 << 20)) if what is fork else {}
+    assert what(a=books(**large, page_table=1 << 52), b=other(**{**large, "uses": 1 << 51}, page_table=1 << 53), **rest) == 0 and kernels(), L.ac_last_error()
+    large["ld_page_table"] += 1
+    refused(B.AC_ERR_UNSUPPORTED, what, a=books(**large, page_table=1 << 52), b=other(**{**large, "uses": 1 << 51}, page_table=1 << 53), **rest)
+assert L.ac_pages_workspace_bytes(byref(books(**large, page_table=1 << 52))) == 0
+""")
+
+
 def test_caches(run):
     run("""
 for what in (fork, compact, copy):

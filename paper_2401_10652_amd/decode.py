@@ -73,7 +73,7 @@ class Decoder:
         self.caches = [B.kv_cache(torch.zeros((pages, self.heads_kv, page, d), **codes), torch.zeros((pages, self.heads_kv, page // 16, d, 16), **codes),
                                   torch.ones((pages, self.heads_kv, page // 16), device=dev), torch.ones((pages, self.heads_kv, page // 16), device=dev))
                        for _ in layers]
-        self.all_caches = B.kv_caches(self.caches)
+        self.all_caches, self.no_caches = B.kv_caches(self.caches), B.kv_caches([])
         angle = torch.arange(max_tokens, dtype=torch.float64)[:, None] * base ** (-torch.arange(d // 2, dtype=torch.float64) / (d // 2))
         self.rotary = B.rotary(angle.cos().float().to(dev), angle.sin().float().to(dev))
         self.lengths = [0] * sequences
@@ -147,7 +147,7 @@ class Decoder:
             self.lengths[b] = self.ends[b] = 0
 
     def fork(self, parents, lengths=None):
-        """Sequence j goes on as sequence parents[j] (or, -1, has no tokens).  parents may be on the device (int32), with the lengths, that it does not tell, by the caller."""
+        """Sequence j goes on as sequence parents[j] (or, -1, has no tokens); where pages run out all stay as they are.  parents may be on the device (int32), with the lengths, that it does not tell, by the caller."""
         import torch
         self._sharing()
         n = len(self.lengths)
@@ -164,8 +164,11 @@ class Decoder:
         if not torch.is_tensor(parents):
             parents = torch.tensor(parents, dtype=torch.int32).to("cuda")
         now = torch.tensor(self.lengths, dtype=torch.int32).to("cuda")
-        B.ac_op_cache_fork(self.all_caches, self.books, self.next_books, parents, now, torch.empty_like(now), self.books_workspace, self.missing)
-        self._enough(ends)
+        to = (self.books, self.next_books, parents, now, torch.empty_like(now), self.books_workspace, self.missing)
+        if sum(ends) > self.uses.shape[0]:                              # the books alone first: copies go into pages that a sequence may have still, if this fails
+            B.ac_op_cache_fork(self.no_caches, *to)
+            self._enough(ends)
+        B.ac_op_cache_fork(self.all_caches, *to)
         # (the graph of a step knows the table by its address)
         self.table.copy_(self.next_table)
         self.uses.copy_(self.next_uses)

@@ -140,6 +140,21 @@ def test_forks_want_pages(B):
             call()
 
 
+def test_a_fork_that_fails_leaves_the_sequences(B):
+    """Pages that it would have freed and taken for copies are still a sequence's."""
+    import torch
+    m, x = model("f32", 4, 130, pages=5)
+    own, _ = model("f32", 4, 130)
+    for a in (m, own):
+        a.forward(x[:60], [40, 20, 0, 0])
+    before = [t[:5].clone() for c in m.caches for t in c.keep]
+    with pytest.raises(RuntimeError, match="1 pages are missing"):
+        m.fork([0, 0, 0, 0])
+    assert all(torch.equal(t[:5], u) for t, u in zip((t for c in m.caches for t in c.keep), before))
+    assert m.lengths == [40, 20, 0, 0] and held(m) == 5
+    assert torch.equal(m.forward(x[60:68], [3, 5, 0, 0]), own.forward(x[60:68], [3, 5, 0, 0]))
+
+
 @pytest.mark.parametrize("end", [-1, 7])
 def test_beam_search(B, end):
     """Every step's choice against the definition in 64 bits, from logits of a model that read each beam's tokens by itself."""

@@ -2,7 +2,7 @@
 // run of a row needs its `keep` largest logits and, for the sum, its maximum and the sum of exponentials behind it: one pass over the logits, which HBM bounds.  A second
 // kernel puts a prompt's runs together and ranks their candidates by totals in 64 bits: of two beams' candidates the larger is wanted, however close they are.
 //
-// 64 prompts of eight beams over 131072 tokens in bf16, eight kept, 15 % of the beams ended, 114 MB: 29 us for the runs (3.9 TB/s; 26 without looking for candidates) and 8 for the ranks; one prompt of four over 49999 in fp32: 5.5 and 7.  What
+// 64 prompts of eight beams over 131072 tokens in bf16, eight kept, 15 % of the beams ended, 114 MB: 30 us for the runs (3.8 TB/s; 26 without looking for candidates) and 8 for the ranks; one prompt of four over 49999 in fp32: 5.5 and 7.  What
 // bounds the runs is vector work (250 instruction slots for 32 logits a lane, of which the exponentials are half) beside HBM, and that beams which ended leave some CUs with less than others; the
 // ranks are latency: sums, their logarithm, the border, the candidates' entries.
 #include <float.h>

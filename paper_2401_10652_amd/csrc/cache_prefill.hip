@@ -43,9 +43,8 @@ template <int HD> constexpr size_t lds_bytes() {
   return ring > join ? ring : join;
 }
 
-// 2048 rows behind 14336 tokens through 4096 and 64 sinks, 16 heads of 128: 87 us, 0.80 PFLOP/s: a block has 33 steps of each side, behind a prologue and before a join that take 6 us.
-//
-// WINDOWED: tiles of keys are made of the blocks of the block's Reach, the sinks' and then the window's; key numbers count these blocks.
+// WINDOWED: tiles of keys are made of the blocks of the block's Reach, the sinks' and then the window's; key numbers count these blocks.  2048 rows behind 14336 tokens through 4096 and 64
+// sinks, 16 heads of 128: 84 us, 0.83 PFLOP/s (0.95 without a window): a block has 33 steps of each side, behind a prologue and before a join that take 6 us.
 template <int HD, bool WINDOWED>
 __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(CacheAttnArgs g) {
   constexpr int TILE = kTile * HD, BLOCK = kBlock * HD, CHUNKS = TILE / 1024;   // bytes of a tile's keys or values and of a block; KB of the former

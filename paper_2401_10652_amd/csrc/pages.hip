@@ -5,7 +5,7 @@
 // changed by integer atomics, whose order does not matter.  Pages are copied by one kernel, 16 bytes a lane.
 //
 // A call is bound by launches and by one memory latency after another, not by its bytes, so small books go through in one launch and middling updates in two.  us on the GPU, and in a row of calls from
-// Python (which takes 3 to 4 us of the host a launch): an update of 16 sequences of 67 places 4.3 and 6.9 in one launch, 6.3 and 9.0 in two, 9.3 and 16 in four; 64 of 75 (4800 places, past
+// Python (which takes 3 to 4 us of the host a launch): an update of 16 sequences of 67 places 3.5 and 6.9 in one launch, 6.3 and 9.0 in two, 9.3 and 16 in four; 64 of 75 (4800 places, past
 // what one block takes) 8.6 and 9.4 in two, 11.6 and 16.4 in four; 64 of 534 9.8 and 11.9; 1000 of 101 10.6 and 12.8; 250 of 2048 16.1 and 17.8; with 22706 pages two take 22 (whose second launch
 // goes through uses alone) and four 16.3.  Forks of 128 sequences of 28 places 10.6 in two launches, 13.6 in five; compactions of 24 sequences 9.7 and 12.5.  One block for the ranks of wants
 // and pages instead of two launches of many: 16.3 and 17.3 with 22706 pages, 11.9 and 13.6 with 1112.
@@ -426,23 +426,24 @@ __global__ void __launch_bounds__(kSecondThreads) pages_second(PagesArgs g) {
 // ---- all of it in one block -------------------------------------------------------------------------------------------------
 //
 // What the launches above do one after another, for tables of which each thread has a few entries: uses, lists and what is known of rows lie in LDS, and a barrier stands where a
-// launch does.  What bounds it is one memory latency after another.
+// launch does.  What bounds it is one memory latency after another, and EACH, the entries of a thread: with one an update of 4 sequences of 67 places takes 2.8 us (3.9 with four), a fork of 4 of 28 with its
+// copies 7.8 (9.0); with two 16 of 67 3.5 (4.4), 64 of 28 9.1 (10.0); with eight, for tables of 4800 places, updates take 9.8 and forks 15.0, in several launches 8.8 and 13.8.
 constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / kWave, kOnePages = 8192, kOneBatch = 1024, kOneEach = 4, kOnePlaces = kOneThreads * kOneEach;
 enum { UPDATE, FORK_ROWS, COMPACT };
 
-template <int KIND>
+template <int KIND, int EACH>
 __global__ void __launch_bounds__(kOneThreads) pages_at_once(PagesArgs g, Divisor of_row) {
   extern __shared__ __attribute__((aligned(16))) int32_t lds[];
   __shared__ int of_wave[kOneWaves];
-  const int tid = threadIdx.x, places = (int)g.places, first_entry = tid * kOneEach, entries = (int)(g.batch * g.places);
+  const int tid = threadIdx.x, places = (int)g.places, first_entry = tid * EACH, entries = (int)(g.batch * g.places);
   int32_t* const uses = lds;                                       // [pages], what it is at the end
   int32_t* const list = uses + (g.pages + 3) / 4 * 4;              // [pages]: free ones in order; of a compaction sources' ranks
   int32_t* const row = list + g.pages;                             // [4][batch]: of an update the ranges' ends, of a fork parent, whole pages and first; of a compaction targets [pages]
   const int mine = tid < g.batch ? tid : -1;
   int sum, wants = 0, before = 0, rank = 0;
-  int32_t was[kOneEach], now[kOneEach];
+  int32_t was[EACH], now[EACH];
 #pragma unroll
-  for (int e = 0; e < kOneEach; ++e) was[e] = now[e] = first_entry + e < entries ? g.table_from[first_entry + e] : -1;
+  for (int e = 0; e < EACH; ++e) was[e] = now[e] = first_entry + e < entries ? g.table_from[first_entry + e] : -1;
 
   int source = -1, rest = 0, parent = -1, length = 0;              // of a fork, row `mine`
   if (KIND == UPDATE && mine >= 0) {
@@ -474,14 +475,14 @@ __global__ void __launch_bounds__(kOneThreads) pages_at_once(PagesArgs g, Diviso
     }
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < kOneEach; ++e) {
+    for (int e = 0; e < EACH; ++e) {
       now[e] = -1;
       if (first_entry + e >= entries) continue;
       const int b = quotient(first_entry + e, of_row), i = first_entry + e - b * places, p = row[b];
       if (p >= 0 && (i < row[g.batch + b] || row[2 * g.batch + b] != 0)) now[e] = g.table_from[p * places + i];
     }
 #pragma unroll
-    for (int e = 0; e < kOneEach; ++e)
+    for (int e = 0; e < EACH; ++e)
       if (now[e] != was[e]) {
         if (names(g, was[e])) atomicAdd(&uses[was[e]], -1);
         if (names(g, now[e])) atomicAdd(&uses[now[e]], 1);
@@ -490,7 +491,7 @@ __global__ void __launch_bounds__(kOneThreads) pages_at_once(PagesArgs g, Diviso
   }
   if (KIND == UPDATE) {
 #pragma unroll
-    for (int e = 0; e < kOneEach; ++e) {
+    for (int e = 0; e < EACH; ++e) {
       if (first_entry + e >= entries) break;
       const int b = quotient(first_entry + e, of_row), i = first_entry + e - b * places;
       if (i >= row[b] && i < row[g.batch + b] && names(g, now[e])) {
@@ -518,7 +519,7 @@ __global__ void __launch_bounds__(kOneThreads) pages_at_once(PagesArgs g, Diviso
     if (tid == 0 && g.count) *g.count = n;
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < kOneEach; ++e)
+    for (int e = 0; e < EACH; ++e)
       if (names(g, was[e]) && was[e] >= n && uses[was[e]] > 0) now[e] = row[list[was[e]]];
     __syncthreads();
     for (int p = tid; p < g.pages; p += kOneThreads)
@@ -555,21 +556,21 @@ __global__ void __launch_bounds__(kOneThreads) pages_at_once(PagesArgs g, Diviso
       }
       __syncthreads();
 #pragma unroll
-      for (int e = 0; e < kOneEach; ++e) {
+      for (int e = 0; e < EACH; ++e) {
         if (first_entry + e >= entries) break;
         const int b = quotient(first_entry + e, of_row);
         if (row[2 * g.batch + b] != 0 && first_entry + e - b * places == row[g.batch + b]) now[e] = target[b];
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < kOneEach; ++e)
+      for (int e = 0; e < EACH; ++e)
         if (wanting >> e & 1) now[e] = give();
     }
   } else if (tid == 0 && g.count) {
     *g.count = 0;
   }
 #pragma unroll
-  for (int e = 0; e < kOneEach; ++e)
+  for (int e = 0; e < EACH; ++e)
     if (first_entry + e < entries && (g.table != g.table_from || now[e] != was[e])) g.table[first_entry + e] = now[e];
   __syncthreads();
   for (int p = tid; p < g.pages; p += kOneThreads) g.uses[p] = uses[p];
@@ -663,14 +664,19 @@ PagesArgs pages_args(const ac_page_books& from, const ac_page_books& to, void* w
 
 // Whether one launch does it, and an update in two: see the head of this file.
 bool at_once(const PagesArgs& g) { return g.pages <= kOnePages && g.batch <= kOneBatch && g.batch * g.places <= kOnePlaces; }
-template <int KIND>
-hipError_t once_launch(const PagesArgs& g, hipStream_t s) {
+template <int KIND, int EACH>
+hipError_t once_with(const PagesArgs& g, hipStream_t s) {
   constexpr int MOST = 2 * kOnePages + 4 + (kOnePages > 4 * kOneBatch ? kOnePages : 4 * kOneBatch);
-  static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_at_once<KIND>), hipFuncAttributeMaxDynamicSharedMemorySize, MOST * (int)sizeof(int32_t));
+  static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_at_once<KIND, EACH>), hipFuncAttributeMaxDynamicSharedMemorySize, MOST * (int)sizeof(int32_t));
   if (attr_status != hipSuccess) return attr_status;
   const int words = (g.pages + 3) / 4 * 4 + g.pages + (KIND == COMPACT ? g.pages : 4 * g.batch);
-  hipLaunchKernelGGL((pages_at_once<KIND>), dim3(1), dim3(kOneThreads), (size_t)words * sizeof(int32_t), s, g, divisor((uint32_t)(g.places > 0 ? g.places : 1)));
+  hipLaunchKernelGGL((pages_at_once<KIND, EACH>), dim3(1), dim3(kOneThreads), (size_t)words * sizeof(int32_t), s, g, divisor((uint32_t)(g.places > 0 ? g.places : 1)));
   return hipGetLastError();
+}
+template <int KIND>
+hipError_t once_launch(const PagesArgs& g, hipStream_t s) {
+  const int64_t entries = g.batch * g.places;
+  return entries <= kOneThreads ? once_with<KIND, 1>(g, s) : entries <= 2 * kOneThreads ? once_with<KIND, 2>(g, s) : once_with<KIND, kOneEach>(g, s);
 }
 
 bool in_two(int64_t pages, int64_t batch, int64_t places) { return pages <= kSecondPages && batch <= kSecondBatch && batch * places <= kSecondPlaces; }

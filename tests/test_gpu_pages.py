@@ -91,6 +91,15 @@ def test_update(B, pages, batch, places, page, same):
         dev.check(after, short)
 
 
+@pytest.mark.parametrize("pages,batch,places,page", [(700, 64, 16, 16), (600, 41, 25, 32), (900, 64, 32, 16), (1500, 3, 683, 16), (2000, 17, 241, 16)])
+def test_tables_that_fill_their_threads(B, pages, batch, places, page):
+    """Up to 1024, 2048 and 4096 places, and one more: a thread has one, two or four, or several launches go through them."""
+    for same in ((), ("uses", "table")):
+        test_update(B, pages, batch, places, page, same)
+        test_compact(B, pages, batch, places, page, same)
+    test_fork(B, pages, batch, places, page, ())
+
+
 def test_update_runs_dry_and_frees_what_it_takes(B):
     """One page for many places; pages that this very call frees are taken; no one counts what is missing."""
     books = P.Books([1, 1, 0, 1], [[0, 1, -1, -1], [3, -1, -1, -1]], 16)

@@ -37,7 +37,10 @@ class Decoder:
     queries and keys are rotated by their places, which no plan of the framework does, so that a plan's rows are not these.
 
     window, sinks: a token sees the last `window` ones, itself among them, and the first `sinks` ones.  pages: the cache has so many, which sequences take as they grow, give
-    up as their windows leave them, and share when one goes on as several (fork); without it, and without a window, each sequence has its own, enough for max_tokens."""
+    up as their windows leave them, and share when one goes on as several (fork); without it, and without a window, each sequence has its own, enough for max_tokens.
+
+    `lengths`, the sequences' numbers of tokens, may be set back, whole or one of it, between calls: a sequence then goes on behind as many of its tokens; behind a fork in pages of its own, so that
+    the others keep theirs."""
 
     window, sinks, shares = None, 0, False
 
@@ -67,6 +70,7 @@ class Decoder:
             self.books_workspace = B.empty_workspace(B.ac_pages_workspace_bytes(self.books))
             self.missing = torch.zeros(1, dtype=torch.int32, device=dev)
             self.ends = [0] * sequences
+            self.common = [0] * sequences                               # tokens before these lie in pages that others may have too
         else:
             self.table = torch.arange(pages, dtype=torch.int32, device=dev).view(sequences, each)
         codes = dict(dtype=torch.uint8, device=dev)
@@ -95,6 +99,8 @@ class Decoder:
         lengths = [a + b for a, b in zip(self.lengths, counts)]
         if max(lengths) > self.max_tokens:
             raise ValueError(f"{max(lengths)} tokens: the cache holds {self.max_tokens} of a sequence")
+        if self.shares:
+            self._part(b for b, c in enumerate(counts) if c > 0)
         begin = [0]
         for c in counts:
             begin.append(begin[-1] + c)
@@ -134,6 +140,36 @@ class Decoder:
         if not self.shares:
             raise ValueError("sequences of this cache have their own pages: give it a number of `pages` to share")
 
+    def _part(self, sequences):
+        """Of these sequences, those that were set back into what they have in common with others go on in pages of their own: a copy of the page that they write next, as far as they have
+        it, and none behind it.  (The device is asked: where nobody else has the pages any more they stay.)"""
+        import torch
+        for b in sequences:
+            n, page = self.lengths[b], self.page
+            if n >= self.common[b]:
+                continue
+            place, rest = divmod(n, page)
+            row = self.table[b, place:]
+            others = ((row >= 0) & (self.uses[row.clamp(min=0).long()] > 1)).nonzero().view(-1).tolist()
+            if others:
+                first, copies = place + others[0], others[0] == 0 and rest > 0
+                drop, take, tokens = [0] * (2 * len(self.lengths)), [0] * (2 * len(self.lengths)), [rest]
+                drop[2 * b], drop[2 * b + 1] = first * page, (1 << 31) - 1
+                if copies:
+                    take[2 * b], take[2 * b + 1] = place * page, n
+                at = torch.tensor(drop[0::2] + drop[1::2] + take[0::2] + take[1::2] + tokens, dtype=torch.int32).to("cuda")
+                ranges = at[:-1].view(4, -1)
+                B.ac_op_pages_update(self.books, self.next_books, self.books_workspace, (ranges[0], ranges[1]), (ranges[2], ranges[3]), self.missing)
+                if copies:
+                    missing = self.missing.item()
+                    if missing:
+                        raise RuntimeError(f"{missing} pages are missing: the cache has {self.uses.shape[0]}")
+                    B.ac_op_cache_copy_pages(self.all_caches, self.table[b, place:place + 1], self.next_table[b, place:place + 1], at[-1:])
+                self.table.copy_(self.next_table)
+                self.uses.copy_(self.next_uses)
+                self.ends[b] = max(first, place + copies)
+            self.common[b] = place * page
+
     def release(self, sequences):
         """The sequences have no tokens any more; their pages are free, but for those that others share."""
         import torch
@@ -144,7 +180,7 @@ class Decoder:
         ends = torch.tensor([0] * n + [(1 << 31) - 1 if b in gone else 0 for b in range(n)], dtype=torch.int32).to("cuda").view(2, n)
         B.ac_op_pages_update(self.books, self.books, self.books_workspace, drop=(ends[0], ends[1]))
         for b in gone:
-            self.lengths[b] = self.ends[b] = 0
+            self.lengths[b] = self.ends[b] = self.common[b] = 0
 
     def fork(self, parents, lengths=None):
         """Sequence j goes on as sequence parents[j] (or, -1, has no tokens); where pages run out all stay as they are.  parents may be on the device (int32), with the lengths, that it does not tell, by the caller."""
@@ -161,6 +197,7 @@ class Decoder:
             ends = [max(self.ends)] * n
         if len(lengths) != n:
             raise ValueError(f"{len(lengths)} lengths of {n} sequences")
+        self._part(range(n) if torch.is_tensor(parents) else sorted({p for p in parents if 0 <= p < n}))
         if not torch.is_tensor(parents):
             parents = torch.tensor(parents, dtype=torch.int32).to("cuda")
         now = torch.tensor(self.lengths, dtype=torch.int32).to("cuda")
@@ -173,6 +210,7 @@ class Decoder:
         self.table.copy_(self.next_table)
         self.uses.copy_(self.next_uses)
         self.lengths, self.ends = list(lengths), ends
+        self.common = [t // self.page * self.page for t in lengths]
 
     def compact(self):
         """Moves the pages in use to the front of the cache; how many they are, on the device."""
@@ -252,6 +290,8 @@ class Decoder:
                 raise ValueError(f"rows {tuple(new.shape)} of {new.dtype} for {n} sequences of {x.shape[1]} x {x.dtype}")
             if max(self.lengths) >= self.max_tokens:
                 raise ValueError(f"the cache holds {self.max_tokens} tokens of a sequence")
+            if self.shares:
+                self._part(range(n))
             if self.lengths != on_device:
                 length.copy_(torch.tensor(self.lengths, dtype=torch.int32))
             x.copy_(new)

@@ -40,7 +40,7 @@ class Decoder:
     up as their windows leave them, and share when one goes on as several (fork); without it, and without a window, each sequence has its own, enough for max_tokens.
 
     `lengths`, the sequences' numbers of tokens, may be set back, whole or one of it, between calls: a sequence then goes on behind as many of its tokens; behind a fork in pages of its own, so that
-    the others keep theirs."""
+    the others keep theirs, and behind a window only where what its next row sees is held still: each call gives up pages that are wholly before the first row's window, the sinks' apart."""
 
     window, sinks, shares = None, 0, False
 
@@ -71,6 +71,7 @@ class Decoder:
             self.missing = torch.zeros(1, dtype=torch.int32, device=dev)
             self.ends = [0] * sequences
             self.common = [0] * sequences                               # tokens before these lie in pages that others may have too
+            self.lost = [0] * sequences                                 # tokens before these, but for the sinks' pages, may have been given up
         else:
             self.table = torch.arange(pages, dtype=torch.int32, device=dev).view(sequences, each)
         codes = dict(dtype=torch.uint8, device=dev)
@@ -100,7 +101,9 @@ class Decoder:
         if max(lengths) > self.max_tokens:
             raise ValueError(f"{max(lengths)} tokens: the cache holds {self.max_tokens} of a sequence")
         if self.shares:
-            self._part(b for b, c in enumerate(counts) if c > 0)
+            reading = [b for b, c in enumerate(counts) if c > 0]
+            self._sees_all(reading)
+            self._part(reading)
         begin = [0]
         for c in counts:
             begin.append(begin[-1] + c)
@@ -115,7 +118,9 @@ class Decoder:
             before, drop_begin, drop_end = where[2 * seqs + 1:].view(3, seqs)
             B.ac_op_pages_update(self.books, self.books, self.books_workspace, (drop_begin, drop_end), (before, length), self.missing)
             self.ends = [max(e, -(-n // self.page)) for e, n in zip(self.ends, lengths)]
+            self._gave_up()
             self._enough(self.ends, self.lengths)
+            self._wrote(reading)
         rows = B.cache_rows(where[:seqs + 1], length, self.table, max(counts), max(lengths))
         need = self._workspace_bytes(n, rows)
         if need > self.workspace.numel():
@@ -139,6 +144,27 @@ class Decoder:
     def _sharing(self):
         if not self.shares:
             raise ValueError("sequences of this cache have their own pages: give it a number of `pages` to share")
+
+    def _sees_all(self, sequences):
+        """Refuses lengths of these sequences that were set back to where a window needs tokens whose pages have been given up."""
+        if self.window is None:
+            return
+        sinks = -(-self.sinks // self.page) * self.page
+        for b in sequences:
+            n = self.lengths[b]
+            if max(n - self.window + 1, sinks) < min(n, self.lost[b]):
+                raise ValueError(f"sequence {b} cannot go on behind {n} tokens: of its window of {self.window} those before {self.lost[b]} are gone")
+
+    def _gave_up(self):
+        """Notes what a call behind these lengths gives up."""
+        if self.window is not None:
+            self.lost = [max(e, (n - self.window + 1) // self.page * self.page) for e, n in zip(self.lost, self.lengths)]
+
+    def _wrote(self, sequences):
+        """Notes that these sequences' tokens from their lengths on are written (again)."""
+        if self.window is not None:
+            for b in sequences:
+                self.lost[b] = min(self.lost[b], max(self.lengths[b], (self.lengths[b] - self.window + 1) // self.page * self.page))
 
     def _part(self, sequences):
         """Of these sequences, those that were set back into what they have in common with others go on in pages of their own: a copy of the page that they write next, as far as they have
@@ -180,7 +206,7 @@ class Decoder:
         ends = torch.tensor([0] * n + [(1 << 31) - 1 if b in gone else 0 for b in range(n)], dtype=torch.int32).to("cuda").view(2, n)
         B.ac_op_pages_update(self.books, self.books, self.books_workspace, drop=(ends[0], ends[1]))
         for b in gone:
-            self.lengths[b] = self.ends[b] = self.common[b] = 0
+            self.lengths[b] = self.ends[b] = self.common[b] = self.lost[b] = 0
 
     def fork(self, parents, lengths=None):
         """Sequence j goes on as sequence parents[j] (or, -1, has no tokens); where pages run out all stay as they are.  parents may be on the device (int32), with the lengths, that it does not tell, by the caller."""
@@ -192,9 +218,13 @@ class Decoder:
             if len(parents) != n or not all(-1 <= p < n for p in parents):
                 raise ValueError(f"parents {parents} of {n} sequences")
             lengths = [self.lengths[p] if p >= 0 else 0 for p in parents]
-            ends = [self.ends[p] if p >= 0 else 0 for p in parents]
+            ends, lost = ([of[p] if p >= 0 else 0 for p in parents] for of in (self.ends, self.lost))
         else:
             ends = [max(self.ends)] * n
+            of = {}                                                     # (of sequences as long as the parent the most)
+            for t, e in zip(self.lengths, self.lost):
+                of[t] = max(e, of.get(t, 0))
+            lost = [of.get(t, 0) for t in lengths]
         if len(lengths) != n:
             raise ValueError(f"{len(lengths)} lengths of {n} sequences")
         self._part(range(n) if torch.is_tensor(parents) else sorted({p for p in parents if 0 <= p < n}))
@@ -209,7 +239,7 @@ class Decoder:
         # (the graph of a step knows the table by its address)
         self.table.copy_(self.next_table)
         self.uses.copy_(self.next_uses)
-        self.lengths, self.ends = list(lengths), ends
+        self.lengths, self.ends, self.lost = list(lengths), ends, lost
         self.common = [t // self.page * self.page for t in lengths]
 
     def compact(self):
@@ -291,6 +321,7 @@ class Decoder:
             if max(self.lengths) >= self.max_tokens:
                 raise ValueError(f"the cache holds {self.max_tokens} tokens of a sequence")
             if self.shares:
+                self._sees_all(range(n))
                 self._part(range(n))
             if self.lengths != on_device:
                 length.copy_(torch.tensor(self.lengths, dtype=torch.int32))
@@ -299,7 +330,9 @@ class Decoder:
             if self.shares:
                 on_device = None                                        # (where pages are missing lengths are copied again)
                 self.ends = [max(e, -(-(t + 1) // self.page)) for e, t in zip(self.ends, self.lengths)]
+                self._gave_up()
                 self._enough(self.ends, self.lengths)
+                self._wrote(range(n))
             self.lengths = [t + 1 for t in self.lengths]
             on_device = list(self.lengths)                              # (the caller may change the other one in place)
             return y

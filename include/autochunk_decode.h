@@ -128,7 +128,7 @@ uint64_t ac_cache_attention_window_workspace_bytes(int64_t n_rows, int heads, co
  * logits x[r, 0 .. vocab - 1], rows ld elements apart.  A candidate is a beam with a token, with
  *     total(i, t) = scores[r] + x[r, t] - log(sum_u exp x[r, u]).
  * A sequence with ended[r] != 0 has ended: its one candidate is (i, end) with scores[r] as it is, and its logits are not read.  The `keep` candidates with the largest totals come out, largest first, of
- * equal ones the lower i, then the lower t: scores_out, parent (r, the sequence it goes on from) and token, each [batch][keep], and ended_out (may be NULL): 1 where the parent had ended or the token is end, else 0.
+ * equal ones the lower i, then the larger logit, then the lower t: scores_out, parent (r, the sequence it goes on from) and token, each [batch][keep], and ended_out (may be NULL): 1 where the parent had ended or the token is end, else 0.
  * Logits of -inf (tokens that may not come) and scores of -inf (a beam that is none yet) give no candidates, and none comes from a row that holds a NaN; logits of +inf
  * share the probability among them.  Where candidates are fewer than `keep` the others come out as score -inf, parent -1, token -1, ended 0.
  * Totals are compared in 64 bits, from maxima and sums of exponentials held in 32; within a beam the order is that of the logits.

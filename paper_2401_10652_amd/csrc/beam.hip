@@ -27,10 +27,10 @@ struct BeamArgs {
   float* value; int32_t* index;       // [rows][runs][keep], largest first; -inf where there are no more
 };
 
-// (a, i) before (b, j): the larger, of equal ones the lower index.  (Without a branch: one for each comparison takes 80 cycles of a candidate's count.)
-__device__ __forceinline__ bool before(double a, int i, double b, int j) { return (a > b) | ((a == b) & (i < j)); }
-// The same of a logit and its index as one number: the larger comes first.  0: none.
 typedef unsigned long long Key;
+// (a, i) before (b, j): the larger total, of equal ones the lower key.  (Without a branch: one for each comparison takes 80 cycles of a candidate's count.)
+__device__ __forceinline__ bool before(double a, Key i, double b, Key j) { return (a > b) | ((a == b) & (i < j)); }
+// A logit and its index as one number: the larger comes first.  0: none.
 __device__ __forceinline__ Key key_of(float v, int index) {
   const uint32_t u = __builtin_bit_cast(uint32_t, v + 0.f);               // (one zero)
   return (Key)(u ^ ((int)u < 0 ? 0xffffffffu : 0x80000000u)) << 32 | ~(uint32_t)index;
@@ -40,6 +40,15 @@ __device__ __forceinline__ float value_of_key(Key k) {
   return __builtin_bit_cast(float, u ^ ((int)u < 0 ? 0x80000000u : 0xffffffffu));
 }
 __device__ __forceinline__ int index_of_key(Key k) { return (int)~(uint32_t)k; }
+
+// Of equal totals the lower beam comes first, and of a beam's the larger logit (different ones may have one total: it has 53 bits, of a score that may be large), then the lower token: 6, 32 and
+// 24 bits, lowest first.  Never 0, which stands before all of them.  An ended beam has one candidate.
+constexpr int kTokenBits = 24;
+__device__ __forceinline__ Key place_of(int beam, float v, int token) {
+  return (Key)beam << (kTokenBits + 32) | (Key) ~(uint32_t)(key_of(v, 0) >> 32) << kTokenBits | (uint32_t)token;
+}
+__device__ __forceinline__ int beam_of_place(Key k) { return (int)(k >> (kTokenBits + 32)); }
+__device__ __forceinline__ int token_of_place(Key k) { return (int)(k & ((1u << kTokenBits) - 1)); }
 
 // The next number above a finite one.
 __device__ __forceinline__ float above(float v) {
@@ -264,9 +273,9 @@ __global__ void __launch_bounds__(kThreads) beam_rank(BeamArgs g) {
   __shared__ __attribute__((aligned(16))) float largest[kThreads];
   __shared__ int border_at, count_at;
   __shared__ double value_of[kMostCandidates];
-  __shared__ int place_of[kMostCandidates];
+  __shared__ Key place_at[kMostCandidates];
   __shared__ double wave_value[kWaves];
-  __shared__ int wave_place[kWaves];
+  __shared__ Key wave_place[kWaves];
   const int tid = threadIdx.x, lane = tid % kWave, lists = g.beams * g.runs;
   const int64_t row0 = (int64_t)blockIdx.x * g.beams;
   const float* const value = g.value + row0 * g.runs * g.keep;
@@ -315,13 +324,14 @@ __global__ void __launch_bounds__(kThreads) beam_rank(BeamArgs g) {
   const double mine = tid < g.beams ? done[tid] : -INFINITY;
   // f of all of the thread's own entries, below the levels down a list up to the first for which it is false
   auto each = [&](auto f) {
-    if (mine > -INFINITY) f(mine, tid * g.vocab + g.end);
+    if (mine > -INFINITY) f(mine, place_of(tid, INFINITY, g.end));
     for (int item = tid; item < lists * levels; item += kThreads) {
       int k;
-      const int list = list_of(item, k), place = quotient(list, g.of_beam) * g.vocab, down = k == levels - 1 ? g.keep : k + 1;
+      const int list = list_of(item, k), beam = quotient(list, g.of_beam), down = k == levels - 1 ? g.keep : k + 1;
       for (; k < down; ++k) {
-        const double total = total_of(list, value[list * g.keep + k]);
-        if (!(total > -INFINITY) || !f(total, place + index[list * g.keep + k])) break;
+        const float v = value[list * g.keep + k];
+        const double total = total_of(list, v);
+        if (!(total > -INFINITY) || !f(total, place_of(beam, v, index[list * g.keep + k]))) break;
       }
     }
   };
@@ -354,12 +364,12 @@ __global__ void __launch_bounds__(kThreads) beam_rank(BeamArgs g) {
     __syncthreads();
     const float border = of_order(border_at);
     if (most >= border)
-      each([&](double v, int place) {
+      each([&](double v, Key place) {
         if ((float)v < border) return false;
         const int at = atomicAdd(&count_at, 1);
         if (at < kMostCandidates) {
           value_of[at] = v;
-          place_of[at] = place;
+          place_at[at] = place;
         }
         return true;
       });
@@ -368,8 +378,8 @@ __global__ void __launch_bounds__(kThreads) beam_rank(BeamArgs g) {
     __syncthreads();
   }
   const int64_t out = (int64_t)blockIdx.x * g.keep;
-  auto put = [&](int k, double total, int place) {
-    const int i = place / g.vocab, t = place - i * g.vocab;
+  auto put = [&](int k, double total, Key place) {
+    const int i = beam_of_place(place), t = token_of_place(place);
     g.scores_out[out + k] = (float)total;
     g.parent[out + k] = (int)(row0 + i);
     g.token[out + k] = t;
@@ -380,26 +390,26 @@ __global__ void __launch_bounds__(kThreads) beam_rank(BeamArgs g) {
   if (count <= kMostCandidates) {
     for (int c = tid; c < count; c += kThreads) {
       const double v = value_of[c];
-      const int place = place_of[c];
+      const Key place = place_at[c];
       int k = 0;
-      for (int j = 0; j < count; ++j) k += before(value_of[j], place_of[j], v, place);
+      for (int j = 0; j < count; ++j) k += before(value_of[j], place_at[j], v, place);
       if (k < g.keep) put(k, v, place);
     }
   } else {
     // as many equal ones: the first of those that are left, again and again
     double last = INFINITY;
-    int last_place = -1;
+    Key last_place = 0;
     for (n = 0; n < g.keep; ++n) {
       double v = -INFINITY;
-      int place = 0x7fffffff;
-      each([&](double a, int at) {
+      Key place = ~0ull;
+      each([&](double a, Key at) {
         if (before(last, last_place, a, at) && before(a, at, v, place)) { v = a; place = at; }
         return true;
       });
 #pragma unroll
       for (int o = kWave / 2; o > 0; o >>= 1) {
         const double a = __shfl_xor(v, o, kWave);
-        const int at = __shfl_xor(place, o, kWave);
+        const Key at = __shfl_xor(place, o, kWave);
         if (before(a, at, v, place)) { v = a; place = at; }
       }
       if (lane == 0) { wave_value[tid / kWave] = v; wave_place[tid / kWave] = place; }

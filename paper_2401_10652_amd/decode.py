@@ -359,6 +359,7 @@ class BeamSearch:
         self.logits = torch.empty((n, vocab), dtype=model.dtype, device="cuda")
         self.workspace = B.empty_workspace(B.ac_beam_select_workspace_bytes(self.logits, beams, beams))
         self.scores, self.ended = None, None
+        self.pending = None                                             # a choice behind which the sequences were forked, but whose tokens are not read
 
     def _logits(self, y):
         codes, scale, zero = self.head
@@ -385,10 +386,23 @@ class BeamSearch:
         self.scores = torch.full((self.prompts, k), float("-inf"), device="cuda")
         self.scores[:, 0] = 0
         self.ended = None if self.end < 0 else torch.zeros((self.prompts, k), dtype=torch.int32, device="cuda")
-        self.steps = []
+        self.steps, self.pending = [], None
 
     def step(self):
-        """Chooses the beams' next tokens and reads them: (parent, token), int32 [prompts, beams] on the device."""
+        """Chooses the beams' next tokens and reads them: (parent, token), int32 [prompts, beams] on the device.  Where that fails, as where pages run out, what was found stays, and the next
+        call goes on from there."""
+        m = self.model
+        if self.pending is None:
+            self.pending = self._choose()
+        scores, ended, parent, token = self.pending
+        y = m.forward(self.embedding[token.view(-1).clamp(min=0).long()], [1] * len(m.lengths))
+        self._logits(y)
+        self.scores, self.ended, self.pending = scores, ended, None
+        self.steps.append((parent, token))
+        return parent, token
+
+    def _choose(self):
+        """The beams' next tokens, and the sequences forked by their parents."""
         import torch
         m, k = self.model, self.beams
         i32 = dict(dtype=torch.int32, device="cuda")
@@ -397,11 +411,7 @@ class BeamSearch:
         B.ac_op_beam_select(self.logits, self.scores, scores, parent, token, self.workspace, ended=self.ended, ended_out=ended, end=self.end)
         # all beams of a prompt have its length (a beam that is none, too: what it reads has no weight)
         m.fork(parent.view(-1), [m.lengths[b // k * k] for b in range(len(m.lengths))])
-        y = m.forward(self.embedding[token.view(-1).clamp(min=0).long()], [1] * len(m.lengths))
-        self._logits(y)
-        self.scores, self.ended = scores, ended
-        self.steps.append((parent, token))
-        return parent, token
+        return scores, ended, parent, token
 
     def found(self):
         """[[(sum of logarithms, tokens)]] of each prompt, best first; tokens up to and with the end."""

@@ -358,7 +358,10 @@ class BeamSearch:
         n = len(model.lengths)
         self.logits = torch.empty((n, vocab), dtype=model.dtype, device="cuda")
         self.workspace = B.empty_workspace(B.ac_beam_select_workspace_bytes(self.logits, beams, beams))
-        self.scores, self.ended = None, None
+        self._none()
+
+    def _none(self):
+        self.scores, self.ended, self.steps = None, None, []
         self.pending = None                                             # a choice behind which the sequences were forked, but whose tokens are not read
 
     def _logits(self, y):
@@ -371,6 +374,7 @@ class BeamSearch:
         m, k = self.model, self.beams
         if len(prompts) != self.prompts or not all(prompts):
             raise ValueError(f"{self.prompts} prompts of one token at least are wanted")
+        self._none()
         m.release(range(len(m.lengths)))
         y = torch.zeros((self.prompts * k, m.cfg.d_model), dtype=m.dtype, device="cuda")
         for at in range(0, max(len(p) for p in prompts), stretch):
@@ -386,12 +390,13 @@ class BeamSearch:
         self.scores = torch.full((self.prompts, k), float("-inf"), device="cuda")
         self.scores[:, 0] = 0
         self.ended = None if self.end < 0 else torch.zeros((self.prompts, k), dtype=torch.int32, device="cuda")
-        self.steps, self.pending = [], None
 
     def step(self):
         """Chooses the beams' next tokens and reads them: (parent, token), int32 [prompts, beams] on the device.  Where that fails, as where pages run out, what was found stays, and the next
         call goes on from there."""
         m = self.model
+        if self.scores is None:
+            raise ValueError("no search has been started: start reads its prompts")
         if self.pending is None:
             self.pending = self._choose()
         scores, ended, parent, token = self.pending
@@ -415,6 +420,8 @@ class BeamSearch:
 
     def found(self):
         """[[(sum of logarithms, tokens)]] of each prompt, best first; tokens up to and with the end."""
+        if self.scores is None:
+            return [[] for _ in range(self.prompts)]
         scores = self.scores.tolist()
         steps = [(p.view(-1).tolist(), t.view(-1).tolist()) for p, t in self.steps]
         result = []

@@ -84,3 +84,23 @@ def test_the_end_of_the_table(B):  # noqa: F811
         a.start([[1, 2], [3]])
         a.step(), a.step()
     assert equal(state(s), state(other))
+
+
+def test_a_start_that_runs_dry(B):  # noqa: F811
+    """The sequences of before are gone, so there is no search until one starts."""
+    s, other = search(14), search(60)
+    fresh = search(14)
+    with pytest.raises(ValueError, match="start"):
+        fresh.step()
+    for a in (s, other):
+        a.start(PROMPTS)
+        a.step()
+    with pytest.raises((RuntimeError, ValueError)):
+        s.start([[1] * 300, [2] * 4])                                   # (more than the table holds)
+    with pytest.raises(ValueError, match="start"):
+        s.step()
+    assert s.found() == [[], []]
+    for a in (s, other):
+        a.start(PROMPTS)
+        a.step(), a.step()
+    assert equal(state(s), state(other))

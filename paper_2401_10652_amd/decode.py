@@ -374,6 +374,9 @@ class BeamSearch:
         m, k = self.model, self.beams
         if len(prompts) != self.prompts or not all(prompts):
             raise ValueError(f"{self.prompts} prompts of one token at least are wanted")
+        vocab = self.logits.shape[1]
+        if min(map(min, prompts)) < 0 or max(map(max, prompts)) >= vocab:
+            raise ValueError(f"tokens {min(map(min, prompts))} to {max(map(max, prompts))} of a vocabulary of {vocab}")
         self._none()
         m.release(range(len(m.lengths)))
         y = torch.zeros((self.prompts * k, m.cfg.d_model), dtype=m.dtype, device="cuda")

@@ -104,3 +104,19 @@ def test_a_start_that_runs_dry(B):  # noqa: F811
         a.start(PROMPTS)
         a.step(), a.step()
     assert equal(state(s), state(other))
+
+
+@pytest.mark.parametrize("bad", [VOCAB, VOCAB + 1000, -1, 1 << 40])
+def test_tokens_outside_the_vocabulary(B, bad):  # noqa: F811
+    """Refused before anything changes: the embedding has no such row."""
+    s = search(14)
+    s.start(PROMPTS)
+    s.step()
+    before = state(s)
+    for prompts in ([[bad], [1]], [[1, 2], [3, 4, bad, 5]]):
+        with pytest.raises(ValueError, match="40"):
+            s.start(prompts)
+        assert equal(state(s), before)
+    s.step()
+    s.start([[0], [VOCAB - 1]])
+    s.step()

@@ -624,13 +624,13 @@ __global__ void __launch_bounds__(256) pages_copy(CopyArgs g) {
 }
 
 hipError_t copy_launch(const ac_kv_cache* caches, int n_caches, CopyArgs a, int64_t most, hipStream_t s) {
-  if (most <= 0) return hipSuccess;
+  if (most <= 0 || a.pages <= 0) return hipSuccess;
   for (int first = 0; first < n_caches; first += kCaches) {
     const int n = n_caches - first < kCaches ? n_caches - first : kCaches;
     int64_t units = 0;
     for (int i = 0; i < n; ++i) {
       const ac_kv_cache& c = caches[first + i];
-      const uint32_t head = (uint32_t)c.page * c.head_dim / 16, half = head * c.heads;
+      const uint32_t head = (uint32_t)((int64_t)c.page * c.head_dim / 16), half = head * c.heads;       // (below 2^30: a page has less than 2^34 codes)
       a.cache[i] = {(uint8_t*)c.k, (uint8_t*)c.v, c.k_scale, c.v_scale, c.stride_page, c.stride_scale, half, c.heads, divisor(head)};
       if (2 * (int64_t)half > units) units = 2 * (int64_t)half;
     }

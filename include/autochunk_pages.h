@@ -22,7 +22,8 @@ extern "C" {
  * (ld_page_table times page) and entries of a table (batch times ld_page_table) 2^30, else AC_ERR_UNSUPPORTED; arrays on 4-byte boundaries, page a multiple of 16.
  *
  * Every call reads the books `from` and leaves those after it in `to`, of the same sizes; each of `to`'s arrays may be `from`'s own (where a call does not say
- * otherwise) or lies apart from both of them.  workspace: dev, 16-byte aligned, ac_pages_workspace_bytes() large, else AC_ERR_WORKSPACE; what it holds does not matter.
+ * otherwise) or lies apart from both of them.  What a call reads besides (ranges, parents, lengths) lies apart from the books `to`, what it leaves besides (lengths, numbers) from all books
+ * and from everything else, else AC_ERR_ARG; all on 4-byte boundaries, else AC_ERR_ALIGN.  workspace: dev, 16-byte aligned, ac_pages_workspace_bytes() large, else AC_ERR_WORKSPACE; what it holds does not matter.
  */
 typedef struct ac_page_books {
   int32_t* uses;                    /* dev, [pages] */
@@ -61,7 +62,7 @@ int ac_op_cache_compact(const ac_kv_cache* caches, int n_caches, const ac_page_b
 
 /*
  * Page target[i] becomes a copy of page source[i], in all caches: of its first tokens[i] tokens, in whole blocks of 16, or (tokens NULL) of all.  Pairs of which one names no page, or both the
- * same, are left out.  No page may be target of two pairs, or target of one and source of another.  source, target, tokens: dev, [n], n at most 2^24.  The caches have the same pages.
+ * same, are left out.  No page may be target of two pairs, or target of one and source of another.  source, target, tokens: dev, [n], on 4-byte boundaries, else AC_ERR_ALIGN, n at most 2^24.  The caches have the same pages.
  */
 int ac_op_cache_copy_pages(const ac_kv_cache* caches, int n_caches, const int32_t* source, const int32_t* target, const int32_t* tokens, int64_t n,
                            void* stream);

@@ -15,6 +15,7 @@
 
 #include <algorithm>
 #include <array>
+#include <initializer_list>
 #include <mutex>
 #include <new>
 #include <string>
@@ -2391,6 +2392,28 @@ static int books_ok(const char* what, const ac_kv_cache* caches, int n_caches, c
   return AC_OK;
 }
 
+// What a call reads and leaves beside the books: on 4-byte boundaries; what is read apart from the books that come out, and what comes out from everything else.
+struct Ints { const int32_t* at; int64_t n; };
+static int ints_ok(const char* what, const ac_page_books& from, const ac_page_books& to, std::initializer_list<Ints> in, std::initializer_list<Ints> out) {
+  const int64_t table = from.batch * from.ld_page_table;
+  auto apart = [](const Ints& a, const Ints& b) { return !overlap(a.at, a.n, b.at, b.n); };
+  for (const std::initializer_list<Ints>& list : {in, out})
+    for (const Ints& a : list)
+      if (a.n > 0 && (uintptr_t)a.at % 4 != 0) return fail(AC_ERR_ALIGN, "%s: arrays start at multiples of 4 bytes", what);
+  const Ints before[] = {{from.uses, from.pages}, {from.page_table, table}}, after[] = {{to.uses, from.pages}, {to.page_table, table}};
+  bool ok = true;
+  for (const Ints& a : after) {
+    for (const Ints& b : in) ok = ok && apart(a, b);
+    for (const Ints& b : out) ok = ok && apart(a, b);
+  }
+  for (const Ints& a : out) {
+    for (const Ints& b : before) ok = ok && apart(a, b);
+    for (const Ints& b : in) ok = ok && apart(a, b);
+    for (const Ints& b : out) ok = ok && (&a == &b || apart(a, b));
+  }
+  return ok ? AC_OK : fail(AC_ERR_ARG, "%s: arrays that overlap", what);
+}
+
 uint64_t ac_pages_workspace_bytes(const ac_page_books* books) {
   return book_ok("ac_pages_workspace_bytes", books) ? 0 : pages_workspace_bytes(*books);
 }
@@ -2400,6 +2423,8 @@ int ac_op_pages_update(const ac_page_books* from, const ac_page_books* to, const
   const char* const what = "ac_op_pages_update";
   if (const int st = books_ok(what, nullptr, 0, from, to, workspace, workspace_bytes)) return st;
   if (!drop_begin != !drop_end || !take_begin != !take_end) return fail(AC_ERR_ARG, "%s: ranges with one end", what);
+  const int64_t n = from->batch;
+  if (const int st = ints_ok(what, *from, *to, {{drop_begin, n}, {drop_end, n}, {take_begin, n}, {take_end, n}}, {{missing, 1}})) return st;
   return hip_status(launch_pages_update(*from, *to, drop_begin, drop_end, take_begin, take_end, missing, workspace, (hipStream_t)stream), what + 6);
 }
 
@@ -2407,8 +2432,10 @@ int ac_op_cache_fork(const ac_kv_cache* caches, int n_caches, const ac_page_book
                      int32_t* length_to, int32_t* missing, void* workspace, uint64_t workspace_bytes, void* stream) {
   const char* const what = "ac_op_cache_fork";
   if (const int st = books_ok(what, caches, n_caches, from, to, workspace, workspace_bytes)) return st;
-  if (from->batch > 0 && (!parent || !length || !length_to || overlap(length, from->batch, length_to, from->batch) || overlap(parent, from->batch, length_to, from->batch) || (from->ld_page_table > 0 && from->page_table == to->page_table)))
+  const int64_t n = from->batch;
+  if (n > 0 && (!parent || !length || !length_to || (from->ld_page_table > 0 && from->page_table == to->page_table)))
     return fail(AC_ERR_ARG, "%s: parents, lengths, and a table and lengths apart from them are wanted", what);
+  if (const int st = ints_ok(what, *from, *to, {{parent, n}, {length, n}}, {{length_to, n}, {missing, 1}})) return st;
   return hip_status(launch_cache_fork(caches, n_caches, *from, *to, parent, length, length_to, missing, workspace, (hipStream_t)stream), what + 6);
 }
 
@@ -2416,6 +2443,7 @@ int ac_op_cache_compact(const ac_kv_cache* caches, int n_caches, const ac_page_b
                         uint64_t workspace_bytes, void* stream) {
   const char* const what = "ac_op_cache_compact";
   if (const int st = books_ok(what, caches, n_caches, from, to, workspace, workspace_bytes)) return st;
+  if (const int st = ints_ok(what, *from, *to, {}, {{used, 1}})) return st;
   return hip_status(launch_cache_compact(caches, n_caches, *from, *to, used, workspace, (hipStream_t)stream), what + 6);
 }
 
@@ -2425,6 +2453,8 @@ int ac_op_cache_copy_pages(const ac_kv_cache* caches, int n_caches, const int32_
   if (const int st = caches_ok(what, caches, n_caches)) return st;
   if (n < 0 || (n > 0 && (!source || !target))) return fail(AC_ERR_ARG, "%s: bad argument", what);
   if (n > 1 << 24) return fail(AC_ERR_UNSUPPORTED, "%s: at most 2^24 pairs", what);
+  if (n > 0 && ((uintptr_t)source % 4 != 0 || (uintptr_t)target % 4 != 0 || (uintptr_t)tokens % 4 != 0))
+    return fail(AC_ERR_ALIGN, "%s: arrays start at multiples of 4 bytes", what);
   return hip_status(launch_cache_copy_pages(caches, n_caches, source, target, tokens, n, (hipStream_t)stream), what + 6);
 }
 

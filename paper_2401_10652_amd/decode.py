@@ -209,15 +209,19 @@ class Decoder:
             self.lengths[b] = self.ends[b] = self.common[b] = self.lost[b] = 0
 
     def fork(self, parents, lengths=None):
-        """Sequence j goes on as sequence parents[j] (or, -1, has no tokens); where pages run out all stay as they are.  parents may be on the device (int32), with the lengths, that it does not tell, by the caller."""
+        """Sequence j goes on as sequence parents[j] (or, -1, has no tokens); where pages run out all stay as they are.  parents may be on the device (int32); the caller then says the
+        lengths: each its parent's, of one without a parent any."""
         import torch
         self._sharing()
         n = len(self.lengths)
-        if lengths is None:
+        if lengths is None or not (torch.is_tensor(parents) and parents.is_cuda):
             parents = [int(p) for p in parents]
             if len(parents) != n or not all(-1 <= p < n for p in parents):
                 raise ValueError(f"parents {parents} of {n} sequences")
-            lengths = [self.lengths[p] if p >= 0 else 0 for p in parents]
+            of = [self.lengths[p] if p >= 0 else 0 for p in parents]
+            if lengths is not None and (len(lengths) != n or any(p >= 0 and t != of[j] for j, (p, t) in enumerate(zip(parents, lengths)))):
+                raise ValueError(f"lengths {list(lengths)} where the parents' are {of}")
+            lengths = of if lengths is None else lengths
             ends, lost = ([of[p] if p >= 0 else 0 for p in parents] for of in (self.ends, self.lost))
         else:
             ends = [max(self.ends)] * n

@@ -124,3 +124,30 @@ def test_pages_run_out(B):  # noqa: F811
     m.release([0])
     own.lengths[0] = 0
     same(m, own, x[70:73], [0, 1, 2, 0])
+
+
+def test_parents_on_the_host(B):  # noqa: F811
+    """As tensors too, of either kind of number; lengths, where they are said, have to be the parents'."""
+    import torch
+    for kind in (torch.int32, torch.int64):
+        for said in (None, [40, 40, 40, 40], [40, 40, 40, 0]):
+            m, own, x = pair()
+            parents = torch.tensor([1, 0, 2, 2 if said and said[3] else -1], dtype=kind)
+            m.fork(parents, said)
+            same(m, own, x[50:53], [1, 1, 1, 0]) if not said or not said[3] else m.forward(x[50:54], [1] * 4)
+            held(m)
+    m, own, x = pair()
+    table = m.table.clone()
+    for parents, lengths in (([0, 1, 2, -1], [20, 40, 40, 0]), ([0, 1, 2, 2], [40, 40, 40, 41]), ([0, 1, 2, 4], [40] * 4), ([0, 1, 2], [40] * 3), ([0, 1, 2, 0], [40] * 3)):
+        for kind in (list, torch.tensor):
+            with pytest.raises(ValueError):
+                m.fork(kind(parents), lengths)
+    on_device = torch.tensor([0, 1, 2, 2], device="cuda")
+    with pytest.raises(TypeError):
+        m.fork(on_device, [40] * 4)
+    with pytest.raises(ValueError):
+        m.fork(on_device.int()[:3], [40] * 4)
+    with pytest.raises(ValueError):
+        m.fork(on_device.int(), [40] * 3)
+    assert torch.equal(m.table, table) and m.lengths == [40, 40, 40, 0]
+    same(m, own, x[50:53], [1, 1, 1, 0])

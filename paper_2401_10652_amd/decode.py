@@ -48,6 +48,8 @@ class Decoder:
         import torch
         if not cfg.causal:
             raise ValueError(f"{cfg.name} is not causal: its rows cannot be read a token at a time")
+        if not (0 <= (window or 0) <= 1 << 30 and 0 <= sinks <= 1 << 30):
+            raise ValueError(f"a window of {window} tokens, {sinks} sinks: 0 to 2^30 are wanted")
         self.cfg, self.group, self.max_tokens = cfg, group, max_tokens
         self.dtype = {"f32": torch.float32, "bf16": torch.bfloat16}[cfg.dtype]
         dev, d = "cuda", cfg.head_dim

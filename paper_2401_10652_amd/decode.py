@@ -72,8 +72,9 @@ class Decoder:
             self.books_workspace = B.empty_workspace(B.ac_pages_workspace_bytes(self.books))
             self.missing = torch.zeros(1, dtype=torch.int32, device=dev)
             self.ends = [0] * sequences
-            self.common = [0] * sequences                               # tokens before these lie in pages that others may have too
-            self.lost = [0] * sequences                                 # tokens before these, but for the sinks' pages, may have been given up
+            # what is asked of lengths that were set (others pay a comparison): the lengths as the calls left them; those at the last fork, whose whole pages others may have; those at the
+            # begin of the last call, which tell what it gave up; and the tokens before which a call before that one may have given up pages, but for the sinks'
+            self.known, self.forked, self.began, self.lost = ([0] * sequences for _ in range(4))
         else:
             self.table = torch.arange(pages, dtype=torch.int32, device=dev).view(sequences, each)
         codes = dict(dtype=torch.uint8, device=dev)
@@ -102,10 +103,7 @@ class Decoder:
         lengths = [a + b for a, b in zip(self.lengths, counts)]
         if max(lengths) > self.max_tokens:
             raise ValueError(f"{max(lengths)} tokens: the cache holds {self.max_tokens} of a sequence")
-        if self.shares:
-            reading = [b for b, c in enumerate(counts) if c > 0]
-            self._sees_all(reading)
-            self._part(reading)
+        was_set = self.shares and self._was_set(b for b, c in enumerate(counts) if c > 0)
         begin = [0]
         for c in counts:
             begin.append(begin[-1] + c)
@@ -120,14 +118,15 @@ class Decoder:
             before, drop_begin, drop_end = where[2 * seqs + 1:].view(3, seqs)
             B.ac_op_pages_update(self.books, self.books, self.books_workspace, (drop_begin, drop_end), (before, length), self.missing)
             self.ends = [max(e, -(-n // self.page)) for e, n in zip(self.ends, lengths)]
-            self._gave_up()
+            self.began = list(self.lengths)
             self._enough(self.ends, self.lengths)
-            self._wrote(reading)
         rows = B.cache_rows(where[:seqs + 1], length, self.table, max(counts), max(lengths))
         need = self._workspace_bytes(n, rows)
         if need > self.workspace.numel():
             self.workspace = B.empty_workspace(need)
         x = self._run(x.clone(memory_format=torch.contiguous_format), rows, self.workspace)
+        if self.shares:
+            self._read(lengths, was_set, counts)
         self.lengths = lengths
         return x
 
@@ -147,26 +146,29 @@ class Decoder:
         if not self.shares:
             raise ValueError("sequences of this cache have their own pages: give it a number of `pages` to share")
 
-    def _sees_all(self, sequences):
-        """Refuses lengths of these sequences that were set back to where a window needs tokens whose pages have been given up."""
-        if self.window is None:
-            return
-        sinks = -(-self.sinks // self.page) * self.page
-        for b in sequences:
-            n = self.lengths[b]
-            if max(n - self.window + 1, sinks) < min(n, self.lost[b]):
-                raise ValueError(f"sequence {b} cannot go on behind {n} tokens: of its window of {self.window} those before {self.lost[b]} are gone")
-
-    def _gave_up(self):
-        """Notes what a call behind these lengths gives up."""
+    def _was_set(self, sequences):
+        """Before these sequences read on, or are forked: whether lengths were set since the last call.  Refuses those that were set back to where a window needs tokens whose pages have been
+        given up; those that share the pages behind them go on in pages of their own."""
+        if self.lengths == self.known:
+            return False
+        sequences = list(sequences)
         if self.window is not None:
-            self.lost = [max(e, (n - self.window + 1) // self.page * self.page) for e, n in zip(self.lost, self.lengths)]
-
-    def _wrote(self, sequences):
-        """Notes that these sequences' tokens from their lengths on are written (again)."""
-        if self.window is not None:
+            self.lost = [max(e, (n - self.window + 1) // self.page * self.page) for e, n in zip(self.lost, self.began)]
+            sinks = -(-self.sinks // self.page) * self.page
             for b in sequences:
-                self.lost[b] = min(self.lost[b], max(self.lengths[b], (self.lengths[b] - self.window + 1) // self.page * self.page))
+                n = self.lengths[b]
+                if max(n - self.window + 1, sinks) < min(n, self.lost[b]):
+                    raise ValueError(f"sequence {b} cannot go on behind {n} tokens: of its window of {self.window} those before {self.lost[b]} are gone")
+        self._part(sequences)
+        return True
+
+    def _read(self, lengths, was_set, counts):
+        """Notes that sequences have read so many tokens and are `lengths` long now.  (Tokens that were given up and are read again are there; sequences that read none stay as they were set.)"""
+        if was_set:
+            self.lost = [min(e, n) if c > 0 else e for e, n, c in zip(self.lost, self.lengths, counts)]
+            self.known = [n if c > 0 else k for k, n, c in zip(self.known, lengths, counts)]
+        else:
+            self.known = list(lengths)
 
     def _part(self, sequences):
         """Of these sequences, those that were set back into what they have in common with others go on in pages of their own: a copy of the page that they write next, as far as they have
@@ -174,9 +176,9 @@ class Decoder:
         import torch
         for b in sequences:
             n, page = self.lengths[b], self.page
-            if n >= self.common[b]:
-                continue
             place, rest = divmod(n, page)
+            if place >= self.forked[b] // page:
+                continue
             row = self.table[b, place:]
             others = ((row >= 0) & (self.uses[row.clamp(min=0).long()] > 1)).nonzero().view(-1).tolist()
             if others:
@@ -196,7 +198,7 @@ class Decoder:
                 self.table.copy_(self.next_table)
                 self.uses.copy_(self.next_uses)
                 self.ends[b] = max(first, place + copies)
-            self.common[b] = place * page
+            self.forked[b] = n
 
     def release(self, sequences):
         """The sequences have no tokens any more; their pages are free, but for those that others share."""
@@ -208,7 +210,7 @@ class Decoder:
         ends = torch.tensor([0] * n + [(1 << 31) - 1 if b in gone else 0 for b in range(n)], dtype=torch.int32).to("cuda").view(2, n)
         B.ac_op_pages_update(self.books, self.books, self.books_workspace, drop=(ends[0], ends[1]))
         for b in gone:
-            self.lengths[b] = self.ends[b] = self.common[b] = self.lost[b] = 0
+            self.lengths[b] = self.ends[b] = self.known[b] = self.forked[b] = self.began[b] = self.lost[b] = 0
 
     def fork(self, parents, lengths=None):
         """Sequence j goes on as sequence parents[j] (or, -1, has no tokens); where pages run out all stay as they are.  parents may be on the device (int32); the caller then says the
@@ -224,16 +226,19 @@ class Decoder:
             if lengths is not None and (len(lengths) != n or any(p >= 0 and t != of[j] for j, (p, t) in enumerate(zip(parents, lengths)))):
                 raise ValueError(f"lengths {list(lengths)} where the parents' are {of}")
             lengths = of if lengths is None else lengths
-            ends, lost = ([of[p] if p >= 0 else 0 for p in parents] for of in (self.ends, self.lost))
+            ends = [self.ends[p] if p >= 0 else 0 for p in parents]
         else:
             ends = [max(self.ends)] * n
-            of = {}                                                     # (of sequences as long as the parent the most)
-            for t, e in zip(self.lengths, self.lost):
-                of[t] = max(e, of.get(t, 0))
-            lost = [of.get(t, 0) for t in lengths]
         if len(lengths) != n:
             raise ValueError(f"{len(lengths)} lengths of {n} sequences")
-        self._part(range(n) if torch.is_tensor(parents) else sorted({p for p in parents if 0 <= p < n}))
+        was_set = self._was_set(range(n) if torch.is_tensor(parents) else sorted({p for p in parents if p >= 0}))
+        began, lost = self.began, self.lost
+        if not torch.is_tensor(parents):
+            began, lost = ([of[p] if p >= 0 else 0 for p in parents] for of in (began, lost))
+        elif self.window is not None:                                   # (the most of all that are as long as the parent)
+            began, lost = ([of.get(t, 0) for t in lengths] for of in (dict(sorted(zip(self.lengths, a))) for a in (began, lost)))
+        if was_set:
+            began, lost = ([min(e, t) for e, t in zip(a, lengths)] for a in (began, lost))
         if not torch.is_tensor(parents):
             parents = torch.tensor(parents, dtype=torch.int32).to("cuda")
         now = torch.tensor(self.lengths, dtype=torch.int32).to("cuda")
@@ -245,8 +250,8 @@ class Decoder:
         # (the graph of a step knows the table by its address)
         self.table.copy_(self.next_table)
         self.uses.copy_(self.next_uses)
-        self.lengths, self.ends, self.lost = list(lengths), ends, lost
-        self.common = [t // self.page * self.page for t in lengths]
+        self.lengths, self.ends, self.began, self.lost = list(lengths), ends, began, lost
+        self.known, self.forked = list(lengths), list(lengths)
 
     def compact(self):
         """Moves the pages in use to the front of the cache; how many they are, on the device."""
@@ -326,9 +331,7 @@ class Decoder:
                 raise ValueError(f"rows {tuple(new.shape)} of {new.dtype} for {n} sequences of {x.shape[1]} x {x.dtype}")
             if max(self.lengths) >= self.max_tokens:
                 raise ValueError(f"the cache holds {self.max_tokens} tokens of a sequence")
-            if self.shares:
-                self._sees_all(range(n))
-                self._part(range(n))
+            was_set = self.shares and self._was_set(range(n))
             if self.lengths != on_device:
                 length.copy_(torch.tensor(self.lengths, dtype=torch.int32))
             x.copy_(new)
@@ -336,10 +339,12 @@ class Decoder:
             if self.shares:
                 on_device = None                                        # (where pages are missing lengths are copied again)
                 self.ends = [max(e, -(-(t + 1) // self.page)) for e, t in zip(self.ends, self.lengths)]
-                self._gave_up()
+                self.began = list(self.lengths)
                 self._enough(self.ends, self.lengths)
-                self._wrote(range(n))
-            self.lengths = [t + 1 for t in self.lengths]
+            lengths = [t + 1 for t in self.lengths]
+            if self.shares:
+                self._read(lengths, was_set, [1] * n)
+            self.lengths = lengths
             on_device = list(self.lengths)                              # (the caller may change the other one in place)
             return y
         step.keep = (graph, workspace, rows, begin) + ((before, drop_begin, drop_end) if self.shares else ())

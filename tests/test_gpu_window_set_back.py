@@ -111,3 +111,38 @@ def test_forks_releases_and_sequences_without_rows(B, monkeypatch):  # noqa: F81
     r.read(1, 1, 1, 1)
     r.m.release([1, 2])
     r.read(1, 5, 2, 40)
+
+
+@pytest.mark.parametrize("device", [False, True])
+def test_fork_of_sequences_that_were_set_back(B, monkeypatch, device):  # noqa: F811
+    """Their children have what they have; what those read again is there, and a parent that cannot go on is refused."""
+    import torch
+    r = Reader(monkeypatch, 4, 20, 3)
+
+    def fork(parents):
+        r.m.fork(torch.tensor(parents, dtype=torch.int32, device="cuda"), [r.m.lengths[p] if p >= 0 else 0 for p in parents]) if device else r.m.fork(parents)
+    for _ in range(60):
+        r.m.forward(r.rows(2), [1, 1, 0])
+    r.m.lengths = [32, 60, 0]
+    fork([0, 0, 1])
+    for _ in range(10):
+        r.read(1, 1, 1)
+    r.m.lengths = [36, 42, 70]
+    for _ in range(30):
+        r.read(1, 0, 2) if _ % 3 else r.read(1, 1, 0)
+    r.m.lengths[1] = 45                                                 # (its last token, behind 51, left those before 48)
+    r.refused(lambda: r.m.forward(r.rows(2), [0, 1, 1]))
+    r.m.lengths[1] = 51
+    r.read(0, 1, 1)
+    r.m.lengths[1] = 32
+    r.read(0, 2, 1)
+    r.m.lengths[1] = 33
+    r.read(0, 1, 1)
+    r.m.lengths[2] = 60
+    r.refused(lambda: fork([0, 1, 2]))
+    r.refused(lambda: r.m.forward(r.rows(1), [0, 0, 1]))
+    r.m.lengths[0] = 33
+    r.refused(lambda: fork([0, 0, 1]))
+    r.m.lengths = [66, 34, 0]
+    r.m.release([2])
+    r.read(1, 1, 1)

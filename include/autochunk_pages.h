@@ -48,6 +48,8 @@ int ac_op_pages_update(const ac_page_books* from, const ac_page_books* to, const
  * places for tokens to come, stays with the first sequence that has this parent; the others get a page of their own for the partly filled one, into which all caches' codes and scales of
  * its blocks are copied, and no places for tokens to come.  Pages that no place names any more are free, and serve these copies.  Which pages are taken, and what
  * happens where they run out, is as in ac_op_pages_update (the place names none: what it held is lost to that sequence).
+ * A length that was set back below pages that others name, too, is the caller's matter: neither this call nor an update takes such pages from a sequence that goes on to write into them (first give them up,
+ * ac_op_pages_update, and copy the partly filled one, ac_op_cache_copy_pages).
  * caches: the layers' caches, host array of n_caches (at most 4096; NULL with 0).  page_table of `to` and length_to lie apart from those of `from`.
  */
 int ac_op_cache_fork(const ac_kv_cache* caches, int n_caches, const ac_page_books* from, const ac_page_books* to, const int32_t* parent, const int32_t* length,
@@ -55,7 +57,7 @@ int ac_op_cache_fork(const ac_kv_cache* caches, int n_caches, const ac_page_book
 
 /*
  * Moves pages in use to the front: with n of them, they are pages 0 .. n - 1 afterwards and those behind are free.  The last page in use goes to the first free one, and so
- * on, in all caches; uses and page tables follow.  used (dev, may be NULL) receives n.
+ * on, in all caches; uses and page tables follow (a page that a caller keeps for itself moves, too: its number is known where a row of the table names it).  used (dev, may be NULL) receives n.
  */
 int ac_op_cache_compact(const ac_kv_cache* caches, int n_caches, const ac_page_books* from, const ac_page_books* to, int32_t* used, void* workspace,
                         uint64_t workspace_bytes, void* stream);

@@ -12,7 +12,8 @@
 // has them at 0.0017.  With a second term, as where rows are few, half as many matrix instructions again: 2048 rows behind 14336 tokens 425 us for 281, heads of 64 254 for 196.
 //
 // 2048 rows behind 14336 tokens, 16 heads of 128: 280 us, 0.92 PFLOP/s, of 1.27 that a large library product reaches.  What is left is issued beside the matrix
-// instructions: 32 exponentials, their scaling and packing, and as many conversions of codes for every 32 of them.  The matrix cores are busy 37 % of the time, the vector units 58 %.  Heads of 128 spill 15
+// instructions: 32 exponentials, their scaling and packing, and as many conversions of codes for every 32 of them (of the latter three quarters are done by another row wave of the side, too: each converts
+// the whole tile for its rows).  The matrix cores are busy 37 % of the time, the vector units 58 %.  Heads of 128 spill 15
 // registers, 64 bytes a lane (of 96 two): half of the 16 MB that this call writes, 8 being the output.
 #include "cache.h"
 
@@ -44,7 +45,7 @@ template <int HD> constexpr size_t lds_bytes() {
 }
 
 // WINDOWED: tiles of keys are made of the blocks of the block's Reach, the sinks' and then the window's; key numbers count these blocks.  2048 rows behind 14336 tokens through 4096 and 64
-// sinks, 16 heads of 128: 84 us, 0.83 PFLOP/s (0.95 without a window): a block has 33 steps of each side, behind a prologue and before a join that take 6 us.
+// sinks, 16 heads of 128: 87 us, 0.80 PFLOP/s (0.92 without a window): a block has 33 steps of each side, behind a prologue and before a join that take 6 us.
 template <int HD, bool WINDOWED>
 __global__ void __launch_bounds__(256 * sides<HD>(), sides<HD>()) cache_prefill(CacheAttnArgs g) {
   constexpr int TILE = kTile * HD, BLOCK = kBlock * HD, CHUNKS = TILE / 1024;   // bytes of a tile's keys or values and of a block; KB of the former

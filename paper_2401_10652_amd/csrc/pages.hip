@@ -130,7 +130,8 @@ __device__ __forceinline__ void give_row(const PagesArgs& g, int b, int lane, in
   }
 }
 
-// Row j goes on as its parent; whether it wants a page for a copy of the partly filled one.
+// Row j goes on as its parent; whether it wants a page for a copy of the partly filled one.  (The first of a parent's rows is found among those before it, 64 at a time: 65535 rows take the last wave 1024
+// loads, one after another.)
 __device__ __forceinline__ int fork_row(const PagesArgs& g, int j, int lane) {
   const int p = g.parent[j];
   const bool none = (uint32_t)p >= (uint32_t)g.batch;

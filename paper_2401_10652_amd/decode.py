@@ -147,11 +147,14 @@ class Decoder:
             raise ValueError("sequences of this cache have their own pages: give it a number of `pages` to share")
 
     def _was_set(self, sequences):
-        """Before these sequences read on, or are forked: whether lengths were set since the last call.  Refuses those that were set back to where a window needs tokens whose pages have been
-        given up; those that share the pages behind them go on in pages of their own."""
+        """Before these sequences read on, or are forked: whether lengths were set since the last call.  Refuses those that the sequences do not have (any more), and those from which a window
+        reaches tokens whose pages have been given up; those that share the pages behind them go on in pages of their own."""
         if self.lengths == self.known:
             return False
         sequences = list(sequences)
+        for b in sequences:
+            if not 0 <= self.lengths[b] <= self.known[b]:
+                raise ValueError(f"sequence {b} has {self.known[b]} tokens: it cannot go on behind {self.lengths[b]}")
         if self.window is not None:
             self.lost = [max(e, (n - self.window + 1) // self.page * self.page) for e, n in zip(self.lost, self.began)]
             sinks = -(-self.sinks // self.page) * self.page
@@ -198,6 +201,7 @@ class Decoder:
                 self.table.copy_(self.next_table)
                 self.uses.copy_(self.next_uses)
                 self.ends[b] = max(first, place + copies)
+                self.known[b], self.began[b], self.lost[b] = n, min(n, self.began[b]), min(n, self.lost[b])        # (what lay behind is not its own any more, also where the call fails)
             self.forked[b] = n
 
     def release(self, sequences):
@@ -340,6 +344,8 @@ class Decoder:
                 on_device = None                                        # (where pages are missing lengths are copied again)
                 self.ends = [max(e, -(-(t + 1) // self.page)) for e, t in zip(self.ends, self.lengths)]
                 self.began = list(self.lengths)
+                if was_set:                                             # (their next tokens are written, also where pages are missing for others)
+                    self._read(self.lengths, was_set, [1] * n)
                 self._enough(self.ends, self.lengths)
             lengths = [t + 1 for t in self.lengths]
             if self.shares:

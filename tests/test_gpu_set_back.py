@@ -151,3 +151,44 @@ def test_parents_on_the_host(B):  # noqa: F811
         m.fork(on_device.int(), [40] * 3)
     assert torch.equal(m.table, table) and m.lengths == [40, 40, 40, 0]
     same(m, own, x[50:53], [1, 1, 1, 0])
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_a_call_that_fails_behind_a_length_that_was_set_back(B, graph):  # noqa: F811
+    """What it gave up, or wrote again, is not taken for the tokens of before."""
+    m, own, x = pair(pages=7, first=48)                                 # (three whole pages that are shared)
+    step = m.step_graph()
+    back((m, own), {1: 20})
+    if not graph:                                                       # a page for the copy and three for others, of which there are four
+        with pytest.raises(RuntimeError, match="pages are missing"):
+            m.forward(x[50:110], [20, 1, 20, 19])
+    else:
+        m.uses[4:] += 1                                                 # (somebody else has all but one)
+        with pytest.raises(RuntimeError, match="pages are missing"):
+            step(x[50:54])
+        m.uses[4:] -= 1
+    assert m.lengths == [48, 20, 48, 0]
+    back((m,), {1: 48})
+    with pytest.raises(ValueError, match="20 tokens"):
+        m.forward(x[60:61], [0, 1, 0, 0])
+    with pytest.raises(ValueError, match="20 tokens"):
+        m.fork([0, 1, 2, 3])
+    back((m,), {1: 20})
+    same(m, own, x[60:63], [0, 3, 0, 0])
+    same(m, own, x[70:73], [1, 1, 1, 0])
+
+
+def test_lengths_that_a_sequence_does_not_have(B):  # noqa: F811
+    m, own, x = pair()
+    step = m.step_graph()
+    for b, n in ((0, 41), (1, -1), (3, 1), (2, 100)):
+        was = m.lengths[b]
+        back((m,), {b: n})
+        for call in (lambda: m.forward(x[:1], [int(i == b) for i in range(4)]), lambda: step(x[:4]), lambda: m.fork([0, 1, 2, 3])):
+            with pytest.raises(ValueError, match=f"{was} tokens"):
+                call()
+        back((m,), {b: was})
+    back((m, own), {0: 30})
+    same(m, own, x[50:52], [0, 2, 0, 0])
+    back((m, own), {0: 40})
+    same(m, own, x[52:55], [1, 1, 1, 0])

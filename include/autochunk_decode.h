@@ -131,7 +131,7 @@ uint64_t ac_cache_attention_window_workspace_bytes(int64_t n_rows, int heads, co
  * equal ones the lower i, then the larger logit, then the lower t: scores_out, parent (r, the sequence it goes on from) and token, each [batch][keep], and ended_out (may be NULL): 1 where the parent had ended or the token is end, else 0.
  * Logits of -inf (tokens that may not come) and scores of -inf (a beam that is none yet) give no candidates, and none comes from a row that holds a NaN; logits of +inf
  * share the probability among them.  Where candidates are fewer than `keep` the others come out as score -inf, parent -1, token -1, ended 0.
- * Totals are compared in 64 bits, from maxima and sums of exponentials held in 32; within a beam the order is that of the logits.
+ * Totals are compared in 64 bits and come out rounded to 32 (past their range as infinities), from maxima and sums of exponentials held in 32; within a beam the order is that of the logits.
  * ended: NULL = none; end: a token, with ended NULL also -1 = none.  beams and keep at most 64, batch 65535, vocab 2^24, else AC_ERR_UNSUPPORTED.  Rows may start at any element.  Outputs lie apart from scores and ended.
  * workspace: dev, 16-byte aligned, ac_beam_select_workspace_bytes() large, else AC_ERR_WORKSPACE.
  */
